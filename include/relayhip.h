@@ -66,10 +66,13 @@ enum {
 };
 
 /* BaseType.  The paper's FloatType(width) cannot tell bfloat16 from IEEE half,
- * so bfloat16 has a tag of its own. */
-enum { RL_F32 = 0, RL_BF16 = 1 };
+ * so bfloat16 has a tag of its own.  RL_I8 and RL_I32 are its IntType(8) and IntType(32): 8-bit values that stand for
+ * numbers through a scale of their own, flags, token ids.  Only the operators whose types name them take them; the
+ * arithmetic, contraction, pool and layout operators are of the two float types. */
+enum { RL_F32 = 0, RL_BF16 = 1, RL_I8 = 2, RL_I32 = 3 };
 
 #define RL_MAX_RANK 6
+#define RL_MAX_RESULTS 4
 
 /* Tensor(dtype, Shape(dims[0..rank-1])); rank 0 is a scalar. */
 typedef struct rl_type {
@@ -110,7 +113,32 @@ enum {
                                  forward output size does not determine H and W: the declared result states them, and
                                  OH = floor((H + 2 pad - KH)/stride) + 1 is checked (else RL_ERR_TYPE) */
     RL_OP_CONV2D_GRAD_W = 22, /* (dy[N,O,OH,OW], x[N,C,H,W]) -> [O,C,KH,KW]; attrs as above; the declared result states KH and KW */
-    RL_OP_KIND_COUNT = 23
+    /* A gated recurrent language model, served in 8 bits and trained in the float types.  Each is a group of its own; `e` is
+     * f32 or bf16, the base type of the operand named first, and an operand in brackets may be left out. */
+    RL_OP_RMS_NORM_Q8 = 23,   /* (x e[M,D], [r e[M,D],] g f32|e[D]) -> (q i8[M,D], s f32[M][, y e[M,D]]); attrs rl_attr_norm (may be NULL:
+                                 eps 1e-5).  y = x + r rounded to e, the residual stream (x itself without r);
+                                 n = y g / sqrt(mean_d y^2 + eps); s = max_d |n| / 127; q = n / s rounded to the nearest whole
+                                 number, ties to even.  A row of zeros has s = 0 and q = 0, a row that holds an infinity or NaN, or whose
+                                 sum of squares or largest |y g| is past f32, s = NaN and q = 0.  Three results with r, two without */
+    RL_OP_DENSE_Q8 = 24,      /* (x i8[M,K], sx f32[M], w i8[N,K], sw f32[N][, b f32[N]]) -> f32|bf16 [M,N]; attrs rl_attr_contract (may be
+                                 NULL: f32).  sx[m] sw[n] sum_k x[m,k] w[n,k] + b[n], the sum of the 8-bit products exact (32 bits:
+                                 K <= 131071, else RL_ERR_UNSUPPORTED) */
+    RL_OP_LINEAR_SCAN = 25,   /* (z e[B*T,2D] as f|v blocks, h0 f32[B,D][, keep i8[B*T]]) -> (h e[B*T,D], hT f32[B,D]): the rows of z are B
+                                 sequences of T tokens one behind the other (B from h0; T = 1 is a decoding step, hT the next call's h0).
+                                 h_t = a h_(t-1) + (1 - a) v with a = sigmoid(f), the state in f32.  keep: 0: padding, whose z and row of
+                                 dh are not looked at: the state stays as it is and the row of h is zero; 2: the first token of a
+                                 document: the state before it is zero; any other value: a token.  hT may lie over h0 where T = 1 */
+    RL_OP_LINEAR_SCAN_GRAD = 26, /* (z, h0, dh e[B*T,D], dhT f32[B,D][, keep]) -> (dz e[B*T,2D], dh0 f32[B,D]): the derivatives of a loss whose
+                                 derivatives by linear_scan's two results are dh and dhT; the states between are computed anew, in f32 */
+    RL_OP_TOKEN_LOGPROBS = 27,/* (x e[M,V], tok i32[M]) -> (lp f32[M], ent f32[M][, top_lp f32[M,top], top_id i32[M,top]]); attrs
+                                 rl_attr_logprobs (may be NULL: top 0).  lp: log softmax of the row at its token, 0 where tok is
+                                 outside 0..V-1 (no target); ent: -sum p ln p; the `top` largest, from the largest, ties to the lowest
+                                 index.  A logit of -inf has p = 0; a row of nothing else has lp -inf, ent 0 and top_lp -inf at the lowest
+                                 indexes; a row with +inf or NaN has NaN in lp, ent and top_lp, and NaN sorts above +inf in top_id.
+                                 Four results where top > 0, two otherwise */
+    RL_OP_TOKEN_LOGPROBS_GRAD = 28, /* (x, tok, dlp f32[M], dent f32[M]) -> dx e[M,V]: dlp (1[v = tok] - p) - dent p (ln p + ent); no target: as
+                                 with dlp = 0; a row of -inf alone: zeros */
+    RL_OP_KIND_COUNT = 29
 };
 
 typedef struct rl_attr_contract { int32_t out_dtype; /* operand dtype, or RL_F32 */ } rl_attr_contract;
@@ -123,6 +151,10 @@ typedef struct rl_attr_axis { int32_t axis; } rl_attr_axis;
 typedef struct rl_attr_pool2d { int32_t kernel_h, kernel_w, stride_h, stride_w, pad_h, pad_w; } rl_attr_pool2d;
 typedef struct rl_attr_cast { int32_t to; } rl_attr_cast;
 typedef struct rl_attr_layout { int32_t perm[RL_MAX_RANK]; /* a permutation of 0..rank-1 in the first rank entries; else RL_ERR_KIND */ } rl_attr_layout;
+
+typedef struct rl_attr_norm { float eps; /* > 0, finite; else RL_ERR_KIND */ } rl_attr_norm;
+typedef struct rl_attr_logprobs { int32_t top; /* 0 .. RL_TOP_MAX and at most V; else RL_ERR_KIND */ } rl_attr_logprobs;
+#define RL_TOP_MAX 32
 
 typedef struct rl_binding { int32_t value_id; void *dev_ptr; } rl_binding;
 
@@ -137,7 +169,7 @@ const char *rl_last_error(const rl_ctx *ctx);
  * (Tensor-T: dtype known, rank <= RL_MAX_RANK, every dim >= 1).  A param is a
  * constant the plan may ask to have re-laid-out once (rl_plan_prepack).
  * rl_graph_op appends a call.  The caller must state the result type(s)
- * (declared_outs, n_out = 1 except RL_OP_LSTM_GATES which has 2); the library
+ * (declared_outs, n_out = 1 except where a kind's own line above names more, at most RL_MAX_RESULTS); the library
  * infers the result type from the argument types and attributes and rejects
  * the call with RL_ERR_TYPE when they differ (Type-Call), or when the
  * arguments break the operator's rule (Type-UnaryOp, Type-Noncomp-BinaryOp:
@@ -254,7 +286,8 @@ rl_status rl_plan_prepack(const rl_plan *plan, int32_t param_value_id, const voi
  * (packed copy where rl_plan_packed_bytes > 0) and output value id exactly
  * once; intermediates live in workspace_dev (>= rl_plan_workspace_bytes).
  * Inputs and params are read only; outputs and workspace are overwritten.
- * An output may alias an input only for lstm_gates' cell state (c' over c).
+ * An output may alias an input only for lstm_gates' cell state (c' over c) and the state of a linear_scan of one token
+ * (hT over h0).
  * The call only launches kernels on hip_stream (no allocation, no memset, no
  * synchronisation), so it may be made while that stream is being captured into
  * a HIP graph; replays then need the same device pointers to stay valid. */

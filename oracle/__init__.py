@@ -206,8 +206,10 @@ def lstm_gates(z, c):
 
 
 def round_to(x, dtype: str):
-    """Nearest value representable in `dtype` ("f32" | "bf16"), ties to even."""
+    """Nearest value representable in `dtype` ("f32" | "bf16"), ties to even; whole numbers ("i8" | "i32") are themselves."""
     x = _d(x)
+    if dtype in ("i8", "i32"):
+        return x
     y = np.empty_like(x)
     fn = {"f32": lib().oracle_round_f32, "bf16": lib().oracle_round_bf16}[dtype]
     fn(_p(x), _p(y), _i(x.size))
@@ -215,8 +217,10 @@ def round_to(x, dtype: str):
 
 
 def widen(a: np.ndarray, dtype: str) -> np.ndarray:
-    """Exact widening of stored tensor data (float32 array, or uint16 bf16 bit
-    patterns) to float64."""
+    """Exact widening of stored tensor data (float32 array, uint16 bf16 bit
+    patterns, int8 or int32 array) to float64."""
+    if dtype in ("i8", "i32"):
+        return np.asarray(a, dtype=np.int8 if dtype == "i8" else np.int32, order="C").astype(np.float64)
     if dtype == "bf16":
         a = np.asarray(a, dtype=np.uint16, order="C")
         return (a.astype(np.uint32) << np.uint32(16)).view(np.float32).astype(np.float64)

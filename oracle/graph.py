@@ -30,8 +30,10 @@ from typing import Dict, List, Tuple
 import numpy as np
 
 import oracle as O
+from oracle import language as L
 
-DTYPES = ("f32", "bf16")
+DTYPES = ("f32", "bf16", "i8", "i32")
+FLOATS = ("f32", "bf16")
 MAX_RANK = 6
 
 
@@ -72,6 +74,11 @@ def infer(kind: str, ins: List[Tuple[str, Tuple[int, ...]]], attrs: Dict) -> Lis
         if len(ins) != n:
             raise IllTyped("type", f"{kind} takes {n} arguments, got {len(ins)}")
 
+    if kind in LANGUAGE:
+        return _infer_language(kind, ins, attrs)
+    for dt, _ in ins:
+        if dt not in FLOATS:
+            raise IllTyped("type", f"{kind} is of the float types, not of {dt}")
     if kind in ("neg", "sq", "relu", "sigmoid", "tanh"):
         need(1)
         return [ins[0]]
@@ -208,7 +215,7 @@ def infer(kind: str, ins: List[Tuple[str, Tuple[int, ...]]], attrs: Dict) -> Lis
     if kind == "cast":
         need(1)
         to = attrs.get("to")
-        if to not in DTYPES:
+        if to not in FLOATS:
             raise IllTyped("kind", f"cast to {to!r}")
         return [(to, ins[0][1])]
     if kind == "layout_transform":
@@ -226,8 +233,95 @@ def infer(kind: str, ins: List[Tuple[str, Tuple[int, ...]]], attrs: Dict) -> Lis
         if len(sz) != 2 or len(sc) != 2 or sz[0] != sc[0] or sz[1] != 4 * sc[1]:
             raise IllTyped("type", f"lstm_gates shapes {sz} / {sc}")
         hd = attrs.get("h_dtype", None)
+        if hd not in FLOATS + (None,):
+            raise IllTyped("type", f"lstm_gates: h of {hd}")
         return [("f32", sc), (hd, sc)]   # h' dtype is taken from the declaration
     raise IllTyped("kind", f"unknown operator {kind!r}")
+
+
+LANGUAGE = ("rms_norm_q8", "dense_q8", "linear_scan", "linear_scan_grad", "token_logprobs", "token_logprobs_grad")
+TOP_MAX = 32
+
+
+def _infer_language(kind, ins, attrs):
+    """The arrow types of a gated recurrent language model's operators."""
+    def operand(i, *allowed):
+        if ins[i] not in allowed:
+            raise IllTyped("type", f"{kind}: operand {i} is {ins[i]}, not {allowed[0]}")
+
+    def count(*allowed):
+        if len(ins) not in allowed:
+            raise IllTyped("type", f"{kind} takes {allowed} arguments, got {len(ins)}")
+
+    def matrix(i, dtypes=FLOATS):
+        if ins[i][0] not in dtypes or len(ins[i][1]) != 2:
+            raise IllTyped("type", f"{kind}: operand {i} is {ins[i]}, not a matrix of {dtypes}")
+
+    if kind == "rms_norm_q8":
+        if not (0 < attrs.get("eps", 1e-5) < np.inf):
+            raise IllTyped("kind", "eps is not a positive finite number")
+        count(2, 3)
+        matrix(0)
+        e, (m, d) = ins[0]
+        operand(len(ins) - 1, ("f32", (d,)), (e, (d,)))
+        if len(ins) == 2:
+            return [("i8", (m, d)), ("f32", (m,))]
+        operand(1, ins[0])
+        return [("i8", (m, d)), ("f32", (m,)), ins[0]]
+    if kind == "dense_q8":
+        count(4, 5)
+        matrix(0, ("i8",)), matrix(2, ("i8",))
+        (m, k), (n, k2) = ins[0][1], ins[2][1]
+        if k != k2:
+            raise IllTyped("type", f"dense_q8 inner dims {k} vs {k2}")
+        operand(1, ("f32", (m,)))
+        for i in range(3, len(ins)):
+            operand(i, ("f32", (n,)))
+        out = attrs.get("out_dtype", "f32")
+        if out not in FLOATS:
+            raise IllTyped("type", f"dense_q8: out_dtype {out}")
+        return [(out, (m, n))]
+    if kind in ("linear_scan", "linear_scan_grad"):
+        n = 4 if kind.endswith("grad") else 2
+        count(n, n + 1)
+        matrix(0), matrix(1, ("f32",))
+        (e, (rows, d2)), (b, d) = ins[0], ins[1][1]
+        if d2 != 2 * d or rows % b:
+            raise IllTyped("type", f"{kind}: z {ins[0]} is not [B*T,2D] for h0 {ins[1]}")
+        if n == 4:
+            operand(2, (e, (rows, d))), operand(3, ins[1])
+        if len(ins) > n:
+            operand(n, ("i8", (rows,)))
+        return [ins[0] if n == 4 else (e, (rows, d)), ins[1]]
+    top = attrs.get("top", 0) if kind == "token_logprobs" else 0
+    if not 0 <= top <= TOP_MAX:
+        raise IllTyped("kind", "top out of range")
+    count(2 if kind == "token_logprobs" else 4)
+    matrix(0)
+    m, v = ins[0][1]
+    operand(1, ("i32", (m,)))
+    if kind == "token_logprobs_grad":
+        operand(2, ("f32", (m,))), operand(3, ("f32", (m,)))
+        return [ins[0]]
+    if top > v:
+        raise IllTyped("kind", "more alternatives than columns")
+    return [("f32", (m,)), ("f32", (m,))] + ([("f32", (m, top)), ("i32", (m, top))] if top else [])
+
+
+def _run_language(kind, a, attrs, spec, op):
+    if kind == "rms_norm_q8":
+        r, g = (a[1], a[2]) if len(a) == 3 else (None, a[1])
+        out = L.rms_norm_q8(a[0], r, g, float(np.float32(attrs.get("eps", 1e-5))), spec.values[op.inputs[0]].type.dtype)
+        return out[:len(op.outputs)]
+    if kind == "dense_q8":
+        return [L.dense_q8(*a)]
+    if kind == "linear_scan":
+        return L.linear_scan(*a)
+    if kind == "linear_scan_grad":
+        return L.linear_scan_grad(*a)
+    if kind == "token_logprobs":
+        return L.token_logprobs(a[0], a[1], attrs.get("top", 0))
+    return [L.token_logprobs_grad(*a)]
 
 
 INJECTIVE = {"neg", "sq", "relu", "sigmoid", "tanh", "add", "sub", "mul", "div", "bias_add", "cast"}
@@ -388,6 +482,8 @@ def run(spec, data: Dict[str, np.ndarray], keep_all: bool = False, keep=()) -> D
             out = [a[0]]
         elif k == "lstm_gates":
             out = list(O.lstm_gates(a[0], a[1]))
+        elif k in LANGUAGE:
+            out = _run_language(k, a, op.attrs, spec, op)
         else:
             raise IllTyped("kind", k)
         for vid, arr in zip(op.outputs, out):

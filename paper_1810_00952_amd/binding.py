@@ -12,15 +12,16 @@ from typing import Dict, List, Optional, Sequence, Tuple
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "librelayhip.so")
 
-RL_F32, RL_BF16 = 0, 1
+RL_F32, RL_BF16, RL_I8, RL_I32 = 0, 1, 2, 3
 STATIC_WORKSPACE_BYTES = 16 << 20
 RL_MAX_RANK = 6
-DTYPES = {"f32": RL_F32, "bf16": RL_BF16}
-DTYPE_BYTES = {"f32": 4, "bf16": 2}
+DTYPES = {"f32": RL_F32, "bf16": RL_BF16, "i8": RL_I8, "i32": RL_I32}
+DTYPE_BYTES = {"f32": 4, "bf16": 2, "i8": 1, "i32": 4}
 
 OPS = {"dense": 0, "conv2d": 1, "bias_add": 2, "add": 3, "sub": 4, "mul": 5, "div": 6, "neg": 7, "sq": 8, "relu": 9,
        "sigmoid": 10, "tanh": 11, "maxpool2d": 12, "global_avgpool": 13, "flatten": 14, "lstm_gates": 15, "cast": 16,
-       "concat": 17, "layout_transform": 18, "dense_grad_x": 19, "dense_grad_w": 20, "conv2d_grad_x": 21, "conv2d_grad_w": 22}
+       "concat": 17, "layout_transform": 18, "dense_grad_x": 19, "dense_grad_w": 20, "conv2d_grad_x": 21, "conv2d_grad_w": 22,
+       "rms_norm_q8": 23, "dense_q8": 24, "linear_scan": 25, "linear_scan_grad": 26, "token_logprobs": 27, "token_logprobs_grad": 28}
 
 STATUS = {0: "ok", -1: "null", -2: "kind", -3: "shape", -4: "type", -5: "group", -6: "binding", -7: "workspace",
           -8: "align", -9: "unsupported", -10: "hip"}
@@ -52,6 +53,14 @@ class rl_attr_cast(ctypes.Structure):
 
 class rl_attr_layout(ctypes.Structure):
     _fields_ = [("perm", c_int32 * RL_MAX_RANK)]
+
+
+class rl_attr_norm(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float)]
+
+
+class rl_attr_logprobs(ctypes.Structure):
+    _fields_ = [("top", c_int32)]
 
 
 class rl_binding(ctypes.Structure):
@@ -194,7 +203,7 @@ class Context:
 
 def _attrs_for(kind: str, attrs: Dict):
     od = attrs.get("out_dtype")
-    if kind in ("dense", "dense_grad_x", "dense_grad_w"):
+    if kind in ("dense", "dense_grad_x", "dense_grad_w", "dense_q8"):
         return rl_attr_contract(DTYPES[od]) if od is not None else None
     if kind in ("conv2d", "conv2d_grad_x", "conv2d_grad_w"):
         s, p = attrs.get("stride", (1, 1)), attrs.get("pad", (0, 0))
@@ -205,6 +214,10 @@ def _attrs_for(kind: str, attrs: Dict):
     if kind == "maxpool2d":
         k, s, p = attrs["kernel"], attrs.get("stride", (1, 1)), attrs.get("pad", (0, 0))
         return rl_attr_pool2d(k[0], k[1], s[0], s[1], p[0], p[1])
+    if kind == "rms_norm_q8":
+        return rl_attr_norm(attrs["eps"]) if "eps" in attrs else None
+    if kind == "token_logprobs":
+        return rl_attr_logprobs(int(attrs.get("top", 0)))
     if kind == "cast":
         return rl_attr_cast(DTYPES.get(attrs.get("to"), -1))
     if kind == "layout_transform":
@@ -359,6 +372,10 @@ class Plan:
         self.ctx.check(lib().rl_plan_run(self._h, self._bindings(bindings), len(bindings), c_void_p(workspace_ptr),
                                          c_size_t(workspace_bytes), c_void_p(stream)))
 
+    def bind(self, bindings: Dict[int, int], workspace_ptr: int = 0, workspace_bytes: int = 0) -> "BoundPlan":
+        """The plan with the pointers of many runs: run() with them marshalled once."""
+        return BoundPlan(self, bindings, workspace_ptr, workspace_bytes)
+
     def run_static(self, bindings: Dict[int, int], stream: int = 0) -> None:
         """rl_plan_run_static: the library's built-in workspace (STATIC_WORKSPACE_BYTES at most), no device allocation."""
         self.ctx.check(lib().rl_plan_run_static(self._h, self._bindings(bindings), len(bindings), c_void_p(stream)))
@@ -384,3 +401,18 @@ class Plan:
         if getattr(self, "_h", None) and _lib is not None:
             _lib.rl_plan_destroy(self._h)
             self._h = None
+
+
+class BoundPlan:
+    """A plan and the device pointers its runs use (Plan.bind).  The caller keeps the memory behind them."""
+
+    def __init__(self, plan: Plan, bindings: Dict[int, int], workspace_ptr: int, workspace_bytes: int):
+        self.plan = plan
+        self._check = plan.ctx.check
+        self._call = lib().rl_plan_run
+        self._args = (plan._h, plan._bindings(bindings), c_int32(len(bindings)), c_void_p(workspace_ptr), c_size_t(workspace_bytes))
+
+    def run(self, stream: int = 0) -> None:
+        st = self._call(*self._args, stream or None)
+        if st != 0:
+            self._check(st)

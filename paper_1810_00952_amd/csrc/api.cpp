@@ -182,7 +182,7 @@ rl_status rl_graph_op(rl_graph *g, int32_t op_kind, const int32_t *in_ids, int32
     return guarded(err, [&]() -> rl_status {
         if (!in_ids || !declared_outs || !out_value_ids) return fail(err, RL_ERR_NULL, "null argument");
         if (op_kind < 0 || op_kind >= RL_OP_KIND_COUNT) return fail(err, RL_ERR_KIND, "unknown operator kind");
-        if (n_in < 0 || n_in > 8 || n_out < 1 || n_out > 2) return fail(err, RL_ERR_TYPE, "bad operand or result count");
+        if (n_in < 0 || n_in > 8 || n_out < 1 || n_out > RL_MAX_RESULTS) return fail(err, RL_ERR_TYPE, "bad operand or result count");
         std::string msg;
         OpNode op;
         op.kind = op_kind;
@@ -368,7 +368,8 @@ rl_status rl_plan_prepack(const rl_plan *plan, int32_t v, const void *src, void 
         if (it == plan->p.packs.end()) return fail(err, RL_ERR_BINDING, "this value id needs no packing");
         if (((uintptr_t)src & 15) || ((uintptr_t)dst & 15)) return fail(err, RL_ERR_ALIGN, "device pointer is not 16-byte aligned");
         auto pack = [&](const PackSpec &k, void *to) {
-            return k.gather ? launch_pack_gather(src, to, k.gp, (hipStream_t)stream)
+            return k.pad ? launch_pad_bytes(src, to, k.pb, (hipStream_t)stream)
+                 : k.gather ? launch_pack_gather(src, to, k.gp, (hipStream_t)stream)
                  : k.stem == 2 ? launch_pack_weight_stem_direct(src, to, k.O, k.C, k.KH, k.KW, k.pw, (hipStream_t)stream)
                  : k.stem ? launch_pack_weight_stem(src, to, k.O, k.C, k.KH, k.KW, k.Kp, (hipStream_t)stream)
                           : launch_pack_weight(src, to, k.dtype, k.O, k.C, k.T, k.Kp, k.perm_block, (hipStream_t)stream);

@@ -3,6 +3,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <cmath>
 #include <set>
 #include <sstream>
 
@@ -11,7 +12,8 @@ namespace rl {
 static const char *kOpNames[RL_OP_KIND_COUNT] = {
     "dense", "conv2d", "bias_add", "add", "sub", "mul", "div", "neg", "sq", "relu", "sigmoid", "tanh",
     "maxpool2d", "global_avgpool", "flatten", "lstm_gates", "cast", "concat", "layout_transform",
-    "dense_grad_x", "dense_grad_w", "conv2d_grad_x", "conv2d_grad_w"};
+    "dense_grad_x", "dense_grad_w", "conv2d_grad_x", "conv2d_grad_w",
+    "rms_norm_q8", "dense_q8", "linear_scan", "linear_scan_grad", "token_logprobs", "token_logprobs_grad"};
 
 const char *op_name(int kind) { return (kind >= 0 && kind < RL_OP_KIND_COUNT) ? kOpNames[kind] : "?"; }
 bool is_anchor(int kind) { return kind == RL_OP_DENSE || kind == RL_OP_CONV2D; }
@@ -37,7 +39,7 @@ bool same_type(const rl_type &a, const rl_type &b)
 std::string type_str(const rl_type &t)
 {
     std::ostringstream o;
-    o << "Tensor(" << (t.dtype == RL_F32 ? "f32" : t.dtype == RL_BF16 ? "bf16" : "?") << ", Shape(";
+    o << "Tensor(" << (t.dtype == RL_F32 ? "f32" : t.dtype == RL_BF16 ? "bf16" : t.dtype == RL_I8 ? "i8" : t.dtype == RL_I32 ? "i32" : "?") << ", Shape(";
     for (int i = 0; i < t.rank && i < RL_MAX_RANK; ++i) o << (i ? "," : "") << t.dims[i];
     o << "))";
     return o.str();
@@ -50,11 +52,12 @@ int64_t numel(const rl_type &t)
     return n;
 }
 
-size_t dtype_size(int dtype) { return dtype == RL_BF16 ? 2 : 4; }
+size_t dtype_size(int dtype) { return dtype == RL_I8 ? 1 : dtype == RL_BF16 ? 2 : 4; }
+static bool is_float(int dtype) { return dtype == RL_F32 || dtype == RL_BF16; }
 
 rl_status check_tensor_type(const rl_type &t, std::string &msg)
 {
-    if (t.dtype != RL_F32 && t.dtype != RL_BF16) { msg = "unknown base type"; return RL_ERR_KIND; }
+    if (!is_float(t.dtype) && t.dtype != RL_I8 && t.dtype != RL_I32) { msg = "unknown base type"; return RL_ERR_KIND; }
     if (t.rank < 0 || t.rank > RL_MAX_RANK) { msg = "rank out of range"; return RL_ERR_KIND; }
     for (int i = 0; i < t.rank; ++i)
         if (t.dims[i] < 1) { msg = "dimension is not a positive constant"; return RL_ERR_SHAPE; }
@@ -69,7 +72,7 @@ rl_status parse_attrs(int kind, const void *attrs, size_t size, Attrs &a, std::s
         return true;
     };
     switch (kind) {
-    case RL_OP_DENSE: case RL_OP_DENSE_GRAD_X: case RL_OP_DENSE_GRAD_W:
+    case RL_OP_DENSE: case RL_OP_DENSE_GRAD_X: case RL_OP_DENSE_GRAD_W: case RL_OP_DENSE_Q8:
         if (!want(sizeof(rl_attr_contract))) return RL_ERR_KIND;
         if (attrs) a.out_dtype = ((const rl_attr_contract *)attrs)->out_dtype;
         break;
@@ -109,6 +112,16 @@ rl_status parse_attrs(int kind, const void *attrs, size_t size, Attrs &a, std::s
         for (int i = 0; i < RL_MAX_RANK; ++i) a.perm[i] = ((const rl_attr_layout *)attrs)->perm[i];
         break;                                  // checked against the operand's rank in infer_type
     }
+    case RL_OP_RMS_NORM_Q8:
+        if (!want(sizeof(rl_attr_norm))) return RL_ERR_KIND;
+        if (attrs) a.eps = ((const rl_attr_norm *)attrs)->eps;
+        if (!(a.eps > 0.0f) || !std::isfinite(a.eps)) { msg = "rms_norm_q8: eps is not a positive finite number"; return RL_ERR_KIND; }
+        break;
+    case RL_OP_TOKEN_LOGPROBS:
+        if (!want(sizeof(rl_attr_logprobs))) return RL_ERR_KIND;
+        if (attrs) a.top = ((const rl_attr_logprobs *)attrs)->top;
+        if (a.top < 0 || a.top > RL_TOP_MAX) { msg = "token_logprobs: top out of range"; return RL_ERR_KIND; }
+        break;
     default:
         break;
     }
@@ -138,7 +151,79 @@ rl_status infer_type(int kind, const std::vector<rl_type> &in, const Attrs &a, c
         return true;
     };
     out.clear();
+    if (kind < RL_OP_RMS_NORM_Q8)
+        for (const rl_type &t : in)
+            if (!is_float(t.dtype)) { msg = std::string(op_name(kind)) + " is of the float types, not of " + type_str(t); return RL_ERR_TYPE; }
+    // operand i must be Tensor(dtype, dims)
+    auto is = [&](size_t i, int dtype, std::initializer_list<int64_t> dims) -> bool {
+        const rl_type want = make_type(dtype, dims);
+        if (same_type(in[i], want)) return true;
+        msg = std::string(op_name(kind)) + ": operand " + std::to_string(i) + " is " + type_str(in[i]) + ", not " + type_str(want);
+        return false;
+    };
+    // operand i must be a matrix of a float type
+    auto matrix = [&](size_t i) -> bool {
+        if (in[i].rank == 2 && is_float(in[i].dtype)) return true;
+        msg = std::string(op_name(kind)) + ": operand " + std::to_string(i) + " is " + type_str(in[i]) + ", not a matrix of a float type";
+        return false;
+    };
     switch (kind) {
+    case RL_OP_RMS_NORM_Q8: {
+        if (in.size() != 2 && in.size() != 3) { msg = "rms_norm_q8: wrong number of arguments"; return RL_ERR_TYPE; }
+        if (!matrix(0)) return RL_ERR_TYPE;
+        const int64_t M = in[0].dims[0], D = in[0].dims[1];
+        const size_t gi = in.size() - 1;
+        if (gi == 2 && !is(1, in[0].dtype, {M, D})) return RL_ERR_TYPE;
+        if (!is(gi, in[gi].dtype == in[0].dtype ? in[0].dtype : RL_F32, {D})) return RL_ERR_TYPE;
+        out.push_back(make_type(RL_I8, {M, D}));
+        out.push_back(make_type(RL_F32, {M}));
+        if (gi == 2) out.push_back(in[0]);
+        return RL_OK;
+    }
+    case RL_OP_DENSE_Q8: {
+        if (in.size() != 4 && in.size() != 5) { msg = "dense_q8: wrong number of arguments"; return RL_ERR_TYPE; }
+        const rl_type &x = in[0], &w = in[2];
+        if (x.rank != 2 || w.rank != 2 || x.dtype != RL_I8 || w.dtype != RL_I8) { msg = "dense_q8 wants i8 matrices"; return RL_ERR_TYPE; }
+        if (x.dims[1] != w.dims[1]) { msg = "dense_q8 inner dimensions differ"; return RL_ERR_TYPE; }
+        if (!is(1, RL_F32, {x.dims[0]}) || !is(3, RL_F32, {w.dims[0]}) || (in.size() == 5 && !is(4, RL_F32, {w.dims[0]}))) return RL_ERR_TYPE;
+        const int od = a.out_dtype < 0 ? RL_F32 : a.out_dtype;
+        if (!is_float(od)) { msg = "dense_q8: out_dtype is not a float type"; return RL_ERR_TYPE; }
+        out.push_back(make_type(od, {x.dims[0], w.dims[0]}));
+        return RL_OK;
+    }
+    case RL_OP_LINEAR_SCAN: case RL_OP_LINEAR_SCAN_GRAD: {
+        const bool grad = kind == RL_OP_LINEAR_SCAN_GRAD;
+        const size_t n = grad ? 4 : 2;
+        if (in.size() != n && in.size() != n + 1) { msg = std::string(op_name(kind)) + ": wrong number of arguments"; return RL_ERR_TYPE; }
+        if (!matrix(0)) return RL_ERR_TYPE;
+        const rl_type &z = in[0], &h0 = in[1];
+        if (h0.rank != 2 || h0.dtype != RL_F32 || z.dims[1] != 2 * h0.dims[1] || z.dims[0] % h0.dims[0] != 0) {
+            msg = std::string(op_name(kind)) + ": z must be [B*T,2D] for h0 f32 [B,D]";
+            return RL_ERR_TYPE;
+        }
+        const rl_type h = make_type(z.dtype, {z.dims[0], h0.dims[1]});
+        if (grad && (!is(2, z.dtype, {z.dims[0], h0.dims[1]}) || !is(3, RL_F32, {h0.dims[0], h0.dims[1]}))) return RL_ERR_TYPE;
+        if (in.size() == n + 1 && !is(n, RL_I8, {z.dims[0]})) return RL_ERR_TYPE;
+        out.push_back(grad ? z : h);
+        out.push_back(h0);
+        return RL_OK;
+    }
+    case RL_OP_TOKEN_LOGPROBS: case RL_OP_TOKEN_LOGPROBS_GRAD: {
+        const bool grad = kind == RL_OP_TOKEN_LOGPROBS_GRAD;
+        if (!arity(grad ? 4 : 2) || !matrix(0)) return RL_ERR_TYPE;
+        const int64_t M = in[0].dims[0], V = in[0].dims[1];
+        if (!is(1, RL_I32, {M}) || (grad && (!is(2, RL_F32, {M}) || !is(3, RL_F32, {M})))) return RL_ERR_TYPE;
+        if (V > 0x7fffffff) { msg = std::string(op_name(kind)) + ": the tokens' base type does not reach the last column"; return RL_ERR_TYPE; }
+        if (grad) { out.push_back(in[0]); return RL_OK; }
+        if (a.top > V) { msg = "token_logprobs: more alternatives than columns"; return RL_ERR_KIND; }
+        out.push_back(make_type(RL_F32, {M}));
+        out.push_back(make_type(RL_F32, {M}));
+        if (a.top > 0) {
+            out.push_back(make_type(RL_F32, {M, a.top}));
+            out.push_back(make_type(RL_I32, {M, a.top}));
+        }
+        return RL_OK;
+    }
     case RL_OP_NEG: case RL_OP_SQ: case RL_OP_RELU: case RL_OP_SIGMOID: case RL_OP_TANH:      // Type-UnaryOp
         if (!arity(1)) return RL_ERR_TYPE;
         out.push_back(in[0]);
@@ -293,6 +378,7 @@ rl_status infer_type(int kind, const std::vector<rl_type> &in, const Attrs &a, c
             return RL_ERR_TYPE;
         }
         out.push_back(c);
+        if (declared.size() == 2 && !is_float(declared[1].dtype)) { msg = "lstm_gates: h is of a float type"; return RL_ERR_TYPE; }
         rl_type h = c;
         h.dtype = declared.size() == 2 ? declared[1].dtype : RL_F32;   // h' base type comes from the declaration
         out.push_back(h);

@@ -6,7 +6,7 @@
 
 namespace rl {
 
-enum { DT_F32 = 0, DT_BF16 = 1 };
+enum { DT_F32 = 0, DT_BF16 = 1, DT_I8 = 2, DT_I32 = 3 };
 
 // ---- injective epilogue program ------------------------------------------
 // A fused group's injective operators form a chain over one running value v
@@ -320,6 +320,47 @@ struct GatherPack {
 };
 hipError_t launch_pack_gather(const void *src, void *dst, const GatherPack &g, hipStream_t s);
 hipError_t launch_pack_weight_stem(const void *src, void *dst, int32_t O, int32_t C, int32_t KH, int32_t KW, int32_t Kp, hipStream_t s);
+// rows of K bytes copied into rows of Kp, the bytes behind them zero
+struct PadBytes { int64_t R, K, Kp; };
+hipError_t launch_pad_bytes(const void *src, void *dst, const PadBytes &p, hipStream_t s);
+
+// ---- a gated recurrent language model -------------------------------------
+// norm_q8.hip: (x, r?, g) -> (q, s, y?); r and y null: no residual
+struct NormQ8Params {
+    const void *x, *r, *g; void *y; int8_t *q; float *s;
+    int64_t M, D; int32_t dtype, g_dtype; float eps;
+};
+hipError_t launch_norm_q8(const NormQ8Params &p, hipStream_t s);
+// dense_q8.hip: rows of x and w ldx, ldw bytes apart, multiples of 16 and readable to the row's end; behind the K bytes of a row of w
+// there are zeros up to ldw, a multiple of 128
+struct DenseQ8Params {
+    const int8_t *x, *w; const float *sx, *sw, *b; void *y;
+    int64_t M, N, K, ldx, ldw; int32_t y_dtype;
+};
+hipError_t launch_dense_q8(const DenseQ8Params &p, hipStream_t s);
+// linear_scan.hip.  keep null: every row a token.  Forward: h, hT.  Gradient: dh, dhT -> dz, dh0
+struct ScanParams {
+    const void *z; const float *h0; const int8_t *keep;
+    void *h; float *hT;
+    const void *dh; const float *dhT; void *dz; float *dh0;
+    float *part;
+    int64_t B, T, D; int32_t dtype;
+};
+int64_t scan_part_floats(const ScanParams &p, bool grad);      // scratch that the launch wants at part
+hipError_t launch_scan(const ScanParams &p, hipStream_t s);
+hipError_t launch_scan_grad(const ScanParams &p, hipStream_t s);
+// token_logprobs.hip
+struct LogprobsParams {
+    const void *x; const int32_t *tok;
+    float *lp, *ent, *top_lp; int32_t *top_id;
+    const float *dlp, *dent; void *dx;
+    float *part;
+    int64_t M, V; int32_t dtype, top;
+};
+int64_t logprobs_part_floats(const LogprobsParams &p, bool grad);
+hipError_t launch_logprobs(const LogprobsParams &p, hipStream_t s);
+hipError_t launch_logprobs_grad(const LogprobsParams &p, hipStream_t s);
+
 // measurement aid (calibrate.hip): a chain of register-operand bf16 MFMAs per wave; out holds grid * 512 floats
 hipError_t launch_mfma_peak(float *out, int32_t grid, int32_t iters, hipStream_t s);
 hipError_t launch_fold_bn(const float *w, const float *gamma, const float *beta, const float *mean, const float *var,

@@ -991,6 +991,132 @@ struct Planner {
         return RL_OK;
     }
 
+    // ---- a gated recurrent language model ----
+    // the operands of call o, in the order of its Shape, into the step's slots
+    rl_status operands(const OpNode &o, std::initializer_list<int> slots, int *slot)
+    {
+        size_t i = 0;
+        for (int sl : slots) {
+            if (i >= o.in.size()) break;
+            rl_status st = need(o.in[i++], L_NATIVE, slot[sl]);
+            if (st != RL_OK) return st;
+        }
+        return RL_OK;
+    }
+    // a step of the call with those operands; its results into the slots of `outs`, in order
+    Step &call_step(int kind, int gi, int oi, const char *kernel, const int *slot, std::initializer_list<int> outs)
+    {
+        const OpNode &o = g.ops[oi];
+        int to[RL_MAX_RESULTS];
+        size_t n = 0;
+        for (int v : o.out) to[n++] = out_buf(v, L_NATIVE);
+        Step &s = add_step(kind, std::string(op_name(o.kind)) + "#" + std::to_string(oi), kernel);
+        s.group = gi;
+        std::copy(slot, slot + SL_COUNT, s.slot);
+        n = 0;
+        for (int sl : outs)
+            if (n < o.out.size()) s.slot[sl] = to[n++];
+        for (int v : o.in) s.bytes += (double)bytes_of(v);
+        for (int v : o.out) s.bytes += (double)bytes_of(v);
+        return s;
+    }
+
+    rl_status plan_norm_q8(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const bool res = o.in.size() == 3;
+        const rl_type &x = T(o.in[0]);
+        Step t;
+        rl_status st = res ? operands(o, {SL_X, SL_X2, SL_W}, t.slot) : operands(o, {SL_X, SL_W}, t.slot);
+        if (st != RL_OK) return st;
+        NormQ8Params p{};
+        p.M = x.dims[0]; p.D = x.dims[1]; p.dtype = x.dtype; p.g_dtype = T(o.in.back()).dtype; p.eps = o.attrs.eps;
+        if (p.M > 0x7fffffff || p.D > 0x7fffffff) return fail(RL_ERR_UNSUPPORTED, "rms_norm_q8: more rows or columns than a launch has");
+        Step &s = call_step(S_NORM_Q8, gi, oi, "rms_norm_q8", t.slot, {SL_Y, SL_COUT, SL_HOUT});
+        s.nq = p;
+        s.flops = 8.0 * numel(x);
+        return RL_OK;
+    }
+
+    rl_status plan_dense_q8(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const rl_type &x = T(o.in[0]), &w = T(o.in[2]);
+        const int64_t M = x.dims[0], K = x.dims[1], N = w.dims[0];
+        if (K > 131071) return fail(RL_ERR_UNSUPPORTED, "dense_q8: a sum of more than 131071 products may not fit 32 bits");
+        if (M > 0x7fffffff || N > 0x7fffffff) return fail(RL_ERR_UNSUPPORTED, "dense_q8: more rows or columns than a launch has");
+        Step t;
+        rl_status st = operands(o, {SL_X, SL_E0, SL_W, SL_E1, SL_E2}, t.slot);
+        if (st != RL_OK) return st;
+        DenseQ8Params p{};
+        p.M = M; p.N = N; p.K = K; p.ldx = K; p.ldw = round_up(K, 128); p.y_dtype = T(o.out[0]).dtype;
+        auto padded = [&](int src, int64_t rows, int64_t ld) {
+            const int dst = new_ws((size_t)(rows * ld));
+            Step &c = add_step(S_PAD_BYTES, std::string(op_name(o.kind)) + "#" + std::to_string(oi) + ".rows", "pad_bytes");
+            c.group = gi;
+            c.pb = {rows, K, ld};
+            c.slot[SL_X] = src; c.slot[SL_Y] = dst;
+            c.bytes = (double)rows * (K + ld);
+            return dst;
+        };
+        if (K % 128 != 0) {                       // zeros behind a row of w make what stands behind a row of x not count
+            const int wv = o.in[2];
+            if (g.values[wv].role == ROLE_PARAM && consumers[wv].size() == 1 && !out_set.count(wv)) {
+                PackSpec pack;
+                pack.pad = 1; pack.pb = {N, K, p.ldw}; pack.dtype = RL_I8; pack.bytes = (size_t)(N * p.ldw);
+                plan.packs[wv] = pack;
+            } else {
+                t.slot[SL_W] = padded(t.slot[SL_W], N, p.ldw);
+            }
+        }
+        if (K % 16 != 0) {                        // rows of x that start on 16 bytes
+            p.ldx = round_up(K, 16);
+            t.slot[SL_X] = padded(t.slot[SL_X], M, p.ldx);
+        }
+        Step &s = call_step(S_DENSE_Q8, gi, oi, "dense_q8", t.slot, {SL_Y});
+        s.dq = p;
+        s.flops = 2.0 * M * N * K;
+        return RL_OK;
+    }
+
+    rl_status plan_scan(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const bool grad = o.kind == RL_OP_LINEAR_SCAN_GRAD;
+        const rl_type &z = T(o.in[0]), &h0 = T(o.in[1]);
+        Step t;
+        rl_status st = grad ? operands(o, {SL_X, SL_CIN, SL_X2, SL_E1, SL_E0}, t.slot) : operands(o, {SL_X, SL_CIN, SL_E0}, t.slot);
+        if (st != RL_OK) return st;
+        ScanParams p{};
+        p.B = h0.dims[0]; p.D = h0.dims[1]; p.T = z.dims[0] / p.B; p.dtype = z.dtype;
+        if (p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > 0x3fffffff) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": sizes past 31 bits");
+        const int64_t scratch = scan_part_floats(p, grad);
+        if (scratch > 0) t.slot[SL_PART] = new_ws((size_t)scratch * 4);
+        Step &s = call_step(grad ? S_SCAN_GRAD : S_SCAN, gi, oi, grad ? "linear_scan_grad" : "linear_scan", t.slot, {SL_Y, SL_COUT});
+        s.sc = p;
+        s.flops = (grad ? 30.0 : 12.0) * numel(z) / 2;
+        return RL_OK;
+    }
+
+    rl_status plan_logprobs(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const bool grad = o.kind == RL_OP_TOKEN_LOGPROBS_GRAD;
+        const rl_type &x = T(o.in[0]);
+        Step t;
+        rl_status st = operands(o, {SL_X, SL_W, SL_E0, SL_E1}, t.slot);
+        if (st != RL_OK) return st;
+        LogprobsParams p{};
+        p.M = x.dims[0]; p.V = x.dims[1]; p.dtype = x.dtype; p.top = o.attrs.top;
+        if (p.M > 0x7fffffff) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows than a launch has");
+        const int64_t scratch = logprobs_part_floats(p, grad);
+        if (scratch > 0) t.slot[SL_PART] = new_ws((size_t)scratch * 4);
+        Step &s = call_step(grad ? S_LOGPROBS_GRAD : S_LOGPROBS, gi, oi, grad ? "token_logprobs_grad" : "token_logprobs", t.slot, {SL_Y, SL_COUT, SL_HOUT, SL_OUT4});
+        s.lg = p;
+        s.flops = (grad ? 8.0 : 5.0) * numel(x);
+        return RL_OK;
+    }
+
     // ---- partial derivatives of the contractions --------------------------------
     // Each is again a contraction C[m, n] = sum_k A[m, k] Wp[n, k] once its operands are looked at the right way round:
     //   dense_grad_x   m = batch row,       n = input feature k',  k = output feature:   A = dy,            Wp[k'][n] = W[n][k']
@@ -1422,6 +1548,10 @@ struct Planner {
             if (k0 == RL_OP_LSTM_GATES) return plan_gates(gi, ops[0]);
             if (k0 == RL_OP_LAYOUT_TRANSFORM) return plan_layout(gi, ops[0]);
             if (k0 >= RL_OP_DENSE_GRAD_X && k0 <= RL_OP_CONV2D_GRAD_W) return plan_grad(gi, ops[0]);
+            if (k0 == RL_OP_RMS_NORM_Q8) return plan_norm_q8(gi, ops[0]);
+            if (k0 == RL_OP_DENSE_Q8) return plan_dense_q8(gi, ops[0]);
+            if (k0 == RL_OP_LINEAR_SCAN || k0 == RL_OP_LINEAR_SCAN_GRAD) return plan_scan(gi, ops[0]);
+            if (k0 == RL_OP_TOKEN_LOGPROBS || k0 == RL_OP_TOKEN_LOGPROBS_GRAD) return plan_logprobs(gi, ops[0]);
             if (k0 == RL_OP_CONCAT) return fail(RL_ERR_UNSUPPORTED, "concat is only implemented as the operand of a dense in its group");
         }
         return plan_eltwise(gi, ops);
@@ -1858,7 +1988,7 @@ struct Planner {
                     bool apart = true;
                     for (size_t k = si; k < sj; ++k) {
                         for (int q : plan.steps[k].slot) apart &= q < 0 || q != mv[SL_Y];
-                        for (int q : {SL_Y, SL_COUT, SL_HOUT, SL_PART}) apart &= mv[SL_X] < 0 || plan.steps[k].slot[q] != mv[SL_X];
+                        for (int q : {SL_Y, SL_COUT, SL_HOUT, SL_PART, SL_OUT4}) apart &= mv[SL_X] < 0 || plan.steps[k].slot[q] != mv[SL_X];
                     }
                     if (apart && moves_pair_ok(move_params(plan.steps[si]), move_params(plan.steps[sj])))
                         std::rotate(plan.steps.begin() + (long)si + 1, plan.steps.begin() + (long)sj, plan.steps.begin() + (long)sj + 1);
@@ -2143,6 +2273,46 @@ rl_status run_steps(const Plan &plan, void *const *ptrs, hipStream_t stream, std
             PermuteParams p = s.pe;
             p.x = P(s, SL_X); p.y = P(s, SL_Y);
             er = launch_permute(p, stream);
+            break;
+        }
+        case S_PAD_BYTES:
+            er = launch_pad_bytes(P(s, SL_X), P(s, SL_Y), s.pb, stream);
+            break;
+        case S_NORM_Q8: {
+            NormQ8Params p = s.nq;
+            p.x = P(s, SL_X); p.r = P(s, SL_X2); p.g = P(s, SL_W); p.q = (int8_t *)P(s, SL_Y); p.s = (float *)P(s, SL_COUT); p.y = P(s, SL_HOUT);
+            er = launch_norm_q8(p, stream);
+            break;
+        }
+        case S_DENSE_Q8: {
+            DenseQ8Params p = s.dq;
+            p.x = (const int8_t *)P(s, SL_X); p.sx = (const float *)P(s, SL_E0); p.w = (const int8_t *)P(s, SL_W);
+            p.sw = (const float *)P(s, SL_E1); p.b = (const float *)P(s, SL_E2); p.y = P(s, SL_Y);
+            er = launch_dense_q8(p, stream);
+            break;
+        }
+        case S_SCAN: case S_SCAN_GRAD: {
+            ScanParams p = s.sc;
+            p.z = P(s, SL_X); p.h0 = (const float *)P(s, SL_CIN); p.keep = (const int8_t *)P(s, SL_E0); p.part = (float *)P(s, SL_PART);
+            if (s.kind == S_SCAN) {
+                p.h = P(s, SL_Y); p.hT = (float *)P(s, SL_COUT);
+                er = launch_scan(p, stream);
+            } else {
+                p.dh = P(s, SL_X2); p.dhT = (const float *)P(s, SL_E1); p.dz = P(s, SL_Y); p.dh0 = (float *)P(s, SL_COUT);
+                er = launch_scan_grad(p, stream);
+            }
+            break;
+        }
+        case S_LOGPROBS: case S_LOGPROBS_GRAD: {
+            LogprobsParams p = s.lg;
+            p.x = P(s, SL_X); p.tok = (const int32_t *)P(s, SL_W); p.part = (float *)P(s, SL_PART);
+            if (s.kind == S_LOGPROBS) {
+                p.lp = (float *)P(s, SL_Y); p.ent = (float *)P(s, SL_COUT); p.top_lp = (float *)P(s, SL_HOUT); p.top_id = (int32_t *)P(s, SL_OUT4);
+                er = launch_logprobs(p, stream);
+            } else {
+                p.dlp = (const float *)P(s, SL_E0); p.dent = (const float *)P(s, SL_E1); p.dx = P(s, SL_Y);
+                er = launch_logprobs_grad(p, stream);
+            }
             break;
         }
         case S_PACK:

@@ -11,8 +11,9 @@
 
 namespace rl {
 
-enum StepKind { S_IGEMM = 0, S_ELTWISE, S_GATES, S_MAXPOOL, S_GAVG, S_TO_NHWC, S_TO_NCHW, S_STEM_PAD, S_STEM_POOL, S_PERMUTE, S_PACK, S_WGRAD, S_WGRAD_REDUCE, S_DILATE, S_TN, S_PAD_NHWC };
-enum Slot { SL_X = 0, SL_X2, SL_W, SL_Y, SL_E0, SL_E1, SL_E2, SL_E3, SL_E4, SL_E5, SL_CIN, SL_COUT, SL_HOUT, SL_PART, SL_COUNT };
+enum StepKind { S_IGEMM = 0, S_ELTWISE, S_GATES, S_MAXPOOL, S_GAVG, S_TO_NHWC, S_TO_NCHW, S_STEM_PAD, S_STEM_POOL, S_PERMUTE, S_PACK, S_WGRAD, S_WGRAD_REDUCE, S_DILATE, S_TN, S_PAD_NHWC, S_PAD_BYTES,
+                S_NORM_Q8, S_DENSE_Q8, S_SCAN, S_SCAN_GRAD, S_LOGPROBS, S_LOGPROBS_GRAD };
+enum Slot { SL_X = 0, SL_X2, SL_W, SL_Y, SL_E0, SL_E1, SL_E2, SL_E3, SL_E4, SL_E5, SL_CIN, SL_COUT, SL_HOUT, SL_PART, SL_OUT4, SL_COUNT };
 
 struct BufDesc {
     int bound_value = -1;     // >= 0: caller-bound pointer of that value id; -1: workspace
@@ -35,6 +36,8 @@ struct Step {
     TnParams tn{}; int tn_tile = 0;     // S_TN (tile 0: igemm_tn_run.hip)
     double tn_cost = 0;                 // ... estimate of the square tile's time, shader cycles
     GatherPack gp{};                    // S_PACK: an activation gathered into the K-contiguous rows a contraction reads
+    PadBytes pb{};                      // S_PAD_BYTES
+    NormQ8Params nq{}; DenseQ8Params dq{}; ScanParams sc{}; LogprobsParams lg{};
     int t_dtype = 0, t_N = 0, t_C = 0, t_P = 0;
     int st_H = 0, st_W = 0, st_Hp = 0, st_Wp = 0, st_ph = 0, st_pw = 0;   // S_STEM_PAD geometry (t_N, t_C: batch, channels)
     int stem = 0;                       // S_IGEMM: the few-channel stem form (padded 4-channel frame, regrouped taps)
@@ -57,12 +60,13 @@ struct PackSpec {
     int stem = 0, KH = 0, KW = 0;      // stem = 1: few-channel stem layout (launch_pack_weight_stem); 2: launch_pack_weight_stem_direct
     int pw = 0;                         // stem = 2: the convolution's left padding (its parity shifts the filter inside the 8-pixel window)
     int gather = 0; GatherPack gp{};   // gather = 1: launch_pack_gather (operands of the gradient operators)
+    int pad = 0; PadBytes pb{};        // pad = 1: launch_pad_bytes (8-bit weights)
     size_t bytes = 0;
     bool operator==(const PackSpec &o) const
     {
         auto all = [](const PackSpec &k) {
             return std::make_tuple(k.dtype, k.O, k.C, k.T, k.Kp, k.perm_block, k.stem, k.KH, k.KW, k.pw, k.gather, k.bytes, k.gp.dtype, k.gp.R, k.gp.Kp,
-                                   k.gp.T, k.gp.Cq, k.gp.TW, k.gp.base, k.gp.s_row, k.gp.s_c, k.gp.s_ti, k.gp.s_tj, k.gp.Creal);
+                                   k.gp.T, k.gp.Cq, k.gp.TW, k.gp.base, k.gp.s_row, k.gp.s_c, k.gp.s_ti, k.gp.s_tj, k.gp.Creal, k.pad, k.pb.R, k.pb.K, k.pb.Kp);
         };
         return all(*this) == all(o);
     }
