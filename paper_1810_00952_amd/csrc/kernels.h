@@ -338,15 +338,19 @@ struct DenseQ8Params {
     int64_t M, N, K, ldx, ldw; int32_t y_dtype;
 };
 hipError_t launch_dense_q8(const DenseQ8Params &p, hipStream_t s);
-// linear_scan.hip.  keep null: every row a token.  Forward: h, hT.  Gradient: dh, dhT -> dz, dh0
+// linear_scan.hip.  keep null: every row a token.  Forward: h, hT (either may be null).  Gradient: dh, dhT -> dz, dh0.
+// states: the state before every state_rows-th row, [B][ceil(T / state_rows)][D]: the forward pass writes it where it is not null, the
+// gradient reads it where scan_state_rows is not 0, which is what state_rows then is
 struct ScanParams {
     const void *z; const float *h0; const int8_t *keep;
     void *h; float *hT;
     const void *dh; const float *dhT; void *dz; float *dh0;
-    float *part;
-    int64_t B, T, D; int32_t dtype;
+    float *part, *states;
+    int64_t B, T, D, state_rows; int32_t dtype;
 };
+constexpr int64_t SCAN_MAX_D = (int64_t)1 << 20;
 int64_t scan_part_floats(const ScanParams &p, bool grad);      // scratch that the launch wants at part
+int64_t scan_state_rows(const ScanParams &p);
 hipError_t launch_scan(const ScanParams &p, hipStream_t s);
 hipError_t launch_scan_grad(const ScanParams &p, hipStream_t s);
 // token_logprobs.hip

@@ -5,95 +5,566 @@
 // and its gradient, the same recurrence backwards: G_t = dh_t + a_(t+1) G_(t+1),
 //   dv_t = G_t (1 - a_t),   df_t = G_t (h_(t-1) - v_t) a_t (1 - a_t).
 // keep[t] = 0: padding, which holds the state; 2: the state before it is zero.
-#include "device_utils.h"
+//
+// A run of rows takes the state before it to A h + H, with A the product of its gates and H its own result from zero, and two runs
+// one behind the other join as (A2 A1, A2 H1 + H2).  So a tile of 32 W runs of ROWS rows is worked off at once: a workgroup of W waves
+// owns 32 lanes x 4 bytes of channels (whole 128-byte lines) and each half of a wave one run, which it reads once, into registers:
+// prefix products and results of its rows from zero.  The runs' (A, H) meet in LDS, every run adds up those before it, and one fma a
+// row then gives the states.  The workgroup carries the tile's last state on to its next tile, whose rows are requested as
+// the registers of this one's become free.  Nothing is read twice.  What bounds it is HBM.
+//
+// Few channels and many rows: each tile is a workgroup of its own.  A launch ahead finds the tiles' (A, H) (and, of the gradient, G),
+// and every workgroup adds up those before (behind) its tile, at the cost of a second read.
+#include <type_traits>
+
+#include "igemm_lds.h"
 
 namespace rl {
 
 namespace {
 
-// sigmoid(f) and 1 - sigmoid(f), each to its own last bits
+constexpr int FWD_ROWS = 16, BWD_ROWS = 8;      // rows of a run: as many as fit the registers of two waves a SIMD with what they become
+
+// sigmoid(f) and 1 - sigmoid(f), each to its own last bits.  Below -80 the gate stays at e^-80, which no f32 state is changed by.
 __device__ __forceinline__ void gate(float f, float &a, float &rest)
 {
-    a = rcp_(1.0f + __expf(-f));
-    rest = rcp_(1.0f + __expf(f));
+    const float e = __expf(-(f < -80.0f ? -80.0f : f));      // NaN stays NaN
+    a = rcp_(1.0f + e);
+    rest = e * a;
+}
+
+// 4 bytes (two bf16, one f32) or one bf16 of a row
+template <typename E, int VEC> struct Raw { typedef uint32_t type; };
+template <> struct Raw<uint16_t, 1> { typedef uint16_t type; };
+
+template <typename E, int VEC> __device__ __forceinline__ float unpack(typename Raw<E, VEC>::type r, int j)
+{
+    if constexpr (sizeof(E) == 4) return __uint_as_float(r);
+    else return j == 0 ? __uint_as_float((uint32_t)r << 16) : __uint_as_float((uint32_t)r & 0xffff0000u);
+}
+
+template <typename E, int VEC> __device__ __forceinline__ typename Raw<E, VEC>::type pack(const float (&v)[VEC])
+{
+    if constexpr (sizeof(E) == 4) return __float_as_uint(v[0]);
+    else return (typename Raw<E, VEC>::type)pack_bf16x2(v[0], v[VEC - 1]);
+}
+
+// Rows of a tile in memory: `room` bytes from the tile's first row to the sequence's last.  What lies behind them reads as zero and is
+// not written; so does what a lane without channels (offset OOB) asks for.
+struct Rows { rsrc_t rsrc; };
+__device__ __forceinline__ Rows rows_at(const void *first, int64_t room)
+{
+    return {make_rsrc(first, (uint32_t)(room < 0x7fffffff ? room : 0x7fffffff))};
+}
+template <typename R> __device__ __forceinline__ R load(const Rows &r, uint32_t off)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(R) == 4) return __builtin_amdgcn_raw_buffer_load_b32(r.rsrc, off, 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b16(r.rsrc, off, 0, 0);
+#else
+    return 0;
+#endif
+}
+template <typename R> __device__ __forceinline__ void store(const Rows &r, uint32_t off, R v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(R) == 4) __builtin_amdgcn_raw_buffer_store_b32(v, r.rsrc, off, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(v, r.rsrc, off, 0, 0);
+#endif
+}
+// a value the compiler takes as new: the offsets of a tile's rows are added up where they are used, not kept in registers
+__device__ __forceinline__ uint32_t anew(uint32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// What a lane works on: its channels of sequence b and its run of the tile's rows
+template <typename E, int VEC, int ROWS, int W>
+struct Place {
+    static constexpr int TILE = 2 * W * ROWS;
+    int wave, half, run;
+    int32_t b, d, seg;                           // seg: blockIdx's tile where tiles are workgroups
+    bool live;                                   // the channels exist
+    uint32_t off1, off2;                         // bytes from a tile's first row to the run's, in rows of D and of 2 D
+    __device__ __forceinline__ Place(const ScanParams &p, int32_t slabs)
+    {
+        const int lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        half = lane >> 5;
+        run = 2 * wave + half;
+        const uint32_t bid = blockIdx.x, rest = bid / (uint32_t)slabs, B = (uint32_t)p.B;
+        seg = (int32_t)(rest / B);
+        b = (int32_t)(rest - seg * B);
+        d = (int32_t)((bid - rest * slabs) * 32 + (lane & 31)) * VEC;
+        live = d < p.D;
+        if (!live) d = 0;                        // its state is some other channel's, and nothing of it is stored
+        off1 = live ? (uint32_t)((run * ROWS * (uint32_t)p.D + d) * sizeof(E)) : OOB;
+        off2 = live ? (uint32_t)((run * ROWS * 2 * (uint32_t)p.D + d) * sizeof(E)) : OOB;
+    }
+};
+
+// bit i: row t0 + i is padding (or past the sequence), is a document's first
+template <int ROWS> struct Flags { uint32_t pad, first; };
+template <int ROWS, bool KEEP>
+__device__ __forceinline__ Flags<ROWS> flags_of(const ScanParams &p, int64_t b, int64_t t0, int half)
+{
+    const int i = threadIdx.x & 31;
+    const bool in = i < ROWS && t0 + i < p.T;
+    const int k = !in ? 0 : KEEP ? p.keep[b * p.T + t0 + i] : 1;
+    const uint64_t pad = __ballot(k == 0), first = __ballot(k == 2);
+    return {(uint32_t)(pad >> (32 * half)), (uint32_t)(first >> (32 * half))};
 }
 
 }  // namespace
 
-__global__ __launch_bounds__(64) void linear_scan_kernel(const ScanParams p)
+// ---------------------------------------------------------------------------
+// one token a sequence
+// ---------------------------------------------------------------------------
+template <typename E, int VEC>
+__global__ __launch_bounds__(256) void linear_scan_step_kernel(const ScanParams p, int64_t total)
 {
-    const int64_t c = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    if (c >= p.B * p.D) return;
-    const int64_t b = c / p.D, d = c - b * p.D;
-    float h = p.h0[c];
-    for (int64_t t = 0; t < p.T; ++t) {
-        const int64_t row = b * p.T + t;
-        const int keep = p.keep ? p.keep[row] : 1;
-        float out = 0.0f;
-        if (keep) {
-            float a, rest;
-            gate(load_as_f32(p.z, p.dtype, row * 2 * p.D + d), a, rest);
-            const float u = rest * load_as_f32(p.z, p.dtype, row * 2 * p.D + p.D + d);
-            h = keep == 2 ? u : __builtin_fmaf(a, h, u);
-            out = h;
-        }
-        store_from_f32(p.h, p.dtype, row * p.D + d, out);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int64_t c = i * VEC, b = c / p.D, d = c - b * p.D;
+    typedef typename Raw<E, VEC>::type raw_t;
+    const raw_t f = *(const raw_t *)((const E *)p.z + 2 * b * p.D + d), v = *(const raw_t *)((const E *)p.z + (2 * b + 1) * p.D + d);
+    const int keep = p.keep ? p.keep[b] : 1;
+    float out[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        float a, rest, h = p.h0[c + j];
+        gate(unpack<E, VEC>(f, j), a, rest);
+        const float u = rest * unpack<E, VEC>(v, j);
+        if (keep) h = keep == 2 ? u : __builtin_fmaf(a, h, u);
+        p.hT[c + j] = h;
+        out[j] = keep ? h : 0.0f;
     }
-    p.hT[c] = h;
+    *(raw_t *)((E *)p.h + c) = pack<E, VEC>(out);
 }
 
-__global__ __launch_bounds__(64) void linear_scan_grad_kernel(const ScanParams p)
+// ---------------------------------------------------------------------------
+// forward.  MODE 0: a workgroup walks its channels' tiles; 1: (A, H) of one tile into part; 2: one tile, after those before it
+// ---------------------------------------------------------------------------
+template <typename E, int VEC, int W, int MODE, bool KEEP>
+__global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
 {
-    const int64_t c = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    if (c >= p.B * p.D) return;
-    const int64_t b = c / p.D, d = c - b * p.D;
-    float h = p.h0[c];
-    for (int64_t t = 0; t < p.T; ++t) {                     // the states between, into the scratch
-        const int64_t row = b * p.T + t;
-        const int keep = p.keep ? p.keep[row] : 1;
-        p.part[row * p.D + d] = keep == 2 ? 0.0f : h;
-        if (keep) {
-            float a, rest;
-            gate(load_as_f32(p.z, p.dtype, row * 2 * p.D + d), a, rest);
-            const float u = rest * load_as_f32(p.z, p.dtype, row * 2 * p.D + p.D + d);
-            h = keep == 2 ? u : __builtin_fmaf(a, h, u);
+    constexpr int ROWS = FWD_ROWS;
+    typedef Place<E, VEC, ROWS, W> P;
+    typedef typename Raw<E, VEC>::type raw_t;
+    const P at(p, slabs);
+    const int64_t BD = p.B * p.D, chan = at.b * p.D + at.d;
+    const uint32_t line = (uint32_t)p.D * sizeof(E);
+    __shared__ float sa[2][W][32][VEC], sh[2][W][32][VEC];
+    const int l32 = threadIdx.x & 31;
+
+    raw_t rf[ROWS], rv[ROWS];
+    auto rows_of = [&](const void *x, int64_t tile, int wide) {              // rows of `wide` lines
+        const int64_t t = tile * P::TILE;
+        return rows_at((const char *)x + (at.b * p.T + t) * wide * line, (p.T - t) * wide * line);
+    };
+    const int32_t first_tile = MODE ? at.seg : 0, last_tile = MODE ? at.seg + 1 : tiles;
+    Rows z = rows_of(p.z, first_tile, 2);
+    auto request = [&](uint32_t off, int i) {
+        rf[i] = load<raw_t>(z, off + 2 * i * line);
+        rv[i] = load<raw_t>(z, off + (2 * i + 1) * line);
+    };
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) request(at.off2, i);
+
+    float carry[VEC];
+    if (MODE != 1) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) carry[j] = p.h0[chan + j];
+        if (MODE == 2)
+            for (int32_t s = 0; s < at.seg; ++s)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) carry[j] = __builtin_fmaf(p.part[2 * s * BD + chan + j], carry[j], p.part[(2 * s + 1) * BD + chan + j]);
+    }
+    for (int32_t tile = first_tile; tile < last_tile; ++tile) {
+        const int64_t t0 = (int64_t)tile * P::TILE + at.run * ROWS;
+        const bool whole = (int64_t)(tile + 1) * P::TILE <= p.T;
+        const uint32_t off2 = anew(at.off2), off1 = anew(at.off1);
+        if (MODE == 0 && tile + 1 < last_tile) z = rows_of(p.z, tile + 1, 2);
+        float A[ROWS][VEC], H[ROWS][VEC];
+        Flags<ROWS> fl{0, 0};
+        float pa[VEC], ph[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) { pa[j] = 1.0f; ph[j] = 0.0f; }
+        auto rows = [&](auto masked) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float a, rest;
+                    gate(unpack<E, VEC>(rf[i], j), a, rest);
+                    float u = rest * unpack<E, VEC>(rv[i], j);
+                    if (masked) {
+                        const bool pad = fl.pad >> i & 1u;
+                        a = pad ? 1.0f : fl.first >> i & 1u ? 0.0f : a;
+                        u = pad ? 0.0f : u;
+                    }
+                    pa[j] *= a;
+                    ph[j] = __builtin_fmaf(a, ph[j], u);
+                    A[i][j] = pa[j]; H[i][j] = ph[j];
+                }
+                if (MODE == 0 && tile + 1 < last_tile) request(off2, i);
+            }
+        };
+        if (KEEP || !whole) {
+            fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
+            rows(std::true_type{});
+        } else {
+            rows(std::false_type{});
+        }
+        // the wave's two runs as one, the waves' in LDS
+        float oa[VEC], oh[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) { oa[j] = __shfl_xor(pa[j], 32); oh[j] = __shfl_xor(ph[j], 32); }
+        const int buf = MODE == 0 ? tile & 1 : 0;
+        if (at.half) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                sa[buf][at.wave][l32][j] = pa[j] * oa[j];
+                sh[buf][at.wave][l32][j] = __builtin_fmaf(pa[j], oh[j], ph[j]);
+            }
+        }
+        if (W > 1) __syncthreads(); else wave_lds_exchange();
+        float mine[VEC], end[VEC];
+        if (MODE == 1) {
+            if (at.run == 0 && at.live) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float ta = 1.0f, th = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) { th = __builtin_fmaf(sa[0][w][l32][j], th, sh[0][w][l32][j]); ta *= sa[0][w][l32][j]; }
+                    p.part[2 * at.seg * BD + chan + j] = ta;
+                    p.part[(2 * at.seg + 1) * BD + chan + j] = th;
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float c = carry[j];
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                if (w == at.wave) mine[j] = c;
+                c = __builtin_fmaf(sa[buf][w][l32][j], c, sh[buf][w][l32][j]);
+            }
+            end[j] = c;
+            if (at.half) mine[j] = __builtin_fmaf(oa[j], mine[j], oh[j]);
+            carry[j] = end[j];
+        }
+        if (at.live) {
+            if (p.states && t0 % p.state_rows == 0 && t0 < p.T) {
+                const int64_t count = (p.T + p.state_rows - 1) / p.state_rows;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.states[(at.b * count + t0 / p.state_rows) * p.D + at.d + j] = mine[j];
+            }
+            if (p.h) {
+                const Rows h = rows_of(p.h, tile, 1);
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    float out[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        out[j] = __builtin_fmaf(A[i][j], mine[j], H[i][j]);
+                        if (KEEP && (fl.pad >> i & 1u)) out[j] = 0.0f;
+                    }
+                    store(h, off1 + i * line, pack<E, VEC>(out));
+                }
+            }
+            if (p.hT && tile + 1 == tiles && at.run == 0) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.hT[chan + j] = end[j];
+            }
         }
     }
-    float G = p.dhT[c];
-    for (int64_t t = p.T - 1; t >= 0; --t) {
-        const int64_t row = b * p.T + t;
-        const int keep = p.keep ? p.keep[row] : 1;
-        float df = 0.0f, dv = 0.0f;
-        if (keep) {
-            float a, rest;
-            gate(load_as_f32(p.z, p.dtype, row * 2 * p.D + d), a, rest);
-            const float v = load_as_f32(p.z, p.dtype, row * 2 * p.D + p.D + d);
-            G += load_as_f32(p.dh, p.dtype, row * p.D + d);
-            dv = G * rest;
-            df = dv * (p.part[row * p.D + d] - v) * a;
-            G = keep == 2 ? 0.0f : a * G;
-        }
-        store_from_f32(p.dz, p.dtype, row * 2 * p.D + d, df);
-        store_from_f32(p.dz, p.dtype, row * 2 * p.D + p.D + d, dv);
-    }
-    p.dh0[c] = G;
 }
 
-int64_t scan_part_floats(const ScanParams &p, bool grad) { return grad ? p.B * p.T * p.D : 0; }
+// ---------------------------------------------------------------------------
+// gradient.  MODE as above, tiles from the last to the first; part: A, H, G of a tile.  The state before a tile comes from p.states
+// (MODE 0) or from the tiles before it (MODE 2).
+// ---------------------------------------------------------------------------
+template <typename E, int VEC, int W, int MODE, bool KEEP>
+__global__ __launch_bounds__(64 * W) void linear_scan_grad_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
+{
+    constexpr int ROWS = BWD_ROWS;
+    typedef Place<E, VEC, ROWS, W> P;
+    typedef typename Raw<E, VEC>::type raw_t;
+    const P at(p, slabs);
+    const int64_t BD = p.B * p.D, chan = at.b * p.D + at.d;
+    const uint32_t line = (uint32_t)p.D * sizeof(E);
+    __shared__ float sa[2][W][32][VEC], sh[2][W][32][VEC], sg[2][W][32][VEC];
+    const int l32 = threadIdx.x & 31;
 
-static bool sizes_ok(const ScanParams &p) { return p.B >= 1 && p.T >= 1 && p.D >= 1 && (p.B * p.D + 63) / 64 <= 0x7fffffff; }
+    raw_t rf[ROWS], rv[ROWS], rd[ROWS];
+    auto rows_of = [&](const void *x, int64_t tile, int wide) {              // rows of `wide` lines
+        const int64_t t = tile * P::TILE;
+        return rows_at((const char *)x + (at.b * p.T + t) * wide * line, (p.T - t) * wide * line);
+    };
+    const int32_t first_tile = MODE ? at.seg : tiles - 1, last_tile = MODE ? at.seg - 1 : -1;
+    Rows z = rows_of(p.z, first_tile, 2), d = rows_of(p.dh, first_tile, 1);
+    auto request = [&](uint32_t off2, uint32_t off1, int i) {
+        rf[i] = load<raw_t>(z, off2 + 2 * i * line);
+        rv[i] = load<raw_t>(z, off2 + (2 * i + 1) * line);
+        rd[i] = load<raw_t>(d, off1 + i * line);
+    };
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) request(at.off2, at.off1, i);
+
+    const int64_t count = p.states ? (p.T + p.state_rows - 1) / p.state_rows : 0;
+    float gcarry[VEC], start[VEC];
+    if (MODE != 1) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) gcarry[j] = p.dhT[chan + j];
+        if (MODE == 2) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) start[j] = p.h0[chan + j];
+            for (int32_t s = 0; s < at.seg; ++s)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) start[j] = __builtin_fmaf(p.part[3 * s * BD + chan + j], start[j], p.part[(3 * s + 1) * BD + chan + j]);
+            for (int32_t s = tiles - 1; s > at.seg; --s)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) gcarry[j] = __builtin_fmaf(p.part[3 * s * BD + chan + j], gcarry[j], p.part[(3 * s + 2) * BD + chan + j]);
+        }
+    }
+    for (int32_t tile = first_tile; tile > last_tile; --tile) {
+        const int64_t t0 = (int64_t)tile * P::TILE + at.run * ROWS;
+        const bool whole = (int64_t)(tile + 1) * P::TILE <= p.T;
+        const uint32_t off2 = anew(at.off2), off1 = anew(at.off1);
+        if (MODE == 0 && tile > 0) { z = rows_of(p.z, tile - 1, 2); d = rows_of(p.dh, tile - 1, 1); }
+        if (MODE == 0) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) start[j] = tile ? p.states[(at.b * count + tile) * p.D + at.d + j] : p.h0[chan + j];
+        }
+        float a[ROWS][VEC], rest[ROWS][VEC], before[ROWS][VEC];   // before: of the state before the row, the run's own part
+        raw_t kv[ROWS], kd[ROWS];
+        float pa[VEC], ph[VEC], pg[VEC];
+        Flags<ROWS> fl{0, 0};
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) { pa[j] = 1.0f; ph[j] = 0.0f; pg[j] = 0.0f; }
+        auto rows = [&](auto masked) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    gate(unpack<E, VEC>(rf[i], j), a[i][j], rest[i][j]);
+                    float u = rest[i][j] * unpack<E, VEC>(rv[i], j);
+                    float af = a[i][j], dh = unpack<E, VEC>(rd[i], j);
+                    if (masked) {
+                        const bool pad = fl.pad >> i & 1u;
+                        dh = pad ? 0.0f : dh;
+                        af = pad ? 1.0f : fl.first >> i & 1u ? 0.0f : af;
+                        u = pad ? 0.0f : u;
+                    }
+                    before[i][j] = ph[j];
+                    pa[j] *= af;
+                    ph[j] = __builtin_fmaf(af, ph[j], u);
+                    pg[j] = __builtin_fmaf(pa[j], dh, pg[j]);
+                }
+                kv[i] = rv[i]; kd[i] = rd[i];
+                if (MODE == 0 && tile > 0) request(off2, off1, i);
+            }
+        };
+        if (KEEP || !whole) {
+            fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
+            rows(std::true_type{});
+        } else {
+            rows(std::false_type{});
+        }
+        float oa[VEC], oh[VEC], og[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) { oa[j] = __shfl_xor(pa[j], 32); oh[j] = __shfl_xor(ph[j], 32); og[j] = __shfl_xor(pg[j], 32); }
+        const int buf = MODE == 0 ? tile & 1 : 0;
+        if (at.half) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                sa[buf][at.wave][l32][j] = pa[j] * oa[j];
+                sh[buf][at.wave][l32][j] = __builtin_fmaf(pa[j], oh[j], ph[j]);
+                sg[buf][at.wave][l32][j] = __builtin_fmaf(oa[j], pg[j], og[j]);
+            }
+        }
+        if (W > 1) __syncthreads(); else wave_lds_exchange();
+        if (MODE == 1) {
+            if (at.run == 0 && at.live) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float ta = 1.0f, th = 0.0f, tg = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        tg = __builtin_fmaf(ta, sg[0][w][l32][j], tg);
+                        th = __builtin_fmaf(sa[0][w][l32][j], th, sh[0][w][l32][j]);
+                        ta *= sa[0][w][l32][j];
+                    }
+                    p.part[3 * at.seg * BD + chan + j] = ta;
+                    p.part[(3 * at.seg + 1) * BD + chan + j] = th;
+                    p.part[(3 * at.seg + 2) * BD + chan + j] = tg;
+                }
+            }
+            return;
+        }
+        float h[VEC], G[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float c = start[j], g = gcarry[j];
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                if (w == at.wave) h[j] = c;
+                c = __builtin_fmaf(sa[buf][w][l32][j], c, sh[buf][w][l32][j]);
+            }
+            if (at.half) h[j] = __builtin_fmaf(oa[j], h[j], oh[j]);
+#pragma unroll
+            for (int w = W - 1; w >= 0; --w) {
+                if (w == at.wave) G[j] = g;
+                g = __builtin_fmaf(sa[buf][w][l32][j], g, sg[buf][w][l32][j]);
+            }
+            if (!at.half) G[j] = __builtin_fmaf(oa[j], G[j], og[j]);
+            gcarry[j] = g;
+        }
+        if (at.live) {
+            // the state before every row, then the rows backwards
+            auto replay = [&](auto masked) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    float run = h[j];                        // the start times the gates so far
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) {
+                        before[i][j] += run;
+                        float af = a[i][j];
+                        if (masked) {
+                            if (fl.first >> i & 1u) before[i][j] = 0.0f;
+                            af = fl.pad >> i & 1u ? 1.0f : fl.first >> i & 1u ? 0.0f : af;
+                        }
+                        run *= af;
+                    }
+                }
+                const Rows dz = rows_of(p.dz, tile, 2);
+#pragma unroll
+                for (int i = ROWS - 1; i >= 0; --i) {
+                    float df[VEC], dv[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float g = G[j] + unpack<E, VEC>(kd[i], j);
+                        dv[j] = g * rest[i][j];
+                        df[j] = dv[j] * (before[i][j] - unpack<E, VEC>(kv[i], j)) * a[i][j];
+                        const float on = a[i][j] * g;
+                        if (masked) {
+                            const bool pad = fl.pad >> i & 1u;
+                            G[j] = pad ? G[j] : fl.first >> i & 1u ? 0.0f : on;
+                            dv[j] = pad ? 0.0f : dv[j];
+                            df[j] = pad ? 0.0f : df[j];
+                        } else {
+                            G[j] = on;
+                        }
+                    }
+                    store(dz, off2 + 2 * i * line, pack<E, VEC>(df));
+                    store(dz, off2 + (2 * i + 1) * line, pack<E, VEC>(dv));
+                }
+            };
+            if (KEEP || !whole) replay(std::true_type{});
+            else replay(std::false_type{});
+            if (tile == 0 && at.run == 0) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) p.dh0[chan + j] = gcarry[j];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+namespace {
+
+struct Form { int W; bool split; int32_t slabs, tiles; };
+
+// Waves of a workgroup: enough for the rows, eight where there are few workgroups.  split: tiles as workgroups of their own.
+Form form_of(const ScanParams &p, bool grad)
+{
+    const int64_t vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1, rows = grad ? BWD_ROWS : FWD_ROWS;
+    Form f;
+    f.slabs = (int32_t)((p.D + 32 * vec - 1) / (32 * vec));
+    const int64_t wgs = p.B * f.slabs;
+    f.W = p.T <= 2 * rows ? 1 : p.T <= 8 * rows || wgs >= 512 ? 4 : 8;
+    f.tiles = (int32_t)((p.T + 2 * f.W * rows - 1) / (2 * f.W * rows));
+    f.split = wgs < 128 && f.tiles > 1;
+    return f;
+}
+
+template <typename E, int VEC, int W, int MODE>
+void go(bool grad, const ScanParams &p, const Form &f, hipStream_t s)
+{
+    const dim3 grid((unsigned)(p.B * f.slabs * (MODE ? f.tiles : 1))), wg(64 * W);
+    if (grad) {
+        if (p.keep) hipLaunchKernelGGL((linear_scan_grad_kernel<E, VEC, W, MODE, true>), grid, wg, 0, s, p, f.slabs, f.tiles);
+        else hipLaunchKernelGGL((linear_scan_grad_kernel<E, VEC, W, MODE, false>), grid, wg, 0, s, p, f.slabs, f.tiles);
+    } else {
+        if (p.keep) hipLaunchKernelGGL((linear_scan_kernel<E, VEC, W, MODE, true>), grid, wg, 0, s, p, f.slabs, f.tiles);
+        else hipLaunchKernelGGL((linear_scan_kernel<E, VEC, W, MODE, false>), grid, wg, 0, s, p, f.slabs, f.tiles);
+    }
+}
+
+template <typename E, int VEC>
+void go(bool grad, int mode, const ScanParams &p, const Form &f, hipStream_t s)
+{
+    if (mode == 1) go<E, VEC, 8, 1>(grad, p, f, s);
+    else if (mode == 2) go<E, VEC, 8, 2>(grad, p, f, s);
+    else if (f.W == 1) go<E, VEC, 1, 0>(grad, p, f, s);
+    else if (f.W == 4) go<E, VEC, 4, 0>(grad, p, f, s);
+    else go<E, VEC, 8, 0>(grad, p, f, s);
+}
+
+void go(bool grad, int mode, const ScanParams &p, const Form &f, hipStream_t s)
+{
+    if (p.dtype != DT_BF16) go<float, 1>(grad, mode, p, f, s);
+    else if (p.D % 2 == 0) go<uint16_t, 2>(grad, mode, p, f, s);
+    else go<uint16_t, 1>(grad, mode, p, f, s);
+}
+
+bool sizes_ok(const ScanParams &p, const Form &f)
+{
+    // a tile's rows are reached by 31-bit offsets
+    return p.B >= 1 && p.T >= 1 && p.D >= 1 && p.T <= 0x7fffffff && p.D <= SCAN_MAX_D && p.B * f.slabs * f.tiles <= 0x7fffffff;
+}
+
+}  // namespace
+
+int64_t scan_state_rows(const ScanParams &p)
+{
+    const Form f = form_of(p, true);
+    return f.split || f.tiles == 1 ? 0 : 2 * f.W * BWD_ROWS;
+}
+
+int64_t scan_part_floats(const ScanParams &p, bool grad)
+{
+    const Form f = form_of(p, grad);
+    return f.split ? (grad ? 3 : 2) * f.tiles * p.B * p.D : 0;
+}
 
 hipError_t launch_scan(const ScanParams &p, hipStream_t s)
 {
-    if (!sizes_ok(p)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(linear_scan_kernel, dim3((unsigned)((p.B * p.D + 63) / 64)), dim3(64), 0, s, p);
+    const Form f = form_of(p, false);
+    if (!sizes_ok(p, f) || (f.split && !p.part) || (p.states && p.state_rows % FWD_ROWS != 0)) return hipErrorInvalidValue;
+    if (p.T == 1 && p.h) {
+        const int vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1;
+        const int64_t total = p.B * p.D / vec, blocks = (total + 255) / 256;
+        if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+        if (p.dtype != DT_BF16) hipLaunchKernelGGL((linear_scan_step_kernel<float, 1>), dim3((unsigned)blocks), dim3(256), 0, s, p, total);
+        else if (vec == 2) hipLaunchKernelGGL((linear_scan_step_kernel<uint16_t, 2>), dim3((unsigned)blocks), dim3(256), 0, s, p, total);
+        else hipLaunchKernelGGL((linear_scan_step_kernel<uint16_t, 1>), dim3((unsigned)blocks), dim3(256), 0, s, p, total);
+        return hipGetLastError();
+    }
+    if (f.split) go(false, 1, p, f, s);
+    go(false, f.split ? 2 : 0, p, f, s);
     return hipGetLastError();
 }
 
 hipError_t launch_scan_grad(const ScanParams &p, hipStream_t s)
 {
-    if (!sizes_ok(p)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(linear_scan_grad_kernel, dim3((unsigned)((p.B * p.D + 63) / 64)), dim3(64), 0, s, p);
+    const Form f = form_of(p, true);
+    if (!sizes_ok(p, f) || (f.split && !p.part) || (!f.split && f.tiles > 1 && (!p.states || p.state_rows != 2 * f.W * BWD_ROWS))) return hipErrorInvalidValue;
+    if (f.split) go(true, 1, p, f, s);
+    go(true, f.split ? 2 : 0, p, f, s);
     return hipGetLastError();
 }
 

@@ -1089,7 +1089,33 @@ struct Planner {
         if (st != RL_OK) return st;
         ScanParams p{};
         p.B = h0.dims[0]; p.D = h0.dims[1]; p.T = z.dims[0] / p.B; p.dtype = z.dtype;
-        if (p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > 0x3fffffff) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": sizes past 31 bits");
+        if (p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > SCAN_MAX_D) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more channels or rows than the kernels reach");
+        const int64_t every = grad ? scan_state_rows(p) : 0;
+        if (every > 0) {
+            // the states between come from a linear_scan of the same operands in this plan, or from a step of their own
+            Step *made = nullptr;
+            for (Step &q : plan.steps)
+                if (q.kind == S_SCAN && q.slot[SL_X] == t.slot[SL_X] && q.slot[SL_CIN] == t.slot[SL_CIN] && q.slot[SL_E0] == t.slot[SL_E0]) made = &q;
+            if (made && made->slot[SL_OUT4] >= 0) {
+                t.slot[SL_E2] = made->slot[SL_OUT4];
+            } else {
+                t.slot[SL_E2] = new_ws((size_t)(p.B * ((p.T + every - 1) / every) * p.D * 4));
+                if (!made) {
+                    const int64_t scratch = scan_part_floats(p, false);
+                    const int part = scratch > 0 ? new_ws((size_t)scratch * 4) : -1;
+                    made = &add_step(S_SCAN, std::string(op_name(o.kind)) + "#" + std::to_string(oi) + ".states", "linear_scan_states");
+                    made->group = gi;
+                    for (int sl : {SL_X, SL_CIN, SL_E0}) made->slot[sl] = t.slot[sl];
+                    made->slot[SL_PART] = part;
+                    made->sc = p;
+                    made->bytes = (double)bytes_of(o.in[0]);
+                    made->flops = 12.0 * numel(z) / 2;
+                }
+                made->slot[SL_OUT4] = t.slot[SL_E2];
+                made->sc.state_rows = every;
+            }
+            p.state_rows = every;
+        }
         const int64_t scratch = scan_part_floats(p, grad);
         if (scratch > 0) t.slot[SL_PART] = new_ws((size_t)scratch * 4);
         Step &s = call_step(grad ? S_SCAN_GRAD : S_SCAN, gi, oi, grad ? "linear_scan_grad" : "linear_scan", t.slot, {SL_Y, SL_COUT});
@@ -2295,10 +2321,10 @@ rl_status run_steps(const Plan &plan, void *const *ptrs, hipStream_t stream, std
             ScanParams p = s.sc;
             p.z = P(s, SL_X); p.h0 = (const float *)P(s, SL_CIN); p.keep = (const int8_t *)P(s, SL_E0); p.part = (float *)P(s, SL_PART);
             if (s.kind == S_SCAN) {
-                p.h = P(s, SL_Y); p.hT = (float *)P(s, SL_COUT);
+                p.h = P(s, SL_Y); p.hT = (float *)P(s, SL_COUT); p.states = (float *)P(s, SL_OUT4);
                 er = launch_scan(p, stream);
             } else {
-                p.dh = P(s, SL_X2); p.dhT = (const float *)P(s, SL_E1); p.dz = P(s, SL_Y); p.dh0 = (float *)P(s, SL_COUT);
+                p.dh = P(s, SL_X2); p.dhT = (const float *)P(s, SL_E1); p.dz = P(s, SL_Y); p.dh0 = (float *)P(s, SL_COUT); p.states = (float *)P(s, SL_E2);
                 er = launch_scan_grad(p, stream);
             }
             break;
