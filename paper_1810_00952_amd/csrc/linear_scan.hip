@@ -104,6 +104,37 @@ struct Place {
     }
 };
 
+// c, taken through tiles from .. to - 1 (BACK: to - 1 .. from) of `part`, whose vectors of a tile are `stride` floats apart, A first and
+// the addend at `add`.  Every run of the workgroup joins its share of the tiles, then all of them the shares.
+template <int VEC, int W, bool BACK>
+__device__ __forceinline__ void through_tiles(const float *part, int64_t stride, int64_t add, int32_t from, int32_t to, int run, float (&c)[VEC],
+                                              float (&sa)[2 * W][32][VEC], float (&sx)[2 * W][32][VEC])
+{
+    const int n = to - from, l32 = threadIdx.x & 31;
+    const int share = BACK ? 2 * W - 1 - run : run;
+    const int32_t lo = from + (int32_t)((int64_t)n * share / (2 * W)), hi = from + (int32_t)((int64_t)n * (share + 1) / (2 * W));
+    float a[VEC], x[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) { a[j] = 1.0f; x[j] = 0.0f; }
+#pragma unroll 4
+    for (int32_t k = lo; k < hi; ++k) {
+        const float *q = part + (BACK ? lo + hi - 1 - k : k) * stride;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float ka = q[j];
+            x[j] = __builtin_fmaf(ka, x[j], q[add + j]);
+            a[j] *= ka;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) { sa[run][l32][j] = a[j]; sx[run][l32][j] = x[j]; }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int r = 0; r < 2 * W; ++r) c[j] = __builtin_fmaf(sa[r][l32][j], c[j], sx[r][l32][j]);
+}
+
 // bit i: row t0 + i is padding (or past the sequence), is a document's first
 template <int ROWS> struct Flags { uint32_t pad, first; };
 template <int ROWS, bool KEEP>
@@ -176,10 +207,10 @@ __global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p,
     if (MODE != 1) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) carry[j] = p.h0[chan + j];
-        if (MODE == 2)
-            for (int32_t s = 0; s < at.seg; ++s)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) carry[j] = __builtin_fmaf(p.part[2 * s * BD + chan + j], carry[j], p.part[(2 * s + 1) * BD + chan + j]);
+        if constexpr (MODE == 2) {
+            __shared__ float ta[2 * W][32][VEC], th[2 * W][32][VEC];
+            through_tiles<VEC, W, false>(p.part + chan, 2 * BD, BD, 0, at.seg, at.run, carry, ta, th);
+        }
     }
     for (int32_t tile = first_tile; tile < last_tile; ++tile) {
         const int64_t t0 = (int64_t)tile * P::TILE + at.run * ROWS;
@@ -319,15 +350,12 @@ __global__ __launch_bounds__(64 * W) void linear_scan_grad_kernel(const ScanPara
     if (MODE != 1) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) gcarry[j] = p.dhT[chan + j];
-        if (MODE == 2) {
+        if constexpr (MODE == 2) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) start[j] = p.h0[chan + j];
-            for (int32_t s = 0; s < at.seg; ++s)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) start[j] = __builtin_fmaf(p.part[3 * s * BD + chan + j], start[j], p.part[(3 * s + 1) * BD + chan + j]);
-            for (int32_t s = tiles - 1; s > at.seg; --s)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) gcarry[j] = __builtin_fmaf(p.part[3 * s * BD + chan + j], gcarry[j], p.part[(3 * s + 2) * BD + chan + j]);
+            __shared__ float ta[2][2 * W][32][VEC], tx[2][2 * W][32][VEC];
+            through_tiles<VEC, W, false>(p.part + chan, 3 * BD, BD, 0, at.seg, at.run, start, ta[0], tx[0]);
+            through_tiles<VEC, W, true>(p.part + chan, 3 * BD, 2 * BD, at.seg + 1, tiles, at.run, gcarry, ta[1], tx[1]);
         }
     }
     for (int32_t tile = first_tile; tile > last_tile; --tile) {
