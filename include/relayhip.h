@@ -226,7 +226,8 @@ typedef struct rl_plan_opts {
     int32_t no_run_ks;      /* in that kernel's 128x64 form: do not split K over the waves */
     int32_t no_pair;        /* no two steps share a launch: a stride-2 convolution and the 1x1 projection beside it, the two
                                gradients of a layer (whose K slices, and the kernel of the one with respect to the input, are
-                               chosen for the shared launch where there is one), two changes of layout */
+                               chosen for the shared launch where there is one), two changes of layout, a token_logprobs and its
+                               gradient */
     int32_t s2_pair;        /* opt in: such a pair as ONE contraction whose centre tap carries the projection (second
                                accumulators) with the input rows shared in LDS -- correct and tested, but its 64-pixel tiles
                                lose to the two-contractions-in-one-grid form on every shape measured so far */

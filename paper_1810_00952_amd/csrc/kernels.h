@@ -361,9 +361,11 @@ struct LogprobsParams {
     float *part;
     int64_t M, V; int32_t dtype, top;
 };
-int64_t logprobs_part_floats(const LogprobsParams &p, bool grad);
-hipError_t launch_logprobs(const LogprobsParams &p, hipStream_t s);
-hipError_t launch_logprobs_grad(const LogprobsParams &p, hipStream_t s);
+// scratch that the launch wants at part; its top is the forward operator's, 0 of a gradient alone
+constexpr int64_t LOGPROBS_MAX_V = (int64_t)1 << 30;
+constexpr int LOGPROBS_MAX_TOP = 32;
+int64_t logprobs_part_floats(const LogprobsParams &p);
+hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s);
 
 // measurement aid (calibrate.hip): a chain of register-operand bf16 MFMAs per wave; out holds grid * 512 floats
 hipError_t launch_mfma_peak(float *out, int32_t grid, int32_t iters, hipStream_t s);

@@ -16,6 +16,8 @@
 
 namespace rl {
 
+static_assert(LOGPROBS_MAX_TOP == RL_TOP_MAX, "the kernels hold as many alternatives as may be asked for");
+
 namespace {
 
 enum { L_NATIVE = 0, L_NHWC = 1 };
@@ -1134,8 +1136,27 @@ struct Planner {
         if (st != RL_OK) return st;
         LogprobsParams p{};
         p.M = x.dims[0]; p.V = x.dims[1]; p.dtype = x.dtype; p.top = o.attrs.top;
-        if (p.M > 0x7fffffff) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows than a launch has");
-        const int64_t scratch = logprobs_part_floats(p, grad);
+        if (p.M > 0xffffff || p.V > LOGPROBS_MAX_V) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows or columns than a launch has");
+        // right behind the forward operator on the same logits and tokens: one launch reads them for both
+        const int before = (int)plan.steps.size() - 1;
+        auto apart = [&](const Step &f) {          // what the gradient reads beside them is not that call's result
+            for (int q : {SL_E0, SL_E1})
+                if (t.slot[q] == f.slot[SL_Y] || t.slot[q] == f.slot[SL_COUT]) return false;
+            return true;
+        };
+        if (grad && before >= 0 && plan.steps[before].kind == S_LOGPROBS && plan.steps[before].slot[SL_X] == t.slot[SL_X] && plan.steps[before].slot[SL_W] == t.slot[SL_W] &&
+            !plan.opts.no_pair && apart(plan.steps[before])) {
+            Step &s = call_step(S_LOGPROBS_GRAD, gi, oi, "(launched with the step before)", t.slot, {SL_Y});
+            Step &f = plan.steps[before];
+            f.pair = 1; s.pair = 2;
+            f.name += " | " + s.name;
+            f.kernel += " | token_logprobs_grad";
+            f.flops += 3.0 * numel(x);
+            f.bytes += (double)bytes_of(o.out[0]) + 2.0 * bytes_of(o.in[2]);
+            s.bytes = 0;
+            return RL_OK;
+        }
+        const int64_t scratch = logprobs_part_floats(p);
         if (scratch > 0) t.slot[SL_PART] = new_ws((size_t)scratch * 4);
         Step &s = call_step(grad ? S_LOGPROBS_GRAD : S_LOGPROBS, gi, oi, grad ? "token_logprobs_grad" : "token_logprobs", t.slot, {SL_Y, SL_COUT, SL_HOUT, SL_OUT4});
         s.lg = p;
@@ -2330,15 +2351,16 @@ rl_status run_steps(const Plan &plan, void *const *ptrs, hipStream_t stream, std
             break;
         }
         case S_LOGPROBS: case S_LOGPROBS_GRAD: {
+            if (s.pair == 2) break;                 // went out with the step before
             LogprobsParams p = s.lg;
             p.x = P(s, SL_X); p.tok = (const int32_t *)P(s, SL_W); p.part = (float *)P(s, SL_PART);
-            if (s.kind == S_LOGPROBS) {
-                p.lp = (float *)P(s, SL_Y); p.ent = (float *)P(s, SL_COUT); p.top_lp = (float *)P(s, SL_HOUT); p.top_id = (int32_t *)P(s, SL_OUT4);
-                er = launch_logprobs(p, stream);
-            } else {
-                p.dlp = (const float *)P(s, SL_E0); p.dent = (const float *)P(s, SL_E1); p.dx = P(s, SL_Y);
-                er = launch_logprobs_grad(p, stream);
+            const bool forward = s.kind == S_LOGPROBS;
+            if (forward) { p.lp = (float *)P(s, SL_Y); p.ent = (float *)P(s, SL_COUT); p.top_lp = (float *)P(s, SL_HOUT); p.top_id = (int32_t *)P(s, SL_OUT4); }
+            if (!forward || s.pair == 1) {
+                const Step &t = forward ? plan.steps[si] : s;     // si already counts this step: the next one
+                p.dlp = (const float *)P(t, SL_E0); p.dent = (const float *)P(t, SL_E1); p.dx = P(t, SL_Y);
             }
+            er = launch_logprobs(p, forward, p.dx != nullptr, stream);
             break;
         }
         case S_PACK:

@@ -3,143 +3,516 @@
 //   m = max x,  S = sum e^(x - m),  U = sum (x - m) e^(x - m)
 //   lp = x[tok] - m - ln S,   ent = ln S - U / S,   dx = dlp (1[v = tok] - p) - dent p (ln p + ent)
 //
-// A row of -inf alone: lp -inf, ent 0, dx 0.  A row with +inf or NaN: NaN.
-#include "device_utils.h"
+// A row of -inf alone: lp -inf, ent 0, dx 0.  A row with +inf or NaN: S is NaN, and so is everything.
+//
+// A workgroup holds its row in registers, as the 16-byte vectors of memory whatever the row's alignment, so that each logit is read once for
+// the statistics, the alternatives and the gradient; a gradient planned right behind its forward operator shares its launch.  Every lane
+// sums relative to its own maximum, the lanes' (m, S, U) meet once.  Rows too long for that, and few long rows, are cut
+// into segments, whose statistics and alternatives a second launch joins.  What bounds it is HBM.
+//
+// Alternatives: each of 64 groups of lanes has its largest logit; the top-th of those is at most the top-th of the row, so what is not below it
+// is collected (some 1.4 times as many as wanted) and ranked by counting.  A row where too many are not below it (equals), or that
+// holds NaN, finds them one by one instead.
+#include "igemm_lds.h"
 
 namespace rl {
 
 namespace {
 
-constexpr int WG = 256;
+constexpr int CAND = 512;                        // candidates a workgroup collects
+constexpr float LOWEST = -3.0e38f;               // a lane's maximum at least: -inf less it is -inf, not NaN
 
-// maximum, S and U of x - m; a term of -inf adds nothing to either
+// maximum (at least LOWEST), S and U of x less it
 struct Soft { float m, s, u; };
 
-__device__ __forceinline__ Soft join(const Soft &a, const Soft &b)
+__device__ __forceinline__ float e_to(float x) { return __expf(x); }
+
+__device__ __forceinline__ void rescale(Soft &a, float m)
 {
-    Soft r;
-    r.m = fmaxf(a.m, b.m);
-    // a side that has seen nothing above -inf has s = u = 0
-    const float da = a.m == -INFINITY ? 0.0f : a.m - r.m, db = b.m == -INFINITY ? 0.0f : b.m - r.m;
-    const float ea = __expf(da), eb = __expf(db);
-    r.s = a.s * ea + b.s * eb;
-    r.u = (a.u + a.s * da) * ea + (b.u + b.s * db) * eb;
-    return r;
+    const float d = a.m - m, e = e_to(d);
+    a.u = (a.u + a.s * d) * e;
+    a.s *= e;
+    a.m = m;
+}
+
+__device__ __forceinline__ Soft join_lanes(Soft a)
+{
+    float m = a.m;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    rescale(a, m);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { a.s += __shfl_xor(a.s, o); a.u += __shfl_xor(a.u, o); }
+    return a;
 }
 
 // the order of the alternatives as one number: larger for the larger logit, then for the earlier one; NaN above everything
-__device__ __forceinline__ uint64_t rank_key(float x, int64_t v)
+__device__ __forceinline__ uint64_t rank_key(float x, uint32_t v)
 {
     uint32_t u = __float_as_uint(x + 0.0f);
     u = x != x ? 0xfffffffeu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    return ((uint64_t)u << 32) | (0xffffffffu - (uint32_t)v);
+    return ((uint64_t)u << 32) | (0xffffffffu - v);
+}
+__device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
+__device__ __forceinline__ float key_logit(uint64_t key)
+{
+    const uint32_t u = (uint32_t)(key >> 32);
+    return u == 0xfffffffeu ? __builtin_nanf("") : __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
 
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int o)
+__device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t largest_of_wave(uint64_t v)
 {
-    return ((uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o) << 32) | (uint32_t)__shfl_xor((int)(uint32_t)v, o);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        v = larger(v, ((uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o) << 32) | (uint32_t)__shfl_xor((int)(uint32_t)v, o));
+    return v;
 }
 
-// statistics of the row, in every thread
-__device__ __forceinline__ Soft row_stats(const void *x, int dtype, int64_t at, int64_t V)
+template <typename E> struct Vec { static constexpr int N = 16 / sizeof(E); };
+template <typename E> __device__ __forceinline__ float unpack(const u32x4 &r, int k)
 {
-    float m = -INFINITY;
-    for (int64_t v = threadIdx.x; v < V; v += WG) {
-        const float f = load_as_f32(x, dtype, at + v);
-        m = f != f ? INFINITY : fmaxf(m, f);
+    if constexpr (sizeof(E) == 4) return __uint_as_float(r[k]);
+    else return __uint_as_float((k & 1) ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
+}
+// the same vector as a value of its own: what it is unpacked to is not kept from one use for the next
+__device__ __forceinline__ u32x4 anew(u32x4 v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ int32_t anew(int32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+template <typename E> __device__ __forceinline__ u32x4 pack(const float *v)
+{
+    u32x4 r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = sizeof(E) == 4 ? __float_as_uint(v[k]) : pack_bf16x2(v[2 * k], v[2 * k + 1]);
+    return r;
+}
+
+// Vector j of thread t covers columns first + N (j T + t) .. + N - 1 of the row, at a multiple of 16 bytes.  Of vector 0 and of the last only
+// a part may lie in lo .. hi - 1: those are read and written an element at a time, by the thread that has them.
+template <typename E, int T, int NV>
+struct Part {
+    static constexpr int N = Vec<E>::N;
+    static constexpr uint32_t NOTHING = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;    // -inf
+    const E *row;                               // the row's column 0
+    int32_t lo, hi, first, used;                // used: vectors a thread has at most
+    int32_t last_j, last_t;                     // whose the last vector is
+    bool head, tail;                            // the first, the last vector is the thread's and cut
+    u32x4 x[NV];
+
+    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t V, int32_t lo_, int32_t hi_) : lo(lo_), hi(hi_)
+    {
+        row = (const E *)base + r * V;
+        first = lo - (int32_t)((r * V + lo) % N);
+        const int32_t last = (hi - 1 - first) / N;
+        used = last / T + 1;
+        last_j = last / T; last_t = last % T;
+        head = threadIdx.x == 0 && first < lo;
+        tail = (int32_t)threadIdx.x == last_t && first + (last + 1) * N > hi;
     }
-    Soft a{m, 0.0f, 0.0f};
-    if (m > -INFINITY)
-        for (int64_t v = threadIdx.x; v < V; v += WG) {
-            const float f = load_as_f32(x, dtype, at + v);
-            if (f != -INFINITY) {
-                const float d = f - m, e = __expf(d);
-                a.s += e; a.u += d * e;
+    __device__ __forceinline__ int32_t column(int j) const { return first + N * (j * T + (int32_t)threadIdx.x); }
+    // whether the thread's vector j is there and whole; false of the cut ones
+    __device__ __forceinline__ bool whole(int j) const
+    {
+        return !(j == 0 && head) && (j < last_j || (int32_t)threadIdx.x < last_t || ((int32_t)threadIdx.x == last_t && !tail));
+    }
+    __device__ __forceinline__ uint32_t offset(int j) const { return j == 0 || j == last_j ? whole(j) ? threadIdx.x * 16u : OOB : threadIdx.x * 16u; }
+    __device__ __forceinline__ rsrc_t vectors(const void *base) const { return make_rsrc((const E *)base + first, 0x7fffffffu); }
+    __device__ __forceinline__ u32x4 cut(int32_t c) const
+    {
+        u32x4 v = {NOTHING, NOTHING, NOTHING, NOTHING};
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (c + k >= lo && c + k < hi) {
+                if constexpr (sizeof(E) == 4) v[k] = ((const uint32_t *)row)[c + k];
+                else v[k >> 1] = (k & 1) ? (v[k >> 1] & 0xffffu) | (uint32_t)((const uint16_t *)row)[c + k] << 16
+                                         : (v[k >> 1] & 0xffff0000u) | ((const uint16_t *)row)[c + k];
+            }
+        return v;
+    }
+    __device__ __forceinline__ void load()
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const rsrc_t src = vectors(row);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j < used) x[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, offset(j), j * T * 16, 0));
+        if (!whole(0)) x[0] = u32x4{NOTHING, NOTHING, NOTHING, NOTHING};
+        if (head) x[0] = cut(first);
+        u32x4 end = {NOTHING, NOTHING, NOTHING, NOTHING};
+        if (tail) end = cut(column(last_j));
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j == last_j && !whole(j) && !(j == 0 && head)) x[j] = end;
+#endif
+    }
+    // the thread's vectors of a result of the row's shape, one at a time, j rising
+    struct Out { rsrc_t dst; u32x4 first, last; };
+    __device__ __forceinline__ Out out(void *base) const { return {vectors(base), {}, {}}; }
+    __device__ __forceinline__ void put(Out &o, int j, u32x4 v) const
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        __builtin_amdgcn_raw_buffer_store_b128(v, o.dst, offset(j), j * T * 16, 0);
+        if (j == 0) o.first = v;
+        if (j == last_j) o.last = v;
+#endif
+    }
+    __device__ __forceinline__ void put_cut(E *dst, int32_t c, const u32x4 &v) const
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (c + k >= lo && c + k < hi) {
+                if constexpr (sizeof(E) == 4) ((uint32_t *)dst)[c + k] = v[k];
+                else dst[c + k] = (E)(v[k >> 1] >> (16 * (k & 1)));
+            }
+    }
+    __device__ __forceinline__ void finish(const Out &o, E *dst) const
+    {
+        if (head) put_cut(dst, first, o.first);
+        if (tail && !(head && last_j == 0)) put_cut(dst, column(last_j), o.last);
+    }
+    // the lane's own
+    __device__ __forceinline__ Soft stats(float &most) const
+    {
+        float m = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (j >= used) continue;
+#pragma unroll
+            for (int k = 0; k < N; ++k) m = fmaxf(m, unpack<E>(x[j], k));
+        }
+        most = m;
+        Soft a{fmaxf(m, LOWEST), 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (j >= used) continue;
+            const u32x4 q = anew(x[j]);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float d = unpack<E>(q, k) - a.m, e = e_to(d);
+                a.s += e;
+                a.u = __builtin_fmaf(fmaxf(d, -1e4f), e, a.u);        // -inf adds zero; NaN comes with e
             }
         }
+        return a;
+    }
+};
+
+// statistics of all of the workgroup's lanes, in every thread; sh: one a wave
+template <int T>
+__device__ __forceinline__ Soft join_workgroup(Soft a, Soft *sh)
+{
+    a = join_lanes(a);
+    if constexpr (T > 64) {
+        if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = a;
+        __syncthreads();
+        float m = LOWEST;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) a = join(a, Soft{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.u, o)});
-    __shared__ Soft sh[WG / 64];
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = a;
-    __syncthreads();
-    a = sh[0];
+        for (int w = 0; w < T / 64; ++w) m = fmaxf(m, sh[w].m);
+        a = Soft{m, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 1; i < WG / 64; ++i) a = join(a, sh[i]);
+        for (int w = 0; w < T / 64; ++w) {
+            Soft b = sh[w];
+            rescale(b, m);
+            a.s += b.s; a.u += b.u;
+        }
+    }
     return a;
+}
+
+// what a row's results are made of
+struct Result {
+    float m, ls, ent, inv;
+    bool dead;
+    __device__ __forceinline__ explicit Result(const Soft &a)
+    {
+        dead = a.m == LOWEST && a.s == 0.0f;
+        m = a.m;
+        ls = logf(a.s);
+        inv = dead ? 0.0f : 1.0f / a.s;
+        ent = dead ? 0.0f : ls - a.u * inv;
+    }
+    __device__ __forceinline__ float logp(float x) const { return dead ? -INFINITY : x - m - ls; }
+};
+
+__device__ __forceinline__ void store_row(const LogprobsParams &p, int64_t row, const Result &r)
+{
+    const int tok = p.tok[row];
+    const bool given = tok >= 0 && tok < p.V;
+    p.lp[row] = r.ls != r.ls ? r.ls : given ? r.logp(load_as_f32(p.x, p.dtype, row * p.V + tok)) : 0.0f;
+    p.ent[row] = r.ent;
+}
+
+// `top` keys of the workgroup's part into out (LDS), largest first; zero where there are no more.  T >= 64.
+template <typename E, int T, int NV>
+__device__ __forceinline__ void alternatives(const Part<E, T, NV> &x, int top, float most, bool plain, uint64_t *out)
+{
+    constexpr int N = Vec<E>::N, W = T / 64;
+    __shared__ float group[W][64];
+    __shared__ uint64_t cand[CAND], best[W];
+    __shared__ int count;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    group[wave][lane] = most;
+    if (t == 0) count = 0;
+    if (t < top) out[t] = 0;
+    __syncthreads();
+    float mine = group[0][lane];
+#pragma unroll
+    for (int w = 1; w < W; ++w) mine = fmaxf(mine, group[w][lane]);
+    // the top-th largest of 64
+    int above = 0, equal = 0;
+#pragma unroll
+    for (int l = 0; l < 64; ++l) {
+        const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), l));
+        above += other > mine;
+        equal += other == mine;
+    }
+    const uint64_t is = __ballot(above < top && above + equal >= top);
+    bool one_by_one = !plain || is == 0;
+    if (!one_by_one) {
+        const float least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __builtin_ctzll(is)));
+        // fewer than `top` groups above -inf: what is above it, and for the rest the first columns, of which that many at least are -inf
+        // unless what is above it is enough
+        const bool some = least > -INFINITY;
+        static_assert(CAND / 2 >= 2 * LOGPROBS_MAX_TOP, "columns that hold `top` logits beside fewer than `top`");
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (j >= x.used) continue;
+            const u32x4 q = anew(x.x[j]);
+            float f[N], v = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < N; ++k) { f[k] = unpack<E>(q, k); v = fmaxf(v, f[k]); }
+            if (v >= least) {
+                const int32_t c = anew(x.column(j));
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (f[k] >= least && (some || f[k] > -INFINITY || c + k < x.lo + CAND / 2) && c + k >= x.lo && c + k < x.hi) {
+                        const int at = atomicAdd(&count, 1);
+                        if (at < CAND) cand[at] = rank_key(f[k], (uint32_t)(c + k));
+                    }
+            }
+        }
+        __syncthreads();
+        const int n = count;
+        one_by_one = n > CAND;
+        if (!one_by_one)
+            for (int i = t; i < n; i += T) {
+                const uint64_t key = cand[i];
+                int rank = 0;
+                for (int o = 0; o < n; ++o) rank += cand[o] > key;
+                if (rank < top) out[rank] = key;
+            }
+    }
+    if (one_by_one) {
+        uint64_t last = ~(uint64_t)0;
+        for (int i = 0; i < top; ++i) {
+            uint64_t b = 0;                          // below every key: a column is under 2^31
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (j >= x.used) continue;
+                const int32_t c = anew(x.column(j));
+                const u32x4 q = anew(x.x[j]);
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const uint64_t key = rank_key(unpack<E>(q, k), (uint32_t)(c + k));
+                    if (key < last && c + k >= x.lo && c + k < x.hi) b = larger(b, key);
+                }
+            }
+            b = largest_of_wave(b);
+            if (lane == 0) best[wave] = b;
+            __syncthreads();
+            for (int w = 0; w < W; ++w) b = larger(b, best[w]);
+            last = b;
+            if (t == 0) out[i] = b;
+            __syncthreads();
+            if (b == 0) break;
+        }
+    }
+    __syncthreads();
+}
+
+template <typename E, int T, int NV>
+__device__ __forceinline__ void gradient(const LogprobsParams &p, const Part<E, T, NV> &x, int64_t row, const Result &r)
+{
+    constexpr int N = Vec<E>::N;
+    const int tok = p.tok[row];
+    const float dlp = tok >= 0 && tok < p.V && !r.dead ? p.dlp[row] : 0.0f, dent = r.dead ? 0.0f : p.dent[row];
+    const float c = r.dead ? 0.0f : dlp + dent * (r.ent - r.ls), scale = -r.inv;
+    E *dx = (E *)p.dx + row * p.V;
+    auto out = x.out(dx);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (j >= x.used) continue;
+        const int32_t col = anew(x.column(j));
+        const u32x4 q = anew(x.x[j]);
+        float v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float d = unpack<E>(q, k) - r.m;
+            v[k] = e_to(d) * scale * __builtin_fmaf(dent, fmaxf(d, -1e4f), c);
+        }
+        if (tok >= col && tok < col + N) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (tok == col + k) v[k] += dlp;
+        }
+        x.put(out, j, pack<E>(v));
+    }
+    x.finish(out, dx);
+}
+
+// What a segment leaves in part for the second launch: m, S, U, -, then `top` keys
+__device__ __forceinline__ int64_t seg_floats(int top) { return 4 + 2 * top; }
+
+__device__ __forceinline__ Soft join_segments(const LogprobsParams &p, int64_t row, int segs)
+{
+    const float *q = p.part + row * segs * seg_floats(p.top);
+    float m = LOWEST;
+    for (int s = 0; s < segs; ++s) m = fmaxf(m, q[s * seg_floats(p.top)]);
+    Soft a{m, 0.0f, 0.0f};
+    for (int s = 0; s < segs; ++s) {
+        const float *v = q + s * seg_floats(p.top);
+        Soft b{v[0], v[1], v[2]};
+        rescale(b, m);
+        a.s += b.s; a.u += b.u;
+    }
+    return a;
+}
+
+enum { FORWARD = 1, GRADIENT = 2, SEGMENT = 4, JOINED = 8 };     // what a launch does: JOINED takes the statistics from part
+
+}  // namespace
+
+template <typename E, int T, int NV, int WHAT>
+__global__ __launch_bounds__(T) void token_logprobs_kernel(const LogprobsParams p, int32_t segs, int32_t seg_len)
+{
+    __shared__ Soft sh[T / 64];
+    __shared__ uint64_t keys[LOGPROBS_MAX_TOP];
+    const int64_t row = blockIdx.x / (uint32_t)segs;
+    const int32_t seg = (int32_t)(blockIdx.x - (uint32_t)row * segs), lo = seg * seg_len;
+    Part<E, T, NV> x(p.x, row, p.V, lo, (int32_t)min((int64_t)lo + seg_len, p.V));
+    x.load();
+    float most = 0.0f;
+    const Soft a = WHAT & JOINED ? join_segments(p, row, segs) : join_workgroup<T>(x.stats(most), sh);
+    if constexpr (WHAT & (FORWARD | SEGMENT)) {
+        if (p.top > 0) alternatives<E, T, NV>(x, p.top, most, a.s == a.s, keys);
+    }
+    if constexpr (WHAT & SEGMENT) {
+        float *q = p.part + (row * segs + seg) * seg_floats(p.top);
+        if (threadIdx.x == 0) { q[0] = a.m; q[1] = a.s; q[2] = a.u; }
+        if ((int)threadIdx.x < p.top) ((uint64_t *)(q + 4))[threadIdx.x] = keys[threadIdx.x];
+        return;
+    }
+    const Result r(a);
+    if constexpr (WHAT & FORWARD) {
+        if (threadIdx.x == 0) store_row(p, row, r);
+        if ((int)threadIdx.x < p.top) {
+            const uint64_t key = keys[threadIdx.x];
+            p.top_id[row * p.top + threadIdx.x] = (int32_t)key_index(key);
+            p.top_lp[row * p.top + threadIdx.x] = r.logp(key_logit(key));
+        }
+    }
+    if constexpr (WHAT & GRADIENT) gradient<E, T, NV>(p, x, row, r);
+}
+
+// the segments of a row joined: one wave, or as many threads as there are keys to rank
+__global__ __launch_bounds__(256) void token_logprobs_join_kernel(const LogprobsParams p, int32_t segs)
+{
+    const int64_t row = blockIdx.x;
+    const Result r(join_segments(p, row, segs));
+    if (threadIdx.x == 0) store_row(p, row, r);
+    const float *q = p.part + row * segs * seg_floats(p.top);
+    const int n = segs * p.top;
+    auto key_of = [&](int i) { return ((const uint64_t *)(q + (i / p.top) * seg_floats(p.top) + 4))[i % p.top]; };
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const uint64_t key = key_of(i);
+        int rank = 0;
+        for (int o = 0; o < n; ++o) rank += key_of(o) > key;
+        if (key != 0 && rank < p.top) {
+            p.top_id[row * p.top + rank] = (int32_t)key_index(key);
+            p.top_lp[row * p.top + rank] = r.logp(key_logit(key));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+namespace {
+
+struct Form { int segs; int32_t len; int shape; };           // shape: of the kernel, by the bytes it holds
+
+constexpr int64_t SHAPE_BYTES[] = {64 * 4 * 16, 256 * 4 * 16, 512 * 8 * 16, 1024 * 8 * 16, 1024 * 16 * 16};
+
+Form form_of(const LogprobsParams &p)
+{
+    const int64_t e = p.dtype == DT_BF16 ? 2 : 4;
+    Form f{1, (int32_t)p.V, 0};
+    // a row that is not cut, or segments of 16 KB: enough for all CUs where there are few rows
+    const int64_t most = SHAPE_BYTES[4] - 16;                  // 16: a row may begin inside a vector
+    if (p.V * e > most || (p.M < 128 && p.V * e > 32768)) {
+        int64_t segs = p.M < 128 ? (256 + p.M - 1) / p.M : 1;
+        segs = segs < p.V * e / 16000 + 1 ? segs : p.V * e / 16000 + 1;
+        if (segs > 64) segs = 64;
+        const int64_t need = (p.V * e + most - 1) / most;
+        if (segs < need) segs = need;
+        f.len = (int32_t)((p.V + segs - 1) / segs);
+        f.segs = (int)((p.V + f.len - 1) / f.len);
+    }
+    while (f.shape < 4 && f.len * e + 16 > SHAPE_BYTES[f.shape]) ++f.shape;
+    return f;
+}
+
+template <typename E, int T, int NV>
+void go(const LogprobsParams &p, const Form &f, int what, hipStream_t s)
+{
+    const dim3 grid((unsigned)(p.M * f.segs)), wg(T);
+    switch (what) {
+    case FORWARD: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, FORWARD>), grid, wg, 0, s, p, f.segs, f.len); break;
+    case GRADIENT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, GRADIENT>), grid, wg, 0, s, p, f.segs, f.len); break;
+    case FORWARD | GRADIENT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, FORWARD | GRADIENT>), grid, wg, 0, s, p, f.segs, f.len); break;
+    case SEGMENT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, SEGMENT>), grid, wg, 0, s, p, f.segs, f.len); break;
+    default: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, GRADIENT | JOINED>), grid, wg, 0, s, p, f.segs, f.len); break;
+    }
+}
+
+template <typename E>
+void go(const LogprobsParams &p, const Form &f, int what, hipStream_t s)
+{
+    switch (f.shape) {
+    case 0: go<E, 64, 4>(p, f, what, s); break;
+    case 1: go<E, 256, 4>(p, f, what, s); break;
+    case 2: go<E, 512, 8>(p, f, what, s); break;
+    case 3: go<E, 1024, 8>(p, f, what, s); break;
+    default: go<E, 1024, 16>(p, f, what, s); break;
+    }
 }
 
 }  // namespace
 
-__global__ __launch_bounds__(WG) void token_logprobs_kernel(const LogprobsParams p)
+int64_t logprobs_part_floats(const LogprobsParams &p)
 {
-    const int64_t row = blockIdx.x, at = row * p.V;
-    const Soft a = row_stats(p.x, p.dtype, at, p.V);
-    const bool dead = a.m == -INFINITY, broken = a.m == INFINITY;
-    const float ls = logf(a.s);
-    auto logp = [&](float x) { return broken ? __builtin_nanf("") : dead ? -INFINITY : x - a.m - ls; };
-    if (threadIdx.x == 0) {
-        const int tok = p.tok[row];
-        const bool given = tok >= 0 && tok < p.V;
-        p.lp[row] = broken ? __builtin_nanf("") : given ? logp(load_as_f32(p.x, p.dtype, at + tok)) : 0.0f;
-        p.ent[row] = broken ? __builtin_nanf("") : dead ? 0.0f : ls - a.u / a.s;
-    }
-    __shared__ uint64_t sh[WG / 64];
-    uint64_t last = ~(uint64_t)0;
-    for (int k = 0; k < p.top; ++k) {
-        uint64_t best = 0;                                  // below every key: an index is under 2^31
-        for (int64_t v = threadIdx.x; v < p.V; v += WG) {
-            const uint64_t key = rank_key(load_as_f32(p.x, p.dtype, at + v), v);
-            if (key < last && key > best) best = key;
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) { const uint64_t other = shfl_xor64(best, o); best = other > best ? other : best; }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = best;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < WG / 64; ++i) best = sh[i] > best ? sh[i] : best;
-        last = best;
-        if (threadIdx.x == 0) {
-            const uint32_t id = 0xffffffffu - (uint32_t)best;
-            p.top_id[row * p.top + k] = (int32_t)id;
-            p.top_lp[row * p.top + k] = logp(load_as_f32(p.x, p.dtype, at + id));
-        }
-    }
+    const Form f = form_of(p);
+    return f.segs > 1 ? p.M * f.segs * (4 + 2 * (int64_t)p.top) : 0;
 }
 
-__global__ __launch_bounds__(WG) void token_logprobs_grad_kernel(const LogprobsParams p)
+hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s)
 {
-    const int64_t row = blockIdx.x, at = row * p.V;
-    const Soft a = row_stats(p.x, p.dtype, at, p.V);
-    const bool dead = a.m == -INFINITY, broken = a.m == INFINITY;
-    const float ls = logf(a.s), inv = 1.0f / a.s, ent = ls - a.u * inv;
-    const int tok = p.tok[row];
-    const float dlp = tok >= 0 && tok < p.V ? p.dlp[row] : 0.0f, dent = p.dent[row];
-    for (int64_t v = threadIdx.x; v < p.V; v += WG) {
-        const float x = load_as_f32(p.x, p.dtype, at + v);
-        float dx = v == tok ? dlp : 0.0f;
-        if (x != -INFINITY) {
-            const float d = x - a.m, pr = __expf(d) * inv;
-            dx -= pr * (dlp + dent * (d - ls + ent));
-        }
-        store_from_f32(p.dx, p.dtype, at + v, broken ? __builtin_nanf("") : dead ? 0.0f : dx);
+    const Form f = form_of(p);
+    if (p.M < 1 || p.V < 1 || p.V > LOGPROBS_MAX_V || p.M * f.segs > 0x7fffffff || p.top < 0 || p.top > p.V || p.top > LOGPROBS_MAX_TOP || (f.segs > 1 && !p.part) || f.len * (p.dtype == DT_BF16 ? 2 : 4) + 16 > SHAPE_BYTES[4])
+        return hipErrorInvalidValue;
+    auto run = [&](int what) { p.dtype == DT_BF16 ? go<uint16_t>(p, f, what, s) : go<float>(p, f, what, s); };
+    if (f.segs == 1) {
+        run((forward ? FORWARD : 0) | (grad ? GRADIENT : 0));
+    } else {
+        run(SEGMENT);
+        if (forward) hipLaunchKernelGGL(token_logprobs_join_kernel, dim3((unsigned)p.M), dim3(256), 0, s, p, f.segs);
+        if (grad) run(GRADIENT | JOINED);
     }
-}
-
-int64_t logprobs_part_floats(const LogprobsParams &, bool) { return 0; }
-
-hipError_t launch_logprobs(const LogprobsParams &p, hipStream_t s)
-{
-    if (p.M < 1 || p.V < 1 || p.M > 0x7fffffff || p.V > 0x7fffffff || p.top < 0 || p.top > p.V) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(token_logprobs_kernel, dim3((unsigned)p.M), dim3(WG), 0, s, p);
-    return hipGetLastError();
-}
-
-hipError_t launch_logprobs_grad(const LogprobsParams &p, hipStream_t s)
-{
-    if (p.M < 1 || p.V < 1 || p.M > 0x7fffffff || p.V > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(token_logprobs_grad_kernel, dim3((unsigned)p.M), dim3(WG), 0, s, p);
     return hipGetLastError();
 }
 
