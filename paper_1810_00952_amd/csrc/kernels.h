@@ -362,7 +362,7 @@ struct LogprobsParams {
     int64_t M, V; int32_t dtype, top;
 };
 // scratch that the launch wants at part; its top is the forward operator's, 0 of a gradient alone
-constexpr int64_t LOGPROBS_MAX_V = (int64_t)1 << 30;
+constexpr int64_t LOGPROBS_MAX_V = 4000000;     // 64 segments of 65532 f32
 constexpr int LOGPROBS_MAX_TOP = 32;
 int64_t logprobs_part_floats(const LogprobsParams &p);
 hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s);

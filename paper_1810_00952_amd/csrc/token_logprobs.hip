@@ -20,6 +20,7 @@ namespace rl {
 namespace {
 
 constexpr int CAND = 512;                        // candidates a workgroup collects
+constexpr int MAX_SEGS = 64;                     // of a row
 constexpr float LOWEST = -3.0e38f;               // a lane's maximum at least: -inf less it is -inf, not NaN
 
 // maximum (at least LOWEST), S and U of x less it
@@ -35,14 +36,15 @@ __device__ __forceinline__ void rescale(Soft &a, float m)
     a.m = m;
 }
 
-__device__ __forceinline__ Soft join_lanes(Soft a)
+// of LANES lanes side by side, in every one of them
+template <int LANES> __device__ __forceinline__ Soft join_lanes(Soft a)
 {
     float m = a.m;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     rescale(a, m);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) { a.s += __shfl_xor(a.s, o); a.u += __shfl_xor(a.u, o); }
+    for (int o = LANES / 2; o > 0; o >>= 1) { a.s += __shfl_xor(a.s, o); a.u += __shfl_xor(a.u, o); }
     return a;
 }
 
@@ -208,20 +210,11 @@ struct Part {
 template <int T>
 __device__ __forceinline__ Soft join_workgroup(Soft a, Soft *sh)
 {
-    a = join_lanes(a);
+    a = join_lanes<64>(a);
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = a;
         __syncthreads();
-        float m = LOWEST;
-#pragma unroll
-        for (int w = 0; w < T / 64; ++w) m = fmaxf(m, sh[w].m);
-        a = Soft{m, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < T / 64; ++w) {
-            Soft b = sh[w];
-            rescale(b, m);
-            a.s += b.s; a.u += b.u;
-        }
+        a = join_lanes<T / 64>(sh[threadIdx.x & (T / 64 - 1)]);
     }
     return a;
 }
@@ -372,17 +365,10 @@ __device__ __forceinline__ int64_t seg_floats(int top) { return 4 + 2 * top; }
 
 __device__ __forceinline__ Soft join_segments(const LogprobsParams &p, int64_t row, int segs)
 {
-    const float *q = p.part + row * segs * seg_floats(p.top);
-    float m = LOWEST;
-    for (int s = 0; s < segs; ++s) m = fmaxf(m, q[s * seg_floats(p.top)]);
-    Soft a{m, 0.0f, 0.0f};
-    for (int s = 0; s < segs; ++s) {
-        const float *v = q + s * seg_floats(p.top);
-        Soft b{v[0], v[1], v[2]};
-        rescale(b, m);
-        a.s += b.s; a.u += b.u;
-    }
-    return a;
+    static_assert(MAX_SEGS <= 64, "a lane each");
+    const int lane = threadIdx.x & 63;
+    const float *v = p.part + (row * segs + lane) * seg_floats(p.top);
+    return join_lanes<64>(lane < segs ? Soft{v[0], v[1], v[2]} : Soft{LOWEST, 0.0f, 0.0f});
 }
 
 enum { FORWARD = 1, GRADIENT = 2, SEGMENT = 4, JOINED = 8 };     // what a launch does: JOINED takes the statistics from part
@@ -390,7 +376,7 @@ enum { FORWARD = 1, GRADIENT = 2, SEGMENT = 4, JOINED = 8 };     // what a launc
 }  // namespace
 
 template <typename E, int T, int NV, int WHAT>
-__global__ __launch_bounds__(T) void token_logprobs_kernel(const LogprobsParams p, int32_t segs, int32_t seg_len)
+__global__ __launch_bounds__(T, NV == 16 ? 4 : 8) void token_logprobs_kernel(const LogprobsParams p, int32_t segs, int32_t seg_len)
 {
     __shared__ Soft sh[T / 64];
     __shared__ uint64_t keys[LOGPROBS_MAX_TOP];
@@ -421,20 +407,42 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(const LogprobsParams 
     if constexpr (WHAT & GRADIENT) gradient<E, T, NV>(p, x, row, r);
 }
 
-// the segments of a row joined: one wave, or as many threads as there are keys to rank
+// the segments of a row joined, their alternatives ranked by counting those that can be among the row's
 __global__ __launch_bounds__(256) void token_logprobs_join_kernel(const LogprobsParams p, int32_t segs)
 {
+    __shared__ uint64_t keys[MAX_SEGS * LOGPROBS_MAX_TOP], cand[MAX_SEGS * LOGPROBS_MAX_TOP], least;
+    __shared__ int count;
     const int64_t row = blockIdx.x;
-    const Result r(join_segments(p, row, segs));
-    if (threadIdx.x == 0) store_row(p, row, r);
     const float *q = p.part + row * segs * seg_floats(p.top);
-    const int n = segs * p.top;
-    auto key_of = [&](int i) { return ((const uint64_t *)(q + (i / p.top) * seg_floats(p.top) + 4))[i % p.top]; };
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const uint64_t key = key_of(i);
+    const int n = segs * p.top, t = threadIdx.x;
+    for (int i = t; i < n; i += 256) keys[i] = ((const uint64_t *)(q + (i / p.top) * seg_floats(p.top) + 4))[i % p.top];
+    if (t == 0) count = 0;
+    const Result r(join_segments(p, row, segs));
+    if (t == 0) store_row(p, row, r);
+    if (p.top == 0) return;
+    __syncthreads();
+    // the top-th of the segments' first `each`, which are `top` or a few more: nothing below it is wanted
+    const int each = (p.top + segs - 1) / segs, some = segs * each;
+    static_assert(MAX_SEGS + LOGPROBS_MAX_TOP <= 256, "a thread each");
+    if (t < some) {
+        const uint64_t key = keys[t / each * p.top + t % each];
         int rank = 0;
-        for (int o = 0; o < n; ++o) rank += key_of(o) > key;
-        if (key != 0 && rank < p.top) {
+        for (int s = 0; s < segs; ++s)
+            for (int k = 0; k < each; ++k) {
+                const uint64_t other = keys[s * p.top + k];
+                rank += other > key || (other == key && s * each + k < t);          // equal: the zeros of a segment with fewer
+            }
+        if (rank == p.top - 1) least = key;
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += 256)
+        if (keys[i] >= least && keys[i] != 0) cand[atomicAdd(&count, 1)] = keys[i];
+    __syncthreads();
+    for (int i = t; i < count; i += 256) {
+        const uint64_t key = cand[i];
+        int rank = 0;
+        for (int o = 0; o < count; ++o) rank += cand[o] > key;
+        if (rank < p.top) {
             p.top_id[row * p.top + rank] = (int32_t)key_index(key);
             p.top_lp[row * p.top + rank] = r.logp(key_logit(key));
         }
@@ -457,7 +465,7 @@ Form form_of(const LogprobsParams &p)
     if (p.V * e > most || (p.M < 128 && p.V * e > 32768)) {
         int64_t segs = p.M < 128 ? (256 + p.M - 1) / p.M : 1;
         segs = segs < p.V * e / 16000 + 1 ? segs : p.V * e / 16000 + 1;
-        if (segs > 64) segs = 64;
+        if (segs > MAX_SEGS) segs = MAX_SEGS;
         const int64_t need = (p.V * e + most - 1) / most;
         if (segs < need) segs = need;
         f.len = (int32_t)((p.V + segs - 1) / segs);
@@ -503,7 +511,7 @@ int64_t logprobs_part_floats(const LogprobsParams &p)
 hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s)
 {
     const Form f = form_of(p);
-    if (p.M < 1 || p.V < 1 || p.V > LOGPROBS_MAX_V || p.M * f.segs > 0x7fffffff || p.top < 0 || p.top > p.V || p.top > LOGPROBS_MAX_TOP || (f.segs > 1 && !p.part) || f.len * (p.dtype == DT_BF16 ? 2 : 4) + 16 > SHAPE_BYTES[4])
+    if (p.M < 1 || p.V < 1 || p.V > LOGPROBS_MAX_V || f.segs > MAX_SEGS || p.M * f.segs > 0x7fffffff || p.top < 0 || p.top > p.V || p.top > LOGPROBS_MAX_TOP || (f.segs > 1 && !p.part) || f.len * (p.dtype == DT_BF16 ? 2 : 4) + 16 > SHAPE_BYTES[4])
         return hipErrorInvalidValue;
     auto run = [&](int what) { p.dtype == DT_BF16 ? go<uint16_t>(p, f, what, s) : go<float>(p, f, what, s); };
     if (f.segs == 1) {
