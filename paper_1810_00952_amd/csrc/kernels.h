@@ -346,7 +346,7 @@ struct ScanParams {
     void *h; float *hT;
     const void *dh; const float *dhT; void *dz; float *dh0;
     float *part, *states;
-    int64_t B, T, D, state_rows; int32_t dtype;
+    int64_t B, T, D, state_rows; int32_t dtype, keeps;      // keeps: whether there is a keep
 };
 constexpr int64_t SCAN_MAX_D = (int64_t)1 << 20;
 int64_t scan_part_floats(const ScanParams &p, bool grad);      // scratch that the launch wants at part

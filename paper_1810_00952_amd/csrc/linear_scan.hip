@@ -23,7 +23,10 @@ namespace rl {
 
 namespace {
 
-constexpr int FWD_ROWS = 16, BWD_ROWS = 8;      // rows of a run: as many as fit the registers of two waves a SIMD with what they become
+// Rows of a run: as many as fit the registers with what they become, of two waves a SIMD where a workgroup walks its tiles, of four where
+// tiles are workgroups (of the gradient, 32 x 1024 x 2048 bf16, forward and backward pass: 250 us with sixteen, 273 with eight)
+constexpr int FWD_ROWS = 16;
+constexpr int bwd_rows(bool walks, bool keep) { return walks && !keep ? 16 : 8; }
 
 // sigmoid(f) and 1 - sigmoid(f), each to its own last bits.  Below -80 the gate stays at e^-80, which no f32 state is changed by.
 __device__ __forceinline__ void gate(float f, float &a, float &rest)
@@ -72,8 +75,9 @@ template <typename R> __device__ __forceinline__ void store(const Rows &r, uint3
     else __builtin_amdgcn_raw_buffer_store_b16(v, r.rsrc, off, 0, 0);
 #endif
 }
-// a value the compiler takes as new: the offsets of a tile's rows are added up where they are used, not kept in registers
-__device__ __forceinline__ uint32_t anew(uint32_t v)
+// a value the compiler takes as new: what is made of it (the offsets of a tile's rows, unpacked operands) is made where it is used, not kept
+// in registers from an earlier use
+template <typename R> __device__ __forceinline__ R anew(R v)
 {
     asm volatile("" : "+v"(v));
     return v;
@@ -129,10 +133,10 @@ __device__ __forceinline__ void through_tiles(const float *part, int64_t stride,
 #pragma unroll
     for (int j = 0; j < VEC; ++j) { sa[run][l32][j] = a[j]; sx[run][l32][j] = x[j]; }
     __syncthreads();
+#pragma unroll 4
+    for (int r = 0; r < 2 * W; ++r)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j)
-#pragma unroll
-        for (int r = 0; r < 2 * W; ++r) c[j] = __builtin_fmaf(sa[r][l32][j], c[j], sx[r][l32][j]);
+        for (int j = 0; j < VEC; ++j) c[j] = __builtin_fmaf(sa[r][l32][j], c[j], sx[r][l32][j]);
 }
 
 // bit i: row t0 + i is padding (or past the sequence), is a document's first
@@ -178,9 +182,9 @@ __global__ __launch_bounds__(256) void linear_scan_step_kernel(const ScanParams 
 // forward.  MODE 0: a workgroup walks its channels' tiles; 1: (A, H) of one tile into part; 2: one tile, after those before it
 // ---------------------------------------------------------------------------
 template <typename E, int VEC, int W, int MODE, bool KEEP>
-__global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
+__global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
 {
-    constexpr int ROWS = FWD_ROWS;
+    constexpr int ROWS = FWD_ROWS, AT_ONCE = MODE == 0 ? W : 4;      // other waves' sums read at once: those of all where there are registers for them
     typedef Place<E, VEC, ROWS, W> P;
     typedef typename Raw<E, VEC>::type raw_t;
     const P at(p, slabs);
@@ -261,7 +265,7 @@ __global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p,
             }
         }
         if (W > 1) __syncthreads(); else wave_lds_exchange();
-        float mine[VEC], end[VEC];
+        float mine[VEC];
         if (MODE == 1) {
             if (at.run == 0 && at.live) {
 #pragma unroll
@@ -275,17 +279,16 @@ __global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p,
             }
             return;
         }
+#pragma unroll AT_ONCE
+        for (int w = 0; w < W; ++w)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            float c = carry[j];
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                if (w == at.wave) mine[j] = c;
-                c = __builtin_fmaf(sa[buf][w][l32][j], c, sh[buf][w][l32][j]);
+            for (int j = 0; j < VEC; ++j) {
+                if (w == at.wave) mine[j] = carry[j];
+                carry[j] = __builtin_fmaf(sa[buf][w][l32][j], carry[j], sh[buf][w][l32][j]);
             }
-            end[j] = c;
-            if (at.half) mine[j] = __builtin_fmaf(oa[j], mine[j], oh[j]);
-            carry[j] = end[j];
+        if (at.half) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) mine[j] = __builtin_fmaf(oa[j], mine[j], oh[j]);
         }
         if (at.live) {
             if (p.states && t0 % p.state_rows == 0 && t0 < p.T) {
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p,
             }
             if (p.hT && tile + 1 == tiles && at.run == 0) {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) p.hT[chan + j] = end[j];
+                for (int j = 0; j < VEC; ++j) p.hT[chan + j] = carry[j];
             }
         }
     }
@@ -319,9 +322,9 @@ __global__ __launch_bounds__(64 * W) void linear_scan_kernel(const ScanParams p,
 // (MODE 0) or from the tiles before it (MODE 2).
 // ---------------------------------------------------------------------------
 template <typename E, int VEC, int W, int MODE, bool KEEP>
-__global__ __launch_bounds__(64 * W) void linear_scan_grad_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
+__global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
 {
-    constexpr int ROWS = BWD_ROWS;
+    constexpr int ROWS = bwd_rows(MODE == 0, KEEP), AT_ONCE = MODE == 0 ? W : 4;
     typedef Place<E, VEC, ROWS, W> P;
     typedef typename Raw<E, VEC>::type raw_t;
     const P at(p, slabs);
@@ -433,23 +436,28 @@ __global__ __launch_bounds__(64 * W) void linear_scan_grad_kernel(const ScanPara
             }
             return;
         }
-        float h[VEC], G[VEC];
+        float h[VEC], G[VEC], c[VEC];
+        // the states and gradients that reach the wave, the gradient on to the next tile
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) c[j] = start[j];
+#pragma unroll AT_ONCE
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                if (w == at.wave) h[j] = c[j];
+                c[j] = __builtin_fmaf(sa[buf][w][l32][j], c[j], sh[buf][w][l32][j]);
+            }
+#pragma unroll AT_ONCE
+        for (int w = W - 1; w >= 0; --w)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                if (w == at.wave) G[j] = gcarry[j];
+                gcarry[j] = __builtin_fmaf(sa[buf][w][l32][j], gcarry[j], sg[buf][w][l32][j]);
+            }
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            float c = start[j], g = gcarry[j];
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                if (w == at.wave) h[j] = c;
-                c = __builtin_fmaf(sa[buf][w][l32][j], c, sh[buf][w][l32][j]);
-            }
             if (at.half) h[j] = __builtin_fmaf(oa[j], h[j], oh[j]);
-#pragma unroll
-            for (int w = W - 1; w >= 0; --w) {
-                if (w == at.wave) G[j] = g;
-                g = __builtin_fmaf(sa[buf][w][l32][j], g, sg[buf][w][l32][j]);
-            }
-            if (!at.half) G[j] = __builtin_fmaf(oa[j], G[j], og[j]);
-            gcarry[j] = g;
+            else G[j] = __builtin_fmaf(oa[j], G[j], og[j]);
         }
         if (at.live) {
             // the state before every row, then the rows backwards
@@ -471,12 +479,13 @@ __global__ __launch_bounds__(64 * W) void linear_scan_grad_kernel(const ScanPara
                 const Rows dz = rows_of(p.dz, tile, 2);
 #pragma unroll
                 for (int i = ROWS - 1; i >= 0; --i) {
+                    const raw_t qv = MODE == 0 ? kv[i] : anew(kv[i]), qd = MODE == 0 ? kd[i] : anew(kd[i]);
                     float df[VEC], dv[VEC];
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-                        const float g = G[j] + unpack<E, VEC>(kd[i], j);
+                        const float g = G[j] + unpack<E, VEC>(qd, j);
                         dv[j] = g * rest[i][j];
-                        df[j] = dv[j] * (before[i][j] - unpack<E, VEC>(kv[i], j)) * a[i][j];
+                        df[j] = dv[j] * (before[i][j] - unpack<E, VEC>(qv, j)) * a[i][j];
                         const float on = a[i][j] * g;
                         if (masked) {
                             const bool pad = fl.pad >> i & 1u;
@@ -504,18 +513,23 @@ __global__ __launch_bounds__(64 * W) void linear_scan_grad_kernel(const ScanPara
 // ---------------------------------------------------------------------------
 namespace {
 
-struct Form { int W; bool split; int32_t slabs, tiles; };
+struct Form { int W, rows; bool split; int32_t slabs, tiles; };
 
 // Waves of a workgroup: enough for the rows, eight where there are few workgroups.  split: tiles as workgroups of their own.
 Form form_of(const ScanParams &p, bool grad)
 {
-    const int64_t vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1, rows = grad ? BWD_ROWS : FWD_ROWS;
+    const int64_t vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1;
     Form f;
     f.slabs = (int32_t)((p.D + 32 * vec - 1) / (32 * vec));
     const int64_t wgs = p.B * f.slabs;
-    f.W = p.T <= 2 * rows ? 1 : p.T <= 8 * rows || wgs >= 512 ? 4 : 8;
-    f.tiles = (int32_t)((p.T + 2 * f.W * rows - 1) / (2 * f.W * rows));
-    f.split = wgs < 128 && f.tiles > 1;
+    f.split = false;
+    for (int walks = 1; walks >= 0; --walks) {
+        f.rows = grad ? bwd_rows(walks, p.keeps) : FWD_ROWS;
+        f.W = p.T <= 2 * f.rows ? 1 : p.T <= 8 * f.rows || wgs >= 512 ? 4 : 8;
+        f.tiles = (int32_t)((p.T + 2 * f.W * f.rows - 1) / (2 * f.W * f.rows));
+        if (wgs >= 128 || f.tiles == 1) break;
+        f.split = true;
+    }
     return f;
 }
 
@@ -560,7 +574,7 @@ bool sizes_ok(const ScanParams &p, const Form &f)
 int64_t scan_state_rows(const ScanParams &p)
 {
     const Form f = form_of(p, true);
-    return f.split || f.tiles == 1 ? 0 : 2 * f.W * BWD_ROWS;
+    return f.split || f.tiles == 1 ? 0 : 2 * f.W * f.rows;
 }
 
 int64_t scan_part_floats(const ScanParams &p, bool grad)
@@ -572,7 +586,7 @@ int64_t scan_part_floats(const ScanParams &p, bool grad)
 hipError_t launch_scan(const ScanParams &p, hipStream_t s)
 {
     const Form f = form_of(p, false);
-    if (!sizes_ok(p, f) || (f.split && !p.part) || (p.states && p.state_rows % FWD_ROWS != 0)) return hipErrorInvalidValue;
+    if (!sizes_ok(p, f) || p.keeps != (p.keep != nullptr) || (f.split && !p.part) || (p.states && p.state_rows % FWD_ROWS != 0)) return hipErrorInvalidValue;
     if (p.T == 1 && p.h) {
         const int vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1;
         const int64_t total = p.B * p.D / vec, blocks = (total + 255) / 256;
@@ -590,7 +604,7 @@ hipError_t launch_scan(const ScanParams &p, hipStream_t s)
 hipError_t launch_scan_grad(const ScanParams &p, hipStream_t s)
 {
     const Form f = form_of(p, true);
-    if (!sizes_ok(p, f) || (f.split && !p.part) || (!f.split && f.tiles > 1 && (!p.states || p.state_rows != 2 * f.W * BWD_ROWS))) return hipErrorInvalidValue;
+    if (!sizes_ok(p, f) || p.keeps != (p.keep != nullptr) || (f.split && !p.part) || (!f.split && f.tiles > 1 && (!p.states || p.state_rows != 2 * f.W * f.rows))) return hipErrorInvalidValue;
     if (f.split) go(true, 1, p, f, s);
     go(true, f.split ? 2 : 0, p, f, s);
     return hipGetLastError();

@@ -1090,7 +1090,7 @@ struct Planner {
         rl_status st = grad ? operands(o, {SL_X, SL_CIN, SL_X2, SL_E1, SL_E0}, t.slot) : operands(o, {SL_X, SL_CIN, SL_E0}, t.slot);
         if (st != RL_OK) return st;
         ScanParams p{};
-        p.B = h0.dims[0]; p.D = h0.dims[1]; p.T = z.dims[0] / p.B; p.dtype = z.dtype;
+        p.B = h0.dims[0]; p.D = h0.dims[1]; p.T = z.dims[0] / p.B; p.dtype = z.dtype; p.keeps = t.slot[SL_E0] >= 0;
         if (p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > SCAN_MAX_D) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more channels or rows than the kernels reach");
         const int64_t every = grad ? scan_state_rows(p) : 0;
         if (every > 0) {
