@@ -2,16 +2,16 @@
 //
 //   y = x + r (rounded as it is stored);  i = (mean y^2 + eps)^-1/2;  s = i max|y g| / 127;  q = rint(y g 127 / max|y g|)
 //
-// i cancels out of q, so the row's sum of squares and its largest |y g| are one reduction.
-#include "device_utils.h"
+// i cancels out of q, so the row's sum of squares and its largest |y g| are one reduction.  A workgroup holds its row in registers
+// and reads it once; what bounds it is HBM.  Rows past 128 KB are read twice.
+#include "row_vectors.h"
 
 namespace rl {
 
 namespace {
 
-constexpr int WG = 256;
-
-// sum of a and largest of b over the workgroup, in every thread
+// sum of a and largest of b over the workgroup of T threads, in every thread
+template <int T>
 __device__ __forceinline__ void reduce_sum_max(float &a, float &b)
 {
 #pragma unroll
@@ -19,17 +19,119 @@ __device__ __forceinline__ void reduce_sum_max(float &a, float &b)
         a += __shfl_xor(a, o);
         b = fmaxf(b, __shfl_xor(b, o));
     }
-    __shared__ float sa[WG / 64], sb[WG / 64];
-    const int w = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) { sa[w] = a; sb[w] = b; }
-    __syncthreads();
-    a = sa[0]; b = sb[0];
+    if constexpr (T > 64) {
+        __shared__ float sa[T / 64], sb[T / 64];
+        const int w = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) { sa[w] = a; sb[w] = b; }
+        __syncthreads();
+        a = sa[threadIdx.x & (T / 64 - 1)]; b = sb[threadIdx.x & (T / 64 - 1)];
 #pragma unroll
-    for (int i = 1; i < WG / 64; ++i) { a += sa[i]; b = fmaxf(b, sb[i]); }
+        for (int o = T / 128; o > 0; o >>= 1) {
+            a += __shfl_xor(a, o);
+            b = fmaxf(b, __shfl_xor(b, o));
+        }
+    }
+}
+
+// what becomes of a row: its scale, and the factors that take y g to the number that is rounded
+struct Scale {
+    float s, up, to_q;
+    bool whole;
+    __device__ __forceinline__ Scale(const NormQ8Params &p, float sum, float most)
+    {
+        whole = sum < INFINITY && most < INFINITY;                  // an infinity or NaN in the row is one in its sum of squares
+        s = whole ? most * rsqrtf(sum / (float)p.D + p.eps) / 127.0f : __builtin_nanf("");
+        up = most < 1e-30f ? 0x1p100f : 1.0f;                       // the factor of a tiny row would be past f32
+        to_q = whole && most > 0.0f ? 127.0f / (most * up) : 0.0f;
+    }
+    __device__ __forceinline__ int quantised(float yg) const
+    {
+        const float n = whole ? yg * up * to_q : 0.0f;
+        return (int)rintf(fminf(fmaxf(n, -127.0f), 127.0f));
+    }
+};
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// the gains of columns c .. c + N - 1, all of them there
+template <int N> __device__ __forceinline__ void gains(const NormQ8Params &p, int32_t c, float (&g)[N])
+{
+    if (p.g_dtype == DT_F32) {
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const f32x4_any v = *(const f32x4_any *)((const float *)p.g + c + k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[k + i] = v[i];
+        }
+    } else if (p.D % N == 0) {
+        if constexpr (N == 8) load8(p.g, DT_BF16, c, g);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) g[k] = load_as_f32(p.g, DT_BF16, c + k);
+    }
 }
 
 }  // namespace
 
+template <typename E, int T, int NV, bool RES>
+__global__ __launch_bounds__(T) void norm_q8_row_kernel(const NormQ8Params p)
+{
+    typedef RowVectors<E, T, NV> Row;
+    constexpr int N = Row::N;
+    const int64_t r = blockIdx.x;
+    const Row row(r, p.D, 0, (int32_t)p.D);
+    u32x4 x[NV], res[NV];
+    row.load((const E *)p.x + r * p.D, 0, x);
+    if (RES) row.load((const E *)p.r + r * p.D, 0, res);
+    float yg[NV][N], sum = 0.0f, most = 0.0f;
+    E *const yrow = RES ? (E *)p.y + r * p.D : nullptr;
+    typename Row::Out yo{};
+    if (RES) yo = row.out(yrow);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (j >= row.used) continue;
+        const int32_t c = row.column(j);
+        float g[N];
+        if (c >= 0 && c + N <= row.hi) {
+            gains<N>(p, c, g);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) g[k] = c + k >= 0 && c + k < row.hi ? load_as_f32(p.g, p.g_dtype, c + k) : 0.0f;
+        }
+        if (RES) {
+            float v[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = unpack<E>(x[j], k) + unpack<E>(res[j], k);
+            x[j] = pack<E>(v);                             // what is normalised is the stream as it is stored
+            row.put(yo, j, x[j]);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float y = unpack<E>(x[j], k);
+            sum = __builtin_fmaf(y, y, sum);
+            yg[j][k] = y * g[k];
+            most = fmaxf(most, fabsf(yg[j][k]));
+        }
+    }
+    if (RES) row.finish(yo, yrow);
+    reduce_sum_max<T>(sum, most);
+    const Scale scale(p, sum, most);
+    if (threadIdx.x == 0) p.s[r] = scale.s;
+    int8_t *const qrow = p.q + r * p.D;
+    typename Row::OutBytes qo = row.out_bytes(qrow);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (j >= row.used) continue;
+        u32x2 v = {0u, 0u};
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k >> 2] |= (uint32_t)(scale.quantised(yg[j][k]) & 255) << (8 * (k & 3));
+        row.put(qo, j, v);
+    }
+    row.finish(qo, qrow);
+}
+
+// rows of any length
+constexpr int WG = 256;
 __global__ __launch_bounds__(WG) void norm_q8_kernel(const NormQ8Params p)
 {
     const int64_t row = blockIdx.x, at = row * p.D;
@@ -44,28 +146,48 @@ __global__ __launch_bounds__(WG) void norm_q8_kernel(const NormQ8Params p)
         sum += y * y;
         most = fmaxf(most, fabsf(y * load_as_f32(p.g, p.g_dtype, d)));
     }
-    reduce_sum_max(sum, most);
-    // an infinity or NaN in the row is one in its sum of squares
-    const bool whole = sum < INFINITY && most < INFINITY;
-    const float inv = rsqrtf(sum / (float)p.D + p.eps);
-    const float up = most < 1e-30f ? 0x1p100f : 1.0f;              // the factor of a tiny row would be past f32
-    const float to_q = whole && most > 0.0f ? 127.0f / (most * up) : 0.0f;
-    if (threadIdx.x == 0) p.s[row] = whole ? most * inv / 127.0f : __builtin_nanf("");
+    reduce_sum_max<WG>(sum, most);
+    const Scale scale(p, sum, most);
+    if (threadIdx.x == 0) p.s[row] = scale.s;
     for (int64_t d = threadIdx.x; d < p.D; d += WG) {
         float y = load_as_f32(p.x, p.dtype, at + d);
         if (p.r) {
             y += load_as_f32(p.r, p.dtype, at + d);
             if (p.dtype == DT_BF16) y = round_bf16(y);
         }
-        const float n = whole ? y * load_as_f32(p.g, p.g_dtype, d) * up * to_q : 0.0f;
-        p.q[at + d] = (int8_t)rintf(fminf(fmaxf(n, -127.0f), 127.0f));
+        p.q[at + d] = (int8_t)scale.quantised(y * load_as_f32(p.g, p.g_dtype, d));
     }
 }
+
+namespace {
+
+template <typename E, int T, int NV> void go(const NormQ8Params &p, hipStream_t s)
+{
+    if (p.r) hipLaunchKernelGGL((norm_q8_row_kernel<E, T, NV, true>), dim3((unsigned)p.M), dim3(T), 0, s, p);
+    else hipLaunchKernelGGL((norm_q8_row_kernel<E, T, NV, false>), dim3((unsigned)p.M), dim3(T), 0, s, p);
+}
+
+// by the vectors of a row, one more for a row that begins inside one
+template <typename E> bool go(const NormQ8Params &p, hipStream_t s)
+{
+    const int64_t n = 16 / sizeof(E), vecs = (p.D + n - 1) / n + (p.D % n != 0);
+    if (vecs <= 64) go<E, 64, 1>(p, s);
+    else if (vecs <= 128) go<E, 64, 2>(p, s);
+    else if (vecs <= 256) go<E, 64, 4>(p, s);
+    else if (vecs <= 512) go<E, 256, 2>(p, s);
+    else if (vecs <= 1024) go<E, 256, 4>(p, s);
+    else if (vecs <= 4096) go<E, 1024, 4>(p, s);
+    else if (vecs <= 8192) go<E, 1024, 8>(p, s);
+    else return false;
+    return true;
+}
+
+}  // namespace
 
 hipError_t launch_norm_q8(const NormQ8Params &p, hipStream_t s)
 {
     if (p.M < 1 || p.D < 1 || p.M > 0x7fffffff || (p.r != nullptr) != (p.y != nullptr)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(norm_q8_kernel, dim3((unsigned)p.M), dim3(WG), 0, s, p);
+    if (!(p.dtype == DT_BF16 ? go<uint16_t>(p, s) : go<float>(p, s))) hipLaunchKernelGGL(norm_q8_kernel, dim3((unsigned)p.M), dim3(WG), 0, s, p);
     return hipGetLastError();
 }
 

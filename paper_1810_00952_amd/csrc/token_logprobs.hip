@@ -13,7 +13,7 @@
 // Alternatives: each of 64 groups of lanes has its largest logit; the top-th of those is at most the top-th of the row, so what is not below it
 // is collected (some 1.4 times as many as wanted) and ranked by counting.  A row where too many are not below it (equals), or that
 // holds NaN, finds them one by one instead.
-#include "igemm_lds.h"
+#include "row_vectors.h"
 
 namespace rl {
 
@@ -71,114 +71,16 @@ __device__ __forceinline__ uint64_t largest_of_wave(uint64_t v)
     return v;
 }
 
-template <typename E> struct Vec { static constexpr int N = 16 / sizeof(E); };
-template <typename E> __device__ __forceinline__ float unpack(const u32x4 &r, int k)
-{
-    if constexpr (sizeof(E) == 4) return __uint_as_float(r[k]);
-    else return __uint_as_float((k & 1) ? r[k >> 1] & 0xffff0000u : r[k >> 1] << 16);
-}
-// the same vector as a value of its own: what it is unpacked to is not kept from one use for the next
-__device__ __forceinline__ u32x4 anew(u32x4 v)
-{
-    asm volatile("" : "+v"(v));
-    return v;
-}
-__device__ __forceinline__ int32_t anew(int32_t v)
-{
-    asm volatile("" : "+v"(v));
-    return v;
-}
-template <typename E> __device__ __forceinline__ u32x4 pack(const float *v)
-{
-    u32x4 r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = sizeof(E) == 4 ? __float_as_uint(v[k]) : pack_bf16x2(v[2 * k], v[2 * k + 1]);
-    return r;
-}
-
-// Vector j of thread t covers columns first + N (j T + t) .. + N - 1 of the row, at a multiple of 16 bytes.  Of vector 0 and of the last only
-// a part may lie in lo .. hi - 1: those are read and written an element at a time, by the thread that has them.
+// a workgroup's part of a row, what is no column of it -inf
 template <typename E, int T, int NV>
-struct Part {
-    static constexpr int N = Vec<E>::N;
-    static constexpr uint32_t NOTHING = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;    // -inf
-    const E *row;                               // the row's column 0
-    int32_t lo, hi, first, used;                // used: vectors a thread has at most
-    int32_t last_j, last_t;                     // whose the last vector is
-    bool head, tail;                            // the first, the last vector is the thread's and cut
+struct Part : RowVectors<E, T, NV> {
+    typedef RowVectors<E, T, NV> Row;
+    using Row::N; using Row::used;
+    const E *row;                               // its column 0
     u32x4 x[NV];
 
-    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t V, int32_t lo_, int32_t hi_) : lo(lo_), hi(hi_)
-    {
-        row = (const E *)base + r * V;
-        first = lo - (int32_t)((r * V + lo) % N);
-        const int32_t last = (hi - 1 - first) / N;
-        used = last / T + 1;
-        last_j = last / T; last_t = last % T;
-        head = threadIdx.x == 0 && first < lo;
-        tail = (int32_t)threadIdx.x == last_t && first + (last + 1) * N > hi;
-    }
-    __device__ __forceinline__ int32_t column(int j) const { return first + N * (j * T + (int32_t)threadIdx.x); }
-    // whether the thread's vector j is there and whole; false of the cut ones
-    __device__ __forceinline__ bool whole(int j) const
-    {
-        return !(j == 0 && head) && (j < last_j || (int32_t)threadIdx.x < last_t || ((int32_t)threadIdx.x == last_t && !tail));
-    }
-    __device__ __forceinline__ uint32_t offset(int j) const { return j == 0 || j == last_j ? whole(j) ? threadIdx.x * 16u : OOB : threadIdx.x * 16u; }
-    __device__ __forceinline__ rsrc_t vectors(const void *base) const { return make_rsrc((const E *)base + first, 0x7fffffffu); }
-    __device__ __forceinline__ u32x4 cut(int32_t c) const
-    {
-        u32x4 v = {NOTHING, NOTHING, NOTHING, NOTHING};
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (c + k >= lo && c + k < hi) {
-                if constexpr (sizeof(E) == 4) v[k] = ((const uint32_t *)row)[c + k];
-                else v[k >> 1] = (k & 1) ? (v[k >> 1] & 0xffffu) | (uint32_t)((const uint16_t *)row)[c + k] << 16
-                                         : (v[k >> 1] & 0xffff0000u) | ((const uint16_t *)row)[c + k];
-            }
-        return v;
-    }
-    __device__ __forceinline__ void load()
-    {
-#if defined(__HIP_DEVICE_COMPILE__)
-        const rsrc_t src = vectors(row);
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (j < used) x[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src, offset(j), j * T * 16, 0));
-        if (!whole(0)) x[0] = u32x4{NOTHING, NOTHING, NOTHING, NOTHING};
-        if (head) x[0] = cut(first);
-        u32x4 end = {NOTHING, NOTHING, NOTHING, NOTHING};
-        if (tail) end = cut(column(last_j));
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (j == last_j && !whole(j) && !(j == 0 && head)) x[j] = end;
-#endif
-    }
-    // the thread's vectors of a result of the row's shape, one at a time, j rising
-    struct Out { rsrc_t dst; u32x4 first, last; };
-    __device__ __forceinline__ Out out(void *base) const { return {vectors(base), {}, {}}; }
-    __device__ __forceinline__ void put(Out &o, int j, u32x4 v) const
-    {
-#if defined(__HIP_DEVICE_COMPILE__)
-        __builtin_amdgcn_raw_buffer_store_b128(v, o.dst, offset(j), j * T * 16, 0);
-        if (j == 0) o.first = v;
-        if (j == last_j) o.last = v;
-#endif
-    }
-    __device__ __forceinline__ void put_cut(E *dst, int32_t c, const u32x4 &v) const
-    {
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (c + k >= lo && c + k < hi) {
-                if constexpr (sizeof(E) == 4) ((uint32_t *)dst)[c + k] = v[k];
-                else dst[c + k] = (E)(v[k >> 1] >> (16 * (k & 1)));
-            }
-    }
-    __device__ __forceinline__ void finish(const Out &o, E *dst) const
-    {
-        if (head) put_cut(dst, first, o.first);
-        if (tail && !(head && last_j == 0)) put_cut(dst, column(last_j), o.last);
-    }
+    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t V, int32_t lo, int32_t hi) : Row(r, V, lo, hi), row((const E *)base + r * V) {}
+    __device__ __forceinline__ void load() { Row::load(row, sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u, x); }
     // the lane's own
     __device__ __forceinline__ Soft stats(float &most) const
     {
@@ -246,7 +148,7 @@ __device__ __forceinline__ void store_row(const LogprobsParams &p, int64_t row, 
 template <typename E, int T, int NV>
 __device__ __forceinline__ void alternatives(const Part<E, T, NV> &x, int top, float most, bool plain, uint64_t *out)
 {
-    constexpr int N = Vec<E>::N, W = T / 64;
+    constexpr int N = Part<E, T, NV>::N, W = T / 64;
     __shared__ float group[W][64];
     __shared__ uint64_t cand[CAND], best[W];
     __shared__ int count;
@@ -333,7 +235,7 @@ __device__ __forceinline__ void alternatives(const Part<E, T, NV> &x, int top, f
 template <typename E, int T, int NV>
 __device__ __forceinline__ void gradient(const LogprobsParams &p, const Part<E, T, NV> &x, int64_t row, const Result &r)
 {
-    constexpr int N = Vec<E>::N;
+    constexpr int N = Part<E, T, NV>::N;
     const int tok = p.tok[row];
     const float dlp = tok >= 0 && tok < p.V && !r.dead ? p.dlp[row] : 0.0f, dent = r.dead ? 0.0f : p.dent[row];
     const float c = r.dead ? 0.0f : dlp + dent * (r.ent - r.ls), scale = -r.inv;
