@@ -21,6 +21,8 @@ configurations and the HBM-bound groups:
             (100.7 MB read, 100.7 MB written, ordinary loads and stores), the
             yardstick for the HBM byte counters
   grads     the gradient operators of dense / conv2d at the benchmark graph's shapes
+  recurrent_lm, recurrent_lm_step, recurrent_lm_train  a gated recurrent language model: a prompt scored in 8 bits, one generated token
+            of 64 sequences (states updated in place), and the training step of a layer with its head in bf16
   mfma_peak a chain of bf16 MFMAs on register operands on every SIMD: what the
             matrix pipes deliver here, next to the quoted 2.5 PFLOP/s
 The default line also carries that calibration ("peaks") and the HBM-bound groups
@@ -481,13 +483,40 @@ def bench_grads(args):
     return out
 
 
+def bench_recurrent_lm(args):
+    import workloads as W
+    from paper_1810_00952_amd import harness
+    dim, vocab, layers = 1024, 32000, 4
+    if args.workload == "recurrent_lm_train":
+        batch, steps = 8, 1024
+        spec, data = W.recurrent_lm_train(batch, steps, dim, vocab, "bf16")
+        what, dtype = f"one layer 1024 -> 2048, gated recurrence, head 1024 -> {vocab}, loss and all gradients, {batch} sequences of {steps}, bf16", "bf16"
+    else:
+        batch, steps = (64, 1) if args.workload == "recurrent_lm_step" else (8, 512)
+        spec, data = W.recurrent_lm(batch, steps, dim, layers, vocab, 8, "bf16")
+        what, dtype = f"{layers} layers of 1024, head of {vocab} with 8 alternatives, {batch} sequences of {steps}, 8-bit weights and operands, bf16 stream", "i8"
+    s = harness.Session(spec)
+    s.load(data)
+    if steps == 1:                        # a layer's new state over its old one
+        for l, hT in enumerate(spec.outputs[-layers:]):
+            s.tensors[hT] = s.tensors[s.by_name[f"h{l}"]]
+    s.alloc()
+    ms = time_steps(s.run, args.steps, args.warmup)
+    desc, by_kernel = kernel_table(s, args.profile_reps, ms)
+    dom_name, dom = max(by_kernel.items(), key=lambda kv: kv[1]["ms"])
+    out = base_json(f"tokens/sec {args.workload}", batch * steps / (ms * 1e-3), "tokens/s", args, ms, dtype, what)
+    out["roofline"] = roofline_of(dom_name, dom, PEAK_BF16_TFLOPS)
+    out["kernels"] = kernels_json(by_kernel, PEAK_BF16_TFLOPS)
+    return out
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--warmup", type=int, default=20)
     ap.add_argument("--workload", default="resnet18",
-                    choices=["resnet18", "resnet18_f32_b1", "eltwise", "eltwise32", "gates", "lstm", "mlp", "lenet", "conv", "copy", "layout", "layout32", "block_nhwc", "maxpool", "mfma_peak", "grads", "launch_pitch", "gemm"])
+                    choices=["resnet18", "resnet18_f32_b1", "eltwise", "eltwise32", "gates", "lstm", "mlp", "lenet", "conv", "copy", "layout", "layout32", "block_nhwc", "maxpool", "mfma_peak", "grads", "launch_pitch", "gemm", "recurrent_lm", "recurrent_lm_step", "recurrent_lm_train"])
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--cpu-images", type=int, default=128)
     ap.add_argument("--elements", type=int, default=0, help="copy: number of f32 elements (default 24 Mi)")
@@ -587,6 +616,8 @@ def main():
         out = bench_lstm(args)
     elif wl == "grads":
         out = bench_grads(args)
+    elif wl.startswith("recurrent_lm"):
+        out = bench_recurrent_lm(args)
     elif wl == "mfma_peak":
         pk = measure_peaks()
         out = base_json("TFLOP/s bf16 MFMA chain on register operands", pk["mfma_bf16_tflops_measured"], "TFLOP/s", args, 0.0, "bf16", pk["mfma_measure"])

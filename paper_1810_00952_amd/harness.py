@@ -10,11 +10,13 @@ import torch
 
 from .binding import Context, Plan, graph_from_spec
 
-_TORCH_DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+_TORCH_DT = {"f32": torch.float32, "bf16": torch.bfloat16, "i8": torch.int8, "i32": torch.int32}
 
 
 def to_device(a: np.ndarray, dtype: str, device="cuda:0") -> torch.Tensor:
-    """float32 array, or uint16 bf16 bit patterns, to a device tensor (bit-exact)."""
+    """float32 array, uint16 bf16 bit patterns, or whole numbers to a device tensor (bit-exact)."""
+    if dtype in ("i8", "i32"):
+        return torch.from_numpy(np.asarray(a, dtype=np.int8 if dtype == "i8" else np.int32, order="C")).to(device)
     if dtype == "bf16":
         t = torch.from_numpy(np.asarray(a, dtype=np.uint16, order="C").view(np.int16)).to(device)
         return t.view(torch.bfloat16)
@@ -22,7 +24,7 @@ def to_device(a: np.ndarray, dtype: str, device="cuda:0") -> torch.Tensor:
 
 
 def to_host(t: torch.Tensor) -> np.ndarray:
-    """Device tensor back to float32 array / uint16 bf16 bits."""
+    """Device tensor back to float32 array / uint16 bf16 bits / whole numbers."""
     if t.dtype == torch.bfloat16:
         return t.view(torch.int16).cpu().numpy().view(np.uint16)
     return t.cpu().numpy()

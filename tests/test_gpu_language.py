@@ -393,3 +393,245 @@ def test_other_streams_graphs_and_the_same_bits_twice():
                 np.testing.assert_array_equal(a, b)
             for a, b in zip(call.run().numbers(), want):
                 np.testing.assert_array_equal(a, b)
+
+
+# ---- every form, operators together -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("m,n,k", [(600, 2000, 200), (1500, 1500, 100), (2100, 2050, 144), (2048, 2304, 256), (9, 17, 5000), (40, 5000, 300), (70, 40, 3000)])
+def test_dense_q8_forms(m, n, k):
+    """Grids past the CUs, for each of the tiles, with ragged edges."""
+    for out, bias in (("bf16", True), ("f32", False)):
+        call, data = q8_case(m, n, k, out, bias, seed=m)
+        check_q8(call.run().numbers()[0], data, out, f"dense_q8 {m}x{n}x{k} {out}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,t,d", [(8, 300, 1024), (6, 700, 1111), (40, 150, 515), (130, 260, 64)])
+def test_scan_of_many_tiles(b, t, d, dtype):
+    """Workgroups that walk over the tiles of their channels."""
+    for how in (None, "some"):
+        what = f"scan {b}x{t}x{d} {dtype} keep={how}"
+        print(what, flush=True)
+        call, z, h0, keep = scan_case(b, t, d, dtype, how, seed=t)
+        check_scan(call.run().numbers(), z, h0, keep, dtype, what)
+        case = grad_case(b, t, d, dtype, how, seed=t)
+        check_grad(case[0].run().numbers(), *case[1:], dtype, what)
+
+
+def session_of(build):
+    """A graph's plan on torch tensors: build(graph) -> ({id: tensor}, {id: (dtype, shape)} of results)."""
+    import torch
+    from language_helpers import torch_type
+    from paper_1810_00952_amd import binding as B
+    g = B.Graph(B.Context())
+    ins, outs = build(g)
+    for v in outs:
+        g.output(v)
+    plan = g.plan()
+    got = {v: torch.full(sh, 7, dtype=torch_type(dt), device="cuda:0") for v, (dt, sh) in outs.items()}
+    ws = torch.full((max(256, plan.workspace_bytes()),), 0xa5, dtype=torch.uint8, device="cuda:0")
+    plan.bind({v: t.data_ptr() for v, t in {**ins, **got}.items()}, ws.data_ptr(), ws.numel()).run(torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return plan, [t.cpu() for t in got.values()]
+
+
+@pytest.mark.parametrize("b,t,d,how", [(8, 300, 1024, None), (8, 300, 1024, "some"), (1, 2000, 130, "some"), (3, 20, 70, None), (40, 200, 515, None)])
+def test_scan_gradient_takes_states_from_the_forward_pass(b, t, d, how):
+    """In one plan with its forward pass the gradient is the same to the bit, and launches no pass for the states."""
+    import torch
+    dtype = "bf16"
+    rng, z, h0, keep, operands, tk = scan_inputs(b, t, d, dtype, how, seed=5)
+    tdh, _ = tensor(rng.normal(size=(b * t, d)), dtype)
+    tdT, _ = tensor(rng.normal(size=(b, d)), "f32")
+    last = [(tk, "i8")] if tk is not None else []
+    dz, dh0 = Call("linear_scan_grad", operands + [(tdh, dtype), (tdT, "f32")] + last, [(dtype, (b * t, 2 * d)), ("f32", (b, d))]).run().results
+    h, hT = Call("linear_scan", operands + last, [(dtype, (b * t, d)), ("f32", (b, d))]).run().results
+
+    def build(g):
+        ids = {k: g.input(dt, x.shape) for k, (x, dt) in dict(z=operands[0], h0=operands[1], dh=(tdh, dtype), dT=(tdT, "f32"), **({"keep": last[0]} if last else {})).items()}
+        tail = [ids["keep"]] if last else []
+        types = [(dtype, (b * t, d)), ("f32", (b, d)), (dtype, (b * t, 2 * d)), ("f32", (b, d))]
+        _, a = g.op("linear_scan", [ids["z"], ids["h0"]] + tail, types[:2])
+        _, c = g.op("linear_scan_grad", [ids["z"], ids["h0"], ids["dh"], ids["dT"]] + tail, types[2:])
+        tensors = dict(z=operands[0][0], h0=operands[1][0], dh=tdh, dT=tdT, keep=tk)
+        return {v: tensors[k] for k, v in ids.items()}, dict(zip(list(a) + list(c), types))
+
+    plan, got = session_of(build)
+    assert [s["kernel"] for s in plan.describe()["steps"]] == ["linear_scan", "linear_scan_grad"]
+    for x, y in zip(got, (h, hT, dz, dh0)):
+        assert torch.equal(x, y.cpu())
+
+
+@pytest.mark.parametrize("m,v", [(5, 700), (3, 70000), (300, 5003)])
+def test_logprobs_and_gradient_share_a_launch(m, v):
+    """The pair gives the bits of the two calls alone; a gradient that reads the forward result comes behind it."""
+    import torch
+    dtype = "bf16"
+    rng, tx, x, tt, tok = logits_case(m, v, dtype, True, seed=v)
+    tp, _ = tensor(rng.normal(size=m), "f32")
+    top = 6
+    types = [("f32", (m,)), ("f32", (m,)), ("f32", (m, top)), ("i32", (m, top)), (dtype, (m, v))]
+    alone = Call("token_logprobs", [(tx, dtype), (tt, "i32")], types[:4], top=top).run().results + Call(
+        "token_logprobs_grad", [(tx, dtype), (tt, "i32"), (tp, "f32"), (tp, "f32")], types[4:]).run().results
+
+    def build(g, own=False):
+        ix, it, ip = g.input(dtype, (m, v)), g.input("i32", (m,)), g.input("f32", (m,))
+        _, a = g.op("token_logprobs", [ix, it], types[:4], top=top)
+        _, c = g.op("token_logprobs_grad", [ix, it, a[1] if own else ip, ip], types[4:])
+        return {ix: tx, it: tt, ip: tp}, dict(zip(list(a) + list(c), types))
+
+    plan, got = session_of(build)
+    assert "token_logprobs_grad" in plan.describe()["steps"][0]["kernel"]
+    for a, b in zip(got, alone):
+        np.testing.assert_array_equal(a.double().numpy(), b.double().cpu().numpy())
+    plan, got = session_of(lambda g: build(g, True))         # dlp is the entropy
+    assert [s["kernel"] for s in plan.describe()["steps"]] == ["token_logprobs", "token_logprobs_grad"]
+    want = Call("token_logprobs_grad", [(tx, dtype), (tt, "i32"), (alone[1], "f32"), (tp, "f32")], types[4:]).run().results[0]
+    np.testing.assert_array_equal(got[4].double().numpy(), want.double().cpu().numpy())
+
+
+def check_graph(spec, data, dtype):
+    """Every call of a graph against its definition on what the library computed for its operands."""
+    import torch
+    import oracle as O
+    from helpers import assert_close
+    from paper_1810_00952_amd import harness
+    for op in spec.ops:                             # everything leaves the plan
+        for v in op.outputs:
+            if v not in spec.outputs:
+                spec.output(v)
+    s = harness.Session(spec)
+    s.load(data)
+    s.run()
+    torch.cuda.synchronize()
+    val = {v: O.widen(harness.to_host(s.raw.get(v, t)), spec.values[v].type.dtype) for v, t in s.tensors.items()}    # raw: before it was packed
+    for i, op in enumerate(spec.ops):
+        a, out, what = [val[v] for v in op.inputs], [val[v] for v in op.outputs], f"call {i}: {op.kind}"
+        if op.kind == "rms_norm_q8":
+            check_norm(out, a[0], a[1] if len(a) == 3 else None, a[-1], dtype, what)
+        elif op.kind == "dense_q8":
+            check_q8(out[0], a + ([None] if len(a) == 4 else []), spec.values[op.outputs[0]].type.dtype, what)
+        elif op.kind == "linear_scan":
+            check_scan(out, a[0], a[1], a[2] if len(a) > 2 else None, dtype, what)
+        elif op.kind == "linear_scan_grad":
+            check_grad(out, a[0], a[1], a[2], a[3], a[4] if len(a) > 4 else None, dtype, what)
+        elif op.kind == "token_logprobs":
+            check_logprobs(out, a[0], a[1].astype(int), op.attrs.get("top", 0), what)
+        elif op.kind == "token_logprobs_grad":
+            assert_close(out[0], L.token_logprobs_grad(*a), dtype, what)
+        else:                                       # the contractions that were there: their own gate
+            f = {"dense": O.dense, "dense_grad_x": O.dense_grad_x, "dense_grad_w": O.dense_grad_w}[op.kind]
+            assert_close(out[0], f(a[0], a[1]), dtype, what)
+    return s
+
+
+@pytest.mark.parametrize("args", [dict(), dict(batch=3, steps=37, dim=72, vocab=1001, top=0, packed=True), dict(batch=9, steps=1, dim=128), dict(batch=2, steps=70, dim=50, dtype="f32")])
+def test_recurrent_lm(args):
+    import workloads as W
+    check_graph(*W.recurrent_lm(**args), args.get("dtype", "bf16"))
+
+
+@pytest.mark.parametrize("args", [dict(), dict(batch=2, steps=150, dim=96, vocab=333, packed=True)])
+def test_recurrent_lm_train(args):
+    import workloads as W
+    s = check_graph(*W.recurrent_lm_train(**args), "bf16")
+    names = [k["kernel"] for k in s.plan.describe()["steps"]]
+    assert sum("linear_scan" in n for n in names) == 2 and "token_logprobs | token_logprobs_grad" in names
+
+
+def test_generation_continues_a_prompt():
+    """A prompt, then its next tokens one at a time on the states it left: the states of the whole, each within the recurrence's bound of
+    the steps before (the plan's other operators give the same bits for the same rows)."""
+    import torch
+    import workloads as W
+    from paper_1810_00952_amd import harness
+    b, t, d, layers = 3, 12, 64, 2
+    spec, data = W.recurrent_lm(b, t, d, layers, 300, 4, "f32")
+    whole = harness.Session(spec)
+    whole.load(data)
+    whole.run()
+    step_spec, _ = W.recurrent_lm(b, 1, d, layers, 300, 4, "f32")
+    step = harness.Session(step_spec)
+    state = {f"h{l}": data[f"h{l}"] for l in range(layers)}
+    lps = []
+    for i in range(t):
+        step.tensors = {}
+        step.load({**data, "x": data["x"].reshape(b, t, d)[:, i], "tok": data["tok"].reshape(b, t)[:, i], **state})
+        step.alloc()
+        step.run()
+        torch.cuda.synchronize()
+        lps.append(step.output(0).cpu().numpy())
+        state = {f"h{l}": step.tensors[step_spec.outputs[4 + l]].cpu().numpy() for l in range(layers)}
+    # an 8-bit value next to a border may fall the other way where the state differs in its last bits: a step of 1/127 of a row's largest
+    # in one of d summands a layer
+    torch.cuda.synchronize()
+    want = whole.output(0).cpu().numpy().reshape(b, t)
+    assert np.abs(np.stack(lps, 1) - want).max() < layers * 6 * 3.0 / 127
+    for l in range(layers):
+        ref = whole.tensors[spec.outputs[4 + l]].cpu().numpy()
+        assert np.abs(state[f"h{l}"] - ref).max() < layers * 6 * 3.0 / 127
+
+
+def test_past_32_bits():
+    """Rows behind the first 4 GB (2 G elements where a row index is multiplied) of each operator's largest operand."""
+    import torch
+    dev, f = "cuda:0", torch.float32
+
+    def run(kind, operands, results, params=(), **attrs):
+        from language_helpers import plan_of, torch_type
+        plan, ids, outs = plan_of(kind, [(dt, t.shape) for t, dt in operands], results, params, **attrs)
+        got = [torch.empty(sh, dtype=torch_type(dt), device=dev) for dt, sh in results]
+        ws = torch.empty(max(256, plan.workspace_bytes()), dtype=torch.uint8, device=dev)
+        plan.run({v: t.data_ptr() for v, t in zip(ids + outs, [t for t, _ in operands] + got)}, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        return got
+
+    torch.manual_seed(3)
+    # logits of 40000 x 60001, the last rows
+    print("logits", flush=True)
+    m, v, n = 40000, 60001, 3
+    x = torch.zeros((m, v), dtype=torch.bfloat16, device=dev)
+    x[-n:] = torch.randn((n, v), device=dev).bfloat16()
+    tok = torch.randint(0, v, (m,), dtype=torch.int32, device=dev)
+    one = torch.ones((m,), device=dev)
+    lp, ent, top_lp, top_id = run("token_logprobs", [(x, "bf16"), (tok, "i32")], [("f32", (m,)), ("f32", (m,)), ("f32", (m, 2)), ("i32", (m, 2))], top=2)
+    tail, tt = x[-n:].double().cpu().numpy(), tok[-n:].cpu().numpy()
+    check_logprobs([o[-n:].double().cpu().numpy() for o in (lp, ent, top_lp, top_id)], tail, tt, 2, "last rows")
+    assert bool((top_id[:-n] == torch.tensor([0, 1], device=dev)).all())
+    dx, = run("token_logprobs_grad", [(x, "bf16"), (tok, "i32"), (one, "f32"), (one, "f32")], [("bf16", (m, v))])
+    ref = L.token_logprobs_grad(tail, tt, np.ones(n), np.ones(n))
+    within(dx[-n:].double().cpu().numpy(), ref, 2 * BF16 * np.abs(ref) + 1e-9, "last rows' gradient")
+    del x, dx
+    # a sequence of 300000 x 4096, padding but for its last rows
+    print("sequence", flush=True)
+    t, d, n = 300000, 4096, 5
+    z = torch.zeros((t, 2 * d), dtype=torch.bfloat16, device=dev)
+    z[-n:] = torch.randn((n, 2 * d), device=dev).bfloat16()
+    keep = torch.zeros((t,), dtype=torch.int8, device=dev)
+    keep[-n:] = 1
+    h0, dT = torch.randn((1, d), device=dev), torch.randn((1, d), device=dev)
+    h, hT = run("linear_scan", [(z, "bf16"), (h0, "f32"), (keep, "i8")], [("bf16", (t, d)), ("f32", (1, d))])
+    zt, h0n = z[-n:].double().cpu().numpy(), h0.double().cpu().numpy()
+    check_scan([h[-n:].double().cpu().numpy(), hT.double().cpu().numpy()], zt, h0n, None, "bf16", "last rows")
+    assert not bool(h[:-n].any())
+    dh = torch.zeros((t, d), dtype=torch.bfloat16, device=dev)
+    dh[-n:] = torch.randn((n, d), device=dev).bfloat16()
+    dz, dh0 = run("linear_scan_grad", [(z, "bf16"), (h0, "f32"), (dh, "bf16"), (dT, "f32"), (keep, "i8")], [("bf16", (t, 2 * d)), ("f32", (1, d))])
+    check_grad([dz[-n:].double().cpu().numpy(), dh0.double().cpu().numpy()], zt, h0n, dh[-n:].double().cpu().numpy(), dT.double().cpu().numpy(), None, "bf16", "last rows")
+    assert not bool(dz[:-n].any())
+    del z, h, dh, dz
+    # 1100000 rows of 2048
+    print("rows", flush=True)
+    m, d, n = 1100000, 2048, 4
+    x = torch.zeros((m, d), dtype=torch.bfloat16, device=dev)
+    x[-n:] = torch.randn((n, d), device=dev).bfloat16()
+    g = torch.rand((d,), device=dev) + 0.5
+    q, s = run("rms_norm_q8", [(x, "bf16"), (g, "f32")], [("i8", (m, d)), ("f32", (m,))], eps=1e-5)
+    check_norm([q[-n:].double().cpu().numpy(), s[-n:].double().cpu().numpy()], x[-n:].double().cpu().numpy(), None, g.double().cpu().numpy(), "bf16", "last rows")
+    assert not bool(q[:-n].any())
+    for cols in (40, 300):
+        w = torch.randint(-127, 128, (cols, d), dtype=torch.int8, device=dev)
+        sw = torch.rand((cols,), device=dev)
+        y, = run("dense_q8", [(q, "i8"), (s, "f32"), (w, "i8"), (sw, "f32")], [("f32", (m, cols))], out_dtype="f32")
+        num = lambda a: a.double().cpu().numpy()  # noqa: E731
+        check_q8(num(y[-n:]), (num(q[-n:]), num(s[-n:]), num(w), num(sw), None), "f32", "last rows")
+        assert not bool(y[:-n].any())

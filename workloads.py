@@ -15,7 +15,7 @@ Type-Call).
 
 Tensors are numpy arrays: float32 for dtype "f32"; uint16 bit patterns for
 dtype "bf16" (the upper half of the float32 encoding, rounded to nearest
-even when produced from float32 data here).
+even when produced from float32 data here); int8 and int32 for "i8" and "i32".
 """
 from __future__ import annotations
 
@@ -33,7 +33,7 @@ BASE_SEED = 181000952  # + config index 1..5
 @dataclasses.dataclass(frozen=True)
 class TType:
     """Tensor(dtype, Shape(dims...)) with every dim a positive constant."""
-    dtype: str            # "f32" | "bf16"
+    dtype: str            # "f32" | "bf16" | "i8" | "i32"
     shape: Tuple[int, ...]
 
 
@@ -653,6 +653,102 @@ def lstm_unrolled_graph(steps, batch, d_in, hidden, dtype="bf16", fused=True):
         g.output(h)
     g.output(c)
     return g
+
+
+def recurrent_lm(batch=4, steps=16, dim=64, layers=2, vocab=500, top=5, dtype="bf16", packed=False, config=31):
+    """A gated recurrent language model as it is served, in 8 bits: every layer norms the residual stream into 8 bits, projects it to
+    gates and candidates, runs the recurrence over the batch's sequences, and projects its normed result back; the head gives the
+    log probability of the tokens in `tok`, the entropy and the `top` alternatives.  steps = 1 is one generated token; a layer's
+    state comes in as h<l> and leaves as the output after the head's (in layer order)."""
+    rng, rows = rng_for(config), batch * steps
+    g = GraphSpec("recurrent_lm")
+    data = {}
+
+    def value(role, name, dt, shape, a):
+        data[name] = as_dtype(a, dt) if dt in ("f32", "bf16") else np.asarray(a, dtype=np.int8 if dt == "i8" else np.int32)
+        return (g.input if role == "input" else g.param)(name, dt, shape)
+
+    def alone(kind, ins, outs, **attrs):
+        o, got = g.op(kind, ins, outs, **attrs)
+        g.group([o])
+        return got
+
+    def norm(name, x, r=None):
+        gain = value("param", name + ".gain", "f32", (dim,), uniform(rng, (dim,), 0.5, 1.5))
+        outs = [("i8", (rows, dim)), ("f32", (rows,))] + ([(dtype, (rows, dim))] if r is not None else [])
+        return alone("rms_norm_q8", [x, gain] if r is None else [x, r, gain], outs, eps=1e-5)
+
+    def project(name, q, s, n, out):
+        w = value("param", name + ".w", "i8", (n, dim), rng.integers(-127, 128, size=(n, dim)))
+        sw = value("param", name + ".sw", "f32", (n,), uniform(rng, (n,), 0.5, 1.5) / (73.0 * np.sqrt(dim)))
+        b = value("param", name + ".b", "f32", (n,), normal(rng, (n,), 0.5))
+        return alone("dense_q8", [q, s, w, sw, b], [(out, (rows, n))], out_dtype=out)[0]
+
+    x = value("input", "x", dtype, (rows, dim), normal(rng, (rows, dim)))
+    tok = value("input", "tok", "i32", (rows,), rng.integers(-1, vocab, size=rows))
+    keep = None
+    if packed:
+        flags = np.where(rng.uniform(size=(batch, steps)) < 0.1, 2, 1)
+        flags[0, steps - steps // 4:] = 0
+        keep = value("input", "keep", "i8", (rows,), flags.reshape(-1))
+    r, states = None, []
+    for l in range(layers):
+        normed = norm(f"l{l}.in", x, r)
+        q, s = normed[:2]
+        x = normed[2] if r is not None else x
+        z = project(f"l{l}.z", q, s, 2 * dim, dtype)
+        h0 = value("input", f"h{l}", "f32", (batch, dim), normal(rng, (batch, dim), 0.3))
+        h, hT = alone("linear_scan", [z, h0] + ([keep] if packed else []), [(dtype, (rows, dim)), ("f32", (batch, dim))])
+        states.append(hT)
+        q, s = norm(f"l{l}.out", h)
+        r = project(f"l{l}.o", q, s, dim, dtype)
+    q, s, _ = norm("head", x, r)
+    logits = project("head", q, s, vocab, "f32")
+    outs = [("f32", (rows,)), ("f32", (rows,))] + ([("f32", (rows, top)), ("i32", (rows, top))] if top else [])
+    for v in alone("token_logprobs", [logits, tok], outs, top=top) + states:
+        g.output(v)
+    return g, data
+
+
+def recurrent_lm_train(batch=4, steps=16, dim=64, vocab=500, dtype="bf16", packed=False, config=32):
+    """One layer of that model in a float type and its training step as one graph: forward pass, loss (mean negative log probability of
+    the tokens and an entropy bonus, whose derivatives dlp and dent are inputs), gradients of both weights, of x and of the state.
+    A weight is two params, wz and wv of the forward and wz_b and wv_b of the backward pass: a param has one layout in a plan."""
+    rng, rows = rng_for(config), batch * steps
+    g = GraphSpec("recurrent_lm_train")
+    data = {"x": as_dtype(normal(rng, (rows, dim)), dtype), "wz": as_dtype(normal(rng, (2 * dim, dim), dim ** -0.5), dtype),
+            "wv": as_dtype(normal(rng, (vocab, dim), 2 * dim ** -0.5), dtype), "h0": as_dtype(normal(rng, (batch, dim), 0.3), "f32"),
+            "tok": rng.integers(-1, vocab, size=rows).astype(np.int32), "dlp": as_dtype(np.full(rows, -1.0 / rows), "f32"),
+            "dent": as_dtype(np.full(rows, -0.01 / rows), "f32"), "dhT": as_dtype(np.zeros((batch, dim)), "f32")}
+    data |= {"wz_b": data["wz"], "wv_b": data["wv"]}
+    x, tok = g.input("x", dtype, (rows, dim)), g.input("tok", "i32", (rows,))
+    h0, dhT = g.input("h0", "f32", (batch, dim)), g.input("dhT", "f32", (batch, dim))
+    dlp, dent = g.input("dlp", "f32", (rows,)), g.input("dent", "f32", (rows,))
+    wz, wv = g.param("wz", dtype, (2 * dim, dim)), g.param("wv", dtype, (vocab, dim))
+    wz_b, wv_b = g.param("wz_b", dtype, (2 * dim, dim)), g.param("wv_b", dtype, (vocab, dim))
+    keep = []
+    if packed:
+        data["keep"] = np.where(rng.uniform(size=rows) < 0.1, 2, np.where(rng.uniform(size=rows) < 0.1, 0, 1)).astype(np.int8)
+        keep = [g.input("keep", "i8", (rows,))]
+
+    def alone(kind, ins, outs, **attrs):
+        o, got = g.op(kind, ins, outs, **attrs)
+        g.group([o])
+        for v in got:
+            g.output(v)
+        return got
+
+    z, = alone("dense", [x, wz], [(dtype, (rows, 2 * dim))])
+    h, hT = alone("linear_scan", [z, h0] + keep, [(dtype, (rows, dim)), ("f32", (batch, dim))])
+    logits, = alone("dense", [h, wv], [(dtype, (rows, vocab))])
+    alone("token_logprobs", [logits, tok], [("f32", (rows,)), ("f32", (rows,))], top=0)
+    dlogits, = alone("token_logprobs_grad", [logits, tok, dlp, dent], [(dtype, (rows, vocab))])
+    dh, = alone("dense_grad_x", [dlogits, wv_b], [(dtype, (rows, dim))])
+    alone("dense_grad_w", [dlogits, h], [("f32", (vocab, dim))], out_dtype="f32")
+    dz, dh0 = alone("linear_scan_grad", [z, h0, dh, dhT] + keep, [(dtype, (rows, 2 * dim)), ("f32", (batch, dim))])
+    alone("dense_grad_x", [dz, wz_b], [(dtype, (rows, dim))])
+    alone("dense_grad_w", [dz, x], [("f32", (2 * dim, dim))], out_dtype="f32")
+    return g, data
 
 
 # --------------------------------------------------------------------------
