@@ -515,7 +515,10 @@ namespace {
 
 struct Form { int W, rows; bool split; int32_t slabs, tiles; };
 
-// Waves of a workgroup: enough for the rows, eight where there are few workgroups.  split: tiles as workgroups of their own.
+// Waves of a workgroup: enough for the rows, eight where there are few workgroups.  split: tiles as workgroups of their own, where there are
+// fewer than 128 workgroups that walk (channels of 64 x rows, bf16, forward pass: 64 x 2400 walking 33 us, split 23; 128 x 2400 39 and 42;
+// 192 x 2400 44 and 62; both passes 16 x 600 27 and 18, 128 x 2400 106 and 107); of four waves up to some 4000 rows, eight from there on
+// (both passes, 64 x 2400 58 and 62 us, 16 x 16384 112 and 102)
 Form form_of(const ScanParams &p, bool grad)
 {
     const int64_t vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1;
@@ -525,7 +528,7 @@ Form form_of(const ScanParams &p, bool grad)
     f.split = false;
     for (int walks = 1; walks >= 0; --walks) {
         f.rows = grad ? bwd_rows(walks, p.keeps) : FWD_ROWS;
-        f.W = p.T <= 2 * f.rows ? 1 : p.T <= 8 * f.rows || wgs >= 512 ? 4 : 8;
+        f.W = p.T <= 2 * f.rows ? 1 : p.T <= 8 * f.rows || wgs >= 512 || (!walks && p.T < 4096) ? 4 : 8;
         f.tiles = (int32_t)((p.T + 2 * f.W * f.rows - 1) / (2 * f.W * f.rows));
         if (wgs >= 128 || f.tiles == 1) break;
         f.split = true;
@@ -549,8 +552,8 @@ void go(bool grad, const ScanParams &p, const Form &f, hipStream_t s)
 template <typename E, int VEC>
 void go(bool grad, int mode, const ScanParams &p, const Form &f, hipStream_t s)
 {
-    if (mode == 1) go<E, VEC, 8, 1>(grad, p, f, s);
-    else if (mode == 2) go<E, VEC, 8, 2>(grad, p, f, s);
+    if (mode == 1) f.W == 4 ? go<E, VEC, 4, 1>(grad, p, f, s) : go<E, VEC, 8, 1>(grad, p, f, s);
+    else if (mode == 2) f.W == 4 ? go<E, VEC, 4, 2>(grad, p, f, s) : go<E, VEC, 8, 2>(grad, p, f, s);
     else if (f.W == 1) go<E, VEC, 1, 0>(grad, p, f, s);
     else if (f.W == 4) go<E, VEC, 4, 0>(grad, p, f, s);
     else go<E, VEC, 8, 0>(grad, p, f, s);
