@@ -14,22 +14,15 @@ namespace {
 template <int T>
 __device__ __forceinline__ void reduce_sum_max(float &a, float &b)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        a += __shfl_xor(a, o);
-        b = fmaxf(b, __shfl_xor(b, o));
-    }
+    a = wave_sum(a);
+    b = wave_max(b);
     if constexpr (T > 64) {
         __shared__ float sa[T / 64], sb[T / 64];
-        const int w = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) { sa[w] = a; sb[w] = b; }
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+        if (lane == 0) { sa[w] = a; sb[w] = b; }
         __syncthreads();
-        a = sa[threadIdx.x & (T / 64 - 1)]; b = sb[threadIdx.x & (T / 64 - 1)];
-#pragma unroll
-        for (int o = T / 128; o > 0; o >>= 1) {
-            a += __shfl_xor(a, o);
-            b = fmaxf(b, __shfl_xor(b, o));
-        }
+        a = wave_sum(lane < T / 64 ? sa[lane] : 0.0f);
+        b = wave_max(lane < T / 64 ? sb[lane] : 0.0f);
     }
 }
 

@@ -18,6 +18,27 @@ __device__ __forceinline__ int32_t anew(int32_t v)
     return v;
 }
 
+// Sum and maximum over the wave, in every lane: rows of sixteen lanes by shifts, then the rows one into the next, without the LDS that a
+// shuffle goes through (six dependent instructions, not six round trips).  All lanes have to be active.
+template <bool MAX> __device__ __forceinline__ float over_wave(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+#define RL_STEP(CTRL, ROWS)                                                                                                        \
+    {                                                                                                                              \
+        const int o = __builtin_amdgcn_update_dpp(MAX ? __builtin_bit_cast(int, v) : 0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false); \
+        v = MAX ? fmaxf(v, __builtin_bit_cast(float, o)) : v + __builtin_bit_cast(float, o);                                       \
+    }
+    RL_STEP(0x111, 0xf) RL_STEP(0x112, 0xf) RL_STEP(0x114, 0xf) RL_STEP(0x118, 0xf)      // row_shr 1, 2, 4, 8
+    RL_STEP(0x142, 0xa) RL_STEP(0x143, 0xc)                                              // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+#undef RL_STEP
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+#else
+    return v;
+#endif
+}
+__device__ __forceinline__ float wave_sum(float v) { return over_wave<false>(v); }
+__device__ __forceinline__ float wave_max(float v) { return over_wave<true>(v); }
+
 template <typename E> __device__ __forceinline__ float unpack(const u32x4 &r, int k)
 {
     if constexpr (sizeof(E) == 4) return __uint_as_float(r[k]);

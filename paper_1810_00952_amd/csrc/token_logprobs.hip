@@ -36,15 +36,12 @@ __device__ __forceinline__ void rescale(Soft &a, float m)
     a.m = m;
 }
 
-// of LANES lanes side by side, in every one of them
-template <int LANES> __device__ __forceinline__ Soft join_lanes(Soft a)
+// of the wave's lanes, in every one of them
+__device__ __forceinline__ Soft join_lanes(Soft a)
 {
-    float m = a.m;
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    rescale(a, m);
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) { a.s += __shfl_xor(a.s, o); a.u += __shfl_xor(a.u, o); }
+    rescale(a, wave_max(a.m));
+    a.s = wave_sum(a.s);
+    a.u = wave_sum(a.u);
     return a;
 }
 
@@ -112,11 +109,12 @@ struct Part : RowVectors<E, T, NV> {
 template <int T>
 __device__ __forceinline__ Soft join_workgroup(Soft a, Soft *sh)
 {
-    a = join_lanes<64>(a);
+    a = join_lanes(a);
     if constexpr (T > 64) {
-        if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = a;
+        const int lane = threadIdx.x & 63;
+        if (lane == 0) sh[threadIdx.x >> 6] = a;
         __syncthreads();
-        a = join_lanes<T / 64>(sh[threadIdx.x & (T / 64 - 1)]);
+        a = join_lanes(lane < T / 64 ? sh[lane] : Soft{LOWEST, 0.0f, 0.0f});
     }
     return a;
 }
@@ -136,13 +134,22 @@ struct Result {
     __device__ __forceinline__ float logp(float x) const { return dead ? -INFINITY : x - m - ls; }
 };
 
-__device__ __forceinline__ void store_row(const LogprobsParams &p, int64_t row, const Result &r)
-{
-    const int tok = p.tok[row];
-    const bool given = tok >= 0 && tok < p.V;
-    p.lp[row] = r.ls != r.ls ? r.ls : given ? r.logp(load_as_f32(p.x, p.dtype, row * p.V + tok)) : 0.0f;
-    p.ent[row] = r.ent;
-}
+// the row's token, its logit asked for ahead of the statistics
+struct Target {
+    bool given;
+    float x;
+    __device__ __forceinline__ Target(const LogprobsParams &p, int64_t row)
+    {
+        const int tok = p.tok[row];
+        given = tok >= 0 && tok < p.V;
+        x = load_as_f32(p.x, p.dtype, row * p.V + (given ? tok : 0));
+    }
+    __device__ __forceinline__ void store(const LogprobsParams &p, int64_t row, const Result &r) const
+    {
+        p.lp[row] = r.ls != r.ls ? r.ls : given ? r.logp(x) : 0.0f;
+        p.ent[row] = r.ent;
+    }
+};
 
 // `top` keys of the workgroup's part into out (LDS), largest first; zero where there are no more.  T >= 64.
 template <typename E, int T, int NV>
@@ -270,7 +277,7 @@ __device__ __forceinline__ Soft join_segments(const LogprobsParams &p, int64_t r
     static_assert(MAX_SEGS <= 64, "a lane each");
     const int lane = threadIdx.x & 63;
     const float *v = p.part + (row * segs + lane) * seg_floats(p.top);
-    return join_lanes<64>(lane < segs ? Soft{v[0], v[1], v[2]} : Soft{LOWEST, 0.0f, 0.0f});
+    return join_lanes(lane < segs ? Soft{v[0], v[1], v[2]} : Soft{LOWEST, 0.0f, 0.0f});
 }
 
 enum { FORWARD = 1, GRADIENT = 2, SEGMENT = 4, JOINED = 8 };     // what a launch does: JOINED takes the statistics from part
@@ -286,6 +293,7 @@ __global__ __launch_bounds__(T, NV == 16 ? 4 : 8) void token_logprobs_kernel(con
     const int32_t seg = (int32_t)(blockIdx.x - (uint32_t)row * segs), lo = seg * seg_len;
     Part<E, T, NV> x(p.x, row, p.V, lo, (int32_t)min((int64_t)lo + seg_len, p.V));
     x.load();
+    const Target target(p, row);
     float most = 0.0f;
     const Soft a = WHAT & JOINED ? join_segments(p, row, segs) : join_workgroup<T>(x.stats(most), sh);
     if constexpr (WHAT & (FORWARD | SEGMENT)) {
@@ -299,7 +307,7 @@ __global__ __launch_bounds__(T, NV == 16 ? 4 : 8) void token_logprobs_kernel(con
     }
     const Result r(a);
     if constexpr (WHAT & FORWARD) {
-        if (threadIdx.x == 0) store_row(p, row, r);
+        if (threadIdx.x == 0) target.store(p, row, r);
         if ((int)threadIdx.x < p.top) {
             const uint64_t key = keys[threadIdx.x];
             p.top_id[row * p.top + threadIdx.x] = (int32_t)key_index(key);
@@ -319,8 +327,9 @@ __global__ __launch_bounds__(256) void token_logprobs_join_kernel(const Logprobs
     const int n = segs * p.top, t = threadIdx.x;
     for (int i = t; i < n; i += 256) keys[i] = ((const uint64_t *)(q + (i / p.top) * seg_floats(p.top) + 4))[i % p.top];
     if (t == 0) count = 0;
+    const Target target(p, row);
     const Result r(join_segments(p, row, segs));
-    if (t == 0) store_row(p, row, r);
+    if (t == 0) target.store(p, row, r);
     if (p.top == 0) return;
     __syncthreads();
     // the top-th of the segments' first `each`, which are `top` or a few more: nothing below it is wanted
