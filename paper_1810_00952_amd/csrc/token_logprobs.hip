@@ -21,7 +21,7 @@ namespace {
 
 constexpr int CAND = 512;                        // candidates a workgroup collects
 constexpr int MAX_SEGS = 64;                     // of a row
-constexpr float LOWEST = -3.0e38f;               // a lane's maximum at least: -inf less it is -inf, not NaN
+constexpr float LOWEST = -3.40282347e38f;        // the lowest number, a lane's maximum at least: -inf less it is -inf, not NaN
 
 // maximum (at least LOWEST), S and U of x less it
 struct Soft { float m, s, u; };
@@ -30,7 +30,7 @@ __device__ __forceinline__ float e_to(float x) { return __expf(x); }
 
 __device__ __forceinline__ void rescale(Soft &a, float m)
 {
-    const float d = a.m - m, e = e_to(d);
+    const float d = fmaxf(a.m - m, -1e4f), e = e_to(d);      // two maxima may be further apart than f32 reaches; of +inf S is NaN
     a.u = (a.u + a.s * d) * e;
     a.s *= e;
     a.m = m;

@@ -335,6 +335,42 @@ def test_logits_that_are_no_numbers(v):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [3, 700, 9000, 70001])
+def test_logits_at_the_ends_of_their_type(v, dtype):
+    """Masks of the type's lowest number: among other logits their p is 0, a row of nothing else is a uniform distribution; logits further apart
+    than f32 reaches."""
+    import torch
+    low = float(torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min)
+    rng = np.random.default_rng(v)
+    x = rng.normal(size=(6, v))
+    x[0] = low                                     # nothing but masks
+    x[1] = np.where(np.arange(v) % 3 == 0, low, -np.inf)
+    x[2, ::2] = low                                # some of them
+    x[3] = np.where(np.arange(v) % 5 == 1, -low, 0.0)
+    x[4] = np.where(np.arange(v) % 5 == 1, -low, low)
+    x[5] = -np.inf
+    x[5, v - 1] = low                              # one
+    tx, x = tensor(x, dtype)
+    tok = np.array([v - 1, 0, 1, 1, 1, v - 1])
+    tt, _ = tensor(tok, "i32")
+    ts, one = tensor(np.ones(6), "f32")
+    out = Call("token_logprobs", [(tx, dtype), (tt, "i32")], [("f32", (6,)), ("f32", (6,)), ("f32", (6, 3)), ("i32", (6, 3))], top=3).run().numbers()
+    dx, = Call("token_logprobs_grad", [(tx, dtype), (tt, "i32"), (ts, "f32"), (ts, "f32")], [(dtype, (6, v))]).run().numbers()
+    lp, ent, top_lp, ids = L.token_logprobs(x, tok, 3)
+    ln_s, tol_ent = soft_bounds(x)
+    within(out[0], lp, ln_s + 3 * F32 * np.abs(lp), "lp")
+    within(out[1], ent, tol_ent, "ent")
+    np.testing.assert_array_equal(out[3], ids)
+    shown = np.where(top_lp < low, -np.inf, top_lp)       # ln p past f32 is -inf in it
+    within(out[2], shown, ln_s[:, None] + 3 * F32 * np.abs(np.where(np.isfinite(shown), shown, 0)), "top_lp")
+    ref = L.token_logprobs_grad(x, tok, one, one)
+    logs, p, _ = L._softmax(x)
+    # |ln p| is at most ln V + 12 where p is not 0 in f32: the bound of a factor of that size on every term
+    tol = p * (ln_s + tol_ent + 16 * F32)[:, None] * (2 + 2 * np.log(v) + 12) + 4 * F32 * np.abs(ref)
+    within(dx, ref, tol + (BF16 * (np.abs(ref) + tol) if dtype == "bf16" else 0), "dx")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,v", LOGITS)
 def test_logprobs_grad(m, v, dtype):
     for masked in (False, True):
