@@ -9,7 +9,8 @@
 // A run of rows takes the state before it to A h + H, with A the product of its gates and H its own result from zero, and two runs
 // one behind the other join as (A2 A1, A2 H1 + H2).  So a tile of 32 W runs of ROWS rows is worked off at once: a workgroup of W waves
 // owns 32 lanes x 4 bytes of channels (whole 128-byte lines) and each half of a wave one run, which it reads once, into registers:
-// prefix products and results of its rows from zero.  The runs' (A, H) meet in LDS, every run adds up those before it, and one fma a
+// prefix products and results of its rows from zero.  A run with a document's first row has -0 for A, which no product of gates
+// is: nothing of what comes before goes into what follows, neither an infinity nor NaN.  The runs' (A, H) meet in LDS, every run adds up those before it, and one fma a
 // row then gives the states.  The workgroup carries the tile's last state on to its next tile, whose rows are requested as
 // the registers of this one's become free.  Nothing is read twice.  What bounds it is HBM.
 //
@@ -51,6 +52,16 @@ template <typename E, int VEC> __device__ __forceinline__ typename Raw<E, VEC>::
     if constexpr (sizeof(E) == 4) return __float_as_uint(v[0]);
     else return (typename Raw<E, VEC>::type)pack_bf16x2(v[0], v[VEC - 1]);
 }
+
+// A x + H and A b of runs' A (KEEP: there may be documents' first rows)
+constexpr float FIRST = -0.0f;
+__device__ __forceinline__ bool is_first(float A) { return __float_as_uint(A) == 0x80000000u; }
+template <bool KEEP> __device__ __forceinline__ float through(float A, float x, float H)
+{
+    const float y = __builtin_fmaf(A, x, H);
+    return KEEP && is_first(A) ? H : y;
+}
+template <bool KEEP> __device__ __forceinline__ float both(float A, float b) { return KEEP && (is_first(A) || is_first(b)) ? FIRST : A * b; }
 
 // Rows of a tile in memory: `room` bytes from the tile's first row to the sequence's last.  What lies behind them reads as zero and is
 // not written; so does what a lane without channels (offset OOB) asks for.
@@ -110,7 +121,7 @@ struct Place {
 
 // c, taken through tiles from .. to - 1 (BACK: to - 1 .. from) of `part`, whose vectors of a tile are `stride` floats apart, A first and
 // the addend at `add`.  Every run of the workgroup joins its share of the tiles, then all of them the shares.
-template <int VEC, int W, bool BACK>
+template <int VEC, int W, bool BACK, bool KEEP>
 __device__ __forceinline__ void through_tiles(const float *part, int64_t stride, int64_t add, int32_t from, int32_t to, int run, float (&c)[VEC],
                                               float (&sa)[2 * W][32][VEC], float (&sx)[2 * W][32][VEC])
 {
@@ -126,8 +137,8 @@ __device__ __forceinline__ void through_tiles(const float *part, int64_t stride,
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             const float ka = q[j];
-            x[j] = __builtin_fmaf(ka, x[j], q[add + j]);
-            a[j] *= ka;
+            x[j] = through<KEEP>(ka, x[j], q[add + j]);
+            a[j] = both<KEEP>(a[j], ka);
         }
     }
 #pragma unroll
@@ -136,11 +147,11 @@ __device__ __forceinline__ void through_tiles(const float *part, int64_t stride,
 #pragma unroll 4
     for (int r = 0; r < 2 * W; ++r)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) c[j] = __builtin_fmaf(sa[r][l32][j], c[j], sx[r][l32][j]);
+        for (int j = 0; j < VEC; ++j) c[j] = through<KEEP>(sa[r][l32][j], c[j], sx[r][l32][j]);
 }
 
-// bit i: row t0 + i is padding (or past the sequence), is a document's first
-template <int ROWS> struct Flags { uint32_t pad, first; };
+// bit i: row t0 + i is padding (or past the sequence), is a document's first, is at or behind one of the run
+template <int ROWS> struct Flags { uint32_t pad, first, behind; };
 template <int ROWS, bool KEEP>
 __device__ __forceinline__ Flags<ROWS> flags_of(const ScanParams &p, int64_t b, int64_t t0, int half)
 {
@@ -148,7 +159,8 @@ __device__ __forceinline__ Flags<ROWS> flags_of(const ScanParams &p, int64_t b, 
     const bool in = i < ROWS && t0 + i < p.T;
     const int k = !in ? 0 : KEEP ? p.keep[b * p.T + t0 + i] : 1;
     const uint64_t pad = __ballot(k == 0), first = __ballot(k == 2);
-    return {(uint32_t)(pad >> (32 * half)), (uint32_t)(first >> (32 * half))};
+    const uint32_t f = (uint32_t)(first >> (32 * half));
+    return {(uint32_t)(pad >> (32 * half)), f, (uint32_t)-(int32_t)(f & (uint32_t)-(int32_t)f)};
 }
 
 }  // namespace
@@ -213,7 +225,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
         for (int j = 0; j < VEC; ++j) carry[j] = p.h0[chan + j];
         if constexpr (MODE == 2) {
             __shared__ float ta[2 * W][32][VEC], th[2 * W][32][VEC];
-            through_tiles<VEC, W, false>(p.part + chan, 2 * BD, BD, 0, at.seg, at.run, carry, ta, th);
+            through_tiles<VEC, W, false, KEEP>(p.part + chan, 2 * BD, BD, 0, at.seg, at.run, carry, ta, th);
         }
     }
     for (int32_t tile = first_tile; tile < last_tile; ++tile) {
@@ -222,24 +234,26 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
         const uint32_t off2 = anew(at.off2), off1 = anew(at.off1);
         if (MODE == 0 && tile + 1 < last_tile) z = rows_of(p.z, tile + 1, 2);
         float A[ROWS][VEC], H[ROWS][VEC];
-        Flags<ROWS> fl{0, 0};
+        Flags<ROWS> fl{0, 0, 0};
         float pa[VEC], ph[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) { pa[j] = 1.0f; ph[j] = 0.0f; }
         auto rows = [&](auto masked) {
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
+                const raw_t qf = MODE == 0 ? rf[i] : anew(rf[i]), qv = MODE == 0 ? rv[i] : anew(rv[i]);
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     float a, rest;
-                    gate(unpack<E, VEC>(rf[i], j), a, rest);
-                    float u = rest * unpack<E, VEC>(rv[i], j);
+                    gate(unpack<E, VEC>(qf, j), a, rest);
+                    float u = rest * unpack<E, VEC>(qv, j);
                     if (masked) {
                         const bool pad = fl.pad >> i & 1u;
-                        a = pad ? 1.0f : fl.first >> i & 1u ? 0.0f : a;
+                        a = pad ? 1.0f : a;
                         u = pad ? 0.0f : u;
+                        if (KEEP && (fl.first >> i & 1u)) ph[j] = 0.0f;
                     }
-                    pa[j] *= a;
+                    pa[j] = KEEP && (fl.behind >> i & 1u) ? FIRST : pa[j] * a;
                     ph[j] = __builtin_fmaf(a, ph[j], u);
                     A[i][j] = pa[j]; H[i][j] = ph[j];
                 }
@@ -260,8 +274,8 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
         if (at.half) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                sa[buf][at.wave][l32][j] = pa[j] * oa[j];
-                sh[buf][at.wave][l32][j] = __builtin_fmaf(pa[j], oh[j], ph[j]);
+                sa[buf][at.wave][l32][j] = both<KEEP>(pa[j], oa[j]);
+                sh[buf][at.wave][l32][j] = through<KEEP>(pa[j], oh[j], ph[j]);
             }
         }
         if (W > 1) __syncthreads(); else wave_lds_exchange();
@@ -272,7 +286,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
                 for (int j = 0; j < VEC; ++j) {
                     float ta = 1.0f, th = 0.0f;
 #pragma unroll
-                    for (int w = 0; w < W; ++w) { th = __builtin_fmaf(sa[0][w][l32][j], th, sh[0][w][l32][j]); ta *= sa[0][w][l32][j]; }
+                    for (int w = 0; w < W; ++w) { th = through<KEEP>(sa[0][w][l32][j], th, sh[0][w][l32][j]); ta = both<KEEP>(ta, sa[0][w][l32][j]); }
                     p.part[2 * at.seg * BD + chan + j] = ta;
                     p.part[(2 * at.seg + 1) * BD + chan + j] = th;
                 }
@@ -284,11 +298,11 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 if (w == at.wave) mine[j] = carry[j];
-                carry[j] = __builtin_fmaf(sa[buf][w][l32][j], carry[j], sh[buf][w][l32][j]);
+                carry[j] = through<KEEP>(sa[buf][w][l32][j], carry[j], sh[buf][w][l32][j]);
             }
         if (at.half) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) mine[j] = __builtin_fmaf(oa[j], mine[j], oh[j]);
+            for (int j = 0; j < VEC; ++j) mine[j] = through<KEEP>(oa[j], mine[j], oh[j]);
         }
         if (at.live) {
             if (p.states && t0 % p.state_rows == 0 && t0 < p.T) {
@@ -303,7 +317,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
                     float out[VEC];
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-                        out[j] = __builtin_fmaf(A[i][j], mine[j], H[i][j]);
+                        out[j] = __builtin_fmaf(A[i][j], KEEP && (fl.behind >> i & 1u) ? 0.0f : mine[j], H[i][j]);
                         if (KEEP && (fl.pad >> i & 1u)) out[j] = 0.0f;
                     }
                     store(h, off1 + i * line, pack<E, VEC>(out));
@@ -357,8 +371,8 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
 #pragma unroll
             for (int j = 0; j < VEC; ++j) start[j] = p.h0[chan + j];
             __shared__ float ta[2][2 * W][32][VEC], tx[2][2 * W][32][VEC];
-            through_tiles<VEC, W, false>(p.part + chan, 3 * BD, BD, 0, at.seg, at.run, start, ta[0], tx[0]);
-            through_tiles<VEC, W, true>(p.part + chan, 3 * BD, 2 * BD, at.seg + 1, tiles, at.run, gcarry, ta[1], tx[1]);
+            through_tiles<VEC, W, false, KEEP>(p.part + chan, 3 * BD, BD, 0, at.seg, at.run, start, ta[0], tx[0]);
+            through_tiles<VEC, W, true, KEEP>(p.part + chan, 3 * BD, 2 * BD, at.seg + 1, tiles, at.run, gcarry, ta[1], tx[1]);
         }
     }
     for (int32_t tile = first_tile; tile > last_tile; --tile) {
@@ -373,7 +387,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
         float a[ROWS][VEC], rest[ROWS][VEC], before[ROWS][VEC];   // before: of the state before the row, the run's own part
         raw_t kv[ROWS], kd[ROWS];
         float pa[VEC], ph[VEC], pg[VEC];
-        Flags<ROWS> fl{0, 0};
+        Flags<ROWS> fl{0, 0, 0};
 #pragma unroll
         for (int j = 0; j < VEC; ++j) { pa[j] = 1.0f; ph[j] = 0.0f; pg[j] = 0.0f; }
         auto rows = [&](auto masked) {
@@ -387,13 +401,15 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                     if (masked) {
                         const bool pad = fl.pad >> i & 1u;
                         dh = pad ? 0.0f : dh;
-                        af = pad ? 1.0f : fl.first >> i & 1u ? 0.0f : af;
+                        af = pad ? 1.0f : af;
                         u = pad ? 0.0f : u;
+                        if (KEEP && (fl.first >> i & 1u)) ph[j] = 0.0f;
                     }
+                    const bool behind = KEEP && (fl.behind >> i & 1u);
                     before[i][j] = ph[j];
-                    pa[j] *= af;
+                    pa[j] = behind ? FIRST : pa[j] * af;
                     ph[j] = __builtin_fmaf(af, ph[j], u);
-                    pg[j] = __builtin_fmaf(pa[j], dh, pg[j]);
+                    pg[j] = __builtin_fmaf(pa[j], behind ? 0.0f : dh, pg[j]);
                 }
                 kv[i] = rv[i]; kd[i] = rd[i];
                 if (MODE == 0 && tile > 0) request(off2, off1, i);
@@ -412,9 +428,9 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
         if (at.half) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                sa[buf][at.wave][l32][j] = pa[j] * oa[j];
-                sh[buf][at.wave][l32][j] = __builtin_fmaf(pa[j], oh[j], ph[j]);
-                sg[buf][at.wave][l32][j] = __builtin_fmaf(oa[j], pg[j], og[j]);
+                sa[buf][at.wave][l32][j] = both<KEEP>(pa[j], oa[j]);
+                sh[buf][at.wave][l32][j] = through<KEEP>(pa[j], oh[j], ph[j]);
+                sg[buf][at.wave][l32][j] = through<KEEP>(oa[j], pg[j], og[j]);
             }
         }
         if (W > 1) __syncthreads(); else wave_lds_exchange();
@@ -425,9 +441,9 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                     float ta = 1.0f, th = 0.0f, tg = 0.0f;
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
-                        tg = __builtin_fmaf(ta, sg[0][w][l32][j], tg);
-                        th = __builtin_fmaf(sa[0][w][l32][j], th, sh[0][w][l32][j]);
-                        ta *= sa[0][w][l32][j];
+                        tg = through<KEEP>(ta, sg[0][w][l32][j], tg);
+                        th = through<KEEP>(sa[0][w][l32][j], th, sh[0][w][l32][j]);
+                        ta = both<KEEP>(ta, sa[0][w][l32][j]);
                     }
                     p.part[3 * at.seg * BD + chan + j] = ta;
                     p.part[(3 * at.seg + 1) * BD + chan + j] = th;
@@ -445,19 +461,19 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 if (w == at.wave) h[j] = c[j];
-                c[j] = __builtin_fmaf(sa[buf][w][l32][j], c[j], sh[buf][w][l32][j]);
+                c[j] = through<KEEP>(sa[buf][w][l32][j], c[j], sh[buf][w][l32][j]);
             }
 #pragma unroll AT_ONCE
         for (int w = W - 1; w >= 0; --w)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 if (w == at.wave) G[j] = gcarry[j];
-                gcarry[j] = __builtin_fmaf(sa[buf][w][l32][j], gcarry[j], sg[buf][w][l32][j]);
+                gcarry[j] = through<KEEP>(sa[buf][w][l32][j], gcarry[j], sg[buf][w][l32][j]);
             }
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            if (at.half) h[j] = __builtin_fmaf(oa[j], h[j], oh[j]);
-            else G[j] = __builtin_fmaf(oa[j], G[j], og[j]);
+            if (at.half) h[j] = through<KEEP>(oa[j], h[j], oh[j]);
+            else G[j] = through<KEEP>(oa[j], G[j], og[j]);
         }
         if (at.live) {
             // the state before every row, then the rows backwards
@@ -467,13 +483,9 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                     float run = h[j];                        // the start times the gates so far
 #pragma unroll
                     for (int i = 0; i < ROWS; ++i) {
+                        if (KEEP && (fl.first >> i & 1u)) run = 0.0f;
                         before[i][j] += run;
-                        float af = a[i][j];
-                        if (masked) {
-                            if (fl.first >> i & 1u) before[i][j] = 0.0f;
-                            af = fl.pad >> i & 1u ? 1.0f : fl.first >> i & 1u ? 0.0f : af;
-                        }
-                        run *= af;
+                        run *= masked && (fl.pad >> i & 1u) ? 1.0f : a[i][j];
                     }
                 }
                 const Rows dz = rows_of(p.dz, tile, 2);

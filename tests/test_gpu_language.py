@@ -215,6 +215,58 @@ def test_scan_grad(b, t, d, dtype):
         check_grad(case[0].run().numbers(), *case[1:], dtype, what)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,t,d", [(2, 9, 3), (3, 64, 66), (1, 3001, 40), (1, 6000, 130), (8, 300, 1024), (130, 260, 64)])
+def test_documents_are_apart(b, t, d, dtype):
+    """NaN and infinities of a document, of the state before a first token and behind the last one stay where the definition has them."""
+    import torch
+    rng, z, h0, keep, operands, tk = scan_inputs(b, t, d, dtype, "some", seed=t)
+    keep = keep.reshape(b, t)
+    keep[:, 0] = 2
+    tk.view(b, t)[:, 0] = 2
+    tz, th = operands[0][0], operands[1][0]
+    tdh, dh = tensor(rng.normal(size=(b * t, d)), dtype)
+    tdT, dhT = tensor(rng.normal(size=(b, d)), "f32")
+    dh = np.where(keep.reshape(-1, 1) == 0, 0.0, dh)
+    z, dh, tz, tdh = z.reshape(b, t, 2 * d), dh.reshape(b, t, d), tz.view(b, t, 2 * d), tdh.view(b, t, d)
+    z[:, 0] = tz[:, 0].double().cpu().numpy()      # was padding or a token, and is a first one now
+    dh[:, 0] = tdh[:, 0].double().cpu().numpy()
+    if not np.isfinite(z[:, 0]).all():
+        z[:, 0] = 0.5
+        tz[:, 0] = 0.5
+    for i in range(b):
+        tokens, firsts = np.flatnonzero(keep[i] == 1), np.flatnonzero(keep[i] == 2)
+        for n, t0 in enumerate(rng.choice(tokens, size=min(4, len(tokens)), replace=False)):
+            c = int(rng.integers(0, d))
+            if n % 2 == 0:
+                z[i, t0, [c, d + c][n // 2]] = np.nan
+                tz[i, t0, [c, d + c][n // 2]] = float("nan")
+            else:
+                dh[i, t0, c] = np.nan
+                tdh[i, t0, c] = float("nan")
+        c = int(rng.integers(0, d))
+        dh[i, firsts[-1], c] = np.inf
+        tdh[i, firsts[-1], c] = float("inf")
+    h0[:, 0], th[:, 0] = np.nan, float("nan")
+    dhT[:, d - 1], tdT[:, d - 1] = np.nan, float("nan")
+    z, dh, tz, tdh, keep = z.reshape(b * t, 2 * d), dh.reshape(b * t, d), tz.view(b * t, 2 * d), tdh.view(b * t, d), keep.reshape(-1)
+    types = [(dtype, (b * t, d)), ("f32", (b, d)), (dtype, (b * t, 2 * d)), ("f32", (b, d))]
+    with np.errstate(invalid="ignore"):
+        after, before, last = scan_bounds(z, h0, keep)
+        states, (h, hT) = L.linear_scan(z, h0, keep, states=True)[2], L.linear_scan(z, h0, keep)
+        tf, tv, t0 = scan_grad_bounds(z, h0, dh, dhT, keep, states, before)
+        dz, dh0 = L.linear_scan_grad(z, h0, dh, dhT, keep)
+    # padding, whose result is zero: the bounds stand for a state it does not show
+    after, tol = (np.where(keep[:, None] == 0, 0.0, a.reshape(b * t, -1)) for a in (after, np.stack([tf, tv], 2)))
+    out = Call("linear_scan", [(tz, dtype), (th, "f32"), (tk, "i8")], types[:2]).run().numbers()
+    within(out[0], h, after + (BF16 * (np.abs(h) + after) if dtype == "bf16" else 0), "h")
+    within(out[1], hT, last, "hT")
+    out = Call("linear_scan_grad", [(tz, dtype), (th, "f32"), (tdh, dtype), (tdT, "f32"), (tk, "i8")], types[2:]).run().numbers()
+    within(out[0], dz, tol + (BF16 * (np.abs(dz) + tol) if dtype == "bf16" else 0), "dz")
+    within(out[1], dh0, t0, "dh0")
+    assert not out[1].any()                        # nothing goes back past a first token
+
+
 def test_scan_step_in_place():
     """A decoding step's new state over its old one."""
     for b, d, dtype in ((64, 1024, "f32"), (3, 77, "bf16")):
