@@ -26,13 +26,24 @@ __device__ __forceinline__ void reduce_sum_max(float &a, float &b)
     }
 }
 
+// the largest of |y g| by their bits, which order NaN above everything; where there is one, the sum of squares says so
+struct Largest {
+    uint32_t bits = 0;
+    __device__ __forceinline__ void take(float yg) { bits = max(bits, __float_as_uint(yg) & 0x7fffffffu); }
+    __device__ __forceinline__ float value(float &sum) const
+    {
+        if (bits > 0x7f800000u) sum = __builtin_nanf("");
+        return __uint_as_float(bits);
+    }
+};
+
 // what becomes of a row: its scale, and the factors that take y g to the number that is rounded
 struct Scale {
     float s, up, to_q;
     bool whole;
     __device__ __forceinline__ Scale(const NormQ8Params &p, float sum, float most)
     {
-        whole = sum < INFINITY && most < INFINITY;                  // an infinity or NaN in the row is one in its sum of squares
+        whole = sum < INFINITY && most < INFINITY;                  // an infinity or NaN in the row or NaN among y g is one in its sum of squares
         s = whole ? most * rsqrtf(sum / (float)p.D + p.eps) / 127.0f : __builtin_nanf("");
         up = most < 1e-30f ? 0x1p100f : 1.0f;                       // the factor of a tiny row would be past f32
         to_q = whole && most > 0.0f ? 127.0f / (most * up) : 0.0f;
@@ -76,7 +87,8 @@ __global__ __launch_bounds__(T) void norm_q8_row_kernel(const NormQ8Params p)
     u32x4 x[NV], res[NV];
     row.load((const E *)p.x + r * p.D, 0, x);
     if (RES) row.load((const E *)p.r + r * p.D, 0, res);
-    float yg[NV][N], sum = 0.0f, most = 0.0f;
+    float yg[NV][N], sum = 0.0f;
+    Largest largest;
     E *const yrow = RES ? (E *)p.y + r * p.D : nullptr;
     typename Row::Out yo{};
     if (RES) yo = row.out(yrow);
@@ -103,10 +115,11 @@ __global__ __launch_bounds__(T) void norm_q8_row_kernel(const NormQ8Params p)
             const float y = unpack<E>(x[j], k);
             sum = __builtin_fmaf(y, y, sum);
             yg[j][k] = y * g[k];
-            most = fmaxf(most, fabsf(yg[j][k]));
+            largest.take(yg[j][k]);
         }
     }
     if (RES) row.finish(yo, yrow);
+    float most = largest.value(sum);
     reduce_sum_max<T>(sum, most);
     const Scale scale(p, sum, most);
     if (threadIdx.x == 0) p.s[r] = scale.s;
@@ -128,7 +141,8 @@ constexpr int WG = 256;
 __global__ __launch_bounds__(WG) void norm_q8_kernel(const NormQ8Params p)
 {
     const int64_t row = blockIdx.x, at = row * p.D;
-    float sum = 0.0f, most = 0.0f;
+    float sum = 0.0f;
+    Largest largest;
     for (int64_t d = threadIdx.x; d < p.D; d += WG) {
         float y = load_as_f32(p.x, p.dtype, at + d);
         if (p.r) {
@@ -137,8 +151,9 @@ __global__ __launch_bounds__(WG) void norm_q8_kernel(const NormQ8Params p)
             if (p.dtype == DT_BF16) y = round_bf16(y);
         }
         sum += y * y;
-        most = fmaxf(most, fabsf(y * load_as_f32(p.g, p.g_dtype, d)));
+        largest.take(y * load_as_f32(p.g, p.g_dtype, d));
     }
+    float most = largest.value(sum);
     reduce_sum_max<WG>(sum, most);
     const Scale scale(p, sum, most);
     if (threadIdx.x == 0) p.s[row] = scale.s;

@@ -76,6 +76,19 @@ def test_norm_of_odd_rows(d):
     assert abs(out[0][4]).max() == 127 and out[0][7, 0] == -127
 
 
+@pytest.mark.parametrize("d", [1, 40, 515, 4096, 40000])
+def test_norm_with_a_gain_that_is_no_number(d):
+    """No row has a scale then, a row of zeros neither: 0 times NaN or infinity is NaN."""
+    for gain in (np.nan, -np.nan, np.inf):
+        for residual in (False, True):
+            call, x, r, g = norm_case(4, d, "f32", residual, "f32", seed=d, x=np.concatenate([np.zeros((1, d)), np.random.default_rng(d).normal(size=(3, d))]))
+            call.operands[-1][d // 2] = gain       # the gain
+            if residual:
+                call.operands[1][0] = 0.0
+            out = call.run().numbers()
+            assert np.isnan(out[1]).all() and not out[0].any(), (d, gain, residual)
+
+
 # ---- dense_q8 ------------------------------------------------------------------------------------------------------------
 def q8_case(m, n, k, out, bias, w_param=True, seed=0, edge=False):
     rng = np.random.default_rng(seed)
