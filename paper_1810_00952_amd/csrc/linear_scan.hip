@@ -29,10 +29,11 @@ namespace {
 constexpr int FWD_ROWS = 16;
 constexpr int bwd_rows(bool walks, bool keep) { return walks && !keep ? 16 : 8; }
 
-// sigmoid(f) and 1 - sigmoid(f), each to its own last bits.  Below -80 the gate stays at e^-80, which no f32 state is changed by.
+// sigmoid(f) and 1 - sigmoid(f), each to its own last bits.  Below -87 the gate stays at e^-87, near the least f32 holds to all its bits: it
+// leaves 6 of the largest state at most.
 __device__ __forceinline__ void gate(float f, float &a, float &rest)
 {
-    const float e = __expf(-(f < -80.0f ? -80.0f : f));      // NaN stays NaN
+    const float e = __expf(-(f < -87.0f ? -87.0f : f));      // NaN stays NaN
     a = rcp_(1.0f + e);
     rest = e * a;
 }
