@@ -80,11 +80,13 @@ template <typename R> __device__ __forceinline__ R load(const Rows &r, uint32_t 
     return 0;
 #endif
 }
-template <typename R> __device__ __forceinline__ void store(const Rows &r, uint32_t off, R v)
+// STREAM: not kept in the L2, for results whose 128-byte lines each are one workgroup's (8 x 4096 x 2048 bf16 forward and backward pass: 247 ->
+// 238 us; lines of two workgroups, 5 x 777 x 515 f32: 38.6 -> 42.2)
+template <bool STREAM, typename R> __device__ __forceinline__ void store(const Rows &r, uint32_t off, R v)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    if constexpr (sizeof(R) == 4) __builtin_amdgcn_raw_buffer_store_b32(v, r.rsrc, off, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b16(v, r.rsrc, off, 0, 0);
+    if constexpr (sizeof(R) == 4) __builtin_amdgcn_raw_buffer_store_b32(v, r.rsrc, off, 0, STREAM ? 2 : 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(v, r.rsrc, off, 0, STREAM ? 2 : 0);
 #endif
 }
 // a value the compiler takes as new: what is made of it (the offsets of a tile's rows, unpacked operands) is made where it is used, not kept
@@ -194,7 +196,7 @@ __global__ __launch_bounds__(256) void linear_scan_step_kernel(const ScanParams 
 // ---------------------------------------------------------------------------
 // forward.  MODE 0: a workgroup walks its channels' tiles; 1: (A, H) of one tile into part; 2: one tile, after those before it
 // ---------------------------------------------------------------------------
-template <typename E, int VEC, int W, int MODE, bool KEEP>
+template <typename E, int VEC, int W, int MODE, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
 {
     constexpr int ROWS = FWD_ROWS, AT_ONCE = MODE == 0 ? W : 4;      // other waves' sums read at once: those of all where there are registers for them
@@ -254,18 +256,21 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
                         u = pad ? 0.0f : u;
                         if (KEEP && (fl.first >> i & 1u)) ph[j] = 0.0f;
                     }
-                    pa[j] = KEEP && (fl.behind >> i & 1u) ? FIRST : pa[j] * a;
+                    pa[j] *= a;
                     ph[j] = __builtin_fmaf(a, ph[j], u);
                     A[i][j] = pa[j]; H[i][j] = ph[j];
                 }
                 if (MODE == 0 && tile + 1 < last_tile) request(off2, i);
             }
         };
-        if (KEEP || !whole) {
-            fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
-            rows(std::true_type{});
-        } else {
-            rows(std::false_type{});
+        if (KEEP || !whole) fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
+        // a wave that walks its tiles mostly has tokens alone; tiles as workgroups are launches too short to read two loops' code
+        const bool masked = KEEP ? MODE != 0 || __any((fl.pad | fl.first) != 0) : !whole;
+        if (masked) rows(std::true_type{});
+        else rows(std::false_type{});
+        if (KEEP && fl.first != 0) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) pa[j] = FIRST;
         }
         // the wave's two runs as one, the waves' in LDS
         float oa[VEC], oh[VEC];
@@ -313,16 +318,20 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
             }
             if (p.h) {
                 const Rows h = rows_of(p.h, tile, 1);
+                auto results = [&](auto masked) {
 #pragma unroll
-                for (int i = 0; i < ROWS; ++i) {
-                    float out[VEC];
+                    for (int i = 0; i < ROWS; ++i) {
+                        float out[VEC];
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        out[j] = __builtin_fmaf(A[i][j], KEEP && (fl.behind >> i & 1u) ? 0.0f : mine[j], H[i][j]);
-                        if (KEEP && (fl.pad >> i & 1u)) out[j] = 0.0f;
+                        for (int j = 0; j < VEC; ++j) {
+                            out[j] = masked && (fl.behind >> i & 1u) ? H[i][j] : __builtin_fmaf(A[i][j], mine[j], H[i][j]);
+                            if (masked && (fl.pad >> i & 1u)) out[j] = 0.0f;
+                        }
+                        store<STREAM>(h, off1 + i * line, pack<E, VEC>(out));
                     }
-                    store(h, off1 + i * line, pack<E, VEC>(out));
-                }
+                };
+                if (KEEP && masked) results(std::bool_constant<KEEP>{});
+                else results(std::false_type{});
             }
             if (p.hT && tile + 1 == tiles && at.run == 0) {
 #pragma unroll
@@ -336,7 +345,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
 // gradient.  MODE as above, tiles from the last to the first; part: A, H, G of a tile.  The state before a tile comes from p.states
 // (MODE 0) or from the tiles before it (MODE 2).
 // ---------------------------------------------------------------------------
-template <typename E, int VEC, int W, int MODE, bool KEEP>
+template <typename E, int VEC, int W, int MODE, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_kernel(const ScanParams p, int32_t slabs, int32_t tiles)
 {
     constexpr int ROWS = bwd_rows(MODE == 0, KEEP), AT_ONCE = MODE == 0 ? W : 4;
@@ -406,21 +415,24 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                         u = pad ? 0.0f : u;
                         if (KEEP && (fl.first >> i & 1u)) ph[j] = 0.0f;
                     }
-                    const bool behind = KEEP && (fl.behind >> i & 1u);
+                    const bool behind = KEEP && masked && (fl.behind >> i & 1u);
                     before[i][j] = ph[j];
-                    pa[j] = behind ? FIRST : pa[j] * af;
+                    pa[j] *= af;
                     ph[j] = __builtin_fmaf(af, ph[j], u);
-                    pg[j] = __builtin_fmaf(pa[j], behind ? 0.0f : dh, pg[j]);
+                    if (!behind) pg[j] = __builtin_fmaf(pa[j], dh, pg[j]);
                 }
                 kv[i] = rv[i]; kd[i] = rd[i];
                 if (MODE == 0 && tile > 0) request(off2, off1, i);
             }
         };
-        if (KEEP || !whole) {
-            fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
-            rows(std::true_type{});
-        } else {
-            rows(std::false_type{});
+        if (KEEP || !whole) fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
+        // a wave that walks its tiles mostly has tokens alone; tiles as workgroups are launches too short to read two loops' code
+        const bool masked = KEEP ? MODE != 0 || __any((fl.pad | fl.first) != 0) : !whole;
+        if (masked) rows(std::true_type{});
+        else rows(std::false_type{});
+        if (KEEP && fl.first != 0) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) pa[j] = FIRST;
         }
         float oa[VEC], oh[VEC], og[VEC];
 #pragma unroll
@@ -484,7 +496,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                     float run = h[j];                        // the start times the gates so far
 #pragma unroll
                     for (int i = 0; i < ROWS; ++i) {
-                        if (KEEP && (fl.first >> i & 1u)) run = 0.0f;
+                        if (KEEP && masked && (fl.first >> i & 1u)) run = 0.0f;
                         before[i][j] += run;
                         run *= masked && (fl.pad >> i & 1u) ? 1.0f : a[i][j];
                     }
@@ -509,11 +521,11 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                             G[j] = on;
                         }
                     }
-                    store(dz, off2 + 2 * i * line, pack<E, VEC>(df));
-                    store(dz, off2 + (2 * i + 1) * line, pack<E, VEC>(dv));
+                    store<STREAM>(dz, off2 + 2 * i * line, pack<E, VEC>(df));
+                    store<STREAM>(dz, off2 + (2 * i + 1) * line, pack<E, VEC>(dv));
                 }
             };
-            if (KEEP || !whole) replay(std::true_type{});
+            if (masked) replay(std::true_type{});
             else replay(std::false_type{});
             if (tile == 0 && at.run == 0) {
 #pragma unroll
@@ -549,17 +561,26 @@ Form form_of(const ScanParams &p, bool grad)
     return f;
 }
 
-template <typename E, int VEC, int W, int MODE>
+template <typename E, int VEC, int W, int MODE, bool STREAM>
 void go(bool grad, const ScanParams &p, const Form &f, hipStream_t s)
 {
     const dim3 grid((unsigned)(p.B * f.slabs * (MODE ? f.tiles : 1))), wg(64 * W);
     if (grad) {
-        if (p.keep) hipLaunchKernelGGL((linear_scan_grad_kernel<E, VEC, W, MODE, true>), grid, wg, 0, s, p, f.slabs, f.tiles);
-        else hipLaunchKernelGGL((linear_scan_grad_kernel<E, VEC, W, MODE, false>), grid, wg, 0, s, p, f.slabs, f.tiles);
+        if (p.keep) hipLaunchKernelGGL((linear_scan_grad_kernel<E, VEC, W, MODE, true, STREAM>), grid, wg, 0, s, p, f.slabs, f.tiles);
+        else hipLaunchKernelGGL((linear_scan_grad_kernel<E, VEC, W, MODE, false, STREAM>), grid, wg, 0, s, p, f.slabs, f.tiles);
     } else {
-        if (p.keep) hipLaunchKernelGGL((linear_scan_kernel<E, VEC, W, MODE, true>), grid, wg, 0, s, p, f.slabs, f.tiles);
-        else hipLaunchKernelGGL((linear_scan_kernel<E, VEC, W, MODE, false>), grid, wg, 0, s, p, f.slabs, f.tiles);
+        if (p.keep) hipLaunchKernelGGL((linear_scan_kernel<E, VEC, W, MODE, true, STREAM>), grid, wg, 0, s, p, f.slabs, f.tiles);
+        else hipLaunchKernelGGL((linear_scan_kernel<E, VEC, W, MODE, false, STREAM>), grid, wg, 0, s, p, f.slabs, f.tiles);
     }
+}
+
+template <typename E, int VEC, int W, int MODE>
+void go(bool grad, const ScanParams &p, const Form &f, hipStream_t s)
+{
+    if constexpr (MODE != 1 && VEC * sizeof(E) == 4) {             // the others store nothing, have no whole lines
+        if (p.D * sizeof(E) % 128 == 0) return go<E, VEC, W, MODE, true>(grad, p, f, s);
+    }
+    go<E, VEC, W, MODE, false>(grad, p, f, s);
 }
 
 template <typename E, int VEC>

@@ -27,6 +27,15 @@ constexpr float LOWEST = -3.40282347e38f;        // the lowest number, a lane's 
 struct Soft { float m, s, u; };
 
 __device__ __forceinline__ float e_to(float x) { return __expf(x); }
+// e y, zero where e is, also for an infinite y
+__device__ __forceinline__ float zero_times(float e, float y)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_fmul_legacy(e, y);
+#else
+    return e * y;
+#endif
+}
 
 __device__ __forceinline__ void rescale(Soft &a, float m)
 {
@@ -76,7 +85,7 @@ struct Part : RowVectors<E, T, NV> {
     const E *row;                               // its column 0
     u32x4 x[NV];
 
-    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t V, int32_t lo, int32_t hi) : Row(r, V, lo, hi), row((const E *)base + r * V) {}
+    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t M, int64_t V, int32_t lo, int32_t hi) : Row(r, M, V, lo, hi), row((const E *)base + r * V) {}
     __device__ __forceinline__ void load() { Row::load(row, sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u, x); }
     // the lane's own
     __device__ __forceinline__ Soft stats(float &most) const
@@ -126,7 +135,7 @@ struct Result {
     __device__ __forceinline__ explicit Result(const Soft &a)
     {
         dead = a.m == LOWEST && a.s == 0.0f;
-        m = a.m;
+        m = a.s == a.s ? a.m : a.s;                  // NaN: so is what is relative to it
         ls = logf(a.s);
         inv = dead ? 0.0f : 1.0f / a.s;
         ent = dead ? 0.0f : ls - a.u * inv;
@@ -244,25 +253,27 @@ __device__ __forceinline__ void gradient(const LogprobsParams &p, const Part<E, 
 {
     constexpr int N = Part<E, T, NV>::N;
     const int tok = p.tok[row];
-    const float dlp = tok >= 0 && tok < p.V && !r.dead ? p.dlp[row] : 0.0f, dent = r.dead ? 0.0f : p.dent[row];
-    const float c = r.dead ? 0.0f : dlp + dent * (r.ent - r.ls), scale = -r.inv;
+    const float dlp = tok >= 0 && tok < p.V && !r.dead ? p.dlp[row] : 0.0f;
+    const float dent = r.dead ? 0.0f : -r.inv * p.dent[row], c = r.dead ? 0.0f : __builtin_fmaf(dent, r.ent - r.ls, -r.inv * dlp);
+    // whose the token is
+    const int32_t tok_v = (tok - x.first) / N, tok_k = (tok - x.first) % N, tok_j = tok < x.lo || tok >= x.hi ? -1 : tok_v / T;
+    const uint32_t tok_t = (uint32_t)(tok_v % T);
     E *dx = (E *)p.dx + row * p.V;
     auto out = x.out(dx);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         if (j >= x.used) continue;
-        const int32_t col = anew(x.column(j));
         const u32x4 q = anew(x.x[j]);
         float v[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const float d = unpack<E>(q, k) - r.m;
-            v[k] = e_to(d) * scale * __builtin_fmaf(dent, fmaxf(d, -1e4f), c);
+            v[k] = zero_times(e_to(d), __builtin_fmaf(dent, d, c));
         }
-        if (tok >= col && tok < col + N) {
+        if (j == tok_j && threadIdx.x == tok_t) {
 #pragma unroll
             for (int k = 0; k < N; ++k)
-                if (tok == col + k) v[k] += dlp;
+                if (k == tok_k) v[k] += dlp;
         }
         x.put(out, j, pack<E>(v));
     }
@@ -291,7 +302,7 @@ __global__ __launch_bounds__(T, NV == 16 ? 4 : 8) void token_logprobs_kernel(con
     __shared__ uint64_t keys[LOGPROBS_MAX_TOP];
     const int64_t row = blockIdx.x / (uint32_t)segs;
     const int32_t seg = (int32_t)(blockIdx.x - (uint32_t)row * segs), lo = seg * seg_len;
-    Part<E, T, NV> x(p.x, row, p.V, lo, (int32_t)min((int64_t)lo + seg_len, p.V));
+    Part<E, T, NV> x(p.x, row, p.M, p.V, lo, (int32_t)min((int64_t)lo + seg_len, p.V));
     x.load();
     const Target target(p, row);
     float most = 0.0f;
