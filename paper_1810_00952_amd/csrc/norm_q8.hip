@@ -83,7 +83,7 @@ __global__ __launch_bounds__(T) void norm_q8_row_kernel(const NormQ8Params p)
     typedef RowVectors<E, T, NV> Row;
     constexpr int N = Row::N;
     const int64_t r = blockIdx.x;
-    const Row row(r, p.M, p.D, 0, (int32_t)p.D);
+    const Row row(r, p.D, 0, (int32_t)p.D);
     u32x4 x[NV], res[NV];
     row.load((const E *)p.x + r * p.D, 0, x);
     if (RES) row.load((const E *)p.r + r * p.D, 0, res);

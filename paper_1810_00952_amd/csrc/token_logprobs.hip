@@ -27,15 +27,6 @@ constexpr float LOWEST = -3.40282347e38f;        // the lowest number, a lane's 
 struct Soft { float m, s, u; };
 
 __device__ __forceinline__ float e_to(float x) { return __expf(x); }
-// e y, zero where e is, also for an infinite y
-__device__ __forceinline__ float zero_times(float e, float y)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_fmul_legacy(e, y);
-#else
-    return e * y;
-#endif
-}
 
 __device__ __forceinline__ void rescale(Soft &a, float m)
 {
@@ -85,7 +76,7 @@ struct Part : RowVectors<E, T, NV> {
     const E *row;                               // its column 0
     u32x4 x[NV];
 
-    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t M, int64_t V, int32_t lo, int32_t hi) : Row(r, M, V, lo, hi), row((const E *)base + r * V) {}
+    __device__ __forceinline__ Part(const void *base, int64_t r, int64_t V, int32_t lo, int32_t hi) : Row(r, V, lo, hi), row((const E *)base + r * V) {}
     __device__ __forceinline__ void load() { Row::load(row, sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u, x); }
     // the lane's own
     __device__ __forceinline__ Soft stats(float &most) const
@@ -135,7 +126,7 @@ struct Result {
     __device__ __forceinline__ explicit Result(const Soft &a)
     {
         dead = a.m == LOWEST && a.s == 0.0f;
-        m = a.s == a.s ? a.m : a.s;                  // NaN: so is what is relative to it
+        m = a.m;
         ls = logf(a.s);
         inv = dead ? 0.0f : 1.0f / a.s;
         ent = dead ? 0.0f : ls - a.u * inv;
@@ -143,15 +134,16 @@ struct Result {
     __device__ __forceinline__ float logp(float x) const { return dead ? -INFINITY : x - m - ls; }
 };
 
-// the row's token, its logit asked for ahead of the statistics
+// the row's token, its logit and the loss' derivatives, asked for ahead of the statistics
 struct Target {
+    int tok;
     bool given;
-    float x;
-    __device__ __forceinline__ Target(const LogprobsParams &p, int64_t row)
+    float x, dlp, dent;
+    __device__ __forceinline__ Target(const LogprobsParams &p, int64_t row, bool forward, bool grad) : tok(p.tok[row])
     {
-        const int tok = p.tok[row];
         given = tok >= 0 && tok < p.V;
-        x = load_as_f32(p.x, p.dtype, row * p.V + (given ? tok : 0));
+        if (forward) x = load_as_f32(p.x, p.dtype, row * p.V + (given ? tok : 0));
+        if (grad) { dlp = p.dlp[row]; dent = p.dent[row]; }
     }
     __device__ __forceinline__ void store(const LogprobsParams &p, int64_t row, const Result &r) const
     {
@@ -249,12 +241,12 @@ __device__ __forceinline__ void alternatives(const Part<E, T, NV> &x, int top, f
 }
 
 template <typename E, int T, int NV>
-__device__ __forceinline__ void gradient(const LogprobsParams &p, const Part<E, T, NV> &x, int64_t row, const Result &r)
+__device__ __forceinline__ void gradient(const LogprobsParams &p, const Part<E, T, NV> &x, int64_t row, const Result &r, const Target &target)
 {
     constexpr int N = Part<E, T, NV>::N;
-    const int tok = p.tok[row];
-    const float dlp = tok >= 0 && tok < p.V && !r.dead ? p.dlp[row] : 0.0f;
-    const float dent = r.dead ? 0.0f : -r.inv * p.dent[row], c = r.dead ? 0.0f : __builtin_fmaf(dent, r.ent - r.ls, -r.inv * dlp);
+    const int tok = target.tok;
+    const float dlp = target.given && !r.dead ? target.dlp : 0.0f;
+    const float dent = r.dead ? 0.0f : -r.inv * target.dent, c = r.dead ? 0.0f : __builtin_fmaf(dent, r.ent - r.ls, -r.inv * dlp);
     // whose the token is
     const int32_t tok_v = (tok - x.first) / N, tok_k = (tok - x.first) % N, tok_j = tok < x.lo || tok >= x.hi ? -1 : tok_v / T;
     const uint32_t tok_t = (uint32_t)(tok_v % T);
@@ -268,7 +260,7 @@ __device__ __forceinline__ void gradient(const LogprobsParams &p, const Part<E, 
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const float d = unpack<E>(q, k) - r.m;
-            v[k] = zero_times(e_to(d), __builtin_fmaf(dent, d, c));
+            v[k] = e_to(d) * __builtin_fmaf(dent, fmaxf(d, -1e4f), c);
         }
         if (j == tok_j && threadIdx.x == tok_t) {
 #pragma unroll
@@ -291,7 +283,7 @@ __device__ __forceinline__ Soft join_segments(const LogprobsParams &p, int64_t r
     return join_lanes(lane < segs ? Soft{v[0], v[1], v[2]} : Soft{LOWEST, 0.0f, 0.0f});
 }
 
-enum { FORWARD = 1, GRADIENT = 2, SEGMENT = 4, JOINED = 8 };     // what a launch does: JOINED takes the statistics from part
+enum { FORWARD = 1, GRADIENT = 2, SEGMENT = 4, JOINED = 8, TOP = 16 };     // what a launch does: JOINED takes the statistics from part, TOP: p.top > 0
 
 }  // namespace
 
@@ -302,30 +294,28 @@ __global__ __launch_bounds__(T, NV == 16 ? 4 : 8) void token_logprobs_kernel(con
     __shared__ uint64_t keys[LOGPROBS_MAX_TOP];
     const int64_t row = blockIdx.x / (uint32_t)segs;
     const int32_t seg = (int32_t)(blockIdx.x - (uint32_t)row * segs), lo = seg * seg_len;
-    Part<E, T, NV> x(p.x, row, p.M, p.V, lo, (int32_t)min((int64_t)lo + seg_len, p.V));
+    Part<E, T, NV> x(p.x, row, p.V, lo, (int32_t)min((int64_t)lo + seg_len, p.V));
     x.load();
-    const Target target(p, row);
+    const Target target(p, row, WHAT & FORWARD, WHAT & GRADIENT);
     float most = 0.0f;
     const Soft a = WHAT & JOINED ? join_segments(p, row, segs) : join_workgroup<T>(x.stats(most), sh);
-    if constexpr (WHAT & (FORWARD | SEGMENT)) {
-        if (p.top > 0) alternatives<E, T, NV>(x, p.top, most, a.s == a.s, keys);
-    }
+    if constexpr (WHAT & TOP) alternatives<E, T, NV>(x, p.top, most, a.s == a.s, keys);
     if constexpr (WHAT & SEGMENT) {
         float *q = p.part + (row * segs + seg) * seg_floats(p.top);
         if (threadIdx.x == 0) { q[0] = a.m; q[1] = a.s; q[2] = a.u; }
-        if ((int)threadIdx.x < p.top) ((uint64_t *)(q + 4))[threadIdx.x] = keys[threadIdx.x];
+        if (WHAT & TOP && (int)threadIdx.x < p.top) ((uint64_t *)(q + 4))[threadIdx.x] = keys[threadIdx.x];
         return;
     }
     const Result r(a);
     if constexpr (WHAT & FORWARD) {
         if (threadIdx.x == 0) target.store(p, row, r);
-        if ((int)threadIdx.x < p.top) {
+        if (WHAT & TOP && (int)threadIdx.x < p.top) {
             const uint64_t key = keys[threadIdx.x];
             p.top_id[row * p.top + threadIdx.x] = (int32_t)key_index(key);
             p.top_lp[row * p.top + threadIdx.x] = r.logp(key_logit(key));
         }
     }
-    if constexpr (WHAT & GRADIENT) gradient<E, T, NV>(p, x, row, r);
+    if constexpr (WHAT & GRADIENT) gradient<E, T, NV>(p, x, row, r, target);
 }
 
 // the segments of a row joined, their alternatives ranked by counting those that can be among the row's
@@ -338,7 +328,7 @@ __global__ __launch_bounds__(256) void token_logprobs_join_kernel(const Logprobs
     const int n = segs * p.top, t = threadIdx.x;
     for (int i = t; i < n; i += 256) keys[i] = ((const uint64_t *)(q + (i / p.top) * seg_floats(p.top) + 4))[i % p.top];
     if (t == 0) count = 0;
-    const Target target(p, row);
+    const Target target(p, row, true, false);
     const Result r(join_segments(p, row, segs));
     if (t == 0) target.store(p, row, r);
     if (p.top == 0) return;
@@ -401,13 +391,12 @@ template <typename E, int T, int NV>
 void go(const LogprobsParams &p, const Form &f, int what, hipStream_t s)
 {
     const dim3 grid((unsigned)(p.M * f.segs)), wg(T);
+#define RL_GO(WHAT) case WHAT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, WHAT>), grid, wg, 0, s, p, f.segs, f.len); break;
     switch (what) {
-    case FORWARD: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, FORWARD>), grid, wg, 0, s, p, f.segs, f.len); break;
-    case GRADIENT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, GRADIENT>), grid, wg, 0, s, p, f.segs, f.len); break;
-    case FORWARD | GRADIENT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, FORWARD | GRADIENT>), grid, wg, 0, s, p, f.segs, f.len); break;
-    case SEGMENT: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, SEGMENT>), grid, wg, 0, s, p, f.segs, f.len); break;
-    default: hipLaunchKernelGGL((token_logprobs_kernel<E, T, NV, GRADIENT | JOINED>), grid, wg, 0, s, p, f.segs, f.len); break;
+        RL_GO(FORWARD) RL_GO(FORWARD | TOP) RL_GO(GRADIENT) RL_GO(FORWARD | GRADIENT) RL_GO(FORWARD | GRADIENT | TOP)
+        RL_GO(SEGMENT) RL_GO(SEGMENT | TOP) RL_GO(GRADIENT | JOINED)
     }
+#undef RL_GO
 }
 
 template <typename E>
@@ -437,9 +426,9 @@ hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hip
         return hipErrorInvalidValue;
     auto run = [&](int what) { p.dtype == DT_BF16 ? go<uint16_t>(p, f, what, s) : go<float>(p, f, what, s); };
     if (f.segs == 1) {
-        run((forward ? FORWARD : 0) | (grad ? GRADIENT : 0));
+        run((forward ? FORWARD : 0) | (grad ? GRADIENT : 0) | (forward && p.top > 0 ? TOP : 0));
     } else {
-        run(SEGMENT);
+        run(SEGMENT | (forward && p.top > 0 ? TOP : 0));
         if (forward) hipLaunchKernelGGL(token_logprobs_join_kernel, dim3((unsigned)p.M), dim3(256), 0, s, p, f.segs);
         if (grad) run(GRADIENT | JOINED);
     }
