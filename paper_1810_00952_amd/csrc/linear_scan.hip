@@ -111,7 +111,9 @@ struct Place {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         half = lane >> 5;
         run = 2 * wave + half;
-        const uint32_t bid = blockIdx.x, rest = bid / (uint32_t)slabs, B = (uint32_t)p.B;
+        // where neighbours share lines they go to one XCD, whose L2 reads those once and writes them whole (both passes, 5 x 777 x 515 f32 packed 38.5 ->
+        // 27.2 us, 8 x 1500 x 1000 f32 109 -> 84); with lines of their own one sequence of 16384 x 1024 bf16 is faster over all of them, 37.9 us not 40.5
+        const uint32_t bid = p.D * sizeof(E) % 128 ? (uint32_t)xcd_run(blockIdx.x, gridDim.x) : blockIdx.x, rest = bid / (uint32_t)slabs, B = (uint32_t)p.B;
         seg = (int32_t)(rest / B);
         b = (int32_t)(rest - seg * B);
         d = (int32_t)((bid - rest * slabs) * 32 + (lane & 31)) * VEC;
