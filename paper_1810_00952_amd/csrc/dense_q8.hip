@@ -26,6 +26,12 @@ struct Epi4 {
     f32x4 sw, b;
     __device__ __forceinline__ Epi4(const DenseQ8Params &p, int64_t n)
     {
+        if (p.N % 4 == 0) {                               // n is a multiple of 4
+            const int64_t c = n < p.N ? n : p.N - 4;
+            sw = *(const f32x4 *)(p.sw + c);
+            b = p.b ? *(const f32x4 *)(p.b + c) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int64_t c = n + k < p.N ? n + k : p.N - 1;
@@ -260,6 +266,29 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q8_tile_kernel(const Dense
         for (int i = 0; i < TM; ++i) {
             const int64_t mi = m0 + (wm * TM + i) * 32, m = mi + frow;
             const float sx = p.sx[m < p.M ? m : p.M - 1];
+            if (p.y_dtype == DT_BF16 && whole) {
+                // the halves of the wave swap what they hold of eight columns: a lane has sixteen, in two groups of 16 bytes
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x2 c[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int k = 2 * h + q;
+                        const i32x4 sum = {acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
+                        const f32x4 v = e[k](sum, sx);
+                        c[q] = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                    }
+                    u32x4 out;
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) {
+                        const auto got = __builtin_amdgcn_permlane32_swap(c[0][d], c[1][d], false, false);
+                        out[d] = got[0]; out[2 + d] = got[1];
+                    }
+                    const int64_t n = nj + 16 * h + 8 * fhalf;
+                    if (m < p.M && n < p.N) *(u32x4 *)((uint16_t *)p.y + m * p.N + n) = out;
+                }
+                continue;
+            }
             float *park = (float *)(W * 4096 <= STAGE ? st0 : wave < W / 2 ? st0 : st1) + (W * 4096 <= STAGE ? wave : wave % (W / 2)) * 1024;
             wave_lds_exchange();
 #pragma unroll
@@ -268,15 +297,7 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q8_tile_kernel(const Dense
                 *(f32x4 *)(park + frow * 32 + (((2 * q + fhalf) ^ (frow & 7)) << 2)) = e[q](sum, sx);
             }
             wave_lds_exchange();
-            if (p.y_dtype == DT_BF16 && whole) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {                       // 16 rows of 64 bytes
-                    const int row = h * 16 + (lane >> 2), c = 2 * (lane & 3);
-                    const f32x4 a = *(const f32x4 *)(park + row * 32 + ((c ^ (row & 7)) << 2)), b = *(const f32x4 *)(park + row * 32 + (((c + 1) ^ (row & 7)) << 2));
-                    if (mi + row < p.M && nj + 4 * c < p.N)
-                        *(u32x4 *)((uint16_t *)p.y + (mi + row) * p.N + nj + 4 * c) = u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
-                }
-            } else if (whole) {
+            if (whole) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {                       // 8 rows of 128 bytes
                     const int row = h * 8 + (lane >> 3), c = lane & 7;
