@@ -10,6 +10,9 @@
 // requested into the stage being left and the next tile's first fragments are read under that step's MFMAs.
 // dense_q8_direct: for few rows of x, where the time is w's way from memory: fragments straight into registers, K over the
 // eight waves of a workgroup (whole lines in turn), whose sums meet in LDS: every wave's loads are under way at once.
+//
+// 8192 x 8192 x 4096 270 us (2.03 Pop/s), 4096 x 4096 x 16384 240 us (2.29): power, the MFMAs busy 52 % of the cycles at some 1.9 GHz; all of a tile's
+// requests in one k-step 281 us.  8 x 4096 x 4096 6.4 us: a launch and a chain of latencies.
 #include "igemm_lds.h"
 
 namespace rl {

@@ -12,10 +12,11 @@
 // prefix products and results of its rows from zero.  A run with a document's first row has -0 for A, which no product of gates
 // is: nothing of what comes before goes into what follows, neither an infinity nor NaN.  The runs' (A, H) meet in LDS, every run adds up those before it, and one fma a
 // row then gives the states.  The workgroup carries the tile's last state on to its next tile, whose rows are requested as
-// the registers of this one's become free.  Nothing is read twice.  What bounds it is HBM.
+// the registers of this one's become free.  Nothing is read twice.  What bounds it is HBM, in columns of 128 bytes: 8 x 4096 x 2048 bf16 96 us
+// (4.2 TB/s), its gradient 152 us (4.4 TB/s); two tiles under way are no faster.
 //
 // Few channels and many rows: each tile is a workgroup of its own.  A launch ahead finds the tiles' (A, H) (and, of the gradient, G),
-// and every workgroup adds up those before (behind) its tile, at the cost of a second read.
+// and every workgroup adds up those before (behind) its tile, at the cost of a second read: one sequence of 16384 x 1024 bf16 15 and 25 us.
 #include <type_traits>
 
 #include "igemm_lds.h"
@@ -25,7 +26,8 @@ namespace rl {
 namespace {
 
 // Rows of a run: as many as fit the registers with what they become, of two waves a SIMD where a workgroup walks its tiles, of four where
-// tiles are workgroups (of the gradient, 32 x 1024 x 2048 bf16, forward and backward pass: 250 us with sixteen, 273 with eight)
+// tiles are workgroups (of the gradient, 8 x 4096 x 2048 bf16, forward and backward pass: 238 us with sixteen; 257 with eight and the rows of
+// two tiles under way)
 constexpr int FWD_ROWS = 16;
 constexpr int bwd_rows(bool walks, bool keep) { return walks && !keep ? 16 : 8; }
 
