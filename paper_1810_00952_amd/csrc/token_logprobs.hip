@@ -162,26 +162,27 @@ __device__ __forceinline__ void alternatives(const Part<E, T, NV> &x, int top, f
     __shared__ float group[W][64];
     __shared__ uint64_t cand[CAND], best[W];
     __shared__ int count;
+    __shared__ float border;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     group[wave][lane] = most;
     if (t == 0) count = 0;
     if (t < top) out[t] = 0;
     __syncthreads();
-    float mine = group[0][lane];
+    // the top-th largest of 64: the least of those with fewer than `top` above them
+    if (wave == 0) {
+        float mine = group[0][lane];
 #pragma unroll
-    for (int w = 1; w < W; ++w) mine = fmaxf(mine, group[w][lane]);
-    // the top-th largest of 64
-    int above = 0, equal = 0;
+        for (int w = 1; w < W; ++w) mine = fmaxf(mine, group[w][lane]);
+        int above = 0;
 #pragma unroll
-    for (int l = 0; l < 64; ++l) {
-        const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), l));
-        above += other > mine;
-        equal += other == mine;
+        for (int l = 0; l < 64; ++l) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), l)) > mine;
+        mine = -wave_max(above < top ? -mine : -INFINITY);
+        if (lane == 0) border = mine;
     }
-    const uint64_t is = __ballot(above < top && above + equal >= top);
-    bool one_by_one = !plain || is == 0;
+    __syncthreads();
+    bool one_by_one = !plain;
     if (!one_by_one) {
-        const float least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __builtin_ctzll(is)));
+        const float least = border;
         // fewer than `top` groups above -inf: what is above it, and for the rest the first columns, of which that many at least are -inf
         // unless what is above it is enough
         const bool some = least > -INFINITY;
