@@ -305,7 +305,18 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q8_tile_kernel(const Dense
                 for (int h = 0; h < 4; ++h) {                       // 8 rows of 128 bytes
                     const int row = h * 8 + (lane >> 3), c = lane & 7;
                     const f32x4 a = *(const f32x4 *)(park + row * 32 + ((c ^ (row & 7)) << 2));
-                    if (mi + row < p.M && nj + 4 * c < p.N) *(f32x4 *)((float *)p.y + (mi + row) * p.N + nj + 4 * c) = a;
+                    f32x4 *to = (f32x4 *)((float *)p.y + (mi + row) * p.N + nj + 4 * c);
+                    if (mi + row < p.M && nj + 4 * c < p.N) {
+                        // whole lines go past the L2, whose writing back the next operator would wait for: 4096 x 32000 x 1024 and the log probabilities
+                        // behind it 134 -> 89 us for those, the product the same; lines in parts (of bf16, 8192 x 8192 x 4096) 270 -> 277
+                        if (p.N % 32 == 0) {
+                            asm volatile("");           // on both sides: else the two stores become one, an ordinary one
+                            __builtin_nontemporal_store(a, to);
+                            asm volatile("");
+                        } else {
+                            *to = a;
+                        }
+                    }
                 }
             } else {
 #pragma unroll 4
