@@ -65,6 +65,10 @@ template <bool KEEP> __device__ __forceinline__ float through(float A, float x, 
     return KEEP && is_first(A) ? H : y;
 }
 template <bool KEEP> __device__ __forceinline__ float both(float A, float b) { return KEEP && (is_first(A) || is_first(b)) ? FIRST : A * b; }
+// A product of gates as it is used: at least the least number of f32, not 0, which no product of gates is.  An infinite state outlasts it and
+// does not become NaN; a finite one is off by that number's share of it, a step of the last number there is.  As whole numbers, so that
+// NaN stays and FIRST too.  The products themselves go on without it: it would be one more instruction a row that the next row waits for.
+__device__ __forceinline__ float above_zero(float A) { return __uint_as_float(max(__float_as_uint(A), 1u)); }
 
 // Rows of a tile in memory: `room` bytes from the tile's first row to the sequence's last.  What lies behind them reads as zero and is
 // not written; so does what a lane without channels (offset OOB) asks for.
@@ -149,7 +153,7 @@ __device__ __forceinline__ void through_tiles(const float *part, int64_t stride,
         }
     }
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) { sa[run][l32][j] = a[j]; sx[run][l32][j] = x[j]; }
+    for (int j = 0; j < VEC; ++j) { sa[run][l32][j] = above_zero(a[j]); sx[run][l32][j] = x[j]; }
     __syncthreads();
 #pragma unroll 4
     for (int r = 0; r < 2 * W; ++r)
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
                     }
                     pa[j] *= a;
                     ph[j] = __builtin_fmaf(a, ph[j], u);
-                    A[i][j] = pa[j]; H[i][j] = ph[j];
+                    A[i][j] = above_zero(pa[j]); H[i][j] = ph[j];
                 }
                 if (MODE == 0 && tile + 1 < last_tile) request(off2, i);
             }
@@ -272,10 +276,8 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
         const bool masked = KEEP ? MODE != 0 || __any((fl.pad | fl.first) != 0) : !whole;
         if (masked) rows(std::true_type{});
         else rows(std::false_type{});
-        if (KEEP && fl.first != 0) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) pa[j] = FIRST;
-        }
+        for (int j = 0; j < VEC; ++j) pa[j] = KEEP && fl.first != 0 ? FIRST : above_zero(pa[j]);
         // the wave's two runs as one, the waves' in LDS
         float oa[VEC], oh[VEC];
 #pragma unroll
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
         if (at.half) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                sa[buf][at.wave][l32][j] = both<KEEP>(pa[j], oa[j]);
+                sa[buf][at.wave][l32][j] = above_zero(both<KEEP>(pa[j], oa[j]));
                 sh[buf][at.wave][l32][j] = through<KEEP>(pa[j], oh[j], ph[j]);
             }
         }
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
                     float ta = 1.0f, th = 0.0f;
 #pragma unroll
                     for (int w = 0; w < W; ++w) { th = through<KEEP>(sa[0][w][l32][j], th, sh[0][w][l32][j]); ta = both<KEEP>(ta, sa[0][w][l32][j]); }
-                    p.part[2 * at.seg * BD + chan + j] = ta;
+                    p.part[2 * at.seg * BD + chan + j] = above_zero(ta);
                     p.part[(2 * at.seg + 1) * BD + chan + j] = th;
                 }
             }
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                     before[i][j] = ph[j];
                     pa[j] *= af;
                     ph[j] = __builtin_fmaf(af, ph[j], u);
-                    if (!behind) pg[j] = __builtin_fmaf(pa[j], dh, pg[j]);
+                    if (!behind) pg[j] = __builtin_fmaf(above_zero(pa[j]), dh, pg[j]);
                 }
                 kv[i] = rv[i]; kd[i] = rd[i];
                 if (MODE == 0 && tile > 0) request(off2, off1, i);
@@ -434,10 +436,8 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
         const bool masked = KEEP ? MODE != 0 || __any((fl.pad | fl.first) != 0) : !whole;
         if (masked) rows(std::true_type{});
         else rows(std::false_type{});
-        if (KEEP && fl.first != 0) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) pa[j] = FIRST;
-        }
+        for (int j = 0; j < VEC; ++j) pa[j] = KEEP && fl.first != 0 ? FIRST : above_zero(pa[j]);
         float oa[VEC], oh[VEC], og[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) { oa[j] = __shfl_xor(pa[j], 32); oh[j] = __shfl_xor(ph[j], 32); og[j] = __shfl_xor(pg[j], 32); }
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
         if (at.half) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                sa[buf][at.wave][l32][j] = both<KEEP>(pa[j], oa[j]);
+                sa[buf][at.wave][l32][j] = above_zero(both<KEEP>(pa[j], oa[j]));
                 sh[buf][at.wave][l32][j] = through<KEEP>(pa[j], oh[j], ph[j]);
                 sg[buf][at.wave][l32][j] = through<KEEP>(oa[j], pg[j], og[j]);
             }
@@ -458,11 +458,11 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
                     float ta = 1.0f, th = 0.0f, tg = 0.0f;
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
-                        tg = through<KEEP>(ta, sg[0][w][l32][j], tg);
+                        tg = through<KEEP>(above_zero(ta), sg[0][w][l32][j], tg);
                         th = through<KEEP>(sa[0][w][l32][j], th, sh[0][w][l32][j]);
                         ta = both<KEEP>(ta, sa[0][w][l32][j]);
                     }
-                    p.part[3 * at.seg * BD + chan + j] = ta;
+                    p.part[3 * at.seg * BD + chan + j] = above_zero(ta);
                     p.part[(3 * at.seg + 1) * BD + chan + j] = th;
                     p.part[(3 * at.seg + 2) * BD + chan + j] = tg;
                 }

@@ -301,6 +301,45 @@ def test_scan_steps_continue_a_sequence():
         within(h, ref[0].reshape(b, t, d)[:, i], after[:, i], f"step {i}")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,t,d", [(3, 1, 66), (2, 20, 66), (3, 90, 515), (1, 3001, 40), (1, 6000, 130), (8, 300, 1024), (130, 260, 64)])
+def test_infinite_states_and_derivatives_stay_infinite(b, t, d, dtype):
+    """Gates are above zero, so that an infinite state, and an infinite derivative on its way back, outlasts any number of them; the product of
+    the gates of a run, of a tile, of many tiles, is far below f32."""
+    for packed in (False, True):
+        print(f"{b}x{t}x{d} {dtype} packed={packed}", flush=True)
+        rng = np.random.default_rng(t + d)
+        z = np.clip(rng.normal(size=(b, t, 2 * d)), -5, 5)
+        z[:, :, :d:3] = -60.0                          # a third of the channels: two gates of e^-60 are below f32
+        h0, dh, dhT = rng.normal(size=(b, d)), rng.normal(size=(b, t, d)), rng.normal(size=(b, d))
+        h0[:, 0], h0[:, d // 2] = np.inf, -np.inf
+        dhT[:, 1], dhT[:, d - 1] = np.inf, -np.inf
+        keep = np.ones((b, t))
+        for i in range(b):                             # and of a token's own candidate or derivative
+            z[i, rng.integers(0, t), d + 2] = np.inf
+            z[i, rng.integers(0, t), d + 3] = -np.inf
+            dh[i, rng.integers(0, t), 4], dh[i, rng.integers(0, t), 6] = np.inf, -np.inf
+        if packed:
+            keep[:, 40::200] = 2
+            keep[:, 7::50] = 0
+            z[:, 7::50], dh[:, 7::50] = 0.0, 0.0
+        tz, z = tensor(z.reshape(b * t, 2 * d), dtype)
+        th, h0 = tensor(h0, "f32")
+        tdh, dh = tensor(dh.reshape(b * t, d), dtype)
+        tdT, dhT = tensor(dhT, "f32")
+        tk, keep = tensor(keep.reshape(-1), "i8")
+        last = [(tk, "i8")] if packed else []
+        k = keep if packed else None
+        got = Call("linear_scan", [(tz, dtype), (th, "f32")] + last, [(dtype, (b * t, d)), ("f32", (b, d))]).run().numbers()
+        grad = Call("linear_scan_grad", [(tz, dtype), (th, "f32"), (tdh, dtype), (tdT, "f32")] + last, [(dtype, (b * t, 2 * d)), ("f32", (b, d))]).run().numbers()
+        with np.errstate(invalid="ignore"):
+            want = L.linear_scan(z, h0, k)
+            wgrad = L.linear_scan_grad(z, h0, dh, dhT, k)
+        for a, w, name in zip(got + grad, list(want) + list(wgrad), ("h", "hT", "dz", "dh0")):
+            assert packed or np.isinf(w).any(), name
+            np.testing.assert_array_equal(np.where(np.isfinite(w), 0.0, w), np.where(np.isfinite(a), 0.0, a), err_msg=name)
+
+
 def test_scan_gates_at_their_ends():
     """Gates of +-infinity and far out: the state is kept or replaced, and nothing is NaN."""
     f = np.array([np.inf, -np.inf, 100.0, -100.0, 88.0, -88.0])
