@@ -127,7 +127,8 @@ enum {
                                  sequences of T tokens one behind the other (B from h0; T = 1 is a decoding step, hT the next call's h0).
                                  h_t = a h_(t-1) + (1 - a) v with a = sigmoid(f), the state in f32.  keep: 0: padding, whose z and row of
                                  dh are not looked at: the state stays as it is and the row of h is zero; 2: the first token of a
-                                 document: the state before it is zero; any other value: a token.  hT may lie over h0 where T = 1 */
+                                 document: the state before it is zero; any other value: a token.  hT may lie over h0 where T = 1, h0 is an
+                                 input and no call behind this one reads it; else such bindings are refused (RL_ERR_BINDING) */
     RL_OP_LINEAR_SCAN_GRAD = 26, /* (z, h0, dh e[B*T,D], dhT f32[B,D][, keep]) -> (dz e[B*T,2D], dh0 f32[B,D]): the derivatives of a loss whose
                                  derivatives by linear_scan's two results are dh and dhT; the states between are computed anew, in f32 */
     RL_OP_TOKEN_LOGPROBS = 27,/* (x e[M,V], tok i32[M]) -> (lp f32[M], ent f32[M][, top_lp f32[M,top], top_id i32[M,top]]); attrs
@@ -288,7 +289,7 @@ rl_status rl_plan_prepack(const rl_plan *plan, int32_t param_value_id, const voi
  * once; intermediates live in workspace_dev (>= rl_plan_workspace_bytes).
  * Inputs and params are read only; outputs and workspace are overwritten.
  * An output may alias an input only for lstm_gates' cell state (c' over c) and the state of a linear_scan of one token
- * (hT over h0).
+ * whose h0 nothing behind it reads (hT over h0).
  * The call only launches kernels on hip_stream (no allocation, no memset, no
  * synchronisation), so it may be made while that stream is being captured into
  * a HIP graph; replays then need the same device pointers to stay valid. */

@@ -113,6 +113,12 @@ rl_status resolve(const Plan &p, const rl_binding *b, int32_t nb, void *ws, size
             ptrs[i] = (char *)ws + d.offset;
         }
     }
+    for (const auto &a : p.apart)
+        if (ptrs[a.first] == ptrs[a.second]) {
+            msg = "value id " + std::to_string(p.bufs[a.second].bound_value) + ", a scan's last state, may not lie over its first one, value id " +
+                  std::to_string(p.bufs[a.first].bound_value) + ", here";
+            return RL_ERR_BINDING;
+        }
     return RL_OK;
 }
 

@@ -2128,6 +2128,15 @@ struct Planner {
             placed.push_back(b);
         }
         plan.workspace_bytes = total;
+        // a scan's new state may lie over its old one only if it has one token a sequence (else workgroups read h0 beside the one that writes hT)
+        // and nothing behind it reads the old one
+        for (size_t si = 0; si < plan.steps.size(); ++si) {
+            const Step &s = plan.steps[si];
+            if (s.kind != S_SCAN || s.slot[SL_COUT] < 0) continue;
+            const BufDesc &h0 = plan.bufs[s.slot[SL_CIN]], &hT = plan.bufs[s.slot[SL_COUT]];
+            if (h0.bound_value < 0 || hT.bound_value < 0) continue;
+            if (s.sc.T > 1 || h0.last > (int)si || g.values[h0.bound_value].role != ROLE_INPUT) plan.apart.push_back({s.slot[SL_CIN], s.slot[SL_COUT]});
+        }
     }
 };
 

@@ -78,6 +78,7 @@ struct Plan {
     std::vector<int> outputs;
     std::vector<BufDesc> bufs;
     std::vector<Step> steps;
+    std::vector<std::pair<int, int>> apart;   // a scan's h0 and hT, bound both, that may not be one memory: buffer indices
     std::vector<int> bound_buf;          // value id -> buffer index of its bound pointer, or -1
     std::map<int, PackSpec> packs;       // param value id -> packing
     size_t workspace_bytes = 0;

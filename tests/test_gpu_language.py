@@ -287,6 +287,29 @@ def test_scan_step_in_place():
         check_scan(call.run().numbers(), z, h0, keep, dtype, "step in place")
 
 
+def test_the_last_reader_of_a_state_may_write_over_it():
+    """Two scans of one token from the same state: the second one's new state over it, the first one's beside it."""
+    import torch
+    from paper_1810_00952_amd import binding as B
+    b, d = 5, 70
+    rng = np.random.default_rng(1)
+    z = [tensor(rng.normal(size=(b, 2 * d)), "f32") for _ in range(2)]
+    th, h0 = tensor(rng.normal(size=(b, d)), "f32")
+    g = B.Graph(B.Context())
+    zi, hi = [g.input("f32", (b, 2 * d)) for _ in z], g.input("f32", (b, d))
+    outs = [g.op("linear_scan", [v, hi], [("f32", (b, d)), ("f32", (b, d))])[1] for v in zi]
+    for v in (*outs[0], *outs[1]):
+        g.output(v)
+    plan = g.plan()
+    got = {v: torch.empty((b, d), device="cuda:0") for v in (*outs[0], outs[1][0])}
+    bound = {**{v: t.data_ptr() for v, (t, _) in zip(zi, z)}, hi: th.data_ptr(), **{v: t.data_ptr() for v, t in got.items()}, outs[1][1]: th.data_ptr()}
+    plan.run(bound, 0, 0, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    results = [[got[outs[0][0]], got[outs[0][1]]], [got[outs[1][0]], th]]
+    for (_, zn), res in zip(z, results):
+        check_scan([t.double().cpu().numpy() for t in res], zn, h0, None, "f32", "shared state")
+
+
 def test_scan_steps_continue_a_sequence():
     """T single steps, each on the state of the one before, are the sequence: within the bound of either."""
     b, t, d = 2, 9, 70

@@ -129,6 +129,28 @@ def test_run_refuses_bad_bindings():
         assert e.value.category == category
 
 
+@pytest.mark.parametrize("steps,others", [(1, ["linear_scan_grad"]), (1, ["linear_scan"]), (2, []), (40, [])])
+def test_a_state_in_place_has_no_other_reader(steps, others):
+    """hT may lie over h0 where a sequence has one token and nothing behind the scan reads h0; elsewhere the bindings are refused."""
+    b, d = 3, 8
+    z_t, s_t, h_t = ("f32", (b * steps, 2 * d)), ("f32", (b, d)), ("f32", (b * steps, d))
+    g = B.Graph(B.Context())
+    z, h0, dh, dT = g.input(*z_t), g.input(*s_t), g.input(*h_t), g.input(*s_t)
+    outs = list(g.op("linear_scan", [z, h0], [h_t, s_t])[1])
+    for kind in others:
+        outs += g.op(kind, [z, h0, dh, dT] if kind.endswith("grad") else [z, h0], [z_t, s_t] if kind.endswith("grad") else [h_t, s_t])[1]
+    for v in outs:
+        g.output(v)
+    plan = g.plan()
+    used = [z, h0] + ([dh, dT] if "linear_scan_grad" in others else []) + outs
+    bound = {v: 4096 * (i + 1) for i, v in enumerate(used)}
+    bound[outs[1]] = bound[h0]
+    for run in (lambda: plan.run(bound, 1 << 20, max(256, plan.workspace_bytes())), lambda: plan.bind(bound, 1 << 20, max(256, plan.workspace_bytes())).run()):
+        with pytest.raises(B.RelayError) as e:
+            run()
+        assert e.value.category == "binding", str(e.value)
+
+
 # ---- the oracle ------------------------------------------------------------------------------------------------------------
 def test_norm_by_hand():
     q, s, y = L.rms_norm_q8([[3.0, -4.0], [0.0, 0.0], [1.0, np.inf]], None, [1.0, 0.5], 1e-12, "f32")
