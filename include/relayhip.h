@@ -119,7 +119,7 @@ enum {
                                  eps 1e-5).  y = x + r rounded to e, the residual stream (x itself without r);
                                  n = y g / sqrt(mean_d y^2 + eps); s = max_d |n| / 127; q = n / s rounded to the nearest whole
                                  number, ties to even.  A row of zeros has s = 0 and q = 0, a row that holds an infinity or NaN, one with NaN
-                                 among its y g, or whose sum of squares or largest |y g| is past f32, s = NaN and q = 0.  Three results with r, two without */
+                                 among its y g, or whose sum of squares, largest |y g| or s is past f32, s = NaN and q = 0.  Three results with r, two without */
     RL_OP_DENSE_Q8 = 24,      /* (x i8[M,K], sx f32[M], w i8[N,K], sw f32[N][, b f32[N]]) -> f32|bf16 [M,N]; attrs rl_attr_contract (may be
                                  NULL: f32).  sx[m] sw[n] sum_k x[m,k] w[n,k] + b[n], the sum of the 8-bit products exact (32 bits:
                                  K <= 131071, else RL_ERR_UNSUPPORTED) */

@@ -44,7 +44,11 @@ struct Scale {
     __device__ __forceinline__ Scale(const NormQ8Params &p, float sum, float most)
     {
         whole = sum < INFINITY && most < INFINITY;                  // an infinity or NaN in the row or NaN among y g is one in its sum of squares
-        s = whole ? most * rsqrtf(sum / (float)p.D + p.eps) / 127.0f : __builtin_nanf("");
+        const float i = rsqrtf(sum / (float)p.D + p.eps);
+        s = most * i / 127.0f;
+        if (!(s < INFINITY)) s = most / 127.0f * i;                 // 127 steps may be past f32 where one is not
+        whole = whole && s < INFINITY;
+        s = whole ? s : __builtin_nanf("");
         up = most < 1e-30f ? 0x1p100f : 1.0f;                       // the factor of a tiny row would be past f32
         to_q = whole && most > 0.0f ? 127.0f / (most * up) : 0.0f;
     }

@@ -89,6 +89,25 @@ def test_norm_with_a_gain_that_is_no_number(d):
             assert np.isnan(out[1]).all() and not out[0].any(), (d, gain, residual)
 
 
+@pytest.mark.parametrize("d,past", [(515, False), (4096, False), (4096, True), (40000, False), (40000, True)])
+def test_norm_of_gains_near_the_end_of_f32(d, past):
+    """A row's scale is within f32 where 127 steps of it are not; a scale past f32 is none."""
+    x = np.zeros((2, d))
+    x[0, d // 3] = -1.0
+    x[1] = np.random.default_rng(d).normal(size=d)
+    x[1, d // 3] = 0.5
+    call, x, _, g = norm_case(2, d, "f32", False, "f32", x=x)
+    call.operands[-1][d // 3] = 3.4e38 if past else 2e37
+    g[d // 3] = float(call.operands[-1][d // 3])
+    out = call.run().numbers()
+    ref = L.rms_norm_q8(x, None, g, float(np.float32(1e-5)), "f32")[1]
+    assert ref[0] * 127 > np.finfo(np.float32).max
+    if past and ref[0] > np.finfo(np.float32).max:
+        assert np.isnan(out[1][0]) and not out[0][0].any()
+        out, x = [t[1:] for t in out], x[1:]
+    check_norm(out, x, None, g, "f32", f"gains of {g.max():.1e}")
+
+
 # ---- dense_q8 ------------------------------------------------------------------------------------------------------------
 def q8_case(m, n, k, out, bias, w_param=True, seed=0, edge=False):
     rng = np.random.default_rng(seed)
