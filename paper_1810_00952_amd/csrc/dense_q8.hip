@@ -349,11 +349,11 @@ template <int WM, int WN, int TM, int TN> void go_tile(const DenseQ8Params &p, h
 // Which tile, by an estimate of the time: us per 128-byte line of K of a workgroup that is alone on its CU, and per line and 256 workgroups
 // where there are more (measured; 8 x 4096 x 4096 from the smallest to the largest tile 7, 7, 9, 10, 14, 26, 32, 52 us, 128 x 4096 x 4096 32, 26,
 // 19, 16, 20, 26, 33, 54, 2048 x 4096 x 4096 455, 353, 228, 196, 136, 65, 42, 58)
+constexpr struct { int32_t bm, bn, threads; float alone, share; } forms[] = {
+    {16, 16, 512, 0.14f, 0.14f}, {32, 16, 512, 0.16f, 0.19f}, {32, 32, 512, 0.23f, 0.25f}, {64, 32, 512, 0.41f, 0.40f}, {64, 64, 512, 0.55f, 0.55f},
+    {64, 64, 256, 0.70f, 0.25f}, {128, 128, 256, 0.95f, 0.62f}, {256, 256, 512, 1.60f, 2.10f}};
 int form_of(const DenseQ8Params &p)
 {
-    static const struct { int32_t bm, bn; float alone, share; } forms[] = {
-        {16, 16, 0.14f, 0.14f}, {32, 16, 0.16f, 0.19f}, {32, 32, 0.23f, 0.25f}, {64, 32, 0.41f, 0.40f}, {64, 64, 0.55f, 0.55f},
-        {64, 64, 0.70f, 0.25f}, {128, 128, 0.95f, 0.62f}, {256, 256, 1.60f, 2.10f}};
     int best = 0;
     float least = INFINITY;
     for (int f = 0; f < 8; ++f) {
@@ -366,10 +366,16 @@ int form_of(const DenseQ8Params &p)
 
 }  // namespace
 
+bool dense_q8_fits(const DenseQ8Params &p)
+{
+    if (p.M < 1 || p.N < 1 || p.M > 0x7fffffff || p.N > 0x7fffffff) return false;
+    const auto &f = forms[form_of(p)];
+    return launch_has(((p.M + f.bm - 1) / f.bm) * ((p.N + f.bn - 1) / f.bn), f.threads);
+}
+
 hipError_t launch_dense_q8(const DenseQ8Params &p, hipStream_t s)
 {
-    if (p.M < 1 || p.N < 1 || p.K < 1 || p.K > 131071 || p.ldx < p.K || p.ldw < p.K || p.ldx % 16 != 0 || p.ldw % 128 != 0 || p.ldx > 131072 || p.ldw > 131072 ||
-        ((p.M + 15) / 16) * ((p.N + 15) / 16) > 0x7fffffff)
+    if (p.M < 1 || p.N < 1 || p.K < 1 || p.K > 131071 || p.ldx < p.K || p.ldw < p.K || p.ldx % 16 != 0 || p.ldw % 128 != 0 || p.ldx > 131072 || p.ldw > 131072)
         return hipErrorInvalidValue;
     switch (form_of(p)) {
     case 0: go_direct<1, 1>(p, s); break;

@@ -326,10 +326,13 @@ hipError_t launch_pad_bytes(const void *src, void *dst, const PadBytes &p, hipSt
 
 // ---- a gated recurrent language model -------------------------------------
 // norm_q8.hip: (x, r?, g) -> (q, s, y?); r and y null: no residual
+// *_fits of these operators: whether a launch has the threads they take, looked at once, as a plan is made
+constexpr bool launch_has(int64_t workgroups, int64_t threads) { return workgroups >= 1 && workgroups <= 0x7fffffff && workgroups * threads <= 0xffffffff; }
 struct NormQ8Params {
     const void *x, *r, *g; void *y; int8_t *q; float *s;
     int64_t M, D; int32_t dtype, g_dtype; float eps;
 };
+bool norm_q8_fits(const NormQ8Params &p);
 hipError_t launch_norm_q8(const NormQ8Params &p, hipStream_t s);
 // dense_q8.hip: rows of x and w ldx, ldw bytes apart, multiples of 16 and readable to the row's end; behind the K bytes of a row of w
 // there are zeros up to ldw, a multiple of 128
@@ -337,6 +340,7 @@ struct DenseQ8Params {
     const int8_t *x, *w; const float *sx, *sw, *b; void *y;
     int64_t M, N, K, ldx, ldw; int32_t y_dtype;
 };
+bool dense_q8_fits(const DenseQ8Params &p);
 hipError_t launch_dense_q8(const DenseQ8Params &p, hipStream_t s);
 // linear_scan.hip.  keep null: every row a token.  Forward: h, hT (either may be null).  Gradient: dh, dhT -> dz, dh0.
 // states: the state before every state_rows-th row, [B][ceil(T / state_rows)][D]: the forward pass writes it where it is not null, the
@@ -351,6 +355,7 @@ struct ScanParams {
 constexpr int64_t SCAN_MAX_D = (int64_t)1 << 20;
 int64_t scan_part_floats(const ScanParams &p, bool grad);      // scratch that the launch wants at part
 int64_t scan_state_rows(const ScanParams &p);
+bool scan_fits(const ScanParams &p, bool grad);
 hipError_t launch_scan(const ScanParams &p, hipStream_t s);
 hipError_t launch_scan_grad(const ScanParams &p, hipStream_t s);
 // token_logprobs.hip
@@ -365,6 +370,7 @@ struct LogprobsParams {
 constexpr int64_t LOGPROBS_MAX_V = 4000000;     // 64 segments of 65532 f32
 constexpr int LOGPROBS_MAX_TOP = 32;
 int64_t logprobs_part_floats(const LogprobsParams &p);
+bool logprobs_fits(const LogprobsParams &p);
 hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s);
 
 // measurement aid (calibrate.hip): a chain of register-operand bf16 MFMAs per wave; out holds grid * 512 floats

@@ -544,13 +544,16 @@ namespace {
 
 struct Form { int W, rows; bool split; int32_t slabs, tiles; };
 
+// channels of a lane
+int lane_channels(const ScanParams &p) { return p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1; }
+
 // Waves of a workgroup: enough for the rows, eight where there are few workgroups.  split: tiles as workgroups of their own, where there are
 // fewer than 128 workgroups that walk (channels of 64 x rows, bf16, forward pass: 64 x 2400 walking 33 us, split 23; 128 x 2400 39 and 42;
 // 192 x 2400 44 and 62; both passes 16 x 600 27 and 18, 128 x 2400 106 and 107); of four waves up to some 4000 rows, eight from there on
 // (both passes, 64 x 2400 58 and 62 us, 16 x 16384 112 and 102)
 Form form_of(const ScanParams &p, bool grad)
 {
-    const int64_t vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1;
+    const int64_t vec = lane_channels(p);
     Form f;
     f.slabs = (int32_t)((p.D + 32 * vec - 1) / (32 * vec));
     const int64_t wgs = p.B * f.slabs;
@@ -604,13 +607,21 @@ void go(bool grad, int mode, const ScanParams &p, const Form &f, hipStream_t s)
     else go<uint16_t, 1>(grad, mode, p, f, s);
 }
 
-bool sizes_ok(const ScanParams &p, const Form &f)
+bool sizes_ok(const ScanParams &p)
 {
     // a tile's rows are reached by 31-bit offsets
-    return p.B >= 1 && p.T >= 1 && p.D >= 1 && p.T <= 0x7fffffff && p.D <= SCAN_MAX_D && p.B * f.slabs * f.tiles <= 0x7fffffff;
+    return p.B >= 1 && p.T >= 1 && p.D >= 1 && p.B <= 0x7fffffff && p.T <= 0x7fffffff && p.D <= SCAN_MAX_D;
 }
 
 }  // namespace
+
+bool scan_fits(const ScanParams &p, bool grad)
+{
+    if (!sizes_ok(p)) return false;
+    if (p.T == 1 && !grad) return launch_has((p.B * p.D / lane_channels(p) + 255) / 256, 256);
+    const Form f = form_of(p, grad);
+    return launch_has(p.B * f.slabs * (f.split ? f.tiles : 1), 64 * f.W);
+}
 
 int64_t scan_state_rows(const ScanParams &p)
 {
@@ -627,11 +638,11 @@ int64_t scan_part_floats(const ScanParams &p, bool grad)
 hipError_t launch_scan(const ScanParams &p, hipStream_t s)
 {
     const Form f = form_of(p, false);
-    if (!sizes_ok(p, f) || p.keeps != (p.keep != nullptr) || (f.split && !p.part) || (p.states && p.state_rows % FWD_ROWS != 0)) return hipErrorInvalidValue;
-    if (p.T == 1 && p.h) {
-        const int vec = p.dtype == DT_BF16 && p.D % 2 == 0 ? 2 : 1;
+    if (!sizes_ok(p) || p.keeps != (p.keep != nullptr) || (f.split && !p.part) || (p.states && p.state_rows % FWD_ROWS != 0)) return hipErrorInvalidValue;
+    if (p.T == 1) {                                // (states alone are of longer sequences)
+        if (!p.h || !p.hT) return hipErrorInvalidValue;
+        const int vec = lane_channels(p);
         const int64_t total = p.B * p.D / vec, blocks = (total + 255) / 256;
-        if (blocks > 0x7fffffff) return hipErrorInvalidValue;
         if (p.dtype != DT_BF16) hipLaunchKernelGGL((linear_scan_step_kernel<float, 1>), dim3((unsigned)blocks), dim3(256), 0, s, p, total);
         else if (vec == 2) hipLaunchKernelGGL((linear_scan_step_kernel<uint16_t, 2>), dim3((unsigned)blocks), dim3(256), 0, s, p, total);
         else hipLaunchKernelGGL((linear_scan_step_kernel<uint16_t, 1>), dim3((unsigned)blocks), dim3(256), 0, s, p, total);
@@ -645,7 +656,7 @@ hipError_t launch_scan(const ScanParams &p, hipStream_t s)
 hipError_t launch_scan_grad(const ScanParams &p, hipStream_t s)
 {
     const Form f = form_of(p, true);
-    if (!sizes_ok(p, f) || p.keeps != (p.keep != nullptr) || (f.split && !p.part) || (!f.split && f.tiles > 1 && (!p.states || p.state_rows != 2 * f.W * f.rows))) return hipErrorInvalidValue;
+    if (!sizes_ok(p) || p.keeps != (p.keep != nullptr) || (f.split && !p.part) || (!f.split && f.tiles > 1 && (!p.states || p.state_rows != 2 * f.W * f.rows))) return hipErrorInvalidValue;
     if (f.split) go(true, 1, p, f, s);
     go(true, f.split ? 2 : 0, p, f, s);
     return hipGetLastError();

@@ -180,26 +180,38 @@ template <typename E, int T, int NV> void go(const NormQ8Params &p, hipStream_t 
 }
 
 // by the vectors of a row, one more for a row that begins inside one
-template <typename E> bool go(const NormQ8Params &p, hipStream_t s)
+struct Form { int64_t vecs; int threads; };
+constexpr Form FORMS[] = {{64, 64}, {128, 64}, {256, 64}, {512, 256}, {1024, 256}, {4096, 1024}, {8192, 1024}, {INT64_MAX, WG}};
+int form_of(const NormQ8Params &p)
 {
-    const int64_t n = 16 / sizeof(E), vecs = (p.D + n - 1) / n + (p.D % n != 0);
-    if (vecs <= 64) go<E, 64, 1>(p, s);
-    else if (vecs <= 128) go<E, 64, 2>(p, s);
-    else if (vecs <= 256) go<E, 64, 4>(p, s);
-    else if (vecs <= 512) go<E, 256, 2>(p, s);
-    else if (vecs <= 1024) go<E, 256, 4>(p, s);
-    else if (vecs <= 4096) go<E, 1024, 4>(p, s);
-    else if (vecs <= 8192) go<E, 1024, 8>(p, s);
-    else return false;
-    return true;
+    const int64_t n = p.dtype == DT_BF16 ? 8 : 4, vecs = (p.D + n - 1) / n + (p.D % n != 0);
+    int f = 0;
+    while (vecs > FORMS[f].vecs) ++f;
+    return f;
+}
+
+template <typename E> void go(const NormQ8Params &p, int form, hipStream_t s)
+{
+    switch (form) {
+    case 0: go<E, 64, 1>(p, s); break;
+    case 1: go<E, 64, 2>(p, s); break;
+    case 2: go<E, 64, 4>(p, s); break;
+    case 3: go<E, 256, 2>(p, s); break;
+    case 4: go<E, 256, 4>(p, s); break;
+    case 5: go<E, 1024, 4>(p, s); break;
+    case 6: go<E, 1024, 8>(p, s); break;
+    default: hipLaunchKernelGGL(norm_q8_kernel, dim3((unsigned)p.M), dim3(WG), 0, s, p); break;
+    }
 }
 
 }  // namespace
 
+bool norm_q8_fits(const NormQ8Params &p) { return p.D >= 1 && launch_has(p.M, FORMS[form_of(p)].threads); }
+
 hipError_t launch_norm_q8(const NormQ8Params &p, hipStream_t s)
 {
     if (p.M < 1 || p.D < 1 || p.M > 0x7fffffff || (p.r != nullptr) != (p.y != nullptr)) return hipErrorInvalidValue;
-    if (!(p.dtype == DT_BF16 ? go<uint16_t>(p, s) : go<float>(p, s))) hipLaunchKernelGGL(norm_q8_kernel, dim3((unsigned)p.M), dim3(WG), 0, s, p);
+    p.dtype == DT_BF16 ? go<uint16_t>(p, form_of(p), s) : go<float>(p, form_of(p), s);
     return hipGetLastError();
 }
 

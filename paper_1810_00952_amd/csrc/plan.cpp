@@ -1033,7 +1033,7 @@ struct Planner {
         if (st != RL_OK) return st;
         NormQ8Params p{};
         p.M = x.dims[0]; p.D = x.dims[1]; p.dtype = x.dtype; p.g_dtype = T(o.in.back()).dtype; p.eps = o.attrs.eps;
-        if (p.M > 0x7fffffff || p.D > 0x7fffffff) return fail(RL_ERR_UNSUPPORTED, "rms_norm_q8: more rows or columns than a launch has");
+        if (p.D > 0x7fffffff || !norm_q8_fits(p)) return fail(RL_ERR_UNSUPPORTED, "rms_norm_q8: more rows or columns than a launch has");
         Step &s = call_step(S_NORM_Q8, gi, oi, "rms_norm_q8", t.slot, {SL_Y, SL_COUT, SL_HOUT});
         s.nq = p;
         s.flops = 8.0 * numel(x);
@@ -1046,12 +1046,12 @@ struct Planner {
         const rl_type &x = T(o.in[0]), &w = T(o.in[2]);
         const int64_t M = x.dims[0], K = x.dims[1], N = w.dims[0];
         if (K > 131071) return fail(RL_ERR_UNSUPPORTED, "dense_q8: a sum of more than 131071 products may not fit 32 bits");
-        if (M > 0x7fffffff || N > 0x7fffffff) return fail(RL_ERR_UNSUPPORTED, "dense_q8: more rows or columns than a launch has");
         Step t;
         rl_status st = operands(o, {SL_X, SL_E0, SL_W, SL_E1, SL_E2}, t.slot);
         if (st != RL_OK) return st;
         DenseQ8Params p{};
         p.M = M; p.N = N; p.K = K; p.ldx = K; p.ldw = round_up(K, 128); p.y_dtype = T(o.out[0]).dtype;
+        if (!dense_q8_fits(p)) return fail(RL_ERR_UNSUPPORTED, "dense_q8: more rows or columns than a launch has");
         auto padded = [&](int src, int64_t rows, int64_t ld) {
             const int dst = new_ws((size_t)(rows * ld));
             Step &c = add_step(S_PAD_BYTES, std::string(op_name(o.kind)) + "#" + std::to_string(oi) + ".rows", "pad_bytes");
@@ -1091,7 +1091,7 @@ struct Planner {
         if (st != RL_OK) return st;
         ScanParams p{};
         p.B = h0.dims[0]; p.D = h0.dims[1]; p.T = z.dims[0] / p.B; p.dtype = z.dtype; p.keeps = t.slot[SL_E0] >= 0;
-        if (p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > SCAN_MAX_D) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more channels or rows than the kernels reach");
+        if (!scan_fits(p, grad) || (grad && p.T > 1 && !scan_fits(p, false))) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more channels or rows than the kernels reach");
         const int64_t every = grad ? scan_state_rows(p) : 0;
         if (every > 0) {
             // the states between come from a linear_scan of the same operands in this plan, or from a step of their own
@@ -1136,7 +1136,7 @@ struct Planner {
         if (st != RL_OK) return st;
         LogprobsParams p{};
         p.M = x.dims[0]; p.V = x.dims[1]; p.dtype = x.dtype; p.top = o.attrs.top;
-        if (p.M > 0xffffff || p.V > LOGPROBS_MAX_V) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows or columns than a launch has");
+        if (p.M > 0xffffff || !logprobs_fits(p)) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows or columns than a launch has");
         // right behind the forward operator on the same logits and tokens: one launch reads them for both
         const int before = (int)plan.steps.size() - 1;
         auto apart = [&](const Step &f) {          // what the gradient reads beside them is not that call's result

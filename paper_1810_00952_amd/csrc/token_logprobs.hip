@@ -369,6 +369,7 @@ namespace {
 
 struct Form { int segs; int32_t len; int shape; };           // shape: of the kernel, by the bytes it holds
 
+constexpr int SHAPE_THREADS[] = {64, 256, 512, 1024, 1024};
 constexpr int64_t SHAPE_BYTES[] = {64 * 4 * 16, 256 * 4 * 16, 512 * 8 * 16, 1024 * 8 * 16, 1024 * 16 * 16};
 
 Form form_of(const LogprobsParams &p)
@@ -422,11 +423,18 @@ int64_t logprobs_part_floats(const LogprobsParams &p)
     return f.segs > 1 ? p.M * f.segs * (4 + 2 * (int64_t)p.top) : 0;
 }
 
+bool logprobs_fits(const LogprobsParams &p)
+{
+    if (p.M < 1 || p.V < 1 || p.M > 0x7fffffff || p.V > LOGPROBS_MAX_V) return false;
+    const Form f = form_of(p);
+    return f.segs <= MAX_SEGS && f.len * (p.dtype == DT_BF16 ? 2 : 4) + 16 <= SHAPE_BYTES[4] && launch_has(p.M * f.segs, SHAPE_THREADS[f.shape]);      // the joining launch has no more
+}
+
 hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s)
 {
     const Form f = form_of(p);
-    if (p.M < 1 || p.V < 1 || p.V > LOGPROBS_MAX_V || f.segs > MAX_SEGS || p.M * f.segs > 0x7fffffff || p.top < 0 || p.top > p.V || p.top > LOGPROBS_MAX_TOP || (f.segs > 1 && !p.part) || f.len * (p.dtype == DT_BF16 ? 2 : 4) + 16 > SHAPE_BYTES[4])
-        return hipErrorInvalidValue;
+    if (p.M < 1 || p.V < 1 || p.V > LOGPROBS_MAX_V || f.segs > MAX_SEGS || p.M * f.segs > 0x7fffffff || f.len * (p.dtype == DT_BF16 ? 2 : 4) + 16 > SHAPE_BYTES[4] ||
+        p.top < 0 || p.top > p.V || p.top > LOGPROBS_MAX_TOP || (f.segs > 1 && !p.part)) return hipErrorInvalidValue;
     auto run = [&](int what) { p.dtype == DT_BF16 ? go<uint16_t>(p, f, what, s) : go<float>(p, f, what, s); };
     if (f.segs == 1) {
         run((forward ? FORWARD : 0) | (grad ? GRADIENT : 0) | (forward && p.top > 0 ? TOP : 0));

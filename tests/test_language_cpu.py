@@ -103,6 +103,28 @@ def test_a_sum_past_32_bits_is_refused():
     assert e.value.category == "unsupported"
 
 
+BIG = 1 << 27
+
+
+@pytest.mark.parametrize("kind,operands,results", [
+    ("rms_norm_q8", [("f32", (BIG, 4)), ("f32", (4,))], [("i8", (BIG, 4)), ("f32", (BIG,))]),
+    ("dense_q8", [("i8", (16 * BIG - 1, 16)), ("f32", (16 * BIG - 1,)), ("i8", (1, 16)), ("f32", (1,))], [("f32", (16 * BIG - 1, 1))]),
+    ("linear_scan", [("f32", (BIG, 2)), ("f32", (BIG, 1))], [("f32", (BIG, 1)), ("f32", (BIG, 1))]),
+    ("linear_scan", [("f32", (4 * BIG, 128)), ("f32", (4 * BIG, 64))], [("f32", (4 * BIG, 64)), ("f32", (4 * BIG, 64))]),
+    ("linear_scan", [("f32", (2 * BIG, 2)), ("f32", (BIG, 1))], [("f32", (2 * BIG, 1)), ("f32", (BIG, 1))]),
+    ("linear_scan_grad", [("f32", (2 * BIG, 2)), ("f32", (BIG, 1)), ("f32", (2 * BIG, 1)), ("f32", (BIG, 1))], [("f32", (2 * BIG, 2)), ("f32", (BIG, 1))]),
+    ("token_logprobs", [("f32", (BIG // 8 - 1, 4100)), ("i32", (BIG // 8 - 1,))], [("f32", (BIG // 8 - 1,)), ("f32", (BIG // 8 - 1,))]),
+    ("token_logprobs_grad", [("f32", (BIG // 8 - 1, 4100)), ("i32", (BIG // 8 - 1,)), ("f32", (BIG // 8 - 1,)), ("f32", (BIG // 8 - 1,))], [("f32", (BIG // 8 - 1, 4100))])])
+def test_more_threads_than_a_launch_has_are_refused(kind, operands, results):
+    """A launch has fewer than 2^32 threads: a call that wants more is refused as its plan is made, not as it runs."""
+    if operands[0][1] == (BIG, 2):                 # one token a sequence, a thread a channel: this many are there
+        assert plan_of(kind, operands, results)[0].describe()["steps"]
+        return
+    with pytest.raises(B.RelayError) as e:
+        plan_of(kind, operands, results)
+    assert e.value.category == "unsupported", str(e.value)
+
+
 def test_they_are_groups_of_their_own():
     g = B.Graph(B.Context())
     z, h0 = g.input("f32", (12, 10)), g.input("f32", (3, 5))
