@@ -272,8 +272,9 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
             }
         };
         if (KEEP || !whole) fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
-        // a wave that walks its tiles mostly has tokens alone; tiles as workgroups are launches too short to read two loops' code
-        const bool masked = KEEP ? MODE != 0 || __any((fl.pad | fl.first) != 0) : !whole;
+        // with a keep every row is masked: a second loop for waves of tokens alone is slower (8 x 4096 x 2048 bf16, documents of some 400 tokens,
+        // forward pass 93 -> 96 us, both passes 241 -> 249): what bounds either is memory
+        const bool masked = KEEP || !whole;
         if (masked) rows(std::true_type{});
         else rows(std::false_type{});
 #pragma unroll
@@ -336,8 +337,7 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_kernel(
                         store<STREAM>(h, off1 + i * line, pack<E, VEC>(out));
                     }
                 };
-                if (KEEP && masked) results(std::bool_constant<KEEP>{});
-                else results(std::false_type{});
+                results(std::bool_constant<KEEP>{});
             }
             if (p.hT && tile + 1 == tiles && at.run == 0) {
 #pragma unroll
@@ -432,10 +432,11 @@ __global__ __launch_bounds__(64 * W, MODE == 0 ? 2 : 4) void linear_scan_grad_ke
             }
         };
         if (KEEP || !whole) fl = flags_of<ROWS, KEEP>(p, at.b, t0, at.half);
-        // a wave that walks its tiles mostly has tokens alone; tiles as workgroups are launches too short to read two loops' code
-        const bool masked = KEEP ? MODE != 0 || __any((fl.pad | fl.first) != 0) : !whole;
+        const bool masked = KEEP || !whole;
         if (masked) rows(std::true_type{});
         else rows(std::false_type{});
+        // the rows' masks are made again for the way back: kept from here they are more scalar registers than there are (both passes 246 -> 235 us)
+        if (KEEP && MODE == 0) fl = {anew(fl.pad), anew(fl.first), anew(fl.behind)};
 #pragma unroll
         for (int j = 0; j < VEC; ++j) pa[j] = KEEP && fl.first != 0 ? FIRST : above_zero(pa[j]);
         float oa[VEC], oh[VEC], og[VEC];

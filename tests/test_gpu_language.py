@@ -599,6 +599,40 @@ def test_scan_of_many_tiles(b, t, d, dtype):
         check_grad(case[0].run().numbers(), *case[1:], dtype, what)
 
 
+@pytest.mark.parametrize("b,t,d,dtype", [(8, 700, 1024, "bf16"), (40, 600, 515, "f32"), (9, 1300, 515, "bf16"), (5, 777, 515, "f32"), (1, 3001, 130, "bf16")])
+def test_scan_of_long_documents(b, t, d, dtype):
+    """Documents of some hundred tokens: waves of tokens alone beside ones with first tokens, with padding and with rows past the end, in the
+    workgroups that walk (the first three) and in tiles of their own; one sequence of nothing but tokens; a document that holds NaN."""
+    rng, z, h0, _, operands, _ = scan_inputs(b, t, d, dtype, None, seed=t)
+    keep = np.ones((b, t))
+    for i in range(1 if b > 1 else 0, b):
+        keep[i, rng.choice(np.arange(1, t), size=max(1, t // 350), replace=False)] = 2
+        keep[i, t - int(rng.integers(0, t // 3)):] = 0
+    tdh, dh = tensor(rng.normal(size=(b * t, d)), dtype)
+    tdT, dhT = tensor(rng.normal(size=(b, d)), "f32")
+    z, dh, tz = z.reshape(b, t, 2 * d), dh.reshape(b, t, d), operands[0][0].view(b, t, 2 * d)
+    at = int(np.flatnonzero(keep[b - 1] == 2)[0]) - 1      # the last token of a first document
+    z[b - 1, at, d + 1], tz[b - 1, at, d + 1] = np.nan, float("nan")
+    dh[keep == 0] = 0.0                                    # padding is not looked at
+    z[keep == 0] = 0.0
+    import torch
+    tz[torch.from_numpy(keep == 0).to(tz.device)] = float("nan")
+    z, dh, keep = z.reshape(b * t, 2 * d), dh.reshape(b * t, d), keep.reshape(-1)
+    last = [(tensor(keep, "i8")[0], "i8")]
+    with np.errstate(invalid="ignore"):
+        after, before, end = scan_bounds(z, h0, keep)
+        (h, hT), states = L.linear_scan(z, h0, keep), L.linear_scan(z, h0, keep, states=True)[2]
+        tf, tv, t0 = scan_grad_bounds(z, h0, dh, dhT, keep, states, before)
+        dz, dh0 = L.linear_scan_grad(z, h0, dh, dhT, keep)
+    after, tol = (np.where(keep[:, None] == 0, 0.0, a.reshape(b * t, -1)) for a in (after, np.stack([tf, tv], 2)))
+    out = Call("linear_scan", operands + last, [(dtype, (b * t, d)), ("f32", (b, d))]).run().numbers()
+    within(out[0], h, after + (BF16 * (np.abs(h) + after) if dtype == "bf16" else 0), "h")
+    within(out[1], hT, end, "hT")
+    out = Call("linear_scan_grad", operands + [(tdh, dtype), (tdT, "f32")] + last, [(dtype, (b * t, 2 * d)), ("f32", (b, d))]).run().numbers()
+    within(out[0], dz, tol + (BF16 * (np.abs(dz) + tol) if dtype == "bf16" else 0), "dz")
+    within(out[1], dh0, t0, "dh0")
+
+
 def session_of(build):
     """A graph's plan on torch tensors: build(graph) -> ({id: tensor}, {id: (dtype, shape)} of results)."""
     import torch
