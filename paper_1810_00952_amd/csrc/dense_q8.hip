@@ -258,7 +258,10 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q8_tile_kernel(const Dense
     if (kt < g.nk) body(st0, st1);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the trailing requests; from here the stages are free
 
-    // lane's row of x is frow, its columns 8 q + 4 fhalf .. + 3: through LDS, a wave's own part of it, to whole lines of y
+    // lane's row of x is frow, its columns 8 q + 4 fhalf .. + 3: bf16 of whole lines straight from registers, the rest through LDS, 4 KB of it a
+    // wave's own, to whole lines of y
+    static_assert(W * 4096 <= STAGE, "every wave's part is in the first stage");
+    float *const park = (float *)st0 + wave * 1024;
     const bool whole = p.N % (p.y_dtype == DT_BF16 ? 8 : 4) == 0;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -292,7 +295,6 @@ __global__ __launch_bounds__(64 * WM * WN) void dense_q8_tile_kernel(const Dense
                 }
                 continue;
             }
-            float *park = (float *)(W * 4096 <= STAGE ? st0 : wave < W / 2 ? st0 : st1) + (W * 4096 <= STAGE ? wave : wave % (W / 2)) * 1024;
             wave_lds_exchange();
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
