@@ -705,6 +705,66 @@ def test_logprobs_and_gradient_share_a_launch(m, v):
     np.testing.assert_array_equal(got[4].double().numpy(), want.double().cpu().numpy())
 
 
+@pytest.mark.parametrize("m,v,k", [(5, 700, 64), (3, 70000, 40), (300, 5003, 128)])
+def test_values_between_a_loss_and_its_reader_share_the_workspace(m, v, k):
+    """Logits, loss and gradient that nobody else sees live in one workspace: the results are those of a plan whose every value leaves it."""
+    import torch
+    rng = np.random.default_rng(v)
+    tensors = dict(q=(rng.integers(-127, 128, size=(m, k)), "i8"), s=(rng.uniform(0.01, 0.03, size=m), "f32"), w=(rng.integers(-127, 128, size=(v, k)), "i8"),
+                   sw=(rng.uniform(0.01, 0.02, size=v), "f32"), tok=(rng.integers(-1, v, size=m), "i32"), dlp=(rng.normal(size=m), "f32"), dent=(rng.normal(size=m), "f32"))
+    tensors = {n: (tensor(a, dt)[0], dt) for n, (a, dt) in tensors.items()}
+    row, wide, tops = ("f32", (m,)), ("bf16", (m, v)), [("f32", (m, 3)), ("i32", (m, 3))]
+
+    def build(everything):
+        def f(g):
+            ids = {n: g.input(dt, t.shape) for n, (t, dt) in tensors.items()}
+            x, = g.op("dense_q8", [ids[n] for n in ("q", "s", "w", "sw")], [wide], out_dtype="bf16")[1]
+            made = g.op("token_logprobs", [x, ids["tok"]], [row, row] + tops, top=3)[1]
+            dx, = g.op("token_logprobs_grad", [x, ids["tok"], ids["dlp"], ids["dent"]], [wide])[1]
+            far, = g.op("neg", [dx], [wide])[1]
+            loss, = g.op("neg", [made[0]], [row])[1]
+            outs = {far: wide, loss: row}
+            return {ids[n]: t for n, (t, _) in tensors.items()}, outs | (dict(zip([x, *made, dx], [wide, row, row, *tops, wide])) if everything else {})
+        return f
+
+    plan, got = session_of(build(False))
+    assert any("token_logprobs | token_logprobs_grad" in s["kernel"] for s in plan.describe()["steps"])
+    full, want = session_of(build(True))
+    assert [s["kernel"] for s in full.describe()["steps"]] == [s["kernel"] for s in plan.describe()["steps"]] and plan.workspace_bytes() > full.workspace_bytes()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b) and bool(torch.isfinite(a.float()).all())
+
+
+@pytest.mark.parametrize("b,t,d,how", [(8, 300, 1024, "some"), (8, 300, 1024, None), (1, 2000, 130, "some"), (3, 20, 70, None)])
+def test_values_between_a_scan_and_its_gradient_share_the_workspace(b, t, d, how):
+    """The same of a recurrence whose operands and results are all values of the plan."""
+    import torch
+    _, z, h0, keep, operands, tk = scan_inputs(b, t, d, "f32", how, seed=9)
+    tz = tensor(z, "f32")[0]
+    wide, state, rows = ("f32", (b * t, 2 * d)), ("f32", (b, d)), ("f32", (b * t, d))
+
+    def build(everything):
+        def f(g):
+            iz, ih = g.input(*wide), g.input(*state)
+            tail = [g.input("i8", (b * t,))] if tk is not None else []
+            z, = g.op("neg", [iz], [wide])[1]
+            h0, = g.op("neg", [ih], [state])[1]
+            h, hT = g.op("linear_scan", [z, h0] + tail, [rows, state])[1]
+            dh, = g.op("neg", [h], [rows])[1]
+            dT, = g.op("neg", [hT], [state])[1]
+            dz, d0 = g.op("linear_scan_grad", [z, h0, dh, dT] + tail, [wide, state])[1]
+            y, = g.op("neg", [dz], [wide])[1]
+            y0, = g.op("neg", [d0], [state])[1]
+            return {iz: tz, ih: operands[1][0], **{v: tk for v in tail}}, {y: wide, y0: state} | (dict(zip([z, h0, h, hT, dh, dT, dz, d0], [wide, state, rows, state, rows, state, wide, state])) if everything else {})
+        return f
+
+    plan, got = session_of(build(False))
+    full, want = session_of(build(True))
+    assert [s["kernel"] for s in full.describe()["steps"]] == [s["kernel"] for s in plan.describe()["steps"]] and plan.workspace_bytes() > full.workspace_bytes()
+    for a, b_ in zip(got, want):
+        assert torch.equal(a, b_) and bool(torch.isfinite(a).all())
+
+
 def check_graph(spec, data, dtype):
     """Every call of a graph against its definition on what the library computed for its operands."""
     import torch
