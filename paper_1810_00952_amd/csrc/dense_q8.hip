@@ -11,8 +11,10 @@
 // dense_q8_direct: for few rows of x, where the time is w's way from memory: fragments straight into registers, K over the
 // eight waves of a workgroup (whole lines in turn), whose sums meet in LDS: every wave's loads are under way at once.
 //
-// 8192 x 8192 x 4096 270 us (2.03 Pop/s), 4096 x 4096 x 16384 240 us (2.29): power, the MFMAs busy 52 % of the cycles at some 1.9 GHz; all of a tile's
-// requests in one k-step 281 us.  8 x 4096 x 4096 6.4 us: a launch and a chain of latencies.
+// 8192 x 8192 x 4096 269 us (2.04 Pop/s), 4096 x 4096 x 16384 240 us (2.29), a library product of 8-bit integers without scales 2.2: the MFMAs are busy 52 % of the
+// cycles at some 1.9 GHz without conflicts in LDS; what takes the other half is not known.  All of a tile's requests in one k-step 281 us.
+// Short rows: a workgroup does one tile, whose first requests and results stand alone: K = 1024, 4096 rows by 1024, 2048 and 32000 columns
+// 0.77, 1.08 and 1.36 Pop/s.  8 x 4096 x 4096 6.4 us: a launch and a chain of latencies.
 #include "igemm_lds.h"
 
 namespace rl {
@@ -350,7 +352,9 @@ template <int WM, int WN, int TM, int TN> void go_tile(const DenseQ8Params &p, h
 
 // Which tile, by an estimate of the time: us per 128-byte line of K of a workgroup that is alone on its CU, and per line and 256 workgroups
 // where there are more (measured; 8 x 4096 x 4096 from the smallest to the largest tile 7, 7, 9, 10, 14, 26, 32, 52 us, 128 x 4096 x 4096 32, 26,
-// 19, 16, 20, 26, 33, 54, 2048 x 4096 x 4096 455, 353, 228, 196, 136, 65, 42, 58)
+// 19, 16, 20, 26, 33, 54, 2048 x 4096 x 4096 455, 353, 228, 196, 136, 65, 42, 58).  A tile's time beside its lines is not in it; for short rows it
+// takes the fastest or one that is a little slower (4096 x 2048 x 1024 119, 109, 69, 66, 48, 20, 16.6, 22 us, of which it takes the seventh, 4096 x 1024 x 1024 60, 56, 36,
+// 34, 25, 11.5, 11.9, 19, the seventh, 4096 x 8192 x 512 301, 302, 189, 175, 126, 52, 40, 38, the eighth, 512 x 2048 x 1024 18, 16, 11, 10, 8, 7, 11, 18, the fifth)
 constexpr struct { int32_t bm, bn, threads; float alone, share; } forms[] = {
     {16, 16, 512, 0.14f, 0.14f}, {32, 16, 512, 0.16f, 0.19f}, {32, 32, 512, 0.23f, 0.25f}, {64, 32, 512, 0.41f, 0.40f}, {64, 64, 512, 0.55f, 0.55f},
     {64, 64, 256, 0.70f, 0.25f}, {128, 128, 256, 0.95f, 0.62f}, {256, 256, 512, 1.60f, 2.10f}};

@@ -12,11 +12,13 @@
 // prefix products and results of its rows from zero.  A run with a document's first row has -0 for A, which no product of gates
 // is: nothing of what comes before goes into what follows, neither an infinity nor NaN.  The runs' (A, H) meet in LDS, every run adds up those before it, and one fma a
 // row then gives the states.  The workgroup carries the tile's last state on to its next tile, whose rows are requested as
-// the registers of this one's become free.  Nothing is read twice.  What bounds it is HBM, in columns of 128 bytes: 8 x 4096 x 2048 bf16 96 us
-// (4.2 TB/s), its gradient 152 us (4.4 TB/s); two tiles under way are no faster.
+// the registers of this one's become free.  Nothing is read twice.  What bounds it is HBM, in columns of 128 bytes: 8 x 4096 x 2048 bf16 94 us
+// (4.3 TB/s), its gradient 150 us (4.5 TB/s), both in turn 241; two tiles under way are no faster.  Fewer than 256 workgroups leave CUs without work: 8 x 1024 x
+// 1024 is 128 of them, 18 and 26 us (2.8 and 3.3 TB/s).
 //
 // Few channels and many rows: each tile is a workgroup of its own.  A launch ahead finds the tiles' (A, H) (and, of the gradient, G),
-// and every workgroup adds up those before (behind) its tile, at the cost of a second read: one sequence of 16384 x 1024 bf16 15 and 25 us.
+// and every workgroup adds up those before (behind) its tile, at the cost of a second read: one sequence of 16384 x 1024 bf16 15 and 25 us.  The adding up
+// grows with the square of the tiles: 131072 x 1024 in 345 us, where eight times the shorter sequence's 38 are 307.
 #include <type_traits>
 
 #include "igemm_lds.h"

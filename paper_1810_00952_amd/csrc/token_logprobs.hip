@@ -9,7 +9,7 @@
 // the statistics, the alternatives and the gradient; a gradient planned right behind its forward operator shares its launch.  Every lane
 // sums relative to its own maximum, the lanes' (m, S, U) meet once.  Rows too long for that, and few long rows, are cut
 // into segments, whose statistics and alternatives a second launch joins.  What bounds it is HBM, and beside it two exponentials and some 19
-// other vector operations a logit: 8192 x 50001 bf16 with the gradient 320 us (5.1 TB/s), 2000 x 10007 f32 28 us; four rows of 131072 bf16 with
+// other vector operations a logit: 8192 x 50001 bf16 with the gradient 321 us (5.1 TB/s), 2000 x 10007 f32 28 us; four rows of 131072 bf16 with
 // eight alternatives 7 and 5 us.
 //
 // Alternatives: each of 64 groups of lanes has its largest logit; the top-th of those is at most the top-th of the row, so what is not below it
