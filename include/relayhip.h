@@ -72,7 +72,8 @@ enum {
 enum { RL_F32 = 0, RL_BF16 = 1, RL_I8 = 2, RL_I32 = 3 };
 
 #define RL_MAX_RANK 6
-#define RL_MAX_RESULTS 4
+#define RL_MAX_OPERANDS 12
+#define RL_MAX_RESULTS 8
 
 /* Tensor(dtype, Shape(dims[0..rank-1])); rank 0 is a scalar. */
 typedef struct rl_type {
@@ -139,7 +140,28 @@ enum {
                                  Four results where top > 0, two otherwise */
     RL_OP_TOKEN_LOGPROBS_GRAD = 28, /* (x, tok, dlp f32[M], dent f32[M]) -> dx e[M,V]: dlp (1[v = tok] - p) - dent p (ln p + ent); no target: as
                                  with dlp = 0; a row of -inf alone: zeros */
-    RL_OP_KIND_COUNT = 29
+    /* A selective state-space language model: its tokens mix through a short convolution and a recurrence with several numbers of state
+     * a channel, whose gates come from the tokens; its loss is found without the logits in memory.  Each is a group of its own; e, T, keep
+     * and brackets as above.  Padding is as if its rows were not there: what stands in them (NaN, too) reaches nothing, their results are zeros. */
+    RL_OP_CAUSAL_CONV = 29,   /* (x e[B*T,D], w f32|e[D,K], b f32[D], s0 e[B,K-1,D][, keep i8[B*T]]) -> (y e[B*T,D], sT e[B,K-1,D]); K 2 to 8 (else
+                                 RL_ERR_UNSUPPORTED); attrs rl_attr_conv1d (may be NULL: none).  u_t[d] = b[d] + sum_k w[d,k] x_(t-K+1+k)[d] over the sequence's own tokens, those before
+                                 the first from s0 (its last row the newest), those before a document's first token zero; y = u, or u sigmoid(u)
+                                 with silu.  sT: the last K-1 tokens, the next call's s0.  sT may lie over s0 as hT over h0 */
+    RL_OP_CAUSAL_CONV_GRAD = 30, /* (x, w, b, s0, dy e[B*T,D], dsT e[B,K-1,D][, keep]) -> (dx e[B*T,D], dw f32[D,K], db f32[D], ds0 e[B,K-1,D]); attrs of
+                                 the forward operator.  u is computed anew */
+    RL_OP_SELECTIVE_SCAN = 31, /* (x e[B*T,D], dt e[B*T,D], bc e[B*T,2N] as B|C blocks, a f32[D,N], skip f32[D], h0 f32[B,D,N][, z e[B*T,D]][, keep i8[B*T]])
+                                 -> (y e[B*T,D], hT f32[B,D,N]); N at most 64 (else RL_ERR_UNSUPPORTED).  s = softplus(dt[t,d]);
+                                 h_t[d,n] = exp(s a[d,n]) h_(t-1)[d,n] + s x[t,d] B[t,n]; y[t,d] = (sum_n C[t,n] h_t[d,n] + skip[d] x[t,d]) z sigmoid(z), the
+                                 last factor only where there is a z.  The state is f32; exp(s a) counts down to 2^-126, below it it may be 0.  hT may lie over h0 as linear_scan's */
+    RL_OP_SELECTIVE_SCAN_GRAD = 32, /* (x, dt, bc, a, skip, h0, dy e[B*T,D], dhT f32[B,D,N][, z][, keep]) -> (dx e[B*T,D], ddt e[B*T,D], dbc e[B*T,2N],
+                                 da f32[D,N], dskip f32[D], dh0 f32[B,D,N][, dz e[B*T,D]]): seven results with z, six without; the states between are computed anew */
+    RL_OP_DENSE_LOGPROBS = 33, /* (x e[M,K], w e[V,K], tok i32[M]) -> (lp f32[M], lse f32[M]): with the logits l = x w^T, which are never in memory as a whole,
+                                 lse = ln sum_v e^l[m,v]; lp = l[m,tok] - lse, 0 where tok is outside 0..V-1 (no target).  A logit of -inf has p = 0, a row of nothing else has
+                                 lse -inf and lp -inf; a row with +inf or NaN has NaN in lse, and in lp where it has a target */
+    RL_OP_DENSE_LOGPROBS_GRAD = 34, /* (x, w, tok, lse f32[M], dlp f32[M], dlse f32[M]) -> (dx e[M,K], dw e[V,K]): dl = dlp (1[v = tok] - p) + dlse p with p = e^(l - lse), lse the
+                                 forward operator's; dx = dl w, dw = dl^T x, dl rounded to e between them, as a product's operand.  No target: as with dlp = 0.  A row
+                                 whose dlp and dlse are both 0 takes no part, whatever is in it */
+    RL_OP_KIND_COUNT = 35
 };
 
 typedef struct rl_attr_contract { int32_t out_dtype; /* operand dtype, or RL_F32 */ } rl_attr_contract;
@@ -156,6 +178,7 @@ typedef struct rl_attr_layout { int32_t perm[RL_MAX_RANK]; /* a permutation of 0
 typedef struct rl_attr_norm { float eps; /* > 0, finite; else RL_ERR_KIND */ } rl_attr_norm;
 typedef struct rl_attr_logprobs { int32_t top; /* 0 .. RL_TOP_MAX and at most V; else RL_ERR_KIND */ } rl_attr_logprobs;
 #define RL_TOP_MAX 32
+typedef struct rl_attr_conv1d { int32_t silu; /* 0 or 1; else RL_ERR_KIND */ } rl_attr_conv1d;
 
 typedef struct rl_binding { int32_t value_id; void *dev_ptr; } rl_binding;
 
@@ -288,8 +311,8 @@ rl_status rl_plan_prepack(const rl_plan *plan, int32_t param_value_id, const voi
  * (packed copy where rl_plan_packed_bytes > 0) and output value id exactly
  * once; intermediates live in workspace_dev (>= rl_plan_workspace_bytes).
  * Inputs and params are read only; outputs and workspace are overwritten.
- * An output may alias an input only for lstm_gates' cell state (c' over c) and the state of a linear_scan of one token
- * whose h0 nothing behind it reads (hT over h0).
+ * An output may alias an input only for lstm_gates' cell state (c' over c) and the state of a linear_scan, causal_conv or
+ * selective_scan of one token whose old state nothing behind it reads (hT over h0, sT over s0).
  * The call only launches kernels on hip_stream (no allocation, no memset, no
  * synchronisation), so it may be made while that stream is being captured into
  * a HIP graph; replays then need the same device pointers to stay valid. */

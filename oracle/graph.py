@@ -239,12 +239,13 @@ def infer(kind: str, ins: List[Tuple[str, Tuple[int, ...]]], attrs: Dict) -> Lis
     raise IllTyped("kind", f"unknown operator {kind!r}")
 
 
-LANGUAGE = ("rms_norm_q8", "dense_q8", "linear_scan", "linear_scan_grad", "token_logprobs", "token_logprobs_grad")
+LANGUAGE = ("rms_norm_q8", "dense_q8", "linear_scan", "linear_scan_grad", "token_logprobs", "token_logprobs_grad",
+            "causal_conv", "causal_conv_grad", "selective_scan", "selective_scan_grad", "dense_logprobs", "dense_logprobs_grad")
 TOP_MAX = 32
 
 
 def _infer_language(kind, ins, attrs):
-    """The arrow types of a gated recurrent language model's operators."""
+    """The arrow types of a gated recurrent and of a selective state-space language model's operators."""
     def operand(i, *allowed):
         if ins[i] not in allowed:
             raise IllTyped("type", f"{kind}: operand {i} is {ins[i]}, not {allowed[0]}")
@@ -293,6 +294,56 @@ def _infer_language(kind, ins, attrs):
         if len(ins) > n:
             operand(n, ("i8", (rows,)))
         return [ins[0] if n == 4 else (e, (rows, d)), ins[1]]
+    if kind.startswith("causal_conv"):
+        n = 6 if kind.endswith("grad") else 4
+        if attrs.get("silu", 0) not in (0, 1):
+            raise IllTyped("kind", "silu is neither 0 nor 1")
+        count(n, n + 1)
+        matrix(0), matrix(1)
+        (e, (rows, d)), (wd, k), state = ins[0], ins[1][1], ins[3]
+        operand(1, ("f32", (d, k)), (e, (d, k)))
+        operand(2, ("f32", (d,)))
+        if not 2 <= k <= 8:
+            raise IllTyped("unsupported", f"{kind}: {k} taps")
+        if len(state[1]) != 3 or rows % state[1][0]:
+            raise IllTyped("type", f"{kind}: x {ins[0]} is not [B*T,D] for {state}")
+        before = (e, (state[1][0], k - 1, d))
+        operand(3, before)
+        if n == 6:
+            operand(4, ins[0]), operand(5, before)
+        if len(ins) > n:
+            operand(n, ("i8", (rows,)))
+        return [ins[0], ("f32", (d, k)), ("f32", (d,)), before] if n == 6 else [ins[0], before]
+    if kind.startswith("selective_scan"):
+        n = 8 if kind.endswith("grad") else 6
+        count(n, n + 1, n + 2)
+        matrix(0)
+        (e, (rows, d)), state = ins[0], ins[5]
+        if len(state[1]) != 3 or rows % state[1][0]:
+            raise IllTyped("type", f"{kind}: x {ins[0]} is not [B*T,D] for {state}")
+        b, _, s = state[1]
+        operand(1, ins[0]), operand(2, (e, (rows, 2 * s))), operand(3, ("f32", (d, s))), operand(4, ("f32", (d,))), operand(5, ("f32", (b, d, s)))
+        if n == 8:
+            operand(6, ins[0]), operand(7, state)
+        rest = list(range(n, len(ins)))
+        gated = bool(rest) and ins[n][0] != "i8"
+        if gated:
+            operand(rest.pop(0), ins[0])
+        if rest:
+            operand(rest.pop(0), ("i8", (rows,)))
+        if rest:
+            raise IllTyped("type", f"{kind}: too many operands")
+        if s > 64:
+            raise IllTyped("unsupported", f"{kind}: {s} states")
+        return [ins[0], ins[0], ins[2], ins[3], ins[4], state] + ([ins[0]] if gated else []) if n == 8 else [ins[0], state]
+    if kind.startswith("dense_logprobs"):
+        count(6 if kind.endswith("grad") else 3)
+        matrix(0), matrix(1)
+        (e, (m, k)), (v, _) = ins[0], ins[1][1]
+        operand(1, (e, (v, k))), operand(2, ("i32", (m,)))
+        for i in range(3, len(ins)):
+            operand(i, ("f32", (m,)))
+        return [ins[0], ins[1]] if len(ins) > 3 else [("f32", (m,)), ("f32", (m,))]
     top = attrs.get("top", 0) if kind == "token_logprobs" else 0
     if not 0 <= top <= TOP_MAX:
         raise IllTyped("kind", "top out of range")
@@ -321,6 +372,14 @@ def _run_language(kind, a, attrs, spec, op):
         return L.linear_scan_grad(*a)
     if kind == "token_logprobs":
         return L.token_logprobs(a[0], a[1], attrs.get("top", 0))
+    if kind.startswith("causal_conv"):
+        return getattr(L, kind)(*a, silu=bool(attrs.get("silu", 0)))
+    if kind.startswith("selective_scan"):
+        n = 8 if kind.endswith("grad") else 6
+        gated = len(a) > n and spec.values[op.inputs[n]].type.dtype != "i8"
+        return getattr(L, kind)(*a[:n], z=a[n] if gated else None, keep=a[-1] if len(a) > n + gated else None)
+    if kind.startswith("dense_logprobs"):
+        return getattr(L, kind)(*a)
     return [L.token_logprobs_grad(*a)]
 
 

@@ -21,7 +21,8 @@ DTYPE_BYTES = {"f32": 4, "bf16": 2, "i8": 1, "i32": 4}
 OPS = {"dense": 0, "conv2d": 1, "bias_add": 2, "add": 3, "sub": 4, "mul": 5, "div": 6, "neg": 7, "sq": 8, "relu": 9,
        "sigmoid": 10, "tanh": 11, "maxpool2d": 12, "global_avgpool": 13, "flatten": 14, "lstm_gates": 15, "cast": 16,
        "concat": 17, "layout_transform": 18, "dense_grad_x": 19, "dense_grad_w": 20, "conv2d_grad_x": 21, "conv2d_grad_w": 22,
-       "rms_norm_q8": 23, "dense_q8": 24, "linear_scan": 25, "linear_scan_grad": 26, "token_logprobs": 27, "token_logprobs_grad": 28}
+       "rms_norm_q8": 23, "dense_q8": 24, "linear_scan": 25, "linear_scan_grad": 26, "token_logprobs": 27, "token_logprobs_grad": 28,
+       "causal_conv": 29, "causal_conv_grad": 30, "selective_scan": 31, "selective_scan_grad": 32, "dense_logprobs": 33, "dense_logprobs_grad": 34}
 
 STATUS = {0: "ok", -1: "null", -2: "kind", -3: "shape", -4: "type", -5: "group", -6: "binding", -7: "workspace",
           -8: "align", -9: "unsupported", -10: "hip"}
@@ -57,6 +58,10 @@ class rl_attr_layout(ctypes.Structure):
 
 class rl_attr_norm(ctypes.Structure):
     _fields_ = [("eps", ctypes.c_float)]
+
+
+class rl_attr_conv1d(ctypes.Structure):
+    _fields_ = [("silu", c_int32)]
 
 
 class rl_attr_logprobs(ctypes.Structure):
@@ -218,6 +223,8 @@ def _attrs_for(kind: str, attrs: Dict):
         return rl_attr_norm(attrs["eps"]) if "eps" in attrs else None
     if kind == "token_logprobs":
         return rl_attr_logprobs(int(attrs.get("top", 0)))
+    if kind in ("causal_conv", "causal_conv_grad"):
+        return rl_attr_conv1d(int(attrs.get("silu", 0)))
     if kind == "cast":
         return rl_attr_cast(DTYPES.get(attrs.get("to"), -1))
     if kind == "layout_transform":

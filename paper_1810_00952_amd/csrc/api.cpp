@@ -115,7 +115,7 @@ rl_status resolve(const Plan &p, const rl_binding *b, int32_t nb, void *ws, size
     }
     for (const auto &a : p.apart)
         if (ptrs[a.first] == ptrs[a.second]) {
-            msg = "value id " + std::to_string(p.bufs[a.second].bound_value) + ", a scan's last state, may not lie over its first one, value id " +
+            msg = "value id " + std::to_string(p.bufs[a.second].bound_value) + ", a sequence's last state, may not lie over its first one, value id " +
                   std::to_string(p.bufs[a.first].bound_value) + ", here";
             return RL_ERR_BINDING;
         }
@@ -188,7 +188,7 @@ rl_status rl_graph_op(rl_graph *g, int32_t op_kind, const int32_t *in_ids, int32
     return guarded(err, [&]() -> rl_status {
         if (!in_ids || !declared_outs || !out_value_ids) return fail(err, RL_ERR_NULL, "null argument");
         if (op_kind < 0 || op_kind >= RL_OP_KIND_COUNT) return fail(err, RL_ERR_KIND, "unknown operator kind");
-        if (n_in < 0 || n_in > 8 || n_out < 1 || n_out > RL_MAX_RESULTS) return fail(err, RL_ERR_TYPE, "bad operand or result count");
+        if (n_in < 0 || n_in > RL_MAX_OPERANDS || n_out < 1 || n_out > RL_MAX_RESULTS) return fail(err, RL_ERR_TYPE, "bad operand or result count");
         std::string msg;
         OpNode op;
         op.kind = op_kind;

@@ -13,7 +13,8 @@ static const char *kOpNames[RL_OP_KIND_COUNT] = {
     "dense", "conv2d", "bias_add", "add", "sub", "mul", "div", "neg", "sq", "relu", "sigmoid", "tanh",
     "maxpool2d", "global_avgpool", "flatten", "lstm_gates", "cast", "concat", "layout_transform",
     "dense_grad_x", "dense_grad_w", "conv2d_grad_x", "conv2d_grad_w",
-    "rms_norm_q8", "dense_q8", "linear_scan", "linear_scan_grad", "token_logprobs", "token_logprobs_grad"};
+    "rms_norm_q8", "dense_q8", "linear_scan", "linear_scan_grad", "token_logprobs", "token_logprobs_grad",
+    "causal_conv", "causal_conv_grad", "selective_scan", "selective_scan_grad", "dense_logprobs", "dense_logprobs_grad"};
 
 const char *op_name(int kind) { return (kind >= 0 && kind < RL_OP_KIND_COUNT) ? kOpNames[kind] : "?"; }
 bool is_anchor(int kind) { return kind == RL_OP_DENSE || kind == RL_OP_CONV2D; }
@@ -122,6 +123,11 @@ rl_status parse_attrs(int kind, const void *attrs, size_t size, Attrs &a, std::s
         if (attrs) a.top = ((const rl_attr_logprobs *)attrs)->top;
         if (a.top < 0 || a.top > RL_TOP_MAX) { msg = "token_logprobs: top out of range"; return RL_ERR_KIND; }
         break;
+    case RL_OP_CAUSAL_CONV: case RL_OP_CAUSAL_CONV_GRAD:
+        if (!want(sizeof(rl_attr_conv1d))) return RL_ERR_KIND;
+        if (attrs) a.silu = ((const rl_attr_conv1d *)attrs)->silu;
+        if (a.silu != 0 && a.silu != 1) { msg = std::string(op_name(kind)) + ": silu is neither 0 nor 1"; return RL_ERR_KIND; }
+        break;
     default:
         break;
     }
@@ -222,6 +228,68 @@ rl_status infer_type(int kind, const std::vector<rl_type> &in, const Attrs &a, c
             out.push_back(make_type(RL_F32, {M, a.top}));
             out.push_back(make_type(RL_I32, {M, a.top}));
         }
+        return RL_OK;
+    }
+    case RL_OP_CAUSAL_CONV: case RL_OP_CAUSAL_CONV_GRAD: {
+        const bool grad = kind == RL_OP_CAUSAL_CONV_GRAD;
+        const size_t n = grad ? 6 : 4;
+        if (in.size() != n && in.size() != n + 1) { msg = std::string(op_name(kind)) + ": wrong number of arguments"; return RL_ERR_TYPE; }
+        if (!matrix(0) || !matrix(1)) return RL_ERR_TYPE;
+        const rl_type &x = in[0], &w = in[1], &s0 = in[3];
+        const int64_t rows = x.dims[0], D = x.dims[1], K = w.dims[1];
+        if (!is(1, w.dtype == x.dtype ? x.dtype : RL_F32, {D, K}) || !is(2, RL_F32, {D})) return RL_ERR_TYPE;
+        if (K < 2 || K > 8) { msg = std::string(op_name(kind)) + ": taps other than 2 to 8"; return RL_ERR_UNSUPPORTED; }
+        if (s0.rank != 3 || rows % s0.dims[0] != 0) { msg = std::string(op_name(kind)) + ": x must be [B*T,D] for s0 [B,K-1,D]"; return RL_ERR_TYPE; }
+        if (!is(3, x.dtype, {s0.dims[0], K - 1, D})) return RL_ERR_TYPE;
+        if (grad && (!is(4, x.dtype, {rows, D}) || !is(5, x.dtype, {s0.dims[0], K - 1, D}))) return RL_ERR_TYPE;
+        if (in.size() == n + 1 && !is(n, RL_I8, {rows})) return RL_ERR_TYPE;
+        out.push_back(x);
+        if (grad) {
+            out.push_back(make_type(RL_F32, {D, K}));
+            out.push_back(make_type(RL_F32, {D}));
+        }
+        out.push_back(s0);
+        return RL_OK;
+    }
+    case RL_OP_SELECTIVE_SCAN: case RL_OP_SELECTIVE_SCAN_GRAD: {
+        const bool grad = kind == RL_OP_SELECTIVE_SCAN_GRAD;
+        const size_t n = grad ? 8 : 6;
+        if (in.size() < n || in.size() > n + 2) { msg = std::string(op_name(kind)) + ": wrong number of arguments"; return RL_ERR_TYPE; }
+        if (!matrix(0)) return RL_ERR_TYPE;
+        const rl_type &x = in[0], &h0 = in[5];
+        const int64_t rows = x.dims[0], D = x.dims[1];
+        if (h0.rank != 3 || rows % h0.dims[0] != 0) { msg = std::string(op_name(kind)) + ": x must be [B*T,D] for h0 f32 [B,D,N]"; return RL_ERR_TYPE; }
+        const int64_t B = h0.dims[0], N = h0.dims[2];
+        if (!is(1, x.dtype, {rows, D}) || !is(2, x.dtype, {rows, 2 * N}) || !is(3, RL_F32, {D, N}) || !is(4, RL_F32, {D}) || !is(5, RL_F32, {B, D, N})) return RL_ERR_TYPE;
+        if (grad && (!is(6, x.dtype, {rows, D}) || !is(7, RL_F32, {B, D, N}))) return RL_ERR_TYPE;
+        // z is of a float type, keep is not
+        const bool gated = in.size() > n && in[n].dtype != RL_I8, keeps = in.size() > n + (gated ? 1 : 0);
+        if (gated && !is(n, x.dtype, {rows, D})) return RL_ERR_TYPE;
+        if (keeps && !is(in.size() - 1, RL_I8, {rows})) return RL_ERR_TYPE;
+        if (in.size() > n + (gated ? 1 : 0) + (keeps ? 1 : 0)) { msg = std::string(op_name(kind)) + ": wrong number of arguments"; return RL_ERR_TYPE; }
+        if (N > 64) { msg = std::string(op_name(kind)) + ": more than 64 states a channel"; return RL_ERR_UNSUPPORTED; }
+        out.push_back(x);
+        if (grad) {
+            out.push_back(x);
+            out.push_back(in[2]);
+            out.push_back(in[3]);
+            out.push_back(in[4]);
+        }
+        out.push_back(h0);
+        if (grad && gated) out.push_back(x);
+        return RL_OK;
+    }
+    case RL_OP_DENSE_LOGPROBS: case RL_OP_DENSE_LOGPROBS_GRAD: {
+        const bool grad = kind == RL_OP_DENSE_LOGPROBS_GRAD;
+        if (!arity(grad ? 6 : 3) || !matrix(0) || !matrix(1)) return RL_ERR_TYPE;
+        const int64_t M = in[0].dims[0], V = in[1].dims[0];
+        if (!is(1, in[0].dtype, {V, in[0].dims[1]}) || !is(2, RL_I32, {M})) return RL_ERR_TYPE;
+        for (size_t i = 3; i < in.size(); ++i)
+            if (!is(i, RL_F32, {M})) return RL_ERR_TYPE;
+        if (V > 0x7fffffff) { msg = std::string(op_name(kind)) + ": the tokens' base type does not reach the last column"; return RL_ERR_TYPE; }
+        if (grad) { out.push_back(in[0]); out.push_back(in[1]); return RL_OK; }
+        out.push_back(make_type(RL_F32, {M}));
+        out.push_back(make_type(RL_F32, {M}));
         return RL_OK;
     }
     case RL_OP_NEG: case RL_OP_SQ: case RL_OP_RELU: case RL_OP_SIGMOID: case RL_OP_TANH:      // Type-UnaryOp

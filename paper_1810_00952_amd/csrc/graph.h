@@ -28,6 +28,7 @@ struct Attrs {
     int32_t perm[RL_MAX_RANK] = {0, 1, 2, 3, 4, 5};   // layout_transform
     float eps = 1e-5f;                            // rms_norm_q8
     int32_t top = 0;                              // token_logprobs
+    int32_t silu = 0;                             // causal_conv
 };
 
 enum Role { ROLE_INPUT = 0, ROLE_PARAM = 1, ROLE_OP = 2 };

@@ -373,6 +373,48 @@ int64_t logprobs_part_floats(const LogprobsParams &p);
 bool logprobs_fits(const LogprobsParams &p);
 hipError_t launch_logprobs(const LogprobsParams &p, bool forward, bool grad, hipStream_t s);
 
+// ---- a selective state-space language model --------------------------------
+// causal_conv.hip.  keep null: every row a token.  w [D][K] of w_dtype.  part: causal_conv_part_floats of the gradient
+struct CausalConvParams {
+    const void *x, *w, *s0, *dy, *dsT; const float *b; const int8_t *keep;
+    void *y, *sT, *dx, *ds0; float *dw, *db, *part;
+    int64_t B, T, D, K; int32_t dtype, w_dtype, silu;
+};
+bool causal_conv_fits(const CausalConvParams &p);
+int64_t causal_conv_part_floats(const CausalConvParams &p);
+hipError_t launch_causal_conv(const CausalConvParams &p, hipStream_t s);
+hipError_t launch_causal_conv_grad(const CausalConvParams &p, hipStream_t s);
+// dst[j] = sum over i < P of part[i * stride + j], j < J, in a fixed order; turn > 0: element j goes to (j % turn) * across + j / turn
+struct SumShares { const float *part; void *dst; int64_t P, J, stride, turn, across; int32_t dst_dtype; };
+hipError_t launch_sum_shares(const SumShares &q, hipStream_t s);
+// selective_scan.hip.  z null: no gate; keep null: every row a token.  states: the state before every SSM_STATE_ROWS-th row,
+// [B][ceil(T / SSM_STATE_ROWS)][D][N]: the forward pass writes it where it is not null (y and hT may be null then), the gradient reads it.
+// gated, keeps: whether there is a z, a keep (the scratch is sized before the pointers are known)
+struct SelScanParams {
+    const void *x, *dt, *bc, *z, *dy; const float *a, *skip, *h0, *dhT; const int8_t *keep;
+    void *y, *dx, *ddt, *dbc, *dz; float *hT, *da, *dskip, *dh0;
+    float *part, *states;
+    int64_t B, T, D, N; int32_t dtype, gated, keeps;
+};
+constexpr int SSM_STATE_ROWS = 16, SSM_MAX_STATES = 64;
+int64_t sel_scan_part_floats(const SelScanParams &p, bool grad);
+bool sel_scan_fits(const SelScanParams &p, bool grad);
+hipError_t launch_sel_scan(const SelScanParams &p, hipStream_t s);
+hipError_t launch_sel_scan_grad(const SelScanParams &p, hipStream_t s);
+// dense_logprobs.hip: rows of x and w ldx, ldw bytes apart, multiples of 16, the last of the K elements' 16 bytes filled up with zeros.
+// piece_bytes: about how much of dl is there at a time.  part: dense_logprobs_part_bytes
+struct DenseLogprobsParams {
+    const void *x, *w; const int32_t *tok; const float *lse_in, *dlp, *dlse;
+    float *lp, *lse; void *dx, *dw;
+    void *part;
+    int64_t M, V, K, ldx, ldw, piece_bytes; int32_t dtype;
+};
+constexpr int64_t DENSE_LOGPROBS_MAX_ROWS = 1 << 20, DENSE_LOGPROBS_MAX_K = 1 << 20;
+bool dense_logprobs_fits(const DenseLogprobsParams &p, bool grad);
+int64_t dense_logprobs_part_bytes(const DenseLogprobsParams &p, bool grad);
+hipError_t launch_dense_logprobs(const DenseLogprobsParams &p, hipStream_t s);
+hipError_t launch_dense_logprobs_grad(const DenseLogprobsParams &p, hipStream_t s);
+
 // measurement aid (calibrate.hip): a chain of register-operand bf16 MFMAs per wave; out holds grid * 512 floats
 hipError_t launch_mfma_peak(float *out, int32_t grid, int32_t iters, hipStream_t s);
 hipError_t launch_fold_bn(const float *w, const float *gamma, const float *beta, const float *mean, const float *var,

@@ -1164,6 +1164,115 @@ struct Planner {
         return RL_OK;
     }
 
+    // ---- a selective state-space language model ----
+    rl_status plan_causal_conv(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const bool grad = o.kind == RL_OP_CAUSAL_CONV_GRAD;
+        const rl_type &x = T(o.in[0]), &w = T(o.in[1]);
+        Step t;
+        rl_status st = grad ? operands(o, {SL_X, SL_W, SL_E0, SL_CIN, SL_X2, SL_E1, SL_E2}, t.slot) : operands(o, {SL_X, SL_W, SL_E0, SL_CIN, SL_E2}, t.slot);
+        if (st != RL_OK) return st;
+        CausalConvParams p{};
+        p.B = T(o.in[3]).dims[0]; p.T = x.dims[0] / p.B; p.D = x.dims[1]; p.K = w.dims[1]; p.dtype = x.dtype; p.w_dtype = w.dtype; p.silu = o.attrs.silu;
+        if (!causal_conv_fits(p)) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more channels or rows than the kernels reach");
+        if (grad) t.slot[SL_PART] = new_ws((size_t)causal_conv_part_floats(p) * 4);
+        Step &s = grad ? call_step(S_CAUSAL_CONV_GRAD, gi, oi, "causal_conv_grad", t.slot, {SL_Y, SL_O0, SL_O1, SL_COUT})
+                       : call_step(S_CAUSAL_CONV, gi, oi, "causal_conv", t.slot, {SL_Y, SL_COUT});
+        s.cc = p;
+        s.flops = (double)numel(x) * (grad ? 4 * p.K + 14 : 2 * p.K + 6);
+        return RL_OK;
+    }
+
+    rl_status plan_sel_scan(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const bool grad = o.kind == RL_OP_SELECTIVE_SCAN_GRAD;
+        const rl_type &x = T(o.in[0]), &h0 = T(o.in[5]);
+        const size_t fixed = grad ? 8 : 6;
+        const bool gated = o.in.size() > fixed && T(o.in[fixed]).dtype != RL_I8;
+        Step t;
+        rl_status st = grad ? operands(o, {SL_X, SL_X2, SL_W, SL_E0, SL_E1, SL_CIN, SL_I0, SL_I1, gated ? SL_I2 : SL_I3, SL_I3}, t.slot)
+                            : operands(o, {SL_X, SL_X2, SL_W, SL_E0, SL_E1, SL_CIN, gated ? SL_I2 : SL_I3, SL_I3}, t.slot);
+        if (st != RL_OK) return st;
+        SelScanParams p{};
+        p.B = h0.dims[0]; p.D = h0.dims[1]; p.N = h0.dims[2]; p.T = x.dims[0] / p.B; p.dtype = x.dtype; p.gated = gated; p.keeps = t.slot[SL_I3] >= 0;
+        if (!sel_scan_fits(p, grad) || (grad && !sel_scan_fits(p, false))) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more channels or rows than the kernels reach");
+        if (grad) {
+            // the states between come from a selective_scan of the same operands in this plan, or from a step of their own
+            Step *made = nullptr;
+            auto same = [&](const Step &q) {
+                if (q.kind != S_SEL_SCAN) return false;
+                for (int sl : {SL_X, SL_X2, SL_W, SL_E0, SL_CIN, SL_I3})
+                    if (q.slot[sl] != t.slot[sl]) return false;
+                return true;
+            };
+            for (Step &q : plan.steps)
+                if (same(q)) made = &q;
+            if (made && made->slot[SL_OUT4] >= 0) {
+                t.slot[SL_E2] = made->slot[SL_OUT4];
+            } else {
+                t.slot[SL_E2] = new_ws((size_t)(p.B * ((p.T + SSM_STATE_ROWS - 1) / SSM_STATE_ROWS) * p.D * p.N * 4));
+                if (!made) {
+                    const int64_t scratch = sel_scan_part_floats(p, false);
+                    const int part = scratch > 0 ? new_ws((size_t)scratch * 4) : -1;
+                    made = &add_step(S_SEL_SCAN, std::string(op_name(o.kind)) + "#" + std::to_string(oi) + ".states", "selective_scan_states");
+                    made->group = gi;
+                    for (int sl : {SL_X, SL_X2, SL_W, SL_E0, SL_E1, SL_CIN, SL_I2, SL_I3}) made->slot[sl] = t.slot[sl];
+                    made->slot[SL_PART] = part;
+                    made->ss = p;
+                    for (int i = 0; i < 3; ++i) made->bytes += (double)bytes_of(o.in[i]);
+                    made->flops = 7.0 * numel(x) * p.N;
+                }
+                made->slot[SL_OUT4] = t.slot[SL_E2];
+            }
+        }
+        const int64_t scratch = sel_scan_part_floats(p, grad);
+        if (scratch > 0) t.slot[SL_PART] = new_ws((size_t)scratch * 4);
+        Step &s = grad ? call_step(S_SEL_SCAN_GRAD, gi, oi, "selective_scan_grad", t.slot, {SL_Y, SL_O0, SL_O1, SL_O2, SL_O3, SL_COUT, SL_HOUT})
+                       : call_step(S_SEL_SCAN, gi, oi, "selective_scan", t.slot, {SL_Y, SL_COUT});
+        s.ss = p;
+        s.flops = (grad ? 17.0 : 7.0) * numel(x) * p.N;
+        return RL_OK;
+    }
+
+    rl_status plan_dense_logprobs(int gi, int oi)
+    {
+        const OpNode &o = g.ops[oi];
+        const bool grad = o.kind == RL_OP_DENSE_LOGPROBS_GRAD;
+        const rl_type &x = T(o.in[0]), &w = T(o.in[1]);
+        Step t;
+        rl_status st = operands(o, {SL_X, SL_W, SL_E0, SL_E1, SL_E2, SL_E3}, t.slot);
+        if (st != RL_OK) return st;
+        DenseLogprobsParams p{};
+        p.M = x.dims[0]; p.K = x.dims[1]; p.V = w.dims[0]; p.dtype = x.dtype;
+        const int64_t row = p.K * (int64_t)dtype_size(x.dtype);
+        p.ldx = p.ldw = round_up(row, 16);
+        p.piece_bytes = plan.lean ? 1 << 20 : 128 << 20;
+        if (!dense_logprobs_fits(p, grad)) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows or columns than the kernels reach");
+        if (grad) plan.spent = true;
+        if (row != p.ldx) {                       // rows that start on 16 bytes, made once for the calls of a plan that want them
+            auto padded = [&](int src, int64_t rows) {
+                for (const Step &q : plan.steps)
+                    if (q.kind == S_PAD_BYTES && q.slot[SL_X] == src && q.pb.R == rows && q.pb.K == row && q.pb.Kp == p.ldx) return q.slot[SL_Y];
+                const int dst = new_ws((size_t)(rows * p.ldx));
+                Step &c = add_step(S_PAD_BYTES, std::string(op_name(o.kind)) + "#" + std::to_string(oi) + ".rows", "pad_bytes");
+                c.group = gi;
+                c.pb = {rows, row, p.ldx};
+                c.slot[SL_X] = src; c.slot[SL_Y] = dst;
+                c.bytes = (double)rows * (row + p.ldx);
+                return dst;
+            };
+            t.slot[SL_X] = padded(t.slot[SL_X], p.M);
+            t.slot[SL_W] = padded(t.slot[SL_W], p.V);
+        }
+        t.slot[SL_PART] = new_ws((size_t)dense_logprobs_part_bytes(p, grad));
+        Step &s = call_step(grad ? S_DENSE_LOGPROBS_GRAD : S_DENSE_LOGPROBS, gi, oi, grad ? "dense_logprobs_grad" : "dense_logprobs", t.slot, {SL_Y, SL_COUT});
+        s.dl = p;
+        s.flops = (grad ? 6.0 : 2.0) * p.M * p.V * p.K;
+        return RL_OK;
+    }
+
     // ---- partial derivatives of the contractions --------------------------------
     // Each is again a contraction C[m, n] = sum_k A[m, k] Wp[n, k] once its operands are looked at the right way round:
     //   dense_grad_x   m = batch row,       n = input feature k',  k = output feature:   A = dy,            Wp[k'][n] = W[n][k']
@@ -1599,6 +1708,9 @@ struct Planner {
             if (k0 == RL_OP_DENSE_Q8) return plan_dense_q8(gi, ops[0]);
             if (k0 == RL_OP_LINEAR_SCAN || k0 == RL_OP_LINEAR_SCAN_GRAD) return plan_scan(gi, ops[0]);
             if (k0 == RL_OP_TOKEN_LOGPROBS || k0 == RL_OP_TOKEN_LOGPROBS_GRAD) return plan_logprobs(gi, ops[0]);
+            if (k0 == RL_OP_CAUSAL_CONV || k0 == RL_OP_CAUSAL_CONV_GRAD) return plan_causal_conv(gi, ops[0]);
+            if (k0 == RL_OP_SELECTIVE_SCAN || k0 == RL_OP_SELECTIVE_SCAN_GRAD) return plan_sel_scan(gi, ops[0]);
+            if (k0 == RL_OP_DENSE_LOGPROBS || k0 == RL_OP_DENSE_LOGPROBS_GRAD) return plan_dense_logprobs(gi, ops[0]);
             if (k0 == RL_OP_CONCAT) return fail(RL_ERR_UNSUPPORTED, "concat is only implemented as the operand of a dense in its group");
         }
         return plan_eltwise(gi, ops);
@@ -2128,14 +2240,15 @@ struct Planner {
             placed.push_back(b);
         }
         plan.workspace_bytes = total;
-        // a scan's new state may lie over its old one only if it has one token a sequence (else workgroups read h0 beside the one that writes hT)
+        // a sequence's new state may lie over its old one only if it is of one token (else workgroups read h0 beside the one that writes hT)
         // and nothing behind it reads the old one
         for (size_t si = 0; si < plan.steps.size(); ++si) {
             const Step &s = plan.steps[si];
-            if (s.kind != S_SCAN || s.slot[SL_COUT] < 0) continue;
+            if ((s.kind != S_SCAN && s.kind != S_CAUSAL_CONV && s.kind != S_SEL_SCAN) || s.slot[SL_COUT] < 0) continue;
+            const int64_t T = s.kind == S_SCAN ? s.sc.T : s.kind == S_CAUSAL_CONV ? s.cc.T : s.ss.T;
             const BufDesc &h0 = plan.bufs[s.slot[SL_CIN]], &hT = plan.bufs[s.slot[SL_COUT]];
             if (h0.bound_value < 0 || hT.bound_value < 0) continue;
-            if (s.sc.T > 1 || h0.last > (int)si || g.values[h0.bound_value].role != ROLE_INPUT) plan.apart.push_back({s.slot[SL_CIN], s.slot[SL_COUT]});
+            if (T > 1 || h0.last > (int)si || g.values[h0.bound_value].role != ROLE_INPUT) plan.apart.push_back({s.slot[SL_CIN], s.slot[SL_COUT]});
         }
     }
 };
@@ -2370,6 +2483,47 @@ rl_status run_steps(const Plan &plan, void *const *ptrs, hipStream_t stream, std
                 p.dlp = (const float *)P(t, SL_E0); p.dent = (const float *)P(t, SL_E1); p.dx = P(t, SL_Y);
             }
             er = launch_logprobs(p, forward, p.dx != nullptr, stream);
+            break;
+        }
+        case S_CAUSAL_CONV: case S_CAUSAL_CONV_GRAD: {
+            CausalConvParams p = s.cc;
+            p.x = P(s, SL_X); p.w = P(s, SL_W); p.b = (const float *)P(s, SL_E0); p.s0 = P(s, SL_CIN); p.keep = (const int8_t *)P(s, SL_E2);
+            if (s.kind == S_CAUSAL_CONV) {
+                p.y = P(s, SL_Y); p.sT = P(s, SL_COUT);
+                er = launch_causal_conv(p, stream);
+            } else {
+                p.dy = P(s, SL_X2); p.dsT = P(s, SL_E1); p.part = (float *)P(s, SL_PART);
+                p.dx = P(s, SL_Y); p.dw = (float *)P(s, SL_O0); p.db = (float *)P(s, SL_O1); p.ds0 = P(s, SL_COUT);
+                er = launch_causal_conv_grad(p, stream);
+            }
+            break;
+        }
+        case S_SEL_SCAN: case S_SEL_SCAN_GRAD: {
+            SelScanParams p = s.ss;
+            p.x = P(s, SL_X); p.dt = P(s, SL_X2); p.bc = P(s, SL_W); p.a = (const float *)P(s, SL_E0); p.skip = (const float *)P(s, SL_E1);
+            p.h0 = (const float *)P(s, SL_CIN); p.z = P(s, SL_I2); p.keep = (const int8_t *)P(s, SL_I3); p.part = (float *)P(s, SL_PART);
+            if (s.kind == S_SEL_SCAN) {
+                p.y = P(s, SL_Y); p.hT = (float *)P(s, SL_COUT); p.states = (float *)P(s, SL_OUT4);
+                er = launch_sel_scan(p, stream);
+            } else {
+                p.dy = P(s, SL_I0); p.dhT = (const float *)P(s, SL_I1); p.states = (float *)P(s, SL_E2);
+                p.dx = P(s, SL_Y); p.ddt = P(s, SL_O0); p.dbc = P(s, SL_O1); p.da = (float *)P(s, SL_O2); p.dskip = (float *)P(s, SL_O3);
+                p.dh0 = (float *)P(s, SL_COUT); p.dz = P(s, SL_HOUT);
+                er = launch_sel_scan_grad(p, stream);
+            }
+            break;
+        }
+        case S_DENSE_LOGPROBS: case S_DENSE_LOGPROBS_GRAD: {
+            DenseLogprobsParams p = s.dl;
+            p.x = P(s, SL_X); p.w = P(s, SL_W); p.tok = (const int32_t *)P(s, SL_E0); p.part = P(s, SL_PART);
+            if (s.kind == S_DENSE_LOGPROBS) {
+                p.lp = (float *)P(s, SL_Y); p.lse = (float *)P(s, SL_COUT);
+                er = launch_dense_logprobs(p, stream);
+            } else {
+                p.lse_in = (const float *)P(s, SL_E1); p.dlp = (const float *)P(s, SL_E2); p.dlse = (const float *)P(s, SL_E3);
+                p.dx = P(s, SL_Y); p.dw = P(s, SL_COUT);
+                er = launch_dense_logprobs_grad(p, stream);
+            }
             break;
         }
         case S_PACK:

@@ -12,8 +12,9 @@
 namespace rl {
 
 enum StepKind { S_IGEMM = 0, S_ELTWISE, S_GATES, S_MAXPOOL, S_GAVG, S_TO_NHWC, S_TO_NCHW, S_STEM_PAD, S_STEM_POOL, S_PERMUTE, S_PACK, S_WGRAD, S_WGRAD_REDUCE, S_DILATE, S_TN, S_PAD_NHWC, S_PAD_BYTES,
-                S_NORM_Q8, S_DENSE_Q8, S_SCAN, S_SCAN_GRAD, S_LOGPROBS, S_LOGPROBS_GRAD };
-enum Slot { SL_X = 0, SL_X2, SL_W, SL_Y, SL_E0, SL_E1, SL_E2, SL_E3, SL_E4, SL_E5, SL_CIN, SL_COUT, SL_HOUT, SL_PART, SL_OUT4, SL_COUNT };
+                S_NORM_Q8, S_DENSE_Q8, S_SCAN, S_SCAN_GRAD, S_LOGPROBS, S_LOGPROBS_GRAD,
+                S_CAUSAL_CONV, S_CAUSAL_CONV_GRAD, S_SEL_SCAN, S_SEL_SCAN_GRAD, S_DENSE_LOGPROBS, S_DENSE_LOGPROBS_GRAD };
+enum Slot { SL_X = 0, SL_X2, SL_W, SL_Y, SL_E0, SL_E1, SL_E2, SL_E3, SL_E4, SL_E5, SL_CIN, SL_COUT, SL_HOUT, SL_PART, SL_OUT4, SL_I0, SL_I1, SL_I2, SL_I3, SL_I4, SL_I5, SL_O0, SL_O1, SL_O2, SL_O3, SL_COUNT };
 
 struct BufDesc {
     int bound_value = -1;     // >= 0: caller-bound pointer of that value id; -1: workspace
@@ -38,6 +39,7 @@ struct Step {
     GatherPack gp{};                    // S_PACK: an activation gathered into the K-contiguous rows a contraction reads
     PadBytes pb{};                      // S_PAD_BYTES
     NormQ8Params nq{}; DenseQ8Params dq{}; ScanParams sc{}; LogprobsParams lg{};
+    CausalConvParams cc{}; SelScanParams ss{}; DenseLogprobsParams dl{};
     int t_dtype = 0, t_N = 0, t_C = 0, t_P = 0;
     int st_H = 0, st_W = 0, st_Hp = 0, st_Wp = 0, st_ph = 0, st_pw = 0;   // S_STEM_PAD geometry (t_N, t_C: batch, channels)
     int stem = 0;                       // S_IGEMM: the few-channel stem form (padded 4-channel frame, regrouped taps)
@@ -78,7 +80,7 @@ struct Plan {
     std::vector<int> outputs;
     std::vector<BufDesc> bufs;
     std::vector<Step> steps;
-    std::vector<std::pair<int, int>> apart;   // a scan's h0 and hT, bound both, that may not be one memory: buffer indices
+    std::vector<std::pair<int, int>> apart;   // a sequence's first and last state (h0 and hT, s0 and sT), bound both, that may not be one memory: buffer indices
     std::vector<int> bound_buf;          // value id -> buffer index of its bound pointer, or -1
     std::map<int, PackSpec> packs;       // param value id -> packing
     size_t workspace_bytes = 0;
