@@ -387,8 +387,8 @@ hipError_t launch_causal_conv_grad(const CausalConvParams &p, hipStream_t s);
 // dst[j] = sum over i < P of part[i * stride + j], j < J, in a fixed order; turn > 0: element j goes to (j % turn) * across + j / turn
 struct SumShares { const float *part; void *dst; int64_t P, J, stride, turn, across; int32_t dst_dtype; };
 hipError_t launch_sum_shares(const SumShares &q, hipStream_t s);
-// selective_scan.hip.  z null: no gate; keep null: every row a token.  states: the state before every SSM_STATE_ROWS-th row,
-// [B][ceil(T / SSM_STATE_ROWS)][D][N]: the forward pass writes it where it is not null (y and hT may be null then), the gradient reads it.
+// selective_scan.hip.  z null: no gate; keep null: every row a token.  states: the state before every sel_scan_state_rows-th row,
+// [B][ceil(T / sel_scan_state_rows)][D][N]: the forward pass writes it where it is not null (y and hT may be null then), the gradient reads it.
 // gated, keeps: whether there is a z, a keep (the scratch is sized before the pointers are known)
 struct SelScanParams {
     const void *x, *dt, *bc, *z, *dy; const float *a, *skip, *h0, *dhT; const int8_t *keep;
@@ -396,7 +396,8 @@ struct SelScanParams {
     float *part, *states;
     int64_t B, T, D, N; int32_t dtype, gated, keeps;
 };
-constexpr int SSM_STATE_ROWS = 16, SSM_MAX_STATES = 64;
+constexpr int SSM_MAX_STATES = 64;
+int64_t sel_scan_state_rows(const SelScanParams &p);
 int64_t sel_scan_part_floats(const SelScanParams &p, bool grad);
 bool sel_scan_fits(const SelScanParams &p, bool grad);
 hipError_t launch_sel_scan(const SelScanParams &p, hipStream_t s);

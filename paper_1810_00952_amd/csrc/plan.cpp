@@ -1212,7 +1212,8 @@ struct Planner {
             if (made && made->slot[SL_OUT4] >= 0) {
                 t.slot[SL_E2] = made->slot[SL_OUT4];
             } else {
-                t.slot[SL_E2] = new_ws((size_t)(p.B * ((p.T + SSM_STATE_ROWS - 1) / SSM_STATE_ROWS) * p.D * p.N * 4));
+                const int64_t every = sel_scan_state_rows(p);
+                t.slot[SL_E2] = new_ws((size_t)(p.B * ((p.T + every - 1) / every) * p.D * p.N * 4));
                 if (!made) {
                     const int64_t scratch = sel_scan_part_floats(p, false);
                     const int part = scratch > 0 ? new_ws((size_t)scratch * 4) : -1;

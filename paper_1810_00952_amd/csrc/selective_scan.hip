@@ -6,20 +6,27 @@
 //   dB[t,n] = sum_d G s x,  dC[t,n] = sum_d du h,  dx = skip du + s sum_n G B,  da = sum_t G h_(t-1) exp(s a) s,
 //   ds = sum_n G (h_(t-1) exp(s a) a + x B),  ddt = ds sigmoid(dt).
 //
-// Four states of a channel are a lane's, L lanes a channel's (N <= 4 L), 256 / L channels a workgroup's, which walks the rows by tiles: what a
-// channel needs once a token (softplus, the gate, products) is found by a thread a token and channel, and meets the states in LDS.  A row that is
+// A channel is four lanes', R of its states each (N <= 4 R), a wave sixteen channels', a workgroup of four waves sixty-four channels', which it walks by
+// tiles of rows.  Of every four rows each of a channel's lanes finds what the channel needs once a token (softplus, the gate, products) for one and passes
+// it to the other three as it is used, a lane move within the instruction that reads it; the sums over states go the other way, so that each
+// lane ends with one row's.  B and C meet the lanes in LDS.  The sums over channels (dB, dC) halve the values a lane has with every step, by exchanges of the
+// wave's halves and rows; the waves' meet in LDS, the workgroups' in memory, where another launch adds them up in a fixed order.  A row that is
 // padding has s = s x = B = C = du = 0 and leaves state and derivative as they are.  Few channels: the rows are cut into chunks, a workgroup
 // each; a launch ahead finds what each chunk makes of the state before it (P h + H; the derivative alike), P = exp(a sum s), and the workgroups
 // add up the chunks before theirs.
+#include <type_traits>
+
 #include "igemm_lds.h"
 
 namespace rl {
 
 namespace {
 
-constexpr int R = 4;                          // states of a lane
-constexpr int ROWS = SSM_STATE_ROWS;          // rows of a tile
+constexpr int LANES = 4, CHANNELS = 64;       // lanes of a channel, channels of a workgroup
 constexpr float LOG2E = 1.4426950408889634f;
+
+// Rows of a tile: of the gradient as many as its states and gates fit the registers
+constexpr int rows_of(int R) { return R <= 4 ? 16 : 64 / R; }
 
 // Chunks' P of which a document's first row is part: -0, which no product of gates is
 constexpr float FIRST = -0.0f;
@@ -46,103 +53,204 @@ __device__ __forceinline__ float softplus(float v)
     return v > 20.0f ? v : small;
 }
 
-template <typename E> __device__ __forceinline__ float at(const void *p, int64_t i)
+template <typename E> struct Bits;
+template <> struct Bits<float> { typedef uint32_t raw; };
+template <> struct Bits<uint16_t> { typedef uint16_t raw; };
+template <typename E> __device__ __forceinline__ float number(typename Bits<E>::raw r)
 {
-    if constexpr (sizeof(E) == 4) return ((const float *)p)[i];
-    else return bf16_bits_to_f32(((const uint16_t *)p)[i]);
+    if constexpr (sizeof(E) == 4) return __uint_as_float(r);
+    else return bf16_bits_to_f32(r);
 }
+template <typename E> __device__ __forceinline__ float at(const void *p, int64_t i) { return number<E>(((const typename Bits<E>::raw *)p)[i]); }
 template <typename E> __device__ __forceinline__ void put(void *p, int64_t i, float v)
 {
     if constexpr (sizeof(E) == 4) ((float *)p)[i] = v;
     else ((uint16_t *)p)[i] = (uint16_t)pack_bf16x2(v, v);
 }
 
-// sum over a channel's lanes, in all of them
-template <int L> __device__ __forceinline__ float over_states(float v)
+template <int CTRL> __device__ __forceinline__ float moved(float v)
 {
-#pragma unroll
-    for (int k = 1; k < L; k <<= 1) v += __shfl_xor(v, k);
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+#else
     return v;
+#endif
 }
-// sum over a wave's channels, in all lanes
-template <int L> __device__ __forceinline__ float over_channels(float v)
+// lane k's of the channel's four
+template <int K> __device__ __forceinline__ float of_lane(float v) { return moved<K * 0x55>(v); }
+// four numbers of every lane summed over the channel's lanes: lane l gets the sum of number l
+__device__ __forceinline__ float over_states(const float (&v)[4])
 {
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    const float a = (odd ? v[1] : v[0]) + moved<0xb1>(odd ? v[0] : v[1]), b = (odd ? v[3] : v[2]) + moved<0xb1>(odd ? v[2] : v[3]);
+    return (high ? b : a) + moved<0x4e>(high ? a : b);
+}
+// a in the lower half, b in the upper half of the wave (ROWS: in even and odd rows of sixteen lanes), each summed over both
+template <bool ROWS> __device__ __forceinline__ float halves(float a, float b)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto r = ROWS ? __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false)
+                        : __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+#else
+    return a + b;
+#endif
+}
+// R numbers each of dB and dC summed over a wave's channels.  Number r of B (C) and of a channel's lane l is at i = r / 4, in lane
+// slot_of(which, r, l); lanes with bit 2 hold nothing of use.
+constexpr int sums_of(int R) { return R > 4 ? R / 4 : 1; }
+__device__ __forceinline__ int slot_of(int which, int r, int l) { return which * 32 + (r & 1) * 16 + (r >> 1 & 1) * 8 + l; }
+template <int R> __device__ __forceinline__ void over_channels(const float (&db)[R], const float (&dc)[R], float (&out)[sums_of(R)])
+{
+    float w[R], u[R > 1 ? R / 2 : 1];
 #pragma unroll
-    for (int k = L; k < 64; k <<= 1) v += __shfl_xor(v, k);
-    return v;
+    for (int r = 0; r < R; ++r) w[r] = halves<false>(db[r], dc[r]);
+#pragma unroll
+    for (int r = 0; r < (R > 1 ? R / 2 : 1); ++r) u[r] = halves<true>(w[2 * r < R ? 2 * r : 0], w[2 * r + 1 < R ? 2 * r + 1 : 0]);
+    const bool high = threadIdx.x & 8;
+#pragma unroll
+    for (int i = 0; i < sums_of(R); ++i) {
+        float v;
+        if constexpr (R >= 4) v = (high ? u[2 * i + 1] : u[2 * i]) + moved<0x128>(high ? u[2 * i] : u[2 * i + 1]);      // row_ror 8
+        else v = u[0] + moved<0x128>(u[0]);
+        out[i] = v + moved<0x104>(v);                                                                             // row_shl 4
+    }
 }
 
 // what a lane works on
-template <int L>
+template <int R>
 struct Place {
-    static constexpr int CH = 256 / L;        // channels of a workgroup
-    static constexpr int EACH = ROWS / L;     // rows a thread does the token-and-channel work of (every 256 / CH-th)
-    int l, c, pc, pr;                         // the states' lane: its states l R .., channel c; the channel and first row of the work a token
-    int64_t b, d, pd;                         // ... their numbers in the sequence's rows
+    int l;                                    // its states l R ..; of every four rows the l-th
+    int64_t b, d;
     int32_t chunk, slab;
-    bool live, plive;
+    bool live;
     __device__ __forceinline__ Place(const SelScanParams &p, int32_t slabs)
     {
-        l = threadIdx.x % L; c = threadIdx.x / L;
-        pc = threadIdx.x % CH; pr = threadIdx.x / CH;
+        l = threadIdx.x & 3;
         const uint32_t rest = blockIdx.x / (uint32_t)slabs;
         slab = (int32_t)(blockIdx.x - rest * slabs);
         chunk = (int32_t)(rest / (uint32_t)p.B);
         b = rest - (uint32_t)chunk * (uint32_t)p.B;
-        d = (int64_t)slab * CH + c; pd = (int64_t)slab * CH + pc;
-        live = d < p.D; plive = pd < p.D;
+        d = (int64_t)slab * CHANNELS + (threadIdx.x >> 2);
+        live = d < p.D;
         if (!live) d = 0;                     // some other channel's, of which nothing is stored
-        if (!plive) pd = 0;
     }
-    // R numbers of a [D][N] matrix (rest for the states behind N)
-    __device__ __forceinline__ void load(const SelScanParams &p, const float *m, float (&v)[R], float rest = 0.0f) const
+    // R numbers of a [D][N] matrix, zeros for the states behind N
+    __device__ __forceinline__ void load(const SelScanParams &p, const float *m, float (&v)[R]) const
     {
+        const float *q = m + d * p.N + l * R;
+        if (R % 4 == 0 && p.N == LANES * R) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) v[r] = l * R + r < p.N ? m[d * p.N + l * R + r] : rest;
+            for (int r = 0; r < R; r += 4) {
+                const f32x4 t = *(const f32x4 *)(q + (r < R ? r : 0));
+#pragma unroll
+                for (int k = 0; k < 4 && k < R; ++k) v[r + k < R ? r + k : 0] = t[k];
+            }
+            return;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) v[r] = l * R + r < p.N ? q[r] : 0.0f;
     }
     __device__ __forceinline__ void store(const SelScanParams &p, float *m, const float (&v)[R]) const
     {
         if (!live) return;
+        float *q = m + d * p.N + l * R;
+        if (R % 4 == 0 && p.N == LANES * R) {
+#pragma unroll
+            for (int r = 0; r + 3 < R; r += 4) *(f32x4 *)(q + r) = f32x4{v[r], v[r + 1 < R ? r + 1 : r], v[r + 2 < R ? r + 2 : r], v[r + 3 < R ? r + 3 : r]};
+            return;
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (l * R + r < p.N) m[d * p.N + l * R + r] = v[r];
+            if (l * R + r < p.N) q[r] = v[r];
     }
 };
 
 // rows of a tile that are tokens, that are a document's first
-template <bool KEEP> __device__ __forceinline__ void flags_of(const SelScanParams &p, int64_t b, int64_t t0, uint32_t &tok, uint32_t &first)
+template <bool KEEP, int ROWS> __device__ __forceinline__ void flags_of(const SelScanParams &p, int64_t b, int64_t t0, uint32_t &tok, uint32_t &first)
 {
+    const int64_t left = p.T - t0;
+    if (!KEEP) {
+        tok = left >= ROWS ? ~0u : (1u << (left > 0 ? left : 0)) - 1u;
+        first = 0;
+        return;
+    }
     const int i = threadIdx.x & 63;
-    const bool in = i < ROWS && t0 + i < p.T;
-    const int k = !in ? 0 : KEEP ? p.keep[b * p.T + t0 + i] : 1;
+    const int k = i < ROWS && i < left ? p.keep[b * p.T + t0 + i] : 0;
     tok = (uint32_t)__ballot(k != 0);
-    first = KEEP ? (uint32_t)__ballot(k == 2) : 0;
+    first = (uint32_t)__ballot(k == 2);
 }
 
-// B and C of a tile's rows, zeros behind N and of padding
-template <typename E, int L> __device__ __forceinline__ void stage_bc(const SelScanParams &p, int64_t row0, uint32_t tok, float (&sb)[2][ROWS][4 * L])
+// B and C of a tile's rows on their way to LDS: a thread's share, zeros behind N and of padding
+template <typename E, int R, int ROWS> struct Stage {
+    static constexpr int WIDE = LANES * R, EACH = (2 * ROWS * WIDE + 255) / 256;
+    typename Bits<E>::raw r[EACH];
+    __device__ __forceinline__ void request(const SelScanParams &p, int64_t b, int64_t t0)
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int i = e * 256 + (int)threadIdx.x, n = i % WIDE, which = i / WIDE % 2, t = i / (2 * WIDE);
+            r[e] = 0;
+            if (t < ROWS && n < p.N && t0 + t < p.T && t0 >= 0) r[e] = ((const typename Bits<E>::raw *)p.bc)[(b * p.T + t0 + t) * 2 * p.N + which * p.N + n];
+        }
+    }
+    __device__ __forceinline__ void put(float (&s)[ROWS][2][WIDE], uint32_t tok) const
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int i = e * 256 + (int)threadIdx.x, t = i / (2 * WIDE);
+            if (t < ROWS) (&s[0][0][0])[i] = tok >> t & 1 ? number<E>(r[e]) : 0.0f;
+        }
+    }
+};
+
+// a row's R numbers of B or C
+template <int R> __device__ __forceinline__ void from_lds(const float *s, float (&v)[R])
 {
-    for (int i = threadIdx.x; i < ROWS * 8 * L; i += 256) {
-        const int n = i % (4 * L), t = i / (4 * L) % ROWS, which = i / (4 * L * ROWS);
-        sb[which][t][n] = (tok >> t & 1) && n < p.N ? at<E>(p.bc, (row0 + t) * 2 * p.N + which * p.N + n) : 0.0f;
+    if constexpr (R >= 4) {
+#pragma unroll
+        for (int r = 0; r < R; r += 4) {
+            const f32x4 t = *(const f32x4 *)(s + r);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[r + k] = t[k];
+        }
+    } else if constexpr (R == 2) {
+        const f32x2 t = *(const f32x2 *)s;
+        v[0] = t[0]; v[1] = t[1];
+    } else {
+        v[0] = s[0];
     }
 }
+
+// a lane's rows of a tile: the l-th of every four
+template <typename E, int ROWS> struct Column {
+    typename Bits<E>::raw r[ROWS / 4];
+    __device__ __forceinline__ void request(const SelScanParams &p, const void *x, int64_t row0, int64_t rows, int64_t d, int l)
+    {
+#pragma unroll
+        for (int i = 0; i < ROWS / 4; ++i) {
+            int64_t t = 4 * i + l;
+            t = t < rows ? t : rows - 1;
+            r[i] = ((const typename Bits<E>::raw *)x)[(row0 + t) * p.D + d];
+        }
+    }
+};
 
 }  // namespace
 
 // ---------------------------------------------------------------------------
 // one token a sequence
 // ---------------------------------------------------------------------------
-template <typename E, int L>
+template <typename E, int R>
 __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanParams p, int64_t channels)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
-    const int l = threadIdx.x % L;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    const int l = threadIdx.x % LANES;
     const bool live = i < channels;
     const int64_t c = live ? i : 0, b = c / p.D, d = c - b * p.D;
     const int keep = p.keep ? p.keep[b] : 1;
     const float x = keep ? at<E>(p.x, c) : 0.0f, s = keep ? softplus(at<E>(p.dt, c)) : 0.0f, v = s * x;
-    float sum = 0.0f;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int n = l * R + r;
@@ -151,11 +259,11 @@ __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanP
         const float u = keep ? v * at<E>(p.bc, b * 2 * p.N + n) : 0.0f;
         const float h = keep == 2 ? u : keep ? __builtin_fmaf(e, h0, u) : h0;
         if (live) p.hT[c * p.N + n] = h;
-        sum = __builtin_fmaf(keep ? at<E>(p.bc, (b * 2 + 1) * p.N + n) : 0.0f, h, sum);
+        sum[0] = __builtin_fmaf(keep ? at<E>(p.bc, (b * 2 + 1) * p.N + n) : 0.0f, h, sum[0]);
     }
-    sum = over_states<L>(sum);
+    const float all = over_states(sum);
     if (l == 0 && live) {
-        float y = __builtin_fmaf(p.skip[d], x, sum);
+        float y = __builtin_fmaf(p.skip[d], x, all);
         if (p.z) { const float z = at<E>(p.z, c); y *= z * sigmoidf_(z); }
         put<E>(p.y, c, keep ? y : 0.0f);
     }
@@ -164,16 +272,14 @@ __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanP
 // ---------------------------------------------------------------------------
 // forward.  AHEAD: what a chunk makes of the state before it, into part ([chunk][b] P, H of [D][N])
 // ---------------------------------------------------------------------------
-template <typename E, int L, bool KEEP, bool AHEAD>
+template <typename E, int R, bool KEEP, bool AHEAD>
 __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles)
 {
-    typedef Place<L> P;
-    constexpr int CH = P::CH, EACH = P::EACH;
-    const P at_(p, slabs);
+    constexpr int ROWS = rows_of(R);
+    const Place<R> at_(p, slabs);
     const int64_t DN = p.D * p.N;
-    __shared__ float2 sd[ROWS][CH];                                  // s, s x
-    __shared__ __attribute__((aligned(16))) float sb[2][ROWS][4 * L];
-    __shared__ float sy[ROWS][CH];
+    const int l = at_.l;
+    __shared__ __attribute__((aligned(16))) float sb[2][ROWS][2][LANES * R];
     float a2[R], h[R], total = 0.0f;
     at_.load(p, p.a, a2);
 #pragma unroll
@@ -189,59 +295,85 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
             for (int r = 0; r < R; ++r) h[r] = through(f[r], h[r], H[r]);
         }
     }
-    const float skip = p.skip[at_.pd];
+    const float skip = p.skip[at_.d];
     const int64_t tiles = (p.T + ROWS - 1) / ROWS;
     const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, end_tile = min(first_tile + chunk_tiles, tiles);
+    Column<E, ROWS> qx, qt, qz;
+    Stage<E, R, ROWS> bc;
+    uint32_t tok, first, next_tok = 0, next_first = 0;
+    auto request = [&](int64_t tile) {
+        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
+        qx.request(p, p.x, row0, p.T - t0, at_.d, l);
+        qt.request(p, p.dt, row0, p.T - t0, at_.d, l);
+        if (!AHEAD && p.z) qz.request(p, p.z, row0, p.T - t0, at_.d, l);
+    };
+    request(first_tile);
+    flags_of<KEEP, ROWS>(p, at_.b, first_tile * ROWS, tok, first);
+    bc.request(p, at_.b, first_tile * ROWS);
+    bc.put(sb[first_tile & 1], tok);
+    __syncthreads();
     for (int64_t tile = first_tile; tile < end_tile; ++tile) {
         const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
-        uint32_t tok, first;
-        flags_of<KEEP>(p, at_.b, t0, tok, first);
-        float x[EACH];
+        float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int t = at_.pr + e * L;
-            const bool here = tok >> t & 1;
-            x[e] = here ? at<E>(p.x, (row0 + t) * p.D + at_.pd) : 0.0f;
-            const float s = here ? softplus(at<E>(p.dt, (row0 + t) * p.D + at_.pd)) : 0.0f;
-            sd[t][at_.pc] = float2{s, s * x[e]};
+        for (int i = 0; i < ROWS / 4; ++i) {
+            const bool here = tok >> (4 * i + l) & 1;
+            x[i] = here ? number<E>(qx.r[i]) : 0.0f;
+            s[i] = here ? softplus(number<E>(qt.r[i])) : 0.0f;
+            z[i] = !AHEAD && p.z ? number<E>(qz.r[i]) : 0.0f;
         }
-        stage_bc<E, L>(p, row0, tok, sb);
-        __syncthreads();
+        const bool more = tile + 1 < end_tile;
+        if (more) {
+            request(tile + 1);
+            bc.request(p, at_.b, t0 + ROWS);
+            flags_of<KEEP, ROWS>(p, at_.b, t0 + ROWS, next_tok, next_first);
+        }
         if (p.states && !AHEAD) at_.store(p, p.states + (at_.b * tiles + tile) * DN, h);
+        const float (*const sbt)[2][LANES * R] = sb[tile & 1];
 #pragma unroll
-        for (int t = 0; t < ROWS; ++t) {
-            const float2 sv = sd[t][at_.c];
-            if (KEEP && (first >> t & 1)) {
-                began = true;
+        for (int i = 0; i < ROWS / 4; ++i) {
+            float sum[4];
+            const float v = s[i] * x[i];
+            if (AHEAD) total += s[i];
+            auto row = [&](auto lane) {
+                constexpr int K = decltype(lane)::value;
+                const int t = 4 * i + K;
+                float B[R], C[R];
+                from_lds<R>(&sbt[t][0][l * R], B);
+                if (!AHEAD) from_lds<R>(&sbt[t][1][l * R], C);
+                if (KEEP && (first >> t & 1)) {
+                    began = true;
 #pragma unroll
-                for (int r = 0; r < R; ++r) h[r] = 0.0f;
-            }
-            if (AHEAD) total += sv.x;
-            float sum = 0.0f;
+                    for (int r = 0; r < R; ++r) h[r] = 0.0f;
+                }
+                sum[K] = 0.0f;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                h[r] = __builtin_fmaf(exp2_(sv.x * a2[r]), h[r], sv.y * sb[0][t][at_.l * R + r]);
-                if (!AHEAD) sum = __builtin_fmaf(sb[1][t][at_.l * R + r], h[r], sum);
-            }
+                for (int r = 0; r < R; ++r) {
+                    h[r] = __builtin_fmaf(exp2_(of_lane<K>(s[i]) * a2[r]), h[r], of_lane<K>(v) * B[r]);
+                    if (!AHEAD) sum[K] = __builtin_fmaf(C[r], h[r], sum[K]);
+                }
+            };
+            row(std::integral_constant<int, 0>{});
+            row(std::integral_constant<int, 1>{});
+            row(std::integral_constant<int, 2>{});
+            row(std::integral_constant<int, 3>{});
             if (!AHEAD) {
-                sum = over_states<L>(sum);
-                if (at_.l == 0) sy[t][at_.c] = sum;
+                float y = __builtin_fmaf(skip, x[i], over_states(sum));
+                const int t = 4 * i + l;
+                if (p.z) y *= z[i] * sigmoidf_(z[i]);
+                if (p.y && at_.live && t0 + t < p.T) put<E>(p.y, (row0 + t) * p.D + at_.d, tok >> t & 1 ? y : 0.0f);
             }
+        }
+        if (more) {
+            bc.put(sb[(tile + 1) & 1], next_tok);
+            tok = next_tok;
+            first = next_first;
         }
         __syncthreads();
-        if (!AHEAD && p.y) {
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int t = at_.pr + e * L;
-                if (t0 + t >= p.T || !at_.plive) continue;
-                const int64_t i = (row0 + t) * p.D + at_.pd;
-                float y = __builtin_fmaf(skip, x[e], sy[t][at_.pc]);
-                if (p.z) { const float z = at<E>(p.z, i); y *= z * sigmoidf_(z); }
-                put<E>(p.y, i, tok >> t & 1 ? y : 0.0f);
-            }
-        }
     }
     if (AHEAD) {
+        total += moved<0xb1>(total);                                 // of a channel's four lanes
+        total += moved<0x4e>(total);
         float f[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) f[r] = began ? FIRST : exp2_(fmaxf(total * a2[r], -126.0f));
@@ -255,22 +387,19 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
 // ---------------------------------------------------------------------------
 // gradient, tiles from the last to the first.  AHEAD: what a chunk makes of the derivative behind it, into part
 // ---------------------------------------------------------------------------
-template <typename E, int L, bool KEEP, bool AHEAD>
+template <typename E, int R, bool KEEP, bool AHEAD>
 __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles, float *shares, float *bc_shares)
 {
-    typedef Place<L> P;
-    constexpr int CH = P::CH, EACH = P::EACH;
-    const P at_(p, slabs);
+    constexpr int ROWS = rows_of(R), SUMS = sums_of(R);
+    const Place<R> at_(p, slabs);
     const int64_t DN = p.D * p.N;
-    __shared__ __attribute__((aligned(16))) float4 sd[ROWS][CH];     // s, s x, du
-    __shared__ __attribute__((aligned(16))) float sb[2][ROWS][4 * L];
-    __shared__ float ss[3][ROWS][CH];                                // sum of G B, of G h exp(s a) a, of C h
-    __shared__ float sc[4][2][ROWS][4 * L];                          // dB, dC of a wave's channels
-    const int wave = threadIdx.x >> 6;
-    float a[R], G[R], da[R], total = 0.0f, dskip = 0.0f;
+    const int l = at_.l, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ __attribute__((aligned(16))) float sb[2][ROWS][2][LANES * R];
+    __shared__ float sc[AHEAD ? 1 : 2][4][ROWS][SUMS][64];           // dB, dC of a wave's channels
+    float a[R], a2[R], G[R], da[R], total = 0.0f, dskip = 0.0f;
     at_.load(p, p.a, a);
 #pragma unroll
-    for (int r = 0; r < R; ++r) { G[r] = 0.0f; da[r] = 0.0f; }
+    for (int r = 0; r < R; ++r) { a2[r] = a[r] * LOG2E; G[r] = 0.0f; da[r] = 0.0f; }
     bool began = false;
     if (!AHEAD) {
         at_.load(p, p.dhT + at_.b * DN, G);
@@ -282,120 +411,179 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
             for (int r = 0; r < R; ++r) G[r] = through(f[r], G[r], H[r]);
         }
     }
-    const float skip = p.skip[at_.pd];
+    const float skip = p.skip[at_.d];
     const int64_t tiles = (p.T + ROWS - 1) / ROWS;
-    const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, end_tile = min(first_tile + chunk_tiles, tiles);
-    for (int64_t tile = end_tile - 1; tile >= first_tile; --tile) {
+    const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, last_tile = min(first_tile + chunk_tiles, tiles) - 1;
+    Column<E, ROWS> qx, qt, qd, qz;
+    Stage<E, R, ROWS> bc;
+    uint32_t tok, first, next_tok = 0, next_first = 0;
+    float h[R], next_h[R];
+    auto request = [&](int64_t tile) {
         const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
-        uint32_t tok, first;
-        flags_of<KEEP>(p, at_.b, t0, tok, first);
-        float x[EACH], dt[EACH], dy[EACH], z[EACH];
+        if (!AHEAD) qx.request(p, p.x, row0, p.T - t0, at_.d, l);
+        qt.request(p, p.dt, row0, p.T - t0, at_.d, l);
+        qd.request(p, p.dy, row0, p.T - t0, at_.d, l);
+        if (p.z) qz.request(p, p.z, row0, p.T - t0, at_.d, l);
+        if (!AHEAD) at_.load(p, p.states + (at_.b * tiles + tile) * DN, next_h);
+    };
+    request(last_tile);
+    flags_of<KEEP, ROWS>(p, at_.b, last_tile * ROWS, tok, first);
+    bc.request(p, at_.b, last_tile * ROWS);
+    bc.put(sb[last_tile & 1], tok);
+    __syncthreads();
+    for (int64_t tile = last_tile; tile >= first_tile; --tile) {
+        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
+        float x[ROWS / 4], s[ROWS / 4], dt[ROWS / 4], dy[ROWS / 4], z[ROWS / 4], du[ROWS / 4];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int t = at_.pr + e * L;
-            const bool here = tok >> t & 1;
-            const int64_t i = (row0 + t) * p.D + at_.pd;
-            x[e] = here ? at<E>(p.x, i) : 0.0f;
-            dt[e] = here ? at<E>(p.dt, i) : 0.0f;
-            dy[e] = here ? at<E>(p.dy, i) : 0.0f;
-            z[e] = here && p.z ? at<E>(p.z, i) : 0.0f;
-            const float s = here ? softplus(dt[e]) : 0.0f, du = p.z ? dy[e] * (z[e] * sigmoidf_(z[e])) : dy[e];
-            sd[t][at_.pc] = float4{s, s * x[e], du, 0.0f};
-            if (!AHEAD) dskip = __builtin_fmaf(du, x[e], dskip);
+        for (int i = 0; i < ROWS / 4; ++i) {
+            const bool here = at_.live && tok >> (4 * i + l) & 1;     // channels that are not there add nothing to dB and dC
+            x[i] = !AHEAD && here ? number<E>(qx.r[i]) : 0.0f;
+            dt[i] = number<E>(qt.r[i]);
+            s[i] = here ? softplus(dt[i]) : 0.0f;
+            dy[i] = here ? number<E>(qd.r[i]) : 0.0f;
+            z[i] = here && p.z ? number<E>(qz.r[i]) : 0.0f;
+            du[i] = p.z ? dy[i] * (z[i] * sigmoidf_(z[i])) : dy[i];
+            if (!AHEAD) dskip = __builtin_fmaf(du[i], x[i], dskip);
         }
-        stage_bc<E, L>(p, row0, tok, sb);
-        __syncthreads();
-        if (AHEAD) {
+        if (!AHEAD) {
 #pragma unroll
-            for (int t = ROWS - 1; t >= 0; --t) {
-                const float4 v = sd[t][at_.c];
-                total += v.x;
+            for (int r = 0; r < R; ++r) h[r] = next_h[r];
+        }
+        const bool more = tile > first_tile;
+        if (more) {
+            request(tile - 1);
+            bc.request(p, at_.b, t0 - ROWS);
+            flags_of<KEEP, ROWS>(p, at_.b, t0 - ROWS, next_tok, next_first);
+        }
+        const float (*const sbt)[2][LANES * R] = sb[tile & 1];
+        if constexpr (AHEAD) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    G[r] = __builtin_fmaf(sb[1][t][at_.l * R + r], v.z, G[r]) * exp2_(v.x * (a[r] * LOG2E));
-                    if (KEEP && (first >> t & 1)) G[r] = 0.0f;
-                }
+            for (int i = ROWS / 4 - 1; i >= 0; --i) {
+                total += s[i];
+                auto row = [&](auto lane_) {
+                    constexpr int K = decltype(lane_)::value;
+                    const int t = 4 * i + K;
+                    float C[R];
+                    from_lds<R>(&sbt[t][1][l * R], C);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        G[r] = __builtin_fmaf(C[r], of_lane<K>(du[i]), G[r]) * exp2_(of_lane<K>(s[i]) * a2[r]);
+                        if (KEEP && (first >> t & 1)) G[r] = 0.0f;
+                    }
+                };
+                row(std::integral_constant<int, 3>{});
+                row(std::integral_constant<int, 2>{});
+                row(std::integral_constant<int, 1>{});
+                row(std::integral_constant<int, 0>{});
             }
             began |= KEEP && first != 0;
         } else {
-            float h[R], before[ROWS][R], gate[ROWS][R];
-            at_.load(p, p.states + (at_.b * tiles + tile) * DN, h);
+            float before[ROWS][R], gate[ROWS][R], u[ROWS / 4], dat[R];
 #pragma unroll
-            for (int t = 0; t < ROWS; ++t) {
-                const float4 v = sd[t][at_.c];
-                float sum = 0.0f;
+            for (int i = 0; i < ROWS / 4; ++i) {
+                float sum[4];
+                const float v = s[i] * x[i];
+                auto row = [&](auto lane_) {
+                    constexpr int K = decltype(lane_)::value;
+                    const int t = 4 * i + K;
+                    float B[R], C[R];
+                    from_lds<R>(&sbt[t][0][l * R], B);
+                    from_lds<R>(&sbt[t][1][l * R], C);
+                    if (KEEP && (first >> t & 1)) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if (KEEP && (first >> t & 1)) h[r] = 0.0f;
-                    before[t][r] = h[r];
-                    gate[t][r] = exp2_(v.x * (a[r] * LOG2E));
-                    h[r] = __builtin_fmaf(gate[t][r], h[r], v.y * sb[0][t][at_.l * R + r]);
-                    sum = __builtin_fmaf(sb[1][t][at_.l * R + r], h[r], sum);
-                }
-                if (p.z) {
-                    sum = over_states<L>(sum);
-                    if (at_.l == 0) ss[2][t][at_.c] = sum;
+                        for (int r = 0; r < R; ++r) h[r] = 0.0f;
+                    }
+                    sum[K] = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        before[t][r] = h[r];
+                        gate[t][r] = exp2_(of_lane<K>(s[i]) * a2[r]);
+                        h[r] = __builtin_fmaf(gate[t][r], h[r], of_lane<K>(v) * B[r]);
+                        sum[K] = __builtin_fmaf(C[r], h[r], sum[K]);
+                    }
+                };
+                row(std::integral_constant<int, 0>{});
+                row(std::integral_constant<int, 1>{});
+                row(std::integral_constant<int, 2>{});
+                row(std::integral_constant<int, 3>{});
+                u[i] = p.z ? __builtin_fmaf(skip, x[i], over_states(sum)) : 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) dat[r] = 0.0f;
+#pragma unroll
+            for (int i = ROWS / 4 - 1; i >= 0; --i) {
+                const float v = s[i] * x[i];
+                float gb[4], ga[4];
+                auto row = [&](auto lane_) {
+                    constexpr int K = decltype(lane_)::value;
+                    const int t = 4 * i + K;
+                    float B[R], C[R], db[R], dc[R], out[SUMS];
+                    from_lds<R>(&sbt[t][0][l * R], B);
+                    from_lds<R>(&sbt[t][1][l * R], C);
+                    gb[K] = 0.0f;
+                    ga[K] = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const float he = before[t][r] * gate[t][r];
+                        G[r] = __builtin_fmaf(C[r], of_lane<K>(du[i]), G[r]);
+                        const float arg = G[r] * he;
+                        dat[r] = __builtin_fmaf(of_lane<K>(s[i]), arg, dat[r]);
+                        ga[K] = __builtin_fmaf(arg, a[r], ga[K]);
+                        gb[K] = __builtin_fmaf(G[r], B[r], gb[K]);
+                        db[r] = of_lane<K>(v) * G[r];
+                        dc[r] = of_lane<K>(du[i]) * __builtin_fmaf(of_lane<K>(v), B[r], he);
+                        G[r] *= gate[t][r];
+                        if (KEEP && (first >> t & 1)) G[r] = 0.0f;
+                    }
+                    over_channels<R>(db, dc, out);
+#pragma unroll
+                    for (int k = 0; k < SUMS; ++k) sc[tile & 1][wave][t][k][lane] = out[k];
+                };
+                row(std::integral_constant<int, 3>{});
+                row(std::integral_constant<int, 2>{});
+                row(std::integral_constant<int, 1>{});
+                row(std::integral_constant<int, 0>{});
+                const int t = 4 * i + l;
+                const float sgb = over_states(gb), sga = over_states(ga);
+                if (at_.live && t0 + t < p.T) {
+                    const bool here = tok >> t & 1;
+                    const int64_t at = (row0 + t) * p.D + at_.d;
+                    put<E>(p.dx, at, here ? __builtin_fmaf(skip, du[i], s[i] * sgb) : 0.0f);
+                    put<E>(p.ddt, at, here ? __builtin_fmaf(x[i], sgb, sga) * sigmoidf_(dt[i]) : 0.0f);
+                    if (p.z) {
+                        const float sg = sigmoidf_(z[i]);
+                        put<E>(p.dz, at, here ? dy[i] * u[i] * __builtin_fmaf(z[i] * sg, sigmoidf_(-z[i]), sg) : 0.0f);
+                    }
                 }
             }
 #pragma unroll
-            for (int t = ROWS - 1; t >= 0; --t) {
-                const float4 v = sd[t][at_.c];
-                float gb = 0.0f, ga = 0.0f, db[R], dc[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const float B = sb[0][t][at_.l * R + r], he = before[t][r] * gate[t][r];
-                    G[r] = __builtin_fmaf(sb[1][t][at_.l * R + r], v.z, G[r]);
-                    const float arg = G[r] * he;
-                    da[r] = __builtin_fmaf(arg, v.x, da[r]);
-                    ga = __builtin_fmaf(arg, a[r], ga);
-                    gb = __builtin_fmaf(G[r], B, gb);
-                    db[r] = at_.live ? G[r] * v.y : 0.0f;
-                    dc[r] = at_.live ? v.z * __builtin_fmaf(v.y, B, he) : 0.0f;
-                    G[r] *= gate[t][r];
-                    if (KEEP && (first >> t & 1)) G[r] = 0.0f;
-                }
-                gb = over_states<L>(gb);
-                ga = over_states<L>(ga);
-                if (at_.l == 0) { ss[0][t][at_.c] = gb; ss[1][t][at_.c] = ga; }
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    db[r] = over_channels<L>(db[r]);
-                    dc[r] = over_channels<L>(dc[r]);
-                    if ((threadIdx.x & 63) < L) { sc[wave][0][t][at_.l * R + r] = db[r]; sc[wave][1][t][at_.l * R + r] = dc[r]; }
-                }
-            }
+            for (int r = 0; r < R; ++r) da[r] += dat[r];             // tile by tile: fewer roundings on the way
+        }
+        const uint32_t was = tok;
+        if (more) {
+            bc.put(sb[(tile - 1) & 1], next_tok);
+            tok = next_tok;
+            first = next_first;
         }
         __syncthreads();
-        if (!AHEAD) {
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int t = at_.pr + e * L;
-                if (t0 + t >= p.T || !at_.plive) continue;
-                const bool here = tok >> t & 1;
-                const int64_t i = (row0 + t) * p.D + at_.pd;
-                const float4 v = sd[t][at_.pc];
-                const float gb = ss[0][t][at_.pc], ga = ss[1][t][at_.pc];
-                put<E>(p.dx, i, here ? __builtin_fmaf(skip, v.z, v.x * gb) : 0.0f);
-                put<E>(p.ddt, i, here ? __builtin_fmaf(x[e], gb, ga) * sigmoidf_(dt[e]) : 0.0f);
-                if (p.z) {
-                    const float s = sigmoidf_(z[e]), u = __builtin_fmaf(skip, x[e], ss[2][t][at_.pc]);
-                    put<E>(p.dz, i, here ? dy[e] * u * __builtin_fmaf(z[e] * s, sigmoidf_(-z[e]), s) : 0.0f);
-                }
-            }
+        if constexpr (!AHEAD) {
             for (int i = threadIdx.x; i < ROWS * 2 * (int)p.N; i += 256) {
                 const int n = i % (int)p.N, which = i / (int)p.N % 2, t = i / (2 * (int)p.N);
-                if (t0 + t >= p.T) continue;
-                float sum = sc[0][which][t][n];
+                if (t0 + t >= p.T) break;
+                const int r = n % R, slot = slot_of(which, r, n / R);
+                float sum = sc[tile & 1][0][t][r / 4][slot];
 #pragma unroll
-                for (int w = 1; w < 4; ++w) sum += sc[w][which][t][n];
-                bc_shares[((int64_t)at_.slab * p.B * p.T + row0 + t) * 2 * p.N + which * p.N + n] = tok >> t & 1 ? sum : 0.0f;
+                for (int w = 1; w < 4; ++w) sum += sc[tile & 1][w][t][r / 4][slot];
+                bc_shares[((int64_t)at_.slab * p.B * p.T + row0 + t) * 2 * p.N + which * p.N + n] = was >> t & 1 ? sum : 0.0f;
             }
         }
     }
-    if (AHEAD) {
+    if constexpr (AHEAD) {
+        total += moved<0xb1>(total);
+        total += moved<0x4e>(total);
         float f[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) f[r] = began ? FIRST : exp2_(fmaxf(total * (a[r] * LOG2E), -126.0f));
+        for (int r = 0; r < R; ++r) f[r] = began ? FIRST : exp2_(fmaxf(total * a2[r], -126.0f));
         at_.store(p, p.part + (2 * ((int64_t)at_.chunk * p.B + at_.b)) * DN, f);
         at_.store(p, p.part + (2 * ((int64_t)at_.chunk * p.B + at_.b) + 1) * DN, G);
         return;
@@ -403,32 +591,28 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
     if (at_.chunk == 0) at_.store(p, p.dh0 + at_.b * DN, G);
     float *mine = shares + ((int64_t)at_.chunk * p.B + at_.b) * (DN + p.D);
     at_.store(p, mine, da);
-    // the threads of a channel's tokens add up what they have of dskip
-    __syncthreads();
-    float *const sums = &ss[0][0][0];
-    sums[at_.pr * CH + at_.pc] = dskip;
-    __syncthreads();
-    if (at_.pr == 0 && at_.plive) {
-        for (int k = 1; k < L; ++k) dskip += sums[k * CH + at_.pc];
-        mine[DN + at_.pd] = dskip;
-    }
+    dskip += moved<0xb1>(dskip);
+    dskip += moved<0x4e>(dskip);
+    if (at_.live && l == 0) mine[DN + at_.d] = dskip;
 }
 
 namespace {
 
-struct Form { int L; int32_t slabs, chunks, chunk_tiles; };
+struct Form { int R; int32_t slabs, chunks, chunk_tiles, rows; };
 
 Form form_of(const SelScanParams &p)
 {
     Form f;
-    f.L = 1;
-    while (f.L * R < p.N) f.L *= 2;
-    const int64_t ch = 256 / f.L, tiles = (p.T + ROWS - 1) / ROWS;
-    f.slabs = (int32_t)((p.D + ch - 1) / ch);
+    f.R = 1;
+    while (f.R * LANES < p.N) f.R *= 2;
+    f.rows = rows_of(f.R);
+    const int64_t tiles = (p.T + f.rows - 1) / f.rows;
+    f.slabs = (int32_t)((p.D + CHANNELS - 1) / CHANNELS);
     const int64_t wgs = p.B * f.slabs;
     int64_t chunks = 1;
     if (wgs < 256) chunks = 512 / wgs;
-    if (chunks > tiles / 4) chunks = tiles / 4 > 0 ? tiles / 4 : 1;
+    const int64_t most = tiles * f.rows / 64;
+    if (chunks > most) chunks = most > 0 ? most : 1;
     f.chunk_tiles = (int32_t)((tiles + chunks - 1) / chunks);
     f.chunks = (int32_t)((tiles + f.chunk_tiles - 1) / f.chunk_tiles);
     return f;
@@ -445,28 +629,27 @@ Scratch scratch_of(const SelScanParams &p, const Form &f, bool grad)
     }
     return s;
 }
-
-template <typename E, int L>
+template <typename E, int R>
 hipError_t go(bool grad, const SelScanParams &p, const Form &f, hipStream_t s)
 {
     const dim3 grid((unsigned)(p.B * f.slabs * f.chunks)), wg(256);
     if (!grad) {
         if (f.chunks > 1) {
-            if (p.keep) hipLaunchKernelGGL((selective_scan_kernel<E, L, true, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-            else hipLaunchKernelGGL((selective_scan_kernel<E, L, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+            if (p.keep) hipLaunchKernelGGL((selective_scan_kernel<E, R, true, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+            else hipLaunchKernelGGL((selective_scan_kernel<E, R, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
         }
-        if (p.keep) hipLaunchKernelGGL((selective_scan_kernel<E, L, true, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-        else hipLaunchKernelGGL((selective_scan_kernel<E, L, false, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+        if (p.keep) hipLaunchKernelGGL((selective_scan_kernel<E, R, true, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+        else hipLaunchKernelGGL((selective_scan_kernel<E, R, false, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
         return hipGetLastError();
     }
     const Scratch sc = scratch_of(p, f, true);
     float *const shares = p.part + sc.chunks, *const bc = shares + sc.shares;
     if (f.chunks > 1) {
-        if (p.keep) hipLaunchKernelGGL((selective_scan_grad_kernel<E, L, true, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
-        else hipLaunchKernelGGL((selective_scan_grad_kernel<E, L, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+        if (p.keep) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, true, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+        else hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
     }
-    if (p.keep) hipLaunchKernelGGL((selective_scan_grad_kernel<E, L, true, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
-    else hipLaunchKernelGGL((selective_scan_grad_kernel<E, L, false, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+    if (p.keep) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, true, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+    else hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, false, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
     hipError_t er = hipGetLastError();
     if (er != hipSuccess) return er;
     SumShares q{};
@@ -483,7 +666,7 @@ hipError_t go(bool grad, const SelScanParams &p, const Form &f, hipStream_t s)
 
 template <typename E> hipError_t go(bool grad, const SelScanParams &p, const Form &f, hipStream_t s)
 {
-    switch (f.L) {
+    switch (f.R) {
     case 1: return go<E, 1>(grad, p, f, s);
     case 2: return go<E, 2>(grad, p, f, s);
     case 4: return go<E, 4>(grad, p, f, s);
@@ -492,14 +675,14 @@ template <typename E> hipError_t go(bool grad, const SelScanParams &p, const For
     }
 }
 
-template <typename E, int L> void go_step(const SelScanParams &p, hipStream_t s)
+template <typename E, int R> void go_step(const SelScanParams &p, hipStream_t s)
 {
     const int64_t channels = p.B * p.D;
-    hipLaunchKernelGGL((selective_scan_step_kernel<E, L>), dim3((unsigned)((channels * L + 255) / 256)), dim3(256), 0, s, p, channels);
+    hipLaunchKernelGGL((selective_scan_step_kernel<E, R>), dim3((unsigned)((channels * LANES + 255) / 256)), dim3(256), 0, s, p, channels);
 }
-template <typename E> hipError_t go_step(const SelScanParams &p, int L, hipStream_t s)
+template <typename E> hipError_t go_step(const SelScanParams &p, int R, hipStream_t s)
 {
-    switch (L) {
+    switch (R) {
     case 1: go_step<E, 1>(p, s); break;
     case 2: go_step<E, 2>(p, s); break;
     case 4: go_step<E, 4>(p, s); break;
@@ -515,10 +698,12 @@ bool sel_scan_fits(const SelScanParams &p, bool grad)
 {
     if (p.B < 1 || p.T < 1 || p.D < 1 || p.N < 1 || p.N > SSM_MAX_STATES || p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > SCAN_MAX_D) return false;
     const Form f = form_of(p);
-    if (p.T == 1 && !grad) return launch_has((p.B * p.D * f.L + 255) / 256, 256);
+    if (p.T == 1 && !grad) return launch_has((p.B * p.D * LANES + 255) / 256, 256);
     // the sums over channels are a launch of a thousand threads a 64 columns
     return launch_has(p.B * f.slabs * f.chunks, 256) && (!grad || (p.B * p.T * 2 * p.N + 63) / 64 <= 0x3fffff);
 }
+
+int64_t sel_scan_state_rows(const SelScanParams &p) { return form_of(p).rows; }
 
 int64_t sel_scan_part_floats(const SelScanParams &p, bool grad)
 {
@@ -532,7 +717,7 @@ hipError_t launch_sel_scan(const SelScanParams &p, hipStream_t s)
     if (!sel_scan_fits(p, false) || (f.chunks > 1 && !p.part) || p.gated != (p.z != nullptr) || p.keeps != (p.keep != nullptr)) return hipErrorInvalidValue;
     if (p.T == 1 && !p.states) {
         if (!p.y || !p.hT) return hipErrorInvalidValue;
-        return p.dtype == DT_BF16 ? go_step<uint16_t>(p, f.L, s) : go_step<float>(p, f.L, s);
+        return p.dtype == DT_BF16 ? go_step<uint16_t>(p, f.R, s) : go_step<float>(p, f.R, s);
     }
     return p.dtype == DT_BF16 ? go<uint16_t>(false, p, f, s) : go<float>(false, p, f, s);
 }
