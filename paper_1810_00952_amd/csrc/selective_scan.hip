@@ -181,18 +181,48 @@ template <bool KEEP, int ROWS> __device__ __forceinline__ void flags_of(const Se
     first = (uint32_t)__ballot(k == 2);
 }
 
+// rows in memory: `room` bytes from a tile's first row to the sequence's last.  What lies behind them reads as zero and is not written; so
+// does what a lane without a channel or state (offset OOB) asks for.
+__device__ __forceinline__ rsrc_t rows_at(const void *first, int64_t room)
+{
+    return make_rsrc(first, (uint32_t)(room < 0x7fffffff ? room : 0x7fffffff));
+}
+template <typename E> __device__ __forceinline__ typename Bits<E>::raw fetch(const rsrc_t &r, uint32_t off, uint32_t more)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(E) == 4) return __builtin_amdgcn_raw_buffer_load_b32(r, off, more, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b16(r, off, more, 0);
+#else
+    return 0;
+#endif
+}
+template <typename E> __device__ __forceinline__ void keep(const rsrc_t &r, uint32_t off, uint32_t more, float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, off, more, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16x2(v, v), r, off, more, 0);
+#endif
+}
+
 // B and C of a tile's rows on their way to LDS: a thread's share, zeros behind N and of padding
 template <typename E, int R, int ROWS> struct Stage {
     static constexpr int WIDE = LANES * R, EACH = (2 * ROWS * WIDE + 255) / 256;
     typename Bits<E>::raw r[EACH];
-    __device__ __forceinline__ void request(const SelScanParams &p, int64_t b, int64_t t0)
+    uint32_t off[EACH];
+    __device__ __forceinline__ Stage(const SelScanParams &p)
     {
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int i = e * 256 + (int)threadIdx.x, n = i % WIDE, which = i / WIDE % 2, t = i / (2 * WIDE);
-            r[e] = 0;
-            if (t < ROWS && n < p.N && t0 + t < p.T && t0 >= 0) r[e] = ((const typename Bits<E>::raw *)p.bc)[(b * p.T + t0 + t) * 2 * p.N + which * p.N + n];
+            off[e] = t < ROWS && n < p.N ? (uint32_t)((t * 2 + which) * (int)p.N + n) * (uint32_t)sizeof(E) : OOB;
         }
+    }
+    __device__ __forceinline__ void request(const SelScanParams &p, int64_t b, int64_t t0)
+    {
+        const int64_t line = 2 * p.N * (int64_t)sizeof(E);
+        const rsrc_t rows = rows_at((const char *)p.bc + (b * p.T + t0) * line, (p.T - t0) * line);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) r[e] = fetch<E>(rows, off[e], 0);
     }
     __device__ __forceinline__ void put(float (&s)[ROWS][2][WIDE], uint32_t tok) const
     {
@@ -222,17 +252,13 @@ template <int R> __device__ __forceinline__ void from_lds(const float *s, float 
     }
 }
 
-// a lane's rows of a tile: the l-th of every four
+// a lane's rows of a tile, the l-th of every four: `off` bytes from the tile's first, four rows on from one to the next
 template <typename E, int ROWS> struct Column {
     typename Bits<E>::raw r[ROWS / 4];
-    __device__ __forceinline__ void request(const SelScanParams &p, const void *x, int64_t row0, int64_t rows, int64_t d, int l)
+    __device__ __forceinline__ void request(const rsrc_t &rows, uint32_t off, uint32_t line)
     {
 #pragma unroll
-        for (int i = 0; i < ROWS / 4; ++i) {
-            int64_t t = 4 * i + l;
-            t = t < rows ? t : rows - 1;
-            r[i] = ((const typename Bits<E>::raw *)x)[(row0 + t) * p.D + d];
-        }
+        for (int i = 0; i < ROWS / 4; ++i) r[i] = fetch<E>(rows, off, 4 * i * line);
     }
 };
 
@@ -242,37 +268,40 @@ template <typename E, int ROWS> struct Column {
 // one token a sequence
 // ---------------------------------------------------------------------------
 template <typename E, int R>
-__global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanParams p, int64_t channels)
+__global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanParams p, int32_t slabs)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-    const int l = threadIdx.x % LANES;
-    const bool live = i < channels;
-    const int64_t c = live ? i : 0, b = c / p.D, d = c - b * p.D;
-    const int keep = p.keep ? p.keep[b] : 1;
-    const float x = keep ? at<E>(p.x, c) : 0.0f, s = keep ? softplus(at<E>(p.dt, c)) : 0.0f, v = s * x;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const Place<R> at_(p, slabs);
+    const int64_t DN = p.D * p.N, c = at_.b * p.D + at_.d;
+    const int flag = p.keep ? p.keep[at_.b] : 1;
+    float a[R], h[R], B[R], C[R];
+    at_.load(p, p.h0 + at_.b * DN, h);
+    at_.load(p, p.a, a);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int n = l * R + r;
-        if (n >= p.N) continue;
-        const float h0 = p.h0[c * p.N + n], e = exp2_(s * (p.a[d * p.N + n] * LOG2E));
-        const float u = keep ? v * at<E>(p.bc, b * 2 * p.N + n) : 0.0f;
-        const float h = keep == 2 ? u : keep ? __builtin_fmaf(e, h0, u) : h0;
-        if (live) p.hT[c * p.N + n] = h;
-        sum[0] = __builtin_fmaf(keep ? at<E>(p.bc, (b * 2 + 1) * p.N + n) : 0.0f, h, sum[0]);
+        const int n = at_.l * R + r;
+        B[r] = n < p.N ? at<E>(p.bc, at_.b * 2 * p.N + n) : 0.0f;
+        C[r] = n < p.N ? at<E>(p.bc, (at_.b * 2 + 1) * p.N + n) : 0.0f;
     }
-    const float all = over_states(sum);
-    if (l == 0 && live) {
-        float y = __builtin_fmaf(p.skip[d], x, all);
-        if (p.z) { const float z = at<E>(p.z, c); y *= z * sigmoidf_(z); }
-        put<E>(p.y, c, keep ? y : 0.0f);
+    const float x = at<E>(p.x, c), s = softplus(at<E>(p.dt, c)), v = s * x, skip = p.skip[at_.d], z = p.z ? at<E>(p.z, c) : 0.0f;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (flag) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float e = exp2_(s * (a[r] * LOG2E));
+            h[r] = __builtin_fmaf(e, flag == 2 ? 0.0f : h[r], v * B[r]);
+            sum[0] = __builtin_fmaf(C[r], h[r], sum[0]);
+        }
     }
+    at_.store(p, p.hT + at_.b * DN, h);
+    float y = __builtin_fmaf(skip, x, over_states(sum));
+    if (p.z) y *= z * sigmoidf_(z);
+    if (at_.l == 0 && at_.live) put<E>(p.y, c, flag ? y : 0.0f);
 }
 
 // ---------------------------------------------------------------------------
 // forward.  AHEAD: what a chunk makes of the state before it, into part ([chunk][b] P, H of [D][N])
 // ---------------------------------------------------------------------------
-template <typename E, int R, bool KEEP, bool AHEAD>
+template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
 __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles)
 {
     constexpr int ROWS = rows_of(R);
@@ -299,13 +328,17 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
     const int64_t tiles = (p.T + ROWS - 1) / ROWS;
     const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, end_tile = min(first_tile + chunk_tiles, tiles);
     Column<E, ROWS> qx, qt, qz;
-    Stage<E, R, ROWS> bc;
+    Stage<E, R, ROWS> bc(p);
     uint32_t tok, first, next_tok = 0, next_first = 0;
+    const uint32_t line = (uint32_t)(p.D * sizeof(E)), off = at_.live ? l * line + (uint32_t)(at_.d * sizeof(E)) : OOB;
+    auto rows = [&](const void *x, int64_t tile) {
+        const int64_t t0 = tile * ROWS;
+        return rows_at((const char *)x + (at_.b * p.T + t0) * line, (p.T - t0) * line);
+    };
     auto request = [&](int64_t tile) {
-        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
-        qx.request(p, p.x, row0, p.T - t0, at_.d, l);
-        qt.request(p, p.dt, row0, p.T - t0, at_.d, l);
-        if (!AHEAD && p.z) qz.request(p, p.z, row0, p.T - t0, at_.d, l);
+        qx.request(rows(p.x, tile), off, line);
+        qt.request(rows(p.dt, tile), off, line);
+        if (GATED && !AHEAD) qz.request(rows(p.z, tile), off, line);
     };
     request(first_tile);
     flags_of<KEEP, ROWS>(p, at_.b, first_tile * ROWS, tok, first);
@@ -313,15 +346,16 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
     bc.put(sb[first_tile & 1], tok);
     __syncthreads();
     for (int64_t tile = first_tile; tile < end_tile; ++tile) {
-        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
+        const int64_t t0 = tile * ROWS;
         float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4];
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
             const bool here = tok >> (4 * i + l) & 1;
             x[i] = here ? number<E>(qx.r[i]) : 0.0f;
             s[i] = here ? softplus(number<E>(qt.r[i])) : 0.0f;
-            z[i] = !AHEAD && p.z ? number<E>(qz.r[i]) : 0.0f;
+            z[i] = GATED && !AHEAD ? number<E>(qz.r[i]) : 0.0f;
         }
+        const rsrc_t to = rows(p.y, tile);
         const bool more = tile + 1 < end_tile;
         if (more) {
             request(tile + 1);
@@ -360,8 +394,8 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
             if (!AHEAD) {
                 float y = __builtin_fmaf(skip, x[i], over_states(sum));
                 const int t = 4 * i + l;
-                if (p.z) y *= z[i] * sigmoidf_(z[i]);
-                if (p.y && at_.live && t0 + t < p.T) put<E>(p.y, (row0 + t) * p.D + at_.d, tok >> t & 1 ? y : 0.0f);
+                if (GATED) y *= z[i] * sigmoidf_(z[i]);
+                if (p.y) keep<E>(to, off, 4 * i * line, !KEEP || (tok >> t & 1) ? y : 0.0f);
             }
         }
         if (more) {
@@ -387,7 +421,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
 // ---------------------------------------------------------------------------
 // gradient, tiles from the last to the first.  AHEAD: what a chunk makes of the derivative behind it, into part
 // ---------------------------------------------------------------------------
-template <typename E, int R, bool KEEP, bool AHEAD>
+template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
 __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles, float *shares, float *bc_shares)
 {
     constexpr int ROWS = rows_of(R), SUMS = sums_of(R);
@@ -415,15 +449,19 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
     const int64_t tiles = (p.T + ROWS - 1) / ROWS;
     const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, last_tile = min(first_tile + chunk_tiles, tiles) - 1;
     Column<E, ROWS> qx, qt, qd, qz;
-    Stage<E, R, ROWS> bc;
+    Stage<E, R, ROWS> bc(p);
     uint32_t tok, first, next_tok = 0, next_first = 0;
     float h[R], next_h[R];
+    const uint32_t line = (uint32_t)(p.D * sizeof(E)), off = at_.live ? l * line + (uint32_t)(at_.d * sizeof(E)) : OOB;
+    auto rows = [&](const void *x, int64_t tile) {
+        const int64_t t0 = tile * ROWS;
+        return rows_at((const char *)x + (at_.b * p.T + t0) * line, (p.T - t0) * line);
+    };
     auto request = [&](int64_t tile) {
-        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
-        if (!AHEAD) qx.request(p, p.x, row0, p.T - t0, at_.d, l);
-        qt.request(p, p.dt, row0, p.T - t0, at_.d, l);
-        qd.request(p, p.dy, row0, p.T - t0, at_.d, l);
-        if (p.z) qz.request(p, p.z, row0, p.T - t0, at_.d, l);
+        if (!AHEAD) qx.request(rows(p.x, tile), off, line);
+        qt.request(rows(p.dt, tile), off, line);
+        qd.request(rows(p.dy, tile), off, line);
+        if (GATED) qz.request(rows(p.z, tile), off, line);
         if (!AHEAD) at_.load(p, p.states + (at_.b * tiles + tile) * DN, next_h);
     };
     request(last_tile);
@@ -441,8 +479,8 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
             dt[i] = number<E>(qt.r[i]);
             s[i] = here ? softplus(dt[i]) : 0.0f;
             dy[i] = here ? number<E>(qd.r[i]) : 0.0f;
-            z[i] = here && p.z ? number<E>(qz.r[i]) : 0.0f;
-            du[i] = p.z ? dy[i] * (z[i] * sigmoidf_(z[i])) : dy[i];
+            z[i] = GATED && here ? number<E>(qz.r[i]) : 0.0f;
+            du[i] = GATED ? dy[i] * (z[i] * sigmoidf_(z[i])) : dy[i];
             if (!AHEAD) dskip = __builtin_fmaf(du[i], x[i], dskip);
         }
         if (!AHEAD) {
@@ -478,7 +516,8 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
             }
             began |= KEEP && first != 0;
         } else {
-            float before[ROWS][R], gate[ROWS][R], u[ROWS / 4], dat[R];
+            float decayed[ROWS][R], gate[ROWS][R], u[ROWS / 4], dat[R];       // the state before a row times its gate
+            const rsrc_t to_x = rows(p.dx, tile), to_t = rows(p.ddt, tile), to_z = rows(p.dz, tile);
 #pragma unroll
             for (int i = 0; i < ROWS / 4; ++i) {
                 float sum[4];
@@ -488,7 +527,7 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                     const int t = 4 * i + K;
                     float B[R], C[R];
                     from_lds<R>(&sbt[t][0][l * R], B);
-                    from_lds<R>(&sbt[t][1][l * R], C);
+                    if (GATED) from_lds<R>(&sbt[t][1][l * R], C);
                     if (KEEP && (first >> t & 1)) {
 #pragma unroll
                         for (int r = 0; r < R; ++r) h[r] = 0.0f;
@@ -496,17 +535,17 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                     sum[K] = 0.0f;
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        before[t][r] = h[r];
                         gate[t][r] = exp2_(of_lane<K>(s[i]) * a2[r]);
-                        h[r] = __builtin_fmaf(gate[t][r], h[r], of_lane<K>(v) * B[r]);
-                        sum[K] = __builtin_fmaf(C[r], h[r], sum[K]);
+                        decayed[t][r] = gate[t][r] * h[r];
+                        h[r] = __builtin_fmaf(of_lane<K>(v), B[r], decayed[t][r]);
+                        if (GATED) sum[K] = __builtin_fmaf(C[r], h[r], sum[K]);
                     }
                 };
                 row(std::integral_constant<int, 0>{});
                 row(std::integral_constant<int, 1>{});
                 row(std::integral_constant<int, 2>{});
                 row(std::integral_constant<int, 3>{});
-                u[i] = p.z ? __builtin_fmaf(skip, x[i], over_states(sum)) : 0.0f;
+                u[i] = GATED ? __builtin_fmaf(skip, x[i], over_states(sum)) : 0.0f;
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) dat[r] = 0.0f;
@@ -524,7 +563,7 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                     ga[K] = 0.0f;
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        const float he = before[t][r] * gate[t][r];
+                        const float he = decayed[t][r];
                         G[r] = __builtin_fmaf(C[r], of_lane<K>(du[i]), G[r]);
                         const float arg = G[r] * he;
                         dat[r] = __builtin_fmaf(of_lane<K>(s[i]), arg, dat[r]);
@@ -545,15 +584,12 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                 row(std::integral_constant<int, 0>{});
                 const int t = 4 * i + l;
                 const float sgb = over_states(gb), sga = over_states(ga);
-                if (at_.live && t0 + t < p.T) {
-                    const bool here = tok >> t & 1;
-                    const int64_t at = (row0 + t) * p.D + at_.d;
-                    put<E>(p.dx, at, here ? __builtin_fmaf(skip, du[i], s[i] * sgb) : 0.0f);
-                    put<E>(p.ddt, at, here ? __builtin_fmaf(x[i], sgb, sga) * sigmoidf_(dt[i]) : 0.0f);
-                    if (p.z) {
-                        const float sg = sigmoidf_(z[i]);
-                        put<E>(p.dz, at, here ? dy[i] * u[i] * __builtin_fmaf(z[i] * sg, sigmoidf_(-z[i]), sg) : 0.0f);
-                    }
+                const bool here = !KEEP || (tok >> t & 1);
+                keep<E>(to_x, off, 4 * i * line, here ? __builtin_fmaf(skip, du[i], s[i] * sgb) : 0.0f);
+                keep<E>(to_t, off, 4 * i * line, here ? __builtin_fmaf(x[i], sgb, sga) * sigmoidf_(dt[i]) : 0.0f);
+                if (GATED) {
+                    const float sg = sigmoidf_(z[i]);
+                    keep<E>(to_z, off, 4 * i * line, here ? dy[i] * u[i] * __builtin_fmaf(z[i] * sg, sigmoidf_(-z[i]), sg) : 0.0f);
                 }
             }
 #pragma unroll
@@ -629,29 +665,28 @@ Scratch scratch_of(const SelScanParams &p, const Form &f, bool grad)
     }
     return s;
 }
+template <typename E, int R, bool KEEP, bool GATED>
+void go(bool grad, const SelScanParams &p, const Form &f, float *shares, float *bc, hipStream_t s)
+{
+    const dim3 grid((unsigned)(p.B * f.slabs * f.chunks)), wg(256);
+    if (grad) {
+        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+        hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+    } else {
+        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+        hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+    }
+}
+
 template <typename E, int R>
 hipError_t go(bool grad, const SelScanParams &p, const Form &f, hipStream_t s)
 {
-    const dim3 grid((unsigned)(p.B * f.slabs * f.chunks)), wg(256);
-    if (!grad) {
-        if (f.chunks > 1) {
-            if (p.keep) hipLaunchKernelGGL((selective_scan_kernel<E, R, true, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-            else hipLaunchKernelGGL((selective_scan_kernel<E, R, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-        }
-        if (p.keep) hipLaunchKernelGGL((selective_scan_kernel<E, R, true, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-        else hipLaunchKernelGGL((selective_scan_kernel<E, R, false, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-        return hipGetLastError();
-    }
-    const Scratch sc = scratch_of(p, f, true);
-    float *const shares = p.part + sc.chunks, *const bc = shares + sc.shares;
-    if (f.chunks > 1) {
-        if (p.keep) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, true, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
-        else hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
-    }
-    if (p.keep) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, true, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
-    else hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, false, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+    const Scratch sc = scratch_of(p, f, grad);
+    float *const shares = p.part ? p.part + sc.chunks : nullptr, *const bc = shares ? shares + sc.shares : nullptr;
+    if (p.keep) p.z ? go<E, R, true, true>(grad, p, f, shares, bc, s) : go<E, R, true, false>(grad, p, f, shares, bc, s);
+    else p.z ? go<E, R, false, true>(grad, p, f, shares, bc, s) : go<E, R, false, false>(grad, p, f, shares, bc, s);
     hipError_t er = hipGetLastError();
-    if (er != hipSuccess) return er;
+    if (er != hipSuccess || !grad) return er;
     SumShares q{};
     q.part = shares; q.P = f.chunks * p.B; q.stride = p.D * p.N + p.D; q.dst_dtype = DT_F32;
     q.J = p.D * p.N; q.dst = p.da;
@@ -677,8 +712,8 @@ template <typename E> hipError_t go(bool grad, const SelScanParams &p, const For
 
 template <typename E, int R> void go_step(const SelScanParams &p, hipStream_t s)
 {
-    const int64_t channels = p.B * p.D;
-    hipLaunchKernelGGL((selective_scan_step_kernel<E, R>), dim3((unsigned)((channels * LANES + 255) / 256)), dim3(256), 0, s, p, channels);
+    const int32_t slabs = (int32_t)((p.D + CHANNELS - 1) / CHANNELS);
+    hipLaunchKernelGGL((selective_scan_step_kernel<E, R>), dim3((unsigned)(p.B * slabs)), dim3(256), 0, s, p, slabs);
 }
 template <typename E> hipError_t go_step(const SelScanParams &p, int R, hipStream_t s)
 {
@@ -698,7 +733,6 @@ bool sel_scan_fits(const SelScanParams &p, bool grad)
 {
     if (p.B < 1 || p.T < 1 || p.D < 1 || p.N < 1 || p.N > SSM_MAX_STATES || p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > SCAN_MAX_D) return false;
     const Form f = form_of(p);
-    if (p.T == 1 && !grad) return launch_has((p.B * p.D * LANES + 255) / 256, 256);
     // the sums over channels are a launch of a thousand threads a 64 columns
     return launch_has(p.B * f.slabs * f.chunks, 256) && (!grad || (p.B * p.T * 2 * p.N + 63) / 64 <= 0x3fffff);
 }
