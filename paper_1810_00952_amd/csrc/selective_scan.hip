@@ -45,12 +45,28 @@ __device__ __forceinline__ float exp2_(float v)
 #endif
 }
 
-// ln(1 + e^v): for large v it is v; below, with w = e^v, ln(1 + w) w / ((1 + w) - 1) keeps its last bits where 1 + w loses those of w
+__device__ __forceinline__ float log2_(float v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_logf(v);
+#else
+    return v;
+#endif
+}
+
+// s = ln(1 + e^v) and its slope, sigmoid(v).  With w = e^v: ln of 1 + w as it is rounded, and what the rounding took off w, whose part of the logarithm
+// is itself where 1 + w is below 2, and above it less than the logarithm's last bit.  For v above 20 it is v, as rounded.
+__device__ __forceinline__ float softplus(float v, float &slope)
+{
+    const float w = exp2_(v * LOG2E), u = 1.0f + w, lost = w - (u - 1.0f);
+    const float s = __builtin_fmaf(log2_(u), 0.6931471805599453f, u < 2.0f ? lost : 0.0f);
+    slope = v > 20.0f ? 1.0f : w * rcp_(u);
+    return v > 20.0f ? v : s;
+}
 __device__ __forceinline__ float softplus(float v)
 {
-    const float w = __expf(v), u = 1.0f + w;
-    const float small = u == 1.0f ? w : __logf(u) * (w * rcp_(u - 1.0f));
-    return v > 20.0f ? v : small;
+    float slope;
+    return softplus(v, slope);
 }
 
 template <typename E> struct Bits;
@@ -115,6 +131,14 @@ template <int R> __device__ __forceinline__ void over_channels(const float (&db)
         else v = u[0] + moved<0x128>(u[0]);
         out[i] = v + moved<0x104>(v);                                                                             // row_shl 4
     }
+}
+
+// Barrier of a workgroup whose waves meet in LDS alone: what is under way to and from memory stays so
+__device__ __forceinline__ void lds_barrier()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#endif
 }
 
 // what a lane works on
@@ -252,6 +276,36 @@ template <int R> __device__ __forceinline__ void from_lds(const float *s, float 
     }
 }
 
+// B and C of the rows to come, read AHEAD rows before they are used: the compiler, which counts on more waves than there are, reads them where they are
+template <int R, int ROWS, bool BACK> struct Coming {
+    static constexpr int AHEAD = R >= 16 ? 1 : R >= 8 ? 2 : 4;
+    float b[AHEAD + 1][R], c[AHEAD + 1][R];
+    const float (*s)[2][LANES * R];
+    int l;
+    __device__ __forceinline__ Coming(const float (*s_)[2][LANES * R], int l_, bool with_b, bool with_c) : s(s_), l(l_)
+    {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) read(k, with_b, with_c);
+    }
+    __device__ __forceinline__ void read(int k, bool with_b, bool with_c)      // the k-th row of the walk
+    {
+        if (k >= ROWS) return;
+        const int t = BACK ? ROWS - 1 - k : k;
+        if (with_b) from_lds<R>(&s[t][0][l * R], b[k % (AHEAD + 1)]);
+        if (with_c) from_lds<R>(&s[t][1][l * R], c[k % (AHEAD + 1)]);
+    }
+    // row k is next
+    __device__ __forceinline__ void step(int k, bool with_b, bool with_c)
+    {
+        read(k + AHEAD, with_b, with_c);
+#if defined(__HIP_DEVICE_COMPILE__)
+        __builtin_amdgcn_sched_barrier(0x47f);        // all but accesses of LDS may cross
+#endif
+    }
+    __device__ __forceinline__ float B(int k, int r) const { return b[k % (AHEAD + 1)][r]; }
+    __device__ __forceinline__ float C(int k, int r) const { return c[k % (AHEAD + 1)][r]; }
+};
+
 // a lane's rows of a tile, the l-th of every four: `off` bytes from the tile's first, four rows on from one to the next
 template <typename E, int ROWS> struct Column {
     typename Bits<E>::raw r[ROWS / 4];
@@ -302,7 +356,7 @@ __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanP
 // forward.  AHEAD: what a chunk makes of the state before it, into part ([chunk][b] P, H of [D][N])
 // ---------------------------------------------------------------------------
 template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
-__global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles)
 {
     constexpr int ROWS = rows_of(R);
     const Place<R> at_(p, slabs);
@@ -344,18 +398,24 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
     flags_of<KEEP, ROWS>(p, at_.b, first_tile * ROWS, tok, first);
     bc.request(p, at_.b, first_tile * ROWS);
     bc.put(sb[first_tile & 1], tok);
-    __syncthreads();
-    for (int64_t tile = first_tile; tile < end_tile; ++tile) {
-        const int64_t t0 = tile * ROWS;
-        float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4];
+    lds_barrier();
+    // what the rows need once a token is found before the tile they are of begins: with few waves nothing else hides how long that takes
+    float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4];
+    auto once = [&](uint32_t tokens) {
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
-            const bool here = tok >> (4 * i + l) & 1;
+            const bool here = tokens >> (4 * i + l) & 1;
+            const float step = softplus(number<E>(qt.r[i]));
             x[i] = here ? number<E>(qx.r[i]) : 0.0f;
-            s[i] = here ? softplus(number<E>(qt.r[i])) : 0.0f;
+            s[i] = here ? step : 0.0f;
             z[i] = GATED && !AHEAD ? number<E>(qz.r[i]) : 0.0f;
+            if (GATED && !AHEAD) z[i] *= sigmoidf_(z[i]);
         }
-        const rsrc_t to = rows(p.y, tile);
+    };
+    once(tok);
+    for (int64_t tile = first_tile; tile < end_tile; ++tile) {
+        const int64_t t0 = tile * ROWS;
+        const rsrc_t to = p.y ? rows(p.y, tile) : make_rsrc(nullptr, 0);
         const bool more = tile + 1 < end_tile;
         if (more) {
             request(tile + 1);
@@ -363,7 +423,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
             flags_of<KEEP, ROWS>(p, at_.b, t0 + ROWS, next_tok, next_first);
         }
         if (p.states && !AHEAD) at_.store(p, p.states + (at_.b * tiles + tile) * DN, h);
-        const float (*const sbt)[2][LANES * R] = sb[tile & 1];
+        Coming<R, ROWS, false> bcs(sb[tile & 1], l, true, !AHEAD);
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
             float sum[4];
@@ -372,9 +432,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
             auto row = [&](auto lane) {
                 constexpr int K = decltype(lane)::value;
                 const int t = 4 * i + K;
-                float B[R], C[R];
-                from_lds<R>(&sbt[t][0][l * R], B);
-                if (!AHEAD) from_lds<R>(&sbt[t][1][l * R], C);
+                bcs.step(t, true, !AHEAD);
                 if (KEEP && (first >> t & 1)) {
                     began = true;
 #pragma unroll
@@ -383,8 +441,8 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
                 sum[K] = 0.0f;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    h[r] = __builtin_fmaf(exp2_(of_lane<K>(s[i]) * a2[r]), h[r], of_lane<K>(v) * B[r]);
-                    if (!AHEAD) sum[K] = __builtin_fmaf(C[r], h[r], sum[K]);
+                    h[r] = __builtin_fmaf(exp2_(of_lane<K>(s[i]) * a2[r]), h[r], of_lane<K>(v) * bcs.B(t, r));
+                    if (!AHEAD) sum[K] = __builtin_fmaf(bcs.C(t, r), h[r], sum[K]);
                 }
             };
             row(std::integral_constant<int, 0>{});
@@ -394,16 +452,15 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
             if (!AHEAD) {
                 float y = __builtin_fmaf(skip, x[i], over_states(sum));
                 const int t = 4 * i + l;
-                if (GATED) y *= z[i] * sigmoidf_(z[i]);
-                if (p.y) keep<E>(to, off, 4 * i * line, !KEEP || (tok >> t & 1) ? y : 0.0f);
+                if (GATED) y *= z[i];
+                keep<E>(to, off, 4 * i * line, !KEEP || (tok >> t & 1) ? y : 0.0f);
             }
         }
-        if (more) {
-            bc.put(sb[(tile + 1) & 1], next_tok);
-            tok = next_tok;
-            first = next_first;
-        }
-        __syncthreads();
+        tok = next_tok;
+        first = next_first;
+        once(tok);
+        if (more) bc.put(sb[(tile + 1) & 1], tok);
+        lds_barrier();
     }
     if (AHEAD) {
         total += moved<0xb1>(total);                                 // of a channel's four lanes
@@ -422,7 +479,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const SelScanParams
 // gradient, tiles from the last to the first.  AHEAD: what a chunk makes of the derivative behind it, into part
 // ---------------------------------------------------------------------------
 template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
-__global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles, float *shares, float *bc_shares)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 4 : 2))) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles, float *shares, float *bc_shares)
 {
     constexpr int ROWS = rows_of(R), SUMS = sums_of(R);
     const Place<R> at_(p, slabs);
@@ -468,21 +525,24 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
     flags_of<KEEP, ROWS>(p, at_.b, last_tile * ROWS, tok, first);
     bc.request(p, at_.b, last_tile * ROWS);
     bc.put(sb[last_tile & 1], tok);
-    __syncthreads();
-    for (int64_t tile = last_tile; tile >= first_tile; --tile) {
-        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
-        float x[ROWS / 4], s[ROWS / 4], dt[ROWS / 4], dy[ROWS / 4], z[ROWS / 4], du[ROWS / 4];
+    lds_barrier();
+    float x[ROWS / 4], s[ROWS / 4], slope[ROWS / 4], du[ROWS / 4], dz[ROWS / 4];       // dz: dy times the gate's slope
+    auto once = [&](uint32_t tokens) {
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
-            const bool here = at_.live && tok >> (4 * i + l) & 1;     // channels that are not there add nothing to dB and dC
+            const bool here = at_.live && tokens >> (4 * i + l) & 1;     // channels that are not there add nothing to dB and dC
+            const float step = softplus(number<E>(qt.r[i]), slope[i]), dy = here ? number<E>(qd.r[i]) : 0.0f, z = GATED && here ? number<E>(qz.r[i]) : 0.0f;
             x[i] = !AHEAD && here ? number<E>(qx.r[i]) : 0.0f;
-            dt[i] = number<E>(qt.r[i]);
-            s[i] = here ? softplus(dt[i]) : 0.0f;
-            dy[i] = here ? number<E>(qd.r[i]) : 0.0f;
-            z[i] = GATED && here ? number<E>(qz.r[i]) : 0.0f;
-            du[i] = GATED ? dy[i] * (z[i] * sigmoidf_(z[i])) : dy[i];
+            s[i] = here ? step : 0.0f;
+            const float sg = GATED ? sigmoidf_(z) : 0.0f;
+            du[i] = GATED ? dy * (z * sg) : dy;
+            dz[i] = GATED && !AHEAD ? dy * __builtin_fmaf(z * sg, sigmoidf_(-z), sg) : 0.0f;
             if (!AHEAD) dskip = __builtin_fmaf(du[i], x[i], dskip);
         }
+    };
+    once(tok);
+    for (int64_t tile = last_tile; tile >= first_tile; --tile) {
+        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
         if (!AHEAD) {
 #pragma unroll
             for (int r = 0; r < R; ++r) h[r] = next_h[r];
@@ -493,19 +553,18 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
             bc.request(p, at_.b, t0 - ROWS);
             flags_of<KEEP, ROWS>(p, at_.b, t0 - ROWS, next_tok, next_first);
         }
-        const float (*const sbt)[2][LANES * R] = sb[tile & 1];
         if constexpr (AHEAD) {
+            Coming<R, ROWS, true> bcs(sb[tile & 1], l, false, true);
 #pragma unroll
             for (int i = ROWS / 4 - 1; i >= 0; --i) {
                 total += s[i];
                 auto row = [&](auto lane_) {
                     constexpr int K = decltype(lane_)::value;
                     const int t = 4 * i + K;
-                    float C[R];
-                    from_lds<R>(&sbt[t][1][l * R], C);
+                    bcs.step(ROWS - 1 - t, false, true);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        G[r] = __builtin_fmaf(C[r], of_lane<K>(du[i]), G[r]) * exp2_(of_lane<K>(s[i]) * a2[r]);
+                        G[r] = __builtin_fmaf(bcs.C(ROWS - 1 - t, r), of_lane<K>(du[i]), G[r]) * exp2_(of_lane<K>(s[i]) * a2[r]);
                         if (KEEP && (first >> t & 1)) G[r] = 0.0f;
                     }
                 };
@@ -517,6 +576,7 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
             began |= KEEP && first != 0;
         } else {
             float decayed[ROWS][R], gate[ROWS][R], u[ROWS / 4], dat[R];       // the state before a row times its gate
+            Coming<R, ROWS, false> on(sb[tile & 1], l, true, GATED);
             const rsrc_t to_x = rows(p.dx, tile), to_t = rows(p.ddt, tile), to_z = rows(p.dz, tile);
 #pragma unroll
             for (int i = 0; i < ROWS / 4; ++i) {
@@ -525,9 +585,7 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                 auto row = [&](auto lane_) {
                     constexpr int K = decltype(lane_)::value;
                     const int t = 4 * i + K;
-                    float B[R], C[R];
-                    from_lds<R>(&sbt[t][0][l * R], B);
-                    if (GATED) from_lds<R>(&sbt[t][1][l * R], C);
+                    on.step(t, true, GATED);
                     if (KEEP && (first >> t & 1)) {
 #pragma unroll
                         for (int r = 0; r < R; ++r) h[r] = 0.0f;
@@ -537,8 +595,8 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                     for (int r = 0; r < R; ++r) {
                         gate[t][r] = exp2_(of_lane<K>(s[i]) * a2[r]);
                         decayed[t][r] = gate[t][r] * h[r];
-                        h[r] = __builtin_fmaf(of_lane<K>(v), B[r], decayed[t][r]);
-                        if (GATED) sum[K] = __builtin_fmaf(C[r], h[r], sum[K]);
+                        h[r] = __builtin_fmaf(of_lane<K>(v), on.B(t, r), decayed[t][r]);
+                        if (GATED) sum[K] = __builtin_fmaf(on.C(t, r), h[r], sum[K]);
                     }
                 };
                 row(std::integral_constant<int, 0>{});
@@ -547,6 +605,7 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                 row(std::integral_constant<int, 3>{});
                 u[i] = GATED ? __builtin_fmaf(skip, x[i], over_states(sum)) : 0.0f;
             }
+            Coming<R, ROWS, true> back(sb[tile & 1], l, true, true);
 #pragma unroll
             for (int r = 0; r < R; ++r) dat[r] = 0.0f;
 #pragma unroll
@@ -556,21 +615,21 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                 auto row = [&](auto lane_) {
                     constexpr int K = decltype(lane_)::value;
                     const int t = 4 * i + K;
-                    float B[R], C[R], db[R], dc[R], out[SUMS];
-                    from_lds<R>(&sbt[t][0][l * R], B);
-                    from_lds<R>(&sbt[t][1][l * R], C);
+                    float db[R], dc[R], out[SUMS];
+                    back.step(ROWS - 1 - t, true, true);
                     gb[K] = 0.0f;
                     ga[K] = 0.0f;
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         const float he = decayed[t][r];
-                        G[r] = __builtin_fmaf(C[r], of_lane<K>(du[i]), G[r]);
+                        const float B = back.B(ROWS - 1 - t, r);
+                        G[r] = __builtin_fmaf(back.C(ROWS - 1 - t, r), of_lane<K>(du[i]), G[r]);
                         const float arg = G[r] * he;
                         dat[r] = __builtin_fmaf(of_lane<K>(s[i]), arg, dat[r]);
                         ga[K] = __builtin_fmaf(arg, a[r], ga[K]);
-                        gb[K] = __builtin_fmaf(G[r], B[r], gb[K]);
+                        gb[K] = __builtin_fmaf(G[r], B, gb[K]);
                         db[r] = of_lane<K>(v) * G[r];
-                        dc[r] = of_lane<K>(du[i]) * __builtin_fmaf(of_lane<K>(v), B[r], he);
+                        dc[r] = of_lane<K>(du[i]) * __builtin_fmaf(of_lane<K>(v), B, he);
                         G[r] *= gate[t][r];
                         if (KEEP && (first >> t & 1)) G[r] = 0.0f;
                     }
@@ -586,22 +645,20 @@ __global__ __launch_bounds__(256) void selective_scan_grad_kernel(const SelScanP
                 const float sgb = over_states(gb), sga = over_states(ga);
                 const bool here = !KEEP || (tok >> t & 1);
                 keep<E>(to_x, off, 4 * i * line, here ? __builtin_fmaf(skip, du[i], s[i] * sgb) : 0.0f);
-                keep<E>(to_t, off, 4 * i * line, here ? __builtin_fmaf(x[i], sgb, sga) * sigmoidf_(dt[i]) : 0.0f);
-                if (GATED) {
-                    const float sg = sigmoidf_(z[i]);
-                    keep<E>(to_z, off, 4 * i * line, here ? dy[i] * u[i] * __builtin_fmaf(z[i] * sg, sigmoidf_(-z[i]), sg) : 0.0f);
-                }
+                keep<E>(to_t, off, 4 * i * line, here ? __builtin_fmaf(x[i], sgb, sga) * slope[i] : 0.0f);
+                if (GATED) keep<E>(to_z, off, 4 * i * line, here ? dz[i] * u[i] : 0.0f);
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) da[r] += dat[r];             // tile by tile: fewer roundings on the way
         }
         const uint32_t was = tok;
+        tok = next_tok;
+        first = next_first;
         if (more) {
-            bc.put(sb[(tile - 1) & 1], next_tok);
-            tok = next_tok;
-            first = next_first;
+            once(tok);
+            bc.put(sb[(tile - 1) & 1], tok);
         }
-        __syncthreads();
+        lds_barrier();
         if constexpr (!AHEAD) {
             for (int i = threadIdx.x; i < ROWS * 2 * (int)p.N; i += 256) {
                 const int n = i % (int)p.N, which = i / (int)p.N % 2, t = i / (2 * (int)p.N);
