@@ -14,6 +14,7 @@
 // padding has s = s x = B = C = du = 0 and leaves state and derivative as they are.  Few channels: the rows are cut into chunks, a workgroup
 // each; a launch ahead finds what each chunk makes of the state before it (P h + H; the derivative alike), P = exp(a sum s), and the workgroups
 // add up the chunks before theirs.
+#include <algorithm>
 #include <type_traits>
 
 #include "igemm_lds.h"
@@ -220,7 +221,7 @@ template <typename E> __device__ __forceinline__ typename Bits<E>::raw fetch(con
     return 0;
 #endif
 }
-template <typename E> __device__ __forceinline__ void keep(const rsrc_t &r, uint32_t off, uint32_t more, float v)
+template <typename E> __device__ __forceinline__ void put(const rsrc_t &r, uint32_t off, uint32_t more, float v)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, off, more, 0);
@@ -228,32 +229,67 @@ template <typename E> __device__ __forceinline__ void keep(const rsrc_t &r, uint
 #endif
 }
 
-// B and C of a tile's rows on their way to LDS: a thread's share, zeros behind N and of padding
+// B and C of a tile's rows on their way to LDS, to the wave's own part of it: zeros behind N and of padding.  Where N is all of the lanes' states the rows
+// of a tile lie in memory as they do there, and go by whole vectors.
 template <typename E, int R, int ROWS> struct Stage {
-    static constexpr int WIDE = LANES * R, EACH = (2 * ROWS * WIDE + 255) / 256;
+    static constexpr int WIDE = LANES * R, TOTAL = 2 * ROWS * WIDE, EACH = TOTAL / 64, KV = 16 / sizeof(E), VECS = TOTAL / KV, EACHV = (VECS + 63) / 64;
     typename Bits<E>::raw r[EACH];
-    uint32_t off[EACH];
-    __device__ __forceinline__ Stage(const SelScanParams &p)
+    u32x4 v[EACHV];
+    rsrc_t rows;
+    uint32_t off[EACH], line;
+    bool whole;
+    __device__ __forceinline__ Stage(const SelScanParams &p, int64_t row0, int64_t left)
     {
+        line = (uint32_t)(2 * p.N * sizeof(E));
+        rows = rows_at((const char *)p.bc + row0 * line, left * line);
+        whole = p.N == WIDE;
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const int i = e * 256 + (int)threadIdx.x, n = i % WIDE, which = i / WIDE % 2, t = i / (2 * WIDE);
-            off[e] = t < ROWS && n < p.N ? (uint32_t)((t * 2 + which) * (int)p.N + n) * (uint32_t)sizeof(E) : OOB;
+            const int i = e * 64 + lane, n = i % WIDE, which = i / WIDE % 2, t = i / (2 * WIDE);
+            off[e] = n < p.N ? (uint32_t)((t * 2 + which) * (int)p.N + n) * (uint32_t)sizeof(E) : OOB;
         }
     }
-    __device__ __forceinline__ void request(const SelScanParams &p, int64_t b, int64_t t0)
+    __device__ __forceinline__ void request(uint32_t t0)                       // rows from the first of them
     {
-        const int64_t line = 2 * p.N * (int64_t)sizeof(E);
-        const rsrc_t rows = rows_at((const char *)p.bc + (b * p.T + t0) * line, (p.T - t0) * line);
+#if defined(__HIP_DEVICE_COMPILE__)
+        const uint32_t from = t0 * line;
+        if (whole) {
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) r[e] = fetch<E>(rows, off[e], 0);
+            for (int e = 0; e < EACHV; ++e) v[e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, from + (e * 64 + (threadIdx.x & 63)) * 16, 0, 0));
+        } else {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) r[e] = fetch<E>(rows, off[e], from);
+        }
+#endif
     }
-    __device__ __forceinline__ void put(float (&s)[ROWS][2][WIDE], uint32_t tok) const
+    __device__ __forceinline__ void put(float *s, uint32_t tok) const
     {
+        const int lane = threadIdx.x & 63;
+        if (whole) {
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int i = e * 256 + (int)threadIdx.x, t = i / (2 * WIDE);
-            if (t < ROWS) (&s[0][0][0])[i] = tok >> t & 1 ? number<E>(r[e]) : 0.0f;
+            for (int e = 0; e < EACHV; ++e) {
+                const int i = (e * 64 + lane) * KV;
+                if (VECS % 64 != 0 && i >= TOTAL) break;
+                const bool here = tok >> (i / (2 * WIDE)) & 1;
+#pragma unroll
+                for (int k = 0; k < KV; k += 4) {
+                    f32x4 q;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if constexpr (sizeof(E) == 4) q[c] = __uint_as_float(v[e][c]);
+                        else q[c] = __uint_as_float(c & 1 ? v[e][(k + c) / 2] & 0xffff0000u : v[e][(k + c) / 2] << 16);
+                        if (!here) q[c] = 0.0f;
+                    }
+                    *(f32x4 *)(s + i + k) = q;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const int i = e * 64 + lane;
+                s[i] = tok >> (i / (2 * WIDE)) & 1 ? number<E>(r[e]) : 0.0f;
+            }
         }
     }
 };
@@ -276,34 +312,36 @@ template <int R> __device__ __forceinline__ void from_lds(const float *s, float 
     }
 }
 
-// B and C of the rows to come, read AHEAD rows before they are used: the compiler, which counts on more waves than there are, reads them where they are
-template <int R, int ROWS, bool BACK> struct Coming {
-    static constexpr int AHEAD = R >= 16 ? 1 : R >= 8 ? 2 : 4;
-    float b[AHEAD + 1][R], c[AHEAD + 1][R];
-    const float (*s)[2][LANES * R];
-    int l;
-    __device__ __forceinline__ Coming(const float (*s_)[2][LANES * R], int l_, bool with_b, bool with_c) : s(s_), l(l_)
+// B and C of the rows to come, read AHEAD rows before they are used, across the tiles: the compiler, which counts on more waves than there are, would
+// read them where they are used.  Row k of a walk through a tile; from ROWS on the next tile's, which lies in the other half of the wave's LDS.
+template <int R, int ROWS, bool BACK, bool WITH_B, bool WITH_C> struct Coming {
+    static constexpr int AHEAD = R >= 16 ? 1 : R >= 8 ? 2 : 4, RING = 2 * AHEAD;
+    static_assert(ROWS % RING == 0, "a tile's first row is in the ring's first place");
+    float b[RING][R], c[RING][R];
+    const float *s;                            // the lane's part of the two halves
+    __device__ __forceinline__ void read(int k, int half)
     {
+        const int t = BACK ? ROWS - 1 - k % ROWS : k % ROWS;
+        const float *q = s + (half * ROWS + t) * 2 * LANES * R;
+        if (WITH_B) from_lds<R>(q, b[k % RING]);
+        if (WITH_C) from_lds<R>(q + LANES * R, c[k % RING]);
+    }
+    __device__ __forceinline__ void start(const float *s_, int half)
+    {
+        s = s_;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) read(k, with_b, with_c);
+        for (int k = 0; k < AHEAD; ++k) read(k, half);
     }
-    __device__ __forceinline__ void read(int k, bool with_b, bool with_c)      // the k-th row of the walk
+    // row k of the tile in `half` is next
+    __device__ __forceinline__ void step(int k, int half)
     {
-        if (k >= ROWS) return;
-        const int t = BACK ? ROWS - 1 - k : k;
-        if (with_b) from_lds<R>(&s[t][0][l * R], b[k % (AHEAD + 1)]);
-        if (with_c) from_lds<R>(&s[t][1][l * R], c[k % (AHEAD + 1)]);
-    }
-    // row k is next
-    __device__ __forceinline__ void step(int k, bool with_b, bool with_c)
-    {
-        read(k + AHEAD, with_b, with_c);
+        read(k + AHEAD, k + AHEAD < ROWS ? half : half ^ 1);
 #if defined(__HIP_DEVICE_COMPILE__)
         __builtin_amdgcn_sched_barrier(0x47f);        // all but accesses of LDS may cross
 #endif
     }
-    __device__ __forceinline__ float B(int k, int r) const { return b[k % (AHEAD + 1)][r]; }
-    __device__ __forceinline__ float C(int k, int r) const { return c[k % (AHEAD + 1)][r]; }
+    __device__ __forceinline__ float B(int k, int r) const { return b[k % RING][r]; }
+    __device__ __forceinline__ float C(int k, int r) const { return c[k % RING][r]; }
 };
 
 // a lane's rows of a tile, the l-th of every four: `off` bytes from the tile's first, four rows on from one to the next
@@ -362,7 +400,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
     const Place<R> at_(p, slabs);
     const int64_t DN = p.D * p.N;
     const int l = at_.l;
-    __shared__ __attribute__((aligned(16))) float sb[2][ROWS][2][LANES * R];
+    __shared__ __attribute__((aligned(16))) float sb[4][2][ROWS][2][LANES * R];          // of every wave
     float a2[R], h[R], total = 0.0f;
     at_.load(p, p.a, a2);
 #pragma unroll
@@ -379,60 +417,75 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
         }
     }
     const float skip = p.skip[at_.d];
-    const int64_t tiles = (p.T + ROWS - 1) / ROWS;
-    const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, end_tile = min(first_tile + chunk_tiles, tiles);
+    const int64_t T0 = (int64_t)at_.chunk * chunk_tiles * ROWS, row0 = at_.b * p.T + T0, left = min(p.T - T0, (int64_t)chunk_tiles * ROWS);
+    const int32_t tiles = (int32_t)((left + ROWS - 1) / ROWS);
+    const uint32_t line = (uint32_t)(p.D * sizeof(E));
+    auto rows = [&](const void *x) { return rows_at((const char *)x + row0 * line, x ? left * line : 0); };      // the chunk's
+    const rsrc_t from_x = rows(p.x), from_t = rows(p.dt), from_z = rows(p.z), to = rows(p.y);
+    uint32_t off = at_.live ? l * line + (uint32_t)(at_.d * sizeof(E)) : OOB, ask = off;
+    const uint32_t on = at_.live ? ROWS * line : 0;                  // a tile on
     Column<E, ROWS> qx, qt, qz;
-    Stage<E, R, ROWS> bc(p);
-    uint32_t tok, first, next_tok = 0, next_first = 0;
-    const uint32_t line = (uint32_t)(p.D * sizeof(E)), off = at_.live ? l * line + (uint32_t)(at_.d * sizeof(E)) : OOB;
-    auto rows = [&](const void *x, int64_t tile) {
-        const int64_t t0 = tile * ROWS;
-        return rows_at((const char *)x + (at_.b * p.T + t0) * line, (p.T - t0) * line);
+    Stage<E, R, ROWS> bc(p, row0, left);
+    auto request = [&](int32_t tile) {
+        bc.request((uint32_t)tile * ROWS);
+        qx.request(from_x, ask, line);
+        qt.request(from_t, ask, line);
+        if (GATED && !AHEAD) qz.request(from_z, ask, line);
+        ask += on;
     };
-    auto request = [&](int64_t tile) {
-        qx.request(rows(p.x, tile), off, line);
-        qt.request(rows(p.dt, tile), off, line);
-        if (GATED && !AHEAD) qz.request(rows(p.z, tile), off, line);
-    };
-    request(first_tile);
-    flags_of<KEEP, ROWS>(p, at_.b, first_tile * ROWS, tok, first);
-    bc.request(p, at_.b, first_tile * ROWS);
-    bc.put(sb[first_tile & 1], tok);
-    lds_barrier();
     // what the rows need once a token is found before the tile they are of begins: with few waves nothing else hides how long that takes
-    float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4];
-    auto once = [&](uint32_t tokens) {
+    float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4], nx[ROWS / 4], ns[ROWS / 4], nz[ROWS / 4];
+    uint32_t tok, first, next_tok, next_first;
+    auto once = [&]() {
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
-            const bool here = tokens >> (4 * i + l) & 1;
+            const bool here = next_tok >> (4 * i + l) & 1;
             const float step = softplus(number<E>(qt.r[i]));
-            x[i] = here ? number<E>(qx.r[i]) : 0.0f;
-            s[i] = here ? step : 0.0f;
-            z[i] = GATED && !AHEAD ? number<E>(qz.r[i]) : 0.0f;
-            if (GATED && !AHEAD) z[i] *= sigmoidf_(z[i]);
+            nx[i] = here ? number<E>(qx.r[i]) : 0.0f;
+            ns[i] = here ? step : 0.0f;
+            nz[i] = GATED && !AHEAD ? number<E>(qz.r[i]) : 0.0f;
+            if (GATED && !AHEAD) nz[i] *= sigmoidf_(nz[i]);
         }
     };
-    once(tok);
-    for (int64_t tile = first_tile; tile < end_tile; ++tile) {
-        const int64_t t0 = tile * ROWS;
-        const rsrc_t to = p.y ? rows(p.y, tile) : make_rsrc(nullptr, 0);
-        const bool more = tile + 1 < end_tile;
-        if (more) {
-            request(tile + 1);
-            bc.request(p, at_.b, t0 + ROWS);
-            flags_of<KEEP, ROWS>(p, at_.b, t0 + ROWS, next_tok, next_first);
+    auto turn = [&]() {
+        tok = next_tok;
+        first = next_first;
+#pragma unroll
+        for (int i = 0; i < ROWS / 4; ++i) { x[i] = nx[i]; s[i] = ns[i]; z[i] = nz[i]; }
+    };
+    float *const mine = &sb[threadIdx.x >> 6][0][0][0][0];
+    constexpr int HALF = ROWS * 2 * LANES * R;
+    request(0);
+    flags_of<KEEP, ROWS>(p, at_.b, T0, next_tok, next_first);
+    bc.put(mine, next_tok);
+    once();
+    turn();
+    wave_lds_exchange();
+    Coming<R, ROWS, false, true, !AHEAD> bcs;
+    bcs.start(mine + l * R, 0);
+    float *state = p.states ? p.states + (at_.b * ((p.T + ROWS - 1) / ROWS) + T0 / ROWS) * DN : nullptr;
+    for (int32_t tile = 0; tile < tiles; ++tile) {
+        const int half = tile & 1;
+        request(tile + 1);                                           // behind the chunk: zeros
+        flags_of<KEEP, ROWS>(p, at_.b, T0 + (int64_t)(tile + 1) * ROWS, next_tok, next_first);
+        if (!AHEAD && state) {
+            at_.store(p, state, h);
+            state += DN;
         }
-        if (p.states && !AHEAD) at_.store(p, p.states + (at_.b * tiles + tile) * DN, h);
-        Coming<R, ROWS, false> bcs(sb[tile & 1], l, true, !AHEAD);
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
             float sum[4];
             const float v = s[i] * x[i];
             if (AHEAD) total += s[i];
+            if (i + 1 == ROWS / 4) {
+                bc.put(mine + (half ^ 1) * HALF, next_tok);
+                once();
+                wave_lds_exchange();
+            }
             auto row = [&](auto lane) {
                 constexpr int K = decltype(lane)::value;
                 const int t = 4 * i + K;
-                bcs.step(t, true, !AHEAD);
+                bcs.step(t, half);
                 if (KEEP && (first >> t & 1)) {
                     began = true;
 #pragma unroll
@@ -451,16 +504,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
             row(std::integral_constant<int, 3>{});
             if (!AHEAD) {
                 float y = __builtin_fmaf(skip, x[i], over_states(sum));
-                const int t = 4 * i + l;
                 if (GATED) y *= z[i];
-                keep<E>(to, off, 4 * i * line, !KEEP || (tok >> t & 1) ? y : 0.0f);
+                put<E>(to, off, 4 * i * line, !KEEP || (tok >> (4 * i + l) & 1) ? y : 0.0f);
             }
         }
-        tok = next_tok;
-        first = next_first;
-        once(tok);
-        if (more) bc.put(sb[(tile + 1) & 1], tok);
-        lds_barrier();
+        off += on;
+        turn();
     }
     if (AHEAD) {
         total += moved<0xb1>(total);                                 // of a channel's four lanes
@@ -485,7 +534,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
     const Place<R> at_(p, slabs);
     const int64_t DN = p.D * p.N;
     const int l = at_.l, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    __shared__ __attribute__((aligned(16))) float sb[2][ROWS][2][LANES * R];
+    __shared__ __attribute__((aligned(16))) float sb[4][2][ROWS][2][LANES * R];          // of every wave
     __shared__ float sc[AHEAD ? 1 : 2][4][ROWS][SUMS][64];           // dB, dC of a wave's channels
     float a[R], a2[R], G[R], da[R], total = 0.0f, dskip = 0.0f;
     at_.load(p, p.a, a);
@@ -503,68 +552,88 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         }
     }
     const float skip = p.skip[at_.d];
-    const int64_t tiles = (p.T + ROWS - 1) / ROWS;
-    const int64_t first_tile = (int64_t)at_.chunk * chunk_tiles, last_tile = min(first_tile + chunk_tiles, tiles) - 1;
+    const int64_t T0 = (int64_t)at_.chunk * chunk_tiles * ROWS, row0 = at_.b * p.T + T0, left = min(p.T - T0, (int64_t)chunk_tiles * ROWS);
+    const int32_t tiles = (int32_t)((left + ROWS - 1) / ROWS);
+    const uint32_t line = (uint32_t)(p.D * sizeof(E));
+    auto rows = [&](const void *x) { return rows_at((const char *)x + row0 * line, x ? left * line : 0); };      // the chunk's
+    const rsrc_t from_x = rows(p.x), from_t = rows(p.dt), from_d = rows(p.dy), from_z = rows(p.z), to_x = rows(p.dx), to_t = rows(p.ddt), to_z = rows(p.dz);
+    const uint32_t on = at_.live ? ROWS * line : 0;                  // a tile on
+    uint32_t off = (at_.live ? l * line + (uint32_t)(at_.d * sizeof(E)) : OOB) + (uint32_t)(tiles - 1) * on, ask = off;
     Column<E, ROWS> qx, qt, qd, qz;
-    Stage<E, R, ROWS> bc(p);
-    uint32_t tok, first, next_tok = 0, next_first = 0;
+    Stage<E, R, ROWS> bc(p, row0, left);
     float h[R], next_h[R];
-    const uint32_t line = (uint32_t)(p.D * sizeof(E)), off = at_.live ? l * line + (uint32_t)(at_.d * sizeof(E)) : OOB;
-    auto rows = [&](const void *x, int64_t tile) {
-        const int64_t t0 = tile * ROWS;
-        return rows_at((const char *)x + (at_.b * p.T + t0) * line, (p.T - t0) * line);
+    const float *state = p.states + (at_.b * ((p.T + ROWS - 1) / ROWS) + T0 / ROWS + tiles - 1) * DN;
+    auto request = [&](int32_t tile) {
+        bc.request((uint32_t)tile * ROWS);
+        if (!AHEAD) qx.request(from_x, ask, line);
+        qt.request(from_t, ask, line);
+        qd.request(from_d, ask, line);
+        if (GATED) qz.request(from_z, ask, line);
+        if (!AHEAD) at_.load(p, state, next_h);
+        ask -= on;
+        state -= DN;
     };
-    auto request = [&](int64_t tile) {
-        if (!AHEAD) qx.request(rows(p.x, tile), off, line);
-        qt.request(rows(p.dt, tile), off, line);
-        qd.request(rows(p.dy, tile), off, line);
-        if (GATED) qz.request(rows(p.z, tile), off, line);
-        if (!AHEAD) at_.load(p, p.states + (at_.b * tiles + tile) * DN, next_h);
-    };
-    request(last_tile);
-    flags_of<KEEP, ROWS>(p, at_.b, last_tile * ROWS, tok, first);
-    bc.request(p, at_.b, last_tile * ROWS);
-    bc.put(sb[last_tile & 1], tok);
-    lds_barrier();
-    float x[ROWS / 4], s[ROWS / 4], slope[ROWS / 4], du[ROWS / 4], dz[ROWS / 4];       // dz: dy times the gate's slope
-    auto once = [&](uint32_t tokens) {
+    // once a token, a tile ahead.  dz: dy times the gate's slope
+    float x[ROWS / 4], s[ROWS / 4], slope[ROWS / 4], du[ROWS / 4], dz[ROWS / 4], nx[ROWS / 4], ns[ROWS / 4], nslope[ROWS / 4], ndu[ROWS / 4], ndz[ROWS / 4];
+    uint32_t tok, first, next_tok, next_first;
+    auto once = [&]() {
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
-            const bool here = at_.live && tokens >> (4 * i + l) & 1;     // channels that are not there add nothing to dB and dC
-            const float step = softplus(number<E>(qt.r[i]), slope[i]), dy = here ? number<E>(qd.r[i]) : 0.0f, z = GATED && here ? number<E>(qz.r[i]) : 0.0f;
-            x[i] = !AHEAD && here ? number<E>(qx.r[i]) : 0.0f;
-            s[i] = here ? step : 0.0f;
+            const bool here = at_.live && (next_tok >> (4 * i + l) & 1);     // channels that are not there add nothing to dB and dC
+            const float step = softplus(number<E>(qt.r[i]), nslope[i]), dy = here ? number<E>(qd.r[i]) : 0.0f, z = GATED && here ? number<E>(qz.r[i]) : 0.0f;
+            nx[i] = !AHEAD && here ? number<E>(qx.r[i]) : 0.0f;
+            ns[i] = here ? step : 0.0f;
             const float sg = GATED ? sigmoidf_(z) : 0.0f;
-            du[i] = GATED ? dy * (z * sg) : dy;
-            dz[i] = GATED && !AHEAD ? dy * __builtin_fmaf(z * sg, sigmoidf_(-z), sg) : 0.0f;
-            if (!AHEAD) dskip = __builtin_fmaf(du[i], x[i], dskip);
+            ndu[i] = GATED ? dy * (z * sg) : dy;
+            ndz[i] = GATED && !AHEAD ? dy * __builtin_fmaf(z * sg, sigmoidf_(-z), sg) : 0.0f;
         }
     };
-    once(tok);
-    for (int64_t tile = last_tile; tile >= first_tile; --tile) {
-        const int64_t t0 = tile * ROWS, row0 = at_.b * p.T + t0;
+    auto turn = [&]() {
+        tok = next_tok;
+        first = next_first;
+#pragma unroll
+        for (int i = 0; i < ROWS / 4; ++i) {
+            x[i] = nx[i]; s[i] = ns[i]; slope[i] = nslope[i]; du[i] = ndu[i]; dz[i] = ndz[i];
+        }
         if (!AHEAD) {
 #pragma unroll
             for (int r = 0; r < R; ++r) h[r] = next_h[r];
         }
-        const bool more = tile > first_tile;
-        if (more) {
+    };
+    float *const mine = &sb[wave][0][0][0][0];
+    constexpr int HALF = ROWS * 2 * LANES * R;
+    request(tiles - 1);
+    flags_of<KEEP, ROWS>(p, at_.b, T0 + (int64_t)(tiles - 1) * ROWS, next_tok, next_first);
+    bc.put(mine + ((tiles - 1) & 1) * HALF, next_tok);
+    once();
+    turn();
+    wave_lds_exchange();
+    Coming<R, ROWS, AHEAD, !AHEAD, GATED || AHEAD> fore;             // of the first way through a tile
+    fore.start(mine + l * R, (tiles - 1) & 1);
+    for (int32_t tile = tiles - 1; tile >= 0; --tile) {
+        const int half = tile & 1;
+        // in front of the chunk: what is asked for again is not used
+        if (tile > 0) {
             request(tile - 1);
-            bc.request(p, at_.b, t0 - ROWS);
-            flags_of<KEEP, ROWS>(p, at_.b, t0 - ROWS, next_tok, next_first);
+            flags_of<KEEP, ROWS>(p, at_.b, T0 + (int64_t)(tile - 1) * ROWS, next_tok, next_first);
         }
+        auto stage = [&]() {
+            bc.put(mine + (half ^ 1) * HALF, next_tok);
+            once();
+            wave_lds_exchange();
+        };
         if constexpr (AHEAD) {
-            Coming<R, ROWS, true> bcs(sb[tile & 1], l, false, true);
 #pragma unroll
             for (int i = ROWS / 4 - 1; i >= 0; --i) {
                 total += s[i];
+                if (i == 0) stage();
                 auto row = [&](auto lane_) {
                     constexpr int K = decltype(lane_)::value;
                     const int t = 4 * i + K;
-                    bcs.step(ROWS - 1 - t, false, true);
+                    fore.step(ROWS - 1 - t, half);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        G[r] = __builtin_fmaf(bcs.C(ROWS - 1 - t, r), of_lane<K>(du[i]), G[r]) * exp2_(of_lane<K>(s[i]) * a2[r]);
+                        G[r] = __builtin_fmaf(fore.C(ROWS - 1 - t, r), of_lane<K>(du[i]), G[r]) * exp2_(of_lane<K>(s[i]) * a2[r]);
                         if (KEEP && (first >> t & 1)) G[r] = 0.0f;
                     }
                 };
@@ -576,16 +645,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
             began |= KEEP && first != 0;
         } else {
             float decayed[ROWS][R], gate[ROWS][R], u[ROWS / 4], dat[R];       // the state before a row times its gate
-            Coming<R, ROWS, false> on(sb[tile & 1], l, true, GATED);
-            const rsrc_t to_x = rows(p.dx, tile), to_t = rows(p.ddt, tile), to_z = rows(p.dz, tile);
+            Coming<R, ROWS, true, true, true> back;
 #pragma unroll
             for (int i = 0; i < ROWS / 4; ++i) {
                 float sum[4];
                 const float v = s[i] * x[i];
+                if (i + 1 == ROWS / 4) back.start(mine + l * R, half);
                 auto row = [&](auto lane_) {
                     constexpr int K = decltype(lane_)::value;
                     const int t = 4 * i + K;
-                    on.step(t, true, GATED);
+                    if (t + fore.AHEAD < ROWS) fore.step(t, half);
                     if (KEEP && (first >> t & 1)) {
 #pragma unroll
                         for (int r = 0; r < R; ++r) h[r] = 0.0f;
@@ -595,8 +664,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
                     for (int r = 0; r < R; ++r) {
                         gate[t][r] = exp2_(of_lane<K>(s[i]) * a2[r]);
                         decayed[t][r] = gate[t][r] * h[r];
-                        h[r] = __builtin_fmaf(of_lane<K>(v), on.B(t, r), decayed[t][r]);
-                        if (GATED) sum[K] = __builtin_fmaf(on.C(t, r), h[r], sum[K]);
+                        h[r] = __builtin_fmaf(of_lane<K>(v), fore.B(t, r), decayed[t][r]);
+                        if (GATED) sum[K] = __builtin_fmaf(fore.C(t, r), h[r], sum[K]);
                     }
                 };
                 row(std::integral_constant<int, 0>{});
@@ -605,24 +674,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
                 row(std::integral_constant<int, 3>{});
                 u[i] = GATED ? __builtin_fmaf(skip, x[i], over_states(sum)) : 0.0f;
             }
-            Coming<R, ROWS, true> back(sb[tile & 1], l, true, true);
 #pragma unroll
             for (int r = 0; r < R; ++r) dat[r] = 0.0f;
 #pragma unroll
             for (int i = ROWS / 4 - 1; i >= 0; --i) {
                 const float v = s[i] * x[i];
                 float gb[4], ga[4];
+                if (i == 0) stage();
                 auto row = [&](auto lane_) {
                     constexpr int K = decltype(lane_)::value;
                     const int t = 4 * i + K;
                     float db[R], dc[R], out[SUMS];
-                    back.step(ROWS - 1 - t, true, true);
+                    if (ROWS - 1 - t + back.AHEAD < ROWS) back.step(ROWS - 1 - t, half);
                     gb[K] = 0.0f;
                     ga[K] = 0.0f;
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        const float he = decayed[t][r];
-                        const float B = back.B(ROWS - 1 - t, r);
+                        const float he = decayed[t][r], B = back.B(ROWS - 1 - t, r);
                         G[r] = __builtin_fmaf(back.C(ROWS - 1 - t, r), of_lane<K>(du[i]), G[r]);
                         const float arg = G[r] * he;
                         dat[r] = __builtin_fmaf(of_lane<K>(s[i]), arg, dat[r]);
@@ -635,41 +703,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
                     }
                     over_channels<R>(db, dc, out);
 #pragma unroll
-                    for (int k = 0; k < SUMS; ++k) sc[tile & 1][wave][t][k][lane] = out[k];
+                    for (int k = 0; k < SUMS; ++k) sc[half][wave][t][k][lane] = out[k];
                 };
                 row(std::integral_constant<int, 3>{});
                 row(std::integral_constant<int, 2>{});
                 row(std::integral_constant<int, 1>{});
                 row(std::integral_constant<int, 0>{});
-                const int t = 4 * i + l;
                 const float sgb = over_states(gb), sga = over_states(ga);
-                const bool here = !KEEP || (tok >> t & 1);
-                keep<E>(to_x, off, 4 * i * line, here ? __builtin_fmaf(skip, du[i], s[i] * sgb) : 0.0f);
-                keep<E>(to_t, off, 4 * i * line, here ? __builtin_fmaf(x[i], sgb, sga) * slope[i] : 0.0f);
-                if (GATED) keep<E>(to_z, off, 4 * i * line, here ? dz[i] * u[i] : 0.0f);
+                dskip = __builtin_fmaf(du[i], x[i], dskip);
+                const bool here = !KEEP || (tok >> (4 * i + l) & 1);
+                put<E>(to_x, off, 4 * i * line, here ? __builtin_fmaf(skip, du[i], s[i] * sgb) : 0.0f);
+                put<E>(to_t, off, 4 * i * line, here ? __builtin_fmaf(x[i], sgb, sga) * slope[i] : 0.0f);
+                if (GATED) put<E>(to_z, off, 4 * i * line, here ? dz[i] * u[i] : 0.0f);
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) da[r] += dat[r];             // tile by tile: fewer roundings on the way
-        }
-        const uint32_t was = tok;
-        tok = next_tok;
-        first = next_first;
-        if (more) {
-            once(tok);
-            bc.put(sb[(tile - 1) & 1], tok);
-        }
-        lds_barrier();
-        if constexpr (!AHEAD) {
+            fore.start(mine + l * R, half ^ 1);
+            lds_barrier();
+            const int32_t t0 = tile * ROWS;
             for (int i = threadIdx.x; i < ROWS * 2 * (int)p.N; i += 256) {
                 const int n = i % (int)p.N, which = i / (int)p.N % 2, t = i / (2 * (int)p.N);
-                if (t0 + t >= p.T) break;
+                if (t0 + t >= left) break;
                 const int r = n % R, slot = slot_of(which, r, n / R);
-                float sum = sc[tile & 1][0][t][r / 4][slot];
+                float sum = sc[half][0][t][r / 4][slot];
 #pragma unroll
-                for (int w = 1; w < 4; ++w) sum += sc[tile & 1][w][t][r / 4][slot];
-                bc_shares[((int64_t)at_.slab * p.B * p.T + row0 + t) * 2 * p.N + which * p.N + n] = was >> t & 1 ? sum : 0.0f;
+                for (int w = 1; w < 4; ++w) sum += sc[half][w][t][r / 4][slot];
+                bc_shares[((int64_t)at_.slab * p.B * p.T + row0 + t0 + t) * 2 * p.N + which * p.N + n] = tok >> t & 1 ? sum : 0.0f;
             }
         }
+        off -= on;
+        turn();
     }
     if constexpr (AHEAD) {
         total += moved<0xb1>(total);
@@ -682,11 +745,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         return;
     }
     if (at_.chunk == 0) at_.store(p, p.dh0 + at_.b * DN, G);
-    float *mine = shares + ((int64_t)at_.chunk * p.B + at_.b) * (DN + p.D);
-    at_.store(p, mine, da);
+    float *share = shares + ((int64_t)at_.chunk * p.B + at_.b) * (DN + p.D);
+    at_.store(p, share, da);
     dskip += moved<0xb1>(dskip);
     dskip += moved<0x4e>(dskip);
-    if (at_.live && l == 0) mine[DN + at_.d] = dskip;
+    if (at_.live && l == 0) share[DN + at_.d] = dskip;
 }
 
 namespace {
@@ -706,6 +769,9 @@ Form form_of(const SelScanParams &p)
     if (wgs < 256) chunks = 512 / wgs;
     const int64_t most = tiles * f.rows / 64;
     if (chunks > most) chunks = most > 0 ? most : 1;
+    // a chunk's rows are reached by 31-bit offsets
+    const int64_t line = std::max(p.D, 2 * p.N) * (p.dtype == DT_BF16 ? 2 : 4), reach = ((int64_t)1 << 30) / (line * f.rows);
+    if (chunks < (tiles + reach - 1) / reach) chunks = (tiles + reach - 1) / reach;
     f.chunk_tiles = (int32_t)((tiles + chunks - 1) / chunks);
     f.chunks = (int32_t)((tiles + f.chunk_tiles - 1) / f.chunk_tiles);
     return f;
