@@ -149,13 +149,14 @@ struct Place {
     int64_t b, d;
     int32_t chunk, slab;
     bool live;
-    __device__ __forceinline__ Place(const SelScanParams &p, int32_t slabs)
+    __device__ __forceinline__ Place(const SelScanParams &p, int32_t slabs, int32_t first_chunk = 0)
     {
         l = threadIdx.x & 3;
         const uint32_t rest = blockIdx.x / (uint32_t)slabs;
         slab = (int32_t)(blockIdx.x - rest * slabs);
         chunk = (int32_t)(rest / (uint32_t)p.B);
         b = rest - (uint32_t)chunk * (uint32_t)p.B;
+        chunk += first_chunk;
         d = (int64_t)slab * CHANNELS + (threadIdx.x >> 2);
         live = d < p.D;
         if (!live) d = 0;                     // some other channel's, of which nothing is stored
@@ -191,20 +192,28 @@ struct Place {
     }
 };
 
-// rows of a tile that are tokens, that are a document's first
-template <bool KEEP, int ROWS> __device__ __forceinline__ void flags_of(const SelScanParams &p, int64_t b, int64_t t0, uint32_t &tok, uint32_t &first)
-{
-    const int64_t left = p.T - t0;
-    if (!KEEP) {
-        tok = left >= ROWS ? ~0u : (1u << (left > 0 ? left : 0)) - 1u;
-        first = 0;
-        return;
+// rows of a tile that are tokens, that are a document's first; their flags are asked for a tile before
+template <bool KEEP, int ROWS> struct Flags {
+    uint32_t tok, first;
+    int asked;
+    int64_t left;
+    __device__ __forceinline__ void request(const SelScanParams &p, int64_t b, int64_t t0)
+    {
+        left = p.T - t0;
+        const int i = threadIdx.x & 63;
+        if (KEEP) asked = i < ROWS && i < left ? p.keep[b * p.T + t0 + i] : 0;
     }
-    const int i = threadIdx.x & 63;
-    const int k = i < ROWS && i < left ? p.keep[b * p.T + t0 + i] : 0;
-    tok = (uint32_t)__ballot(k != 0);
-    first = (uint32_t)__ballot(k == 2);
-}
+    __device__ __forceinline__ void look()
+    {
+        if (KEEP) {
+            tok = (uint32_t)__ballot(asked != 0);
+            first = (uint32_t)__ballot(asked == 2);
+        } else {
+            tok = left >= ROWS ? ~0u : (1u << (left > 0 ? left : 0)) - 1u;
+            first = 0;
+        }
+    }
+};
 
 // rows in memory: `room` bytes from a tile's first row to the sequence's last.  What lies behind them reads as zero and is not written; so
 // does what a lane without a channel or state (offset OOB) asks for.
@@ -435,11 +444,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
     };
     // what the rows need once a token is found before the tile they are of begins: with few waves nothing else hides how long that takes
     float x[ROWS / 4], s[ROWS / 4], z[ROWS / 4], nx[ROWS / 4], ns[ROWS / 4], nz[ROWS / 4];
-    uint32_t tok, first, next_tok, next_first;
+    uint32_t tok, first;
+    Flags<KEEP, ROWS> next;
     auto once = [&]() {
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
-            const bool here = next_tok >> (4 * i + l) & 1;
+            const bool here = next.tok >> (4 * i + l) & 1;
             const float step = softplus(number<E>(qt.r[i]));
             nx[i] = here ? number<E>(qx.r[i]) : 0.0f;
             ns[i] = here ? step : 0.0f;
@@ -448,16 +458,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
         }
     };
     auto turn = [&]() {
-        tok = next_tok;
-        first = next_first;
+        tok = next.tok;
+        first = next.first;
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) { x[i] = nx[i]; s[i] = ns[i]; z[i] = nz[i]; }
     };
     float *const mine = &sb[threadIdx.x >> 6][0][0][0][0];
     constexpr int HALF = ROWS * 2 * LANES * R;
     request(0);
-    flags_of<KEEP, ROWS>(p, at_.b, T0, next_tok, next_first);
-    bc.put(mine, next_tok);
+    next.request(p, at_.b, T0);
+    next.look();
+    bc.put(mine, next.tok);
     once();
     turn();
     wave_lds_exchange();
@@ -467,46 +478,55 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
     for (int32_t tile = 0; tile < tiles; ++tile) {
         const int half = tile & 1;
         request(tile + 1);                                           // behind the chunk: zeros
-        flags_of<KEEP, ROWS>(p, at_.b, T0 + (int64_t)(tile + 1) * ROWS, next_tok, next_first);
+        next.request(p, at_.b, T0 + (int64_t)(tile + 1) * ROWS);
         if (!AHEAD && state) {
             at_.store(p, state, h);
             state += DN;
         }
+        // with a document's first row among them, and without: with it every row has its states masked (1 x 16384 x 2048 x 16, documents of some 400 tokens)
+        auto walk = [&](auto masked) {
 #pragma unroll
-        for (int i = 0; i < ROWS / 4; ++i) {
-            float sum[4];
-            const float v = s[i] * x[i];
-            if (AHEAD) total += s[i];
-            if (i + 1 == ROWS / 4) {
-                bc.put(mine + (half ^ 1) * HALF, next_tok);
-                once();
-                wave_lds_exchange();
-            }
-            auto row = [&](auto lane) {
-                constexpr int K = decltype(lane)::value;
-                const int t = 4 * i + K;
-                bcs.step(t, half);
-                if (KEEP && (first >> t & 1)) {
-                    began = true;
-#pragma unroll
-                    for (int r = 0; r < R; ++r) h[r] = 0.0f;
+            for (int i = 0; i < ROWS / 4; ++i) {
+                float sum[4];
+                const float v = s[i] * x[i];
+                if (AHEAD) total += s[i];
+                if (i + 1 == ROWS / 4) {
+                    next.look();
+                    bc.put(mine + (half ^ 1) * HALF, next.tok);
+                    once();
+                    wave_lds_exchange();
                 }
-                sum[K] = 0.0f;
+                auto row = [&](auto lane) {
+                    constexpr int K = decltype(lane)::value;
+                    const int t = 4 * i + K;
+                    bcs.step(t, half);
+                    if (masked && (first >> t & 1)) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    h[r] = __builtin_fmaf(exp2_(of_lane<K>(s[i]) * a2[r]), h[r], of_lane<K>(v) * bcs.B(t, r));
-                    if (!AHEAD) sum[K] = __builtin_fmaf(bcs.C(t, r), h[r], sum[K]);
+                        for (int r = 0; r < R; ++r) h[r] = 0.0f;
+                    }
+                    sum[K] = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        h[r] = __builtin_fmaf(exp2_(of_lane<K>(s[i]) * a2[r]), h[r], of_lane<K>(v) * bcs.B(t, r));
+                        if (!AHEAD) sum[K] = __builtin_fmaf(bcs.C(t, r), h[r], sum[K]);
+                    }
+                };
+                row(std::integral_constant<int, 0>{});
+                row(std::integral_constant<int, 1>{});
+                row(std::integral_constant<int, 2>{});
+                row(std::integral_constant<int, 3>{});
+                if (!AHEAD) {
+                    float y = __builtin_fmaf(skip, x[i], over_states(sum));
+                    if (GATED) y *= z[i];
+                    put<E>(to, off, 4 * i * line, !KEEP || (tok >> (4 * i + l) & 1) ? y : 0.0f);
                 }
-            };
-            row(std::integral_constant<int, 0>{});
-            row(std::integral_constant<int, 1>{});
-            row(std::integral_constant<int, 2>{});
-            row(std::integral_constant<int, 3>{});
-            if (!AHEAD) {
-                float y = __builtin_fmaf(skip, x[i], over_states(sum));
-                if (GATED) y *= z[i];
-                put<E>(to, off, 4 * i * line, !KEEP || (tok >> (4 * i + l) & 1) ? y : 0.0f);
             }
+        };
+        if (KEEP && first) {
+            began = true;
+            walk(std::true_type{});
+        } else {
+            walk(std::false_type{});
         }
         off += on;
         turn();
@@ -531,7 +551,7 @@ template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 4 : 2))) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles, float *shares, float *bc_shares)
 {
     constexpr int ROWS = rows_of(R), SUMS = sums_of(R);
-    const Place<R> at_(p, slabs);
+    const Place<R> at_(p, slabs, AHEAD ? 1 : 0);
     const int64_t DN = p.D * p.N;
     const int l = at_.l, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     __shared__ __attribute__((aligned(16))) float sb[4][2][ROWS][2][LANES * R];          // of every wave
@@ -575,11 +595,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
     };
     // once a token, a tile ahead.  dz: dy times the gate's slope
     float x[ROWS / 4], s[ROWS / 4], slope[ROWS / 4], du[ROWS / 4], dz[ROWS / 4], nx[ROWS / 4], ns[ROWS / 4], nslope[ROWS / 4], ndu[ROWS / 4], ndz[ROWS / 4];
-    uint32_t tok, first, next_tok, next_first;
+    uint32_t tok, first;
+    Flags<KEEP, ROWS> next;
     auto once = [&]() {
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
-            const bool here = at_.live && (next_tok >> (4 * i + l) & 1);     // channels that are not there add nothing to dB and dC
+            const bool here = at_.live && (next.tok >> (4 * i + l) & 1);     // channels that are not there add nothing to dB and dC
             const float step = softplus(number<E>(qt.r[i]), nslope[i]), dy = here ? number<E>(qd.r[i]) : 0.0f, z = GATED && here ? number<E>(qz.r[i]) : 0.0f;
             nx[i] = !AHEAD && here ? number<E>(qx.r[i]) : 0.0f;
             ns[i] = here ? step : 0.0f;
@@ -589,8 +610,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         }
     };
     auto turn = [&]() {
-        tok = next_tok;
-        first = next_first;
+        tok = next.tok;
+        first = next.first;
 #pragma unroll
         for (int i = 0; i < ROWS / 4; ++i) {
             x[i] = nx[i]; s[i] = ns[i]; slope[i] = nslope[i]; du[i] = ndu[i]; dz[i] = ndz[i];
@@ -603,8 +624,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
     float *const mine = &sb[wave][0][0][0][0];
     constexpr int HALF = ROWS * 2 * LANES * R;
     request(tiles - 1);
-    flags_of<KEEP, ROWS>(p, at_.b, T0 + (int64_t)(tiles - 1) * ROWS, next_tok, next_first);
-    bc.put(mine + ((tiles - 1) & 1) * HALF, next_tok);
+    next.request(p, at_.b, T0 + (int64_t)(tiles - 1) * ROWS);
+    next.look();
+    bc.put(mine + ((tiles - 1) & 1) * HALF, next.tok);
     once();
     turn();
     wave_lds_exchange();
@@ -615,10 +637,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         // in front of the chunk: what is asked for again is not used
         if (tile > 0) {
             request(tile - 1);
-            flags_of<KEEP, ROWS>(p, at_.b, T0 + (int64_t)(tile - 1) * ROWS, next_tok, next_first);
+            next.request(p, at_.b, T0 + (int64_t)(tile - 1) * ROWS);
         }
         auto stage = [&]() {
-            bc.put(mine + (half ^ 1) * HALF, next_tok);
+            next.look();
+            bc.put(mine + (half ^ 1) * HALF, next.tok);
             once();
             wave_lds_exchange();
         };
@@ -765,8 +788,7 @@ Form form_of(const SelScanParams &p)
     const int64_t tiles = (p.T + f.rows - 1) / f.rows;
     f.slabs = (int32_t)((p.D + CHANNELS - 1) / CHANNELS);
     const int64_t wgs = p.B * f.slabs;
-    int64_t chunks = 1;
-    if (wgs < 256) chunks = 512 / wgs;
+    int64_t chunks = wgs < 256 ? 256 / wgs : 1;
     const int64_t most = tiles * f.rows / 64;
     if (chunks > most) chunks = most > 0 ? most : 1;
     // a chunk's rows are reached by 31-bit offsets
@@ -791,12 +813,12 @@ Scratch scratch_of(const SelScanParams &p, const Form &f, bool grad)
 template <typename E, int R, bool KEEP, bool GATED>
 void go(bool grad, const SelScanParams &p, const Form &f, float *shares, float *bc, hipStream_t s)
 {
-    const dim3 grid((unsigned)(p.B * f.slabs * f.chunks)), wg(256);
+    const dim3 grid((unsigned)(p.B * f.slabs * f.chunks)), ahead((unsigned)(p.B * f.slabs * (f.chunks - 1))), wg(256);
     if (grad) {
-        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, true>), ahead, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
         hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
     } else {
-        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, false, true>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, false, true>), ahead, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
         hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
     }
 }
