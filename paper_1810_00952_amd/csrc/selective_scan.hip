@@ -403,7 +403,7 @@ __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanP
 // forward.  AHEAD: what a chunk makes of the state before it, into part ([chunk][b] P, H of [D][N])
 // ---------------------------------------------------------------------------
 template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_rows)
 {
     constexpr int ROWS = rows_of(R);
     const Place<R> at_(p, slabs);
@@ -426,7 +426,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
         }
     }
     const float skip = p.skip[at_.d];
-    const int64_t T0 = (int64_t)at_.chunk * chunk_tiles * ROWS, row0 = at_.b * p.T + T0, left = min(p.T - T0, (int64_t)chunk_tiles * ROWS);
+    const int64_t T0 = (int64_t)at_.chunk * chunk_rows, row0 = at_.b * p.T + T0, left = min(p.T - T0, (int64_t)chunk_rows);
     const int32_t tiles = (int32_t)((left + ROWS - 1) / ROWS);
     const uint32_t line = (uint32_t)(p.D * sizeof(E));
     auto rows = [&](const void *x) { return rows_at((const char *)x + row0 * line, x ? left * line : 0); };      // the chunk's
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
 // gradient, tiles from the last to the first.  AHEAD: what a chunk makes of the derivative behind it, into part
 // ---------------------------------------------------------------------------
 template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 4 : 2))) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_tiles, float *shares, float *bc_shares)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 4 : 2))) void selective_scan_grad_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_rows, float *shares, float *bc_shares)
 {
     constexpr int ROWS = rows_of(R), SUMS = sums_of(R);
     const Place<R> at_(p, slabs, AHEAD ? 1 : 0);
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         }
     }
     const float skip = p.skip[at_.d];
-    const int64_t T0 = (int64_t)at_.chunk * chunk_tiles * ROWS, row0 = at_.b * p.T + T0, left = min(p.T - T0, (int64_t)chunk_tiles * ROWS);
+    const int64_t T0 = (int64_t)at_.chunk * chunk_rows, row0 = at_.b * p.T + T0, left = min(p.T - T0, (int64_t)chunk_rows);
     const int32_t tiles = (int32_t)((left + ROWS - 1) / ROWS);
     const uint32_t line = (uint32_t)(p.D * sizeof(E));
     auto rows = [&](const void *x) { return rows_at((const char *)x + row0 * line, x ? left * line : 0); };      // the chunk's
@@ -777,25 +777,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
 
 namespace {
 
-struct Form { int R; int32_t slabs, chunks, chunk_tiles, rows; };
+struct Form { int R; int32_t slabs, chunks, chunk_rows; };
 
-Form form_of(const SelScanParams &p)
+// Chunks where there are fewer workgroups than CUs: of 64 rows and more, in whole tiles, as many as fill the CUs once with the
+// gradient's workgroups, whose registers are a CU's, twice with the forward pass' (1 x 16384 x 2048 x 16 bf16 forward 431 -> 378 us; 3 x 777 x 515 x 24 f32
+// gradient in 297 workgroups 91, in 243 61)
+Form form_of(const SelScanParams &p, bool grad)
 {
     Form f;
     f.R = 1;
     while (f.R * LANES < p.N) f.R *= 2;
-    f.rows = rows_of(f.R);
-    const int64_t tiles = (p.T + f.rows - 1) / f.rows;
+    const int64_t rows = rows_of(f.R), tiles = (p.T + rows - 1) / rows;
     f.slabs = (int32_t)((p.D + CHANNELS - 1) / CHANNELS);
-    const int64_t wgs = p.B * f.slabs;
-    int64_t chunks = wgs < 256 ? 256 / wgs : 1;
-    const int64_t most = tiles * f.rows / 64;
+    const int64_t wgs = p.B * f.slabs, most = tiles * rows / 64;
+    int64_t chunks = wgs < 256 ? (grad ? 256 : 512) / wgs : 1;
     if (chunks > most) chunks = most > 0 ? most : 1;
     // a chunk's rows are reached by 31-bit offsets
-    const int64_t line = std::max(p.D, 2 * p.N) * (p.dtype == DT_BF16 ? 2 : 4), reach = ((int64_t)1 << 30) / (line * f.rows);
+    const int64_t line = std::max(p.D, 2 * p.N) * (p.dtype == DT_BF16 ? 2 : 4), reach = ((int64_t)1 << 30) / (line * rows);
     if (chunks < (tiles + reach - 1) / reach) chunks = (tiles + reach - 1) / reach;
-    f.chunk_tiles = (int32_t)((tiles + chunks - 1) / chunks);
-    f.chunks = (int32_t)((tiles + f.chunk_tiles - 1) / f.chunk_tiles);
+    const int64_t each = (tiles + chunks - 1) / chunks;
+    f.chunk_rows = (int32_t)(each * rows);
+    f.chunks = (int32_t)((tiles + each - 1) / each);
     return f;
 }
 
@@ -815,11 +817,11 @@ void go(bool grad, const SelScanParams &p, const Form &f, float *shares, float *
 {
     const dim3 grid((unsigned)(p.B * f.slabs * f.chunks)), ahead((unsigned)(p.B * f.slabs * (f.chunks - 1))), wg(256);
     if (grad) {
-        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, true>), ahead, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
-        hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles, shares, bc);
+        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, true>), ahead, wg, 0, s, p, f.slabs, f.chunks, f.chunk_rows, shares, bc);
+        hipLaunchKernelGGL((selective_scan_grad_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_rows, shares, bc);
     } else {
-        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, false, true>), ahead, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
-        hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_tiles);
+        if (f.chunks > 1) hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, false, true>), ahead, wg, 0, s, p, f.slabs, f.chunks, f.chunk_rows);
+        hipLaunchKernelGGL((selective_scan_kernel<E, R, KEEP, GATED, false>), grid, wg, 0, s, p, f.slabs, f.chunks, f.chunk_rows);
     }
 }
 
@@ -877,22 +879,22 @@ template <typename E> hipError_t go_step(const SelScanParams &p, int R, hipStrea
 bool sel_scan_fits(const SelScanParams &p, bool grad)
 {
     if (p.B < 1 || p.T < 1 || p.D < 1 || p.N < 1 || p.N > SSM_MAX_STATES || p.B > 0x7fffffff || p.T > 0x7fffffff || p.D > SCAN_MAX_D) return false;
-    const Form f = form_of(p);
+    const Form f = form_of(p, grad);
     // the sums over channels are a launch of a thousand threads a 64 columns
     return launch_has(p.B * f.slabs * f.chunks, 256) && (!grad || (p.B * p.T * 2 * p.N + 63) / 64 <= 0x3fffff);
 }
 
-int64_t sel_scan_state_rows(const SelScanParams &p) { return form_of(p).rows; }
+int64_t sel_scan_state_rows(const SelScanParams &p) { return rows_of(form_of(p, true).R); }
 
 int64_t sel_scan_part_floats(const SelScanParams &p, bool grad)
 {
-    const Scratch s = scratch_of(p, form_of(p), grad);
+    const Scratch s = scratch_of(p, form_of(p, grad), grad);
     return s.chunks + s.shares + s.bc;
 }
 
 hipError_t launch_sel_scan(const SelScanParams &p, hipStream_t s)
 {
-    const Form f = form_of(p);
+    const Form f = form_of(p, false);
     if (!sel_scan_fits(p, false) || (f.chunks > 1 && !p.part) || p.gated != (p.z != nullptr) || p.keeps != (p.keep != nullptr)) return hipErrorInvalidValue;
     if (p.T == 1 && !p.states) {
         if (!p.y || !p.hT) return hipErrorInvalidValue;
@@ -904,7 +906,7 @@ hipError_t launch_sel_scan(const SelScanParams &p, hipStream_t s)
 hipError_t launch_sel_scan_grad(const SelScanParams &p, hipStream_t s)
 {
     if (!sel_scan_fits(p, true) || !p.part || !p.states || p.gated != (p.z != nullptr) || p.keeps != (p.keep != nullptr)) return hipErrorInvalidValue;
-    const Form f = form_of(p);
+    const Form f = form_of(p, true);
     return p.dtype == DT_BF16 ? go<uint16_t>(true, p, f, s) : go<float>(true, p, f, s);
 }
 
