@@ -45,67 +45,217 @@ __device__ __forceinline__ Soft join(Soft a, Soft b)
     return {m, __builtin_fmaf(a.s, fa, b.s * fb)};
 }
 
-// ---- what becomes of a tile's sums.  A lane has row m of x and of w's rows n = n0 + 8 k + i, k, i < 4 (n0 counts the lane's half) --------------
+// ---- what becomes of a tile's sums --------------------------------------------------------------------------------------------
+// A lane has row m of x and, of every 32 of w's rows from n on, those at 8 k + 4 (its half of the wave) + i, k, i < 4.
+
+// n .. n + 31 of row m as bf16, 16 bytes at a time: the halves of the wave swap what they hold of eight columns
+__device__ __forceinline__ void put_row(uint16_t *to, const uint32_t (&c)[4][2], int half, bool in, int64_t n, int64_t N)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        u32x4 out;
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            const auto got = __builtin_amdgcn_permlane32_swap(c[2 * h][d], c[2 * h + 1][d], false, false);
+            out[d] = got[0]; out[2 + d] = got[1];
+        }
+        const int at = 16 * h + 8 * half;
+        if (in && n + at < N) *(u32x4 *)(to + at) = out;
+    }
+#endif
+}
+
 struct StatsEpi {
     float2 *part; float *hit; const int32_t *tok; int64_t M, V;
-    static constexpr bool STATS = true;
+
+    // WN waves' maxima and sums meet in `lds`
+    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t bn, int wm, int wn, unsigned char *lds) const
+    {
+        constexpr int BM = WM * TM * 32;
+        const int lane = threadIdx.x & 63, frow = lane & 31, half = lane >> 5;
+        Soft *const seen = (Soft *)lds;                             // [WN][BM]
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = m0 + (wm * TM + i) * 32 + frow;
+            const int32_t at = m < M ? tok[m] : -1;
+            Soft s{-INFINITY, 0.0f};
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int64_t nj = n0 + (wn * TN + j) * 32;
+                if (nj + 32 > V) {                                  // columns behind the last
+#pragma unroll
+                    for (int q = 0; q < 16; ++q)
+                        if (nj + 4 * half + 8 * (q >> 2) + (q & 3) >= V) acc[i][j][q] = -INFINITY;
+                }
+                const int64_t rel = at - nj - 4 * half;            // of the lane's columns: bit 2 clear, below 32
+                if (at >= 0 && at < V && rel >= 0 && rel < 32 && (rel & 4) == 0) {
+#pragma unroll
+                    for (int q = 0; q < 16; ++q)
+                        if (rel == 8 * (q >> 2) + (q & 3)) hit[m] = acc[i][j][q];
+                }
+#pragma unroll
+                for (int q = 0; q < 16; ++q) s.m = fmaxf(s.m, acc[i][j][q]);
+            }
+            // of NaN a maximum is the other number: the sum has it
+            const float top = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) s.s += __expf(acc[i][j][q] - top);
+            Soft o{__shfl_xor(s.m, 32), __shfl_xor(s.s, 32)};
+            s = join(s, o);
+            if (half == 0) seen[wn * BM + (wm * TM + i) * 32 + frow] = s;
+        }
+        __syncthreads();
+        for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
+            if (m0 + r >= M) break;
+            Soft s = seen[r];
+#pragma unroll
+            for (int w = 1; w < WN; ++w) s = join(s, seen[w * BM + r]);
+            part[(int64_t)bn * M + m0 + r] = float2{s.m, s.s};
+        }
+    }
 };
+
+// dl to g, as it lies, and to gt, transposed
 template <typename E> struct GradEpi {
     E *g, *gt; int64_t ldg, ldgt;             // elements
     const int32_t *tok; const float *lse, *dlp, *dlse;
-    int64_t M, V, v0, Vp, Mp;                 // columns v0 .. of the vocabulary; Vp of them are written, Mp rows
-    static constexpr bool STATS = false;
-    struct Row { float lse, one, all; int32_t tok; };
-    __device__ __forceinline__ Row row(int64_t m) const
+    int64_t M, V, v0, Vp, Mp;                 // columns v0 .. of the vocabulary; Vp of them are written, Mp rows: multiples of 128 bytes
+
+    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t, int wm, int wn, unsigned char *lds) const
     {
-        Row r{0.0f, 0.0f, 0.0f, -1};
-        if (m >= M) return r;
-        r.tok = tok[m];
-        const bool given = r.tok >= 0 && r.tok < V;
-        r.lse = lse[m] == -INFINITY ? INFINITY : lse[m];      // of no logits: p is 0
-        r.one = given ? dlp[m] : 0.0f;
-        r.all = dlse[m] - r.one;
-        return r;
-    }
-    __device__ __forceinline__ void put(int64_t m, int64_t n, const f32x4 &l, const Row &r) const
-    {
-        f32x4 v;
+        const int lane = threadIdx.x & 63, frow = lane & 31, half = lane >> 5;
+        float end[TM], one[TM], all[TM];      // lse, dlp, dlse - dlp of the lane's rows
+        int32_t at[TM];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t col = v0 + n + i;
-            const float p = __expf(l[i] - r.lse);
-            v[i] = (r.one == 0.0f && r.all == 0.0f) || col >= V ? 0.0f : __builtin_fmaf(r.all, p, col == r.tok ? r.one : 0.0f);
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = m0 + (wm * TM + i) * 32 + frow;
+            const bool in = m < M;
+            at[i] = in ? tok[m] : -1;
+            const bool given = at[i] >= 0 && at[i] < V;
+            end[i] = in ? lse[m] : 0.0f;
+            if (end[i] == -INFINITY) end[i] = INFINITY;            // of no logits: p is 0
+            one[i] = in && given ? dlp[m] : 0.0f;
+            all[i] = in ? dlse[m] - one[i] : 0.0f;
         }
+        constexpr int ROW = TM * 64 + 32;     // bytes of a row of the transposed block in LDS, 32 behind its 32 TM bf16: rows begin at other banks
+        unsigned char *const block = lds + (wm * WN + wn) * 32 * ROW;
+        const int64_t mw = m0 + wm * TM * 32;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (n + i >= Vp) continue;
-            if (m < M) store(g, m * ldg + n + i, v[i]);
-            if (m < Mp) store(gt, (n + i) * ldgt + m, v[i]);
+        for (int j = 0; j < TN; ++j) {
+            const int64_t nj = n0 + (wn * TN + j) * 32;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int64_t m = mw + i * 32 + frow;
+                const bool none = one[i] == 0.0f && all[i] == 0.0f;
+                const int64_t rel = at[i] - v0 - nj - 4 * half;
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const int col = 8 * (q >> 2) + (q & 3);
+                    const float v = __builtin_fmaf(all[i], __expf(acc[i][j][q] - end[i]), rel == col ? one[i] : 0.0f);
+                    acc[i][j][q] = none || v0 + nj + 4 * half + col >= V ? 0.0f : v;
+                }
+                if constexpr (sizeof(E) == 4) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int64_t n = nj + 8 * k + 4 * half;
+                        const f32x4 v = {acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
+                        if (n < Vp) {
+                            if (m < M) *(f32x4 *)(g + m * ldg + n) = v;
+                            if (m < Mp) {
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) gt[(n + c) * ldgt + m] = v[c];
+                            }
+                        }
+                    }
+                } else {
+                    uint32_t c[4][2];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int d = 0; d < 2; ++d) c[k][d] = pack_bf16x2(acc[i][j][4 * k + 2 * d], acc[i][j][4 * k + 2 * d + 1]);
+                    // two rows' numbers of one column are a word of the transposed block: an even lane takes the first of two columns, an odd one the other
+                    const bool odd = lane & 1;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int d = 0; d < 2; ++d) {
+                            const uint32_t mine = c[k][d], other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0xb1, 0xf, 0xf, true);
+                            const uint32_t word = odd ? (other >> 16) | (mine & 0xffff0000u) : (mine & 0xffffu) | (other << 16);
+                            *(uint32_t *)(block + (8 * k + 4 * half + 2 * d + (odd ? 1 : 0)) * ROW + i * 64 + (frow & 30) * 2) = word;
+                        }
+                    put_row((uint16_t *)g + m * ldg + nj, c, half, m < M, nj, Vp);
+                }
+            }
+            if constexpr (sizeof(E) == 2) {
+                wave_lds_exchange();
+                constexpr int PER = TM * 4;                         // 16-byte pieces of a row
+#pragma unroll
+                for (int r = 0; r < 32 * PER / 64; ++r) {
+                    const int q = r * 64 + lane, n = q / PER, c = q % PER;
+                    const u32x4 v = *(const u32x4 *)(block + n * ROW + c * 16);
+                    if (nj + n < Vp && mw + c * 8 < Mp) *(u32x4 *)(gt + (nj + n) * ldgt + mw + c * 8) = v;
+                }
+                wave_lds_exchange();
+            }
         }
-    }
-    static __device__ __forceinline__ void store(E *p, int64_t i, float v)
-    {
-        if constexpr (sizeof(E) == 4) p[i] = v;
-        else p[i] = (uint16_t)pack_bf16x2(v, v);
     }
 };
+
 // c (+ what was added up before) to y or, of a slice of K, to its share
 struct OutEpi {
     void *y; const float *before; float *sum;  // sum: f32, in place of y
     int64_t M, N; int32_t y_dtype;
-    static constexpr bool STATS = false;
-    struct Row {};
-    __device__ __forceinline__ Row row(int64_t) const { return {}; }
-    __device__ __forceinline__ void put(int64_t m, int64_t n, const f32x4 &c, const Row &) const
+
+    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t, int wm, int wn, unsigned char *) const
     {
-        if (m >= M) return;
+        const int lane = threadIdx.x & 63, frow = lane & 31, half = lane >> 5;
+        const bool fours = N % 4 == 0, eights = N % 8 == 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (n + i >= N) continue;
-            const int64_t at = m * N + n + i;
-            const float v = before ? c[i] + before[at] : c[i];
-            if (sum) sum[at + (int64_t)blockIdx.y * M * N] = v;
-            else store_from_f32(y, y_dtype, at, v);
+        for (int i = 0; i < TM; ++i) {
+            const int64_t m = m0 + (wm * TM + i) * 32 + frow;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int64_t nj = n0 + (wn * TN + j) * 32;
+                f32x4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[k] = f32x4{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
+                    const int64_t n = nj + 8 * k + 4 * half, to = m * N + n;
+                    if (before && m < M) {
+                        if (fours) {
+                            if (n < N) v[k] += *(const f32x4 *)(before + to);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                if (n + c < N) v[k][c] += before[to + c];
+                        }
+                    }
+                }
+                if (!sum && y_dtype == DT_BF16 && eights) {
+                    uint32_t c[4][2];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int d = 0; d < 2; ++d) c[k][d] = pack_bf16x2(v[k][2 * d], v[k][2 * d + 1]);
+                    put_row((uint16_t *)y + m * N + nj, c, half, m < M, nj, N);
+                    continue;
+                }
+                if (m >= M) continue;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t n = nj + 8 * k + 4 * half, to = m * N + n;
+                    if (fours && (sum || y_dtype != DT_BF16)) {
+                        if (n < N) *(f32x4 *)((sum ? sum : (float *)y) + to) = v[k];
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (n + c < N) store_from_f32(sum ? (void *)sum : y, sum ? DT_F32 : y_dtype, to + c, v[k][c]);
+                    }
+                }
+            }
         }
     }
 };
@@ -116,7 +266,7 @@ struct OutEpi {
 // WM x WN waves, each TM x TN groups of 32 rows of x and of w
 // ---------------------------------------------------------------------------
 template <typename E, int WM, int WN, int TM, int TN, typename Epi>
-__global__ __launch_bounds__(64 * WM * WN) void nt_tile_kernel(const NtParams p, const Epi epi)
+__device__ __forceinline__ void nt_tile(const NtParams &p, const Epi &epi, int32_t block, int32_t slice)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int BM = WM * TM * 32, BN = WN * TN * 32, W = WM * WN, X_BYTES = BM * 128, STAGE = (BM + BN) * 128;
@@ -132,7 +282,7 @@ __global__ __launch_bounds__(64 * WM * WN) void nt_tile_kernel(const NtParams p,
     int32_t bm, bn;
     {
         constexpr int GN = 8;
-        const int32_t bid = xcd_run(blockIdx.x, p.nblk_m * p.nblk_n), grp = bid / (GN * p.nblk_m), within = bid - grp * GN * p.nblk_m;
+        const int32_t bid = xcd_run(block, p.nblk_m * p.nblk_n), grp = bid / (GN * p.nblk_m), within = bid - grp * GN * p.nblk_m;
         const int32_t gw = min(GN, p.nblk_n - grp * GN);
         bm = within / gw; bn = grp * GN + (within - bm * gw);
     }
@@ -153,7 +303,7 @@ __global__ __launch_bounds__(64 * WM * WN) void nt_tile_kernel(const NtParams p,
         voff[i] = in ? (uint32_t)row * (uint32_t)(x ? p.ldx : p.ldw) + chunk * 16 : OOB;
         room[i] = in ? p.kbytes - chunk * 16 : 0;
     }
-    int32_t f_kt = blockIdx.y * p.split_lines;
+    int32_t f_kt = slice * p.split_lines;
     const int32_t end = min(f_kt + p.split_lines, p.nk), lines = end - f_kt;
     int32_t f_at = 0;
     bool f_live = true;
@@ -228,77 +378,56 @@ __global__ __launch_bounds__(64 * WM * WN) void nt_tile_kernel(const NtParams p,
     if (kt < lines) body(st0, st1);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the trailing requests; from here the stages are free
 
-    if constexpr (Epi::STATS) {
-        Soft *const seen = (Soft *)st0;                             // [WN][BM]
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t m = m0 + (wm * TM + i) * 32 + frow;
-            const int32_t tok = m < epi.M ? epi.tok[m] : -1;
-            Soft s{-INFINITY, 0.0f};
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int64_t nj = n0 + (wn * TN + j) * 32 + 4 * fhalf;
-#pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const int64_t n = nj + 8 * (q >> 2) + (q & 3);
-                    const float l = n < epi.V ? acc[i][j][q] : -INFINITY;
-                    acc[i][j][q] = l;
-                    if (n == tok && n < epi.V) epi.hit[m] = l;
-                    s.m = fmaxf(s.m, l);
-                }
-            }
-            // of NaN a maximum is the other number: the sum has it
-            const float top = s.m == -INFINITY ? 0.0f : s.m;
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) s.s += __expf(acc[i][j][q] - top);
-            Soft o{__shfl_xor(s.m, 32), __shfl_xor(s.s, 32)};
-            s = join(s, o);
-            if (fhalf == 0) seen[wn * BM + (wm * TM + i) * 32 + frow] = s;
-        }
-        __syncthreads();
-        for (int r = t; r < BM; r += 64 * W) {
-            if (m0 + r >= epi.M) break;
-            Soft s = seen[r];
-#pragma unroll
-            for (int w = 1; w < WN; ++w) s = join(s, seen[w * BM + r]);
-            epi.part[(int64_t)bn * epi.M + m0 + r] = float2{s.m, s.s};
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t m = m0 + (wm * TM + i) * 32 + frow;
-            const auto row = epi.row(m);
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    epi.put(m, n0 + (wn * TN + j) * 32 + 8 * k + 4 * fhalf, f32x4{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]}, row);
-        }
-    }
+    epi.template operator()<WM, WN, TM, TN>(acc, m0, n0, bn, wm, wn, st0);
 #endif
 }
 
-// ---------------------------------------------------------------------------
-// rows' sums of all tiles; eight threads a row
-// ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void dense_logprobs_join_kernel(const float2 *part, const float *hit, const int32_t *tok, float *lp, float *lse, int64_t M, int64_t V, int32_t tiles)
+template <typename E, int WM, int WN, int TM, int TN, typename Epi>
+__global__ __launch_bounds__(64 * WM * WN) void nt_tile_kernel(const NtParams p, const Epi epi)
 {
-    __shared__ Soft seen[8][32];
-    const int r = threadIdx.x & 31, share = threadIdx.x >> 5;
-    const int64_t m = (int64_t)blockIdx.x * 32 + r;
+    nt_tile<E, WM, WN, TM, TN>(p, epi, blockIdx.x, 0);
+}
+
+// dx's product, its slices of K one behind the other, and dw's
+template <typename E, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN) void nt_pair_kernel(const NtParams a, OutEpi ea, int32_t slices, const NtParams b, const OutEpi eb)
+{
+    const int32_t tiles = a.nblk_m * a.nblk_n, bid = (int32_t)blockIdx.x;
+    const bool first = bid < tiles * slices;
+    const int32_t slice = first ? bid / tiles : 0;
+    if (ea.sum) ea.sum += (int64_t)slice * ea.M * ea.N;
+    nt_tile<E, WM, WN, TM, TN>(first ? a : b, first ? ea : eb, first ? bid - slice * tiles : bid - tiles * slices, slice);
+}
+
+// ---------------------------------------------------------------------------
+// rows' sums of all tiles; ROWS rows a workgroup, 1024 / ROWS threads a row
+// ---------------------------------------------------------------------------
+template <int ROWS>
+__global__ __launch_bounds__(1024) void dense_logprobs_join_kernel(const float2 *part, const float *hit, const int32_t *tok, float *lp, float *lse, int64_t M, int64_t V, int32_t tiles)
+{
+    constexpr int SHARES = 1024 / ROWS;
+    __shared__ Soft seen[SHARES][ROWS];
+    const int r = threadIdx.x % ROWS, share = threadIdx.x / ROWS;
+    const int64_t m = (int64_t)blockIdx.x * ROWS + r;
     Soft s{-INFINITY, 0.0f};
-    if (m < M)
-        for (int32_t t = share; t < tiles; t += 8) {
+    if (m < M) {
+#pragma unroll 4
+        for (int32_t t = share; t < tiles; t += SHARES) {
             const float2 v = part[(int64_t)t * M + m];
             s = join(s, Soft{v.x, v.y});
         }
+    }
     seen[share][r] = s;
     __syncthreads();
-    if (share == 0 && m < M) {
 #pragma unroll
-        for (int k = 1; k < 8; ++k) s = join(s, seen[k][r]);
+    for (int n = SHARES / 2; n > 0; n /= 2) {
+        if (share < n) {
+            s = join(s, seen[share + n][r]);
+            seen[share][r] = s;
+        }
+        __syncthreads();
+    }
+    if (share == 0 && m < M) {
         const float all = s.m == INFINITY ? __uint_as_float(0x7fc00000u) : s.m + __logf(s.s);
         const int32_t at = tok[m];
         lse[m] = all;
@@ -338,14 +467,55 @@ constexpr int64_t LINE = 128, PIECE_MAX = 1 << 20;      // a piece's columns: a 
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 size_t esize(const DenseLogprobsParams &p) { return p.dtype == DT_BF16 ? 2 : 4; }
 
-template <typename E, typename Epi>
-void go_nt(NtParams q, const Epi &epi, int32_t splits, hipStream_t s)
+// Which tile, by an estimate of the time: us per 128-byte line of K of a workgroup that is alone on its CU, and per line and 256 workgroups where there are more
+struct Tile { int32_t side, threads; float alone, share; };
+constexpr Tile tiles_bf16[] = {{64, 256, 0.70f, 0.25f}, {128, 256, 0.95f, 0.62f}, {256, 512, 1.60f, 2.00f}};
+constexpr Tile tiles_f32[] = {{64, 256, 1.00f, 0.50f}, {128, 256, 3.60f, 1.85f}};
+int64_t tiles_along(int64_t n, int64_t side) { return (n + side - 1) / side; }
+// of the products [M, N] (and [M2, N2], in the same launch, as many lines of K), `slices` times the first one's tiles
+template <typename E> int32_t tile_of(int64_t M, int64_t N, int64_t slices = 1, int64_t M2 = 0, int64_t N2 = 0)
 {
-    q.nblk_m = (int32_t)((q.M + 127) / 128);
-    q.nblk_n = (int32_t)((q.N + 127) / 128);
+    int32_t best = 0;
+    float least = INFINITY;
+    auto look = [&](const Tile &t) {
+        const float wgs = (float)(tiles_along(M, t.side) * tiles_along(N, t.side) * slices + tiles_along(M2, t.side) * tiles_along(N2, t.side));
+        const float line = fmaxf(t.alone, t.share * wgs / 256.0f);
+        if (line < least) { least = line; best = t.side; }
+    };
+    if constexpr (sizeof(E) == 2) for (const Tile &t : tiles_bf16) look(t);
+    else for (const Tile &t : tiles_f32) look(t);
+    return best;
+}
+
+template <typename E> void split(NtParams &q, int32_t side, int32_t slices)
+{
+    q.nblk_m = (int32_t)tiles_along(q.M, side);
+    q.nblk_n = (int32_t)tiles_along(q.N, side);
     q.nk = (int32_t)((q.kbytes + LINE - 1) / LINE);
-    q.split_lines = (q.nk + splits - 1) / splits;
-    hipLaunchKernelGGL((nt_tile_kernel<E, 2, 2, 2, 2, Epi>), dim3((unsigned)((int64_t)q.nblk_m * q.nblk_n), (unsigned)splits), dim3(256), 0, s, q, epi);
+    q.split_lines = (q.nk + slices - 1) / slices;
+}
+
+template <typename E, typename Epi> void go_nt(NtParams q, const Epi &epi, int32_t side, hipStream_t s)
+{
+    split<E>(q, side, 1);
+    const dim3 grid((unsigned)((int64_t)q.nblk_m * q.nblk_n));
+    if constexpr (sizeof(E) == 2) {
+        if (side == 256) { hipLaunchKernelGGL((nt_tile_kernel<E, 2, 4, 4, 2, Epi>), grid, dim3(512), 0, s, q, epi); return; }
+    }
+    if (side == 128) hipLaunchKernelGGL((nt_tile_kernel<E, 2, 2, 2, 2, Epi>), grid, dim3(256), 0, s, q, epi);
+    else hipLaunchKernelGGL((nt_tile_kernel<E, 2, 2, 1, 1, Epi>), grid, dim3(256), 0, s, q, epi);
+}
+
+template <typename E> void go_pair(NtParams a, const OutEpi &ea, int32_t slices, NtParams b, const OutEpi &eb, int32_t side, hipStream_t s)
+{
+    split<E>(a, side, slices);
+    split<E>(b, side, 1);
+    const dim3 grid((unsigned)((int64_t)a.nblk_m * a.nblk_n * slices + (int64_t)b.nblk_m * b.nblk_n));
+    if constexpr (sizeof(E) == 2) {
+        if (side == 256) { hipLaunchKernelGGL((nt_pair_kernel<E, 2, 4, 4, 2>), grid, dim3(512), 0, s, a, ea, slices, b, eb); return; }
+    }
+    if (side == 128) hipLaunchKernelGGL((nt_pair_kernel<E, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, ea, slices, b, eb);
+    else hipLaunchKernelGGL((nt_pair_kernel<E, 2, 2, 1, 1>), grid, dim3(256), 0, s, a, ea, slices, b, eb);
 }
 
 // Pieces of the vocabulary: columns of one, and how many slices of K dx's product takes (one piece only)
@@ -393,13 +563,14 @@ template <typename E> hipError_t forward(const DenseLogprobsParams &p, hipStream
 {
     NtParams q{};
     q.x = p.x; q.w = p.w; q.M = p.M; q.N = p.V; q.ldx = p.ldx; q.ldw = p.ldw; q.kbytes = (int32_t)up(p.K * sizeof(E), 16);
-    const int32_t tiles = (int32_t)((p.V + 127) / 128);
+    const int32_t side = tile_of<E>(p.M, p.V), tiles = (int32_t)tiles_along(p.V, side);
     StatsEpi epi{};
     epi.part = (float2 *)p.part; epi.hit = (float *)p.part + 2 * (int64_t)tiles * p.M; epi.tok = p.tok; epi.M = p.M; epi.V = p.V;
-    go_nt<E>(q, epi, 1, s);
+    go_nt<E>(q, epi, side, s);
     hipError_t er = hipGetLastError();
     if (er != hipSuccess) return er;
-    hipLaunchKernelGGL(dense_logprobs_join_kernel, dim3((unsigned)((p.M + 31) / 32)), dim3(256), 0, s, epi.part, epi.hit, p.tok, p.lp, p.lse, p.M, p.V, tiles);
+    if (p.M >= 1024) hipLaunchKernelGGL((dense_logprobs_join_kernel<32>), dim3((unsigned)((p.M + 31) / 32)), dim3(1024), 0, s, epi.part, epi.hit, p.tok, p.lp, p.lse, p.M, p.V, tiles);
+    else hipLaunchKernelGGL((dense_logprobs_join_kernel<4>), dim3((unsigned)((p.M + 3) / 4)), dim3(1024), 0, s, epi.part, epi.hit, p.tok, p.lp, p.lse, p.M, p.V, tiles);
     return hipGetLastError();
 }
 
@@ -429,7 +600,7 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         ge.g = g; ge.gt = gt; ge.ldg = Vp; ge.ldgt = Mp; ge.tok = p.tok; ge.lse = p.lse_in; ge.dlp = p.dlp; ge.dlse = p.dlse;
         ge.M = p.M; ge.V = p.V; ge.v0 = v0; ge.Vp = Vp; ge.Mp = Mp;
         q.M = p.M; q.N = cols;                   // rows of x and w that are there; the tiles cover the padding behind them
-        go_nt<E>(q, ge, 1, s);
+        go_nt<E>(q, ge, tile_of<E>(p.M, cols), s);
         NtParams a{};
         a.x = g; a.w = wt; a.M = p.M; a.N = p.K; a.ldx = a.ldw = Vp * e; a.kbytes = (int32_t)(Vp * e);
         OutEpi o{};
@@ -440,12 +611,11 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
             o.before = i > 0 ? acc : nullptr;
             o.sum = i + 1 < k.count ? acc : nullptr;
         }
-        go_nt<E>(a, o, k.slices, s);
         NtParams b{};
         b.x = gt; b.w = xt; b.M = cols; b.N = p.K; b.ldx = b.ldw = Mp * e; b.kbytes = (int32_t)(Mp * e);
         OutEpi d{};
         d.M = cols; d.N = p.K; d.y = (E *)p.dw + v0 * p.K; d.y_dtype = p.dtype;
-        go_nt<E>(b, d, 1, s);
+        go_pair<E>(a, o, k.slices, b, d, tile_of<E>(p.M, p.K, k.slices, cols, p.K), s);
     }
     hipError_t er = hipGetLastError();
     if (er != hipSuccess || k.slices == 1) return er;
@@ -460,13 +630,13 @@ bool dense_logprobs_fits(const DenseLogprobsParams &p, bool grad)
 {
     // a row's bytes, and those of a row of the transposed operands, are reached by 31-bit offsets from a tile's first row
     if (p.M < 1 || p.V < 1 || p.K < 1 || p.M > DENSE_LOGPROBS_MAX_ROWS || p.V > 0x7fffffff || p.K > DENSE_LOGPROBS_MAX_K) return false;
-    if (!launch_has(((p.M + 127) / 128) * ((p.V + 127) / 128), 256)) return false;
+    if (!launch_has(((p.M + 63) / 64) * ((p.V + 63) / 64), 256)) return false;
     return !grad || (p.M * p.K + 63) / 64 <= 0x3fffff;
 }
 
 int64_t dense_logprobs_part_bytes(const DenseLogprobsParams &p, bool grad)
 {
-    if (!grad) return (2 * ((p.V + 127) / 128) + 1) * p.M * 4;
+    if (!grad) return (2 * ((p.V + 63) / 64) + 1) * p.M * 4;
     return layout_of(p, pieces_of(p)).bytes;
 }
 
