@@ -46,7 +46,7 @@ __device__ __forceinline__ Soft join(Soft a, Soft b)
 }
 
 // ---- what becomes of a tile's sums --------------------------------------------------------------------------------------------
-// A lane has row m of x and, of every 32 of w's rows from n on, those at 8 k + 4 (its half of the wave) + i, k, i < 4.
+// lds is the workgroup's, of its wave's number times 1 KB and more; own, of TM times 4 KB, the wave's.  A lane has row m of x and, of every 32 of w's rows from n on, those at 8 k + 4 (its half of the wave) + i, k, i < 4.
 
 // n .. n + 31 of row m as bf16, 16 bytes at a time: the halves of the wave swap what they hold of eight columns
 __device__ __forceinline__ void put_row(uint16_t *to, const uint32_t (&c)[4][2], int half, bool in, int64_t n, int64_t N)
@@ -70,7 +70,7 @@ struct StatsEpi {
     float2 *part; float *hit; const int32_t *tok; int64_t M, V;
 
     // WN waves' maxima and sums meet in `lds`
-    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t bn, int wm, int wn, unsigned char *lds) const
+    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t bn, int wm, int wn, unsigned char *lds, unsigned char *own) const
     {
         constexpr int BM = WM * TM * 32;
         const int lane = threadIdx.x & 63, frow = lane & 31, half = lane >> 5;
@@ -124,7 +124,7 @@ template <typename E> struct GradEpi {
     const int32_t *tok; const float *lse, *dlp, *dlse;
     int64_t M, V, v0, Vp, Mp;                 // columns v0 .. of the vocabulary; Vp of them are written, Mp rows: multiples of 128 bytes
 
-    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t, int wm, int wn, unsigned char *lds) const
+    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t, int wm, int wn, unsigned char *lds, unsigned char *own) const
     {
         const int lane = threadIdx.x & 63, frow = lane & 31, half = lane >> 5;
         float end[TM], one[TM], all[TM];      // lse, dlp, dlse - dlp of the lane's rows
@@ -141,7 +141,8 @@ template <typename E> struct GradEpi {
             all[i] = in ? dlse[m] - one[i] : 0.0f;
         }
         constexpr int ROW = TM * 64 + 32;     // bytes of a row of the transposed block in LDS, 32 behind its 32 TM bf16: rows begin at other banks
-        unsigned char *const block = lds + (wm * WN + wn) * 32 * ROW;
+        static_assert(32 * ROW <= TM * 4096, "the wave's own part of LDS");
+        unsigned char *const block = own;
         const int64_t mw = m0 + wm * TM * 32;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -209,7 +210,7 @@ struct OutEpi {
     void *y; const float *before; float *sum;  // sum: f32, in place of y
     int64_t M, N; int32_t y_dtype;
 
-    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t, int wm, int wn, unsigned char *) const
+    template <int WM, int WN, int TM, int TN> __device__ __forceinline__ void operator()(f32x16 (&acc)[TM][TN], int64_t m0, int64_t n0, int32_t, int wm, int wn, unsigned char *, unsigned char *) const
     {
         const int lane = threadIdx.x & 63, frow = lane & 31, half = lane >> 5;
         const bool fours = N % 4 == 0, eights = N % 8 == 0;
@@ -269,11 +270,15 @@ template <typename E, int WM, int WN, int TM, int TN, typename Epi>
 __device__ __forceinline__ void nt_tile(const NtParams &p, const Epi &epi, int32_t block, int32_t slice)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, W = WM * WN, X_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-    constexpr int LPT = (BM + BN) / 8 / W, XL = BM / 8 / W;        // direct loads per wave and tile, those of x first
-    static_assert((BM / 8) % W == 0 && (BN / 8) % W == 0 && LPT % 2 == 0, "a tile's loads in whole halves of every wave's");
-    __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE];
-    __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGE];
+    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, W = WM * WN, UNIT = BM * 128;
+    constexpr int XL = BM / 8 / W, LPT = 2 * XL;                   // direct loads per wave: of a unit, of a line of both
+    static_assert(BM == BN && (BM / 8) % W == 0, "lines of x and of w take one unit each, in whole loads of every wave's");
+    // arrays of their own: of requests into one the compiler would make every read wait
+    __shared__ __attribute__((aligned(1024))) unsigned char st0[UNIT];
+    __shared__ __attribute__((aligned(1024))) unsigned char st1[UNIT];
+    __shared__ __attribute__((aligned(1024))) unsigned char st2[UNIT];
+    __shared__ __attribute__((aligned(1024))) unsigned char st3[UNIT];
+    __shared__ __attribute__((aligned(1024))) unsigned char st4[UNIT];
 
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -303,14 +308,12 @@ __device__ __forceinline__ void nt_tile(const NtParams &p, const Epi &epi, int32
         voff[i] = in ? (uint32_t)row * (uint32_t)(x ? p.ldx : p.ldw) + chunk * 16 : OOB;
         room[i] = in ? p.kbytes - chunk * 16 : 0;
     }
-    int32_t f_kt = slice * p.split_lines;
-    const int32_t end = min(f_kt + p.split_lines, p.nk), lines = end - f_kt;
-    int32_t f_at = 0;
-    bool f_live = true;
-    auto begin = [&]() { f_live = f_kt < end; f_at = f_live ? f_kt * 128 : 0; ++f_kt; };
-    auto dma = [&](unsigned char *st, int d) {
-        unsigned char *to = d < XL ? st + (wave * XL + d) * 1024 : st + X_BYTES + (wave * (LPT - XL) + d - XL) * 1024;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(d < XL ? rx : rw, RL_LDS_PTR(to), 16, f_live && f_at < room[d] ? voff[d] + f_at : OOB, 0, 0, 0);
+    const int32_t begin = slice * p.split_lines, end = min(begin + p.split_lines, p.nk), lines = end - begin;
+    // the d-th load of a line of x or w into a unit; behind the last line: zeros
+    auto dma = [&](unsigned char *to, bool w, int32_t line, int d) {
+        const int i = w ? XL + d : d;
+        const int32_t at = (begin + line) * 128;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(w ? rw : rx, RL_LDS_PTR(to + (wave * XL + d) * 1024), 16, line < lines && at < room[i] ? voff[i] + at : OOB, 0, 0, 0);
     };
 
     f32x16 acc[TM][TN];
@@ -325,60 +328,74 @@ __device__ __forceinline__ void nt_tile(const NtParams &p, const Epi &epi, int32
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) f_off[ks] = frow * 128 + (((2 * ks + fhalf) ^ ((frow >> 1) & 7)) << 4);
     u32x4 fw[2][TN], fx[2][TM];
-    auto fragments = [&](const unsigned char *st, int ks) {
+    auto fragments = [&](const unsigned char *x, const unsigned char *w, int ks) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fw[ks & 1][j] = *(const u32x4 *)(st + X_BYTES + (wn * TN + j) * 4096 + f_off[ks]);
+        for (int j = 0; j < TN; ++j) fw[ks & 1][j] = *(const u32x4 *)(w + (wn * TN + j) * 4096 + f_off[ks]);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) fx[ks & 1][i] = *(const u32x4 *)(st + (wm * TM + i) * 4096 + f_off[ks]);
+        for (int i = 0; i < TM; ++i) fx[ks & 1][i] = *(const u32x4 *)(x + (wm * TM + i) * 4096 + f_off[ks]);
         __builtin_amdgcn_sched_barrier(0);
     };
-    // a k-step's MFMAs; req 0, 1: the first, second half of a tile's direct loads between them, 2: none
-    auto multiply = [&](int ks, unsigned char *to, int req) {
-        constexpr int HALF = LPT / 2, N = TM * TN;
+    // a k-step's MFMAs; to: a unit's requests between them
+    auto multiply = [&](int ks, unsigned char *to, bool w, int32_t line) {
+        constexpr int N = TM * TN;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 Mfma<E>::go(acc[i][j], fw[ks & 1][j], fx[ks & 1][i]);
-                if (req < 2) {
+                if (to) {
                     const int n = i * TN + j;
 #pragma unroll
-                    for (int d = n * HALF / N; d < (n + 1) * HALF / N; ++d) dma(to, req * HALF + d);
+                    for (int d = n * XL / N; d < (n + 1) * XL / N; ++d) dma(to, w, line, d);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
     };
-    // tile t in cur, the first half of tile t + 1's loads under way into nxt
-    auto body = [&](unsigned char *cur, unsigned char *nxt) {
-        fragments(cur, 1);
-        multiply(0, nxt, 1);
-        fragments(cur, 2);
-        multiply(1, cur, 2);
-        fragments(cur, 3);
-        multiply(2, cur, 2);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        begin();
-        fragments(nxt, 0);
-        multiply(3, cur, 0);
+    // Line t of x in x0, of w in w0; the next ones in x1 and w1, of which w's is under way; x's of the line after that goes where w's of the line
+    // before was, w's of it to x0, which is free from the barrier on: the last k-step's fragments are in registers by then.
+    int32_t t_ = 0;
+    auto body = [&](unsigned char *x0, unsigned char *w0, unsigned char *x1, unsigned char *w1, unsigned char *x2) {
+        fragments(x0, w0, 1);
+        multiply(0, x2, false, t_ + 2);
+        fragments(x0, w0, 2);
+        multiply(1, nullptr, false, 0);
+        fragments(x0, w0, 3);
+        multiply(2, nullptr, false, 0);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(XL) : "memory");
+        fragments(x1, w1, 0);
+        multiply(3, x0, true, t_ + 2);
+        ++t_;
     };
-    begin();
 #pragma unroll
-    for (int d = 0; d < LPT; ++d) dma(st0, d);
-    begin();
+    for (int d = 0; d < XL; ++d) dma(st0, false, 0, d);
 #pragma unroll
-    for (int d = 0; d < LPT / 2; ++d) dma(st1, d);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LPT / 2) : "memory");
-    fragments(st0, 0);
-    int32_t kt = 0;
+    for (int d = 0; d < XL; ++d) dma(st1, true, 0, d);
+#pragma unroll
+    for (int d = 0; d < XL; ++d) dma(st2, false, 1, d);
+#pragma unroll
+    for (int d = 0; d < XL; ++d) dma(st3, true, 1, d);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(2 * XL) : "memory");
+    fragments(st0, st1, 0);
+    // item k of x0, w0, x1, w1, .. is in unit k % 5
 #pragma unroll 1
-    for (; kt + 2 <= lines; kt += 2) {
-        body(st0, st1);
-        body(st1, st0);
+    while (t_ + 5 <= lines) {
+        body(st0, st1, st2, st3, st4);
+        body(st2, st3, st4, st0, st1);
+        body(st4, st0, st1, st2, st3);
+        body(st1, st2, st3, st4, st0);
+        body(st3, st4, st0, st1, st2);
     }
-    if (kt < lines) body(st0, st1);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the trailing requests; from here the stages are free
+    if (t_ < lines) body(st0, st1, st2, st3, st4);
+    if (t_ < lines) body(st2, st3, st4, st0, st1);
+    if (t_ < lines) body(st4, st0, st1, st2, st3);
+    if (t_ < lines) body(st1, st2, st3, st4, st0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the trailing requests; from here the units are free
 
-    epi.template operator()<WM, WN, TM, TN>(acc, m0, n0, bn, wm, wn, st0);
+    // a wave's own part: half of a unit where there are eight waves, else a unit
+    constexpr int SHARE = W > 4 ? 2 : 1;
+    unsigned char *const unit = wave / SHARE == 0 ? st1 : wave / SHARE == 1 ? st2 : wave / SHARE == 2 ? st3 : st4;
+    static_assert(UNIT / SHARE >= TM * 4096 && WN * BM * sizeof(Soft) <= UNIT, "what an epilogue wants is there");
+    epi.template operator()<WM, WN, TM, TN>(acc, m0, n0, bn, wm, wn, st0, unit + wave % SHARE * (UNIT / SHARE));
 #endif
 }
 
