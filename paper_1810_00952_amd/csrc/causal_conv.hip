@@ -9,6 +9,8 @@
 // the last K - 1 tokens in registers; those before its run it finds by itself.  keep is the same for all lanes: a run's flags are two
 // masks.  Of the gradient the wave also walks on behind its run, until its own tokens have all they get from later ones; its share of
 // dw and db goes to memory, and a second launch adds the shares up, in a fixed order.
+#include <type_traits>
+
 #include "igemm_lds.h"
 
 namespace rl {
@@ -16,10 +18,12 @@ namespace rl {
 namespace {
 
 constexpr int RUN = 64;                       // rows of a run at most: a mask's bits
+constexpr int AHEAD = 8;                      // rows asked for before the first of them is worked off; runs are of a multiple
 
 template <typename E, int VEC> struct Row;
 template <> struct Row<float, 4> { typedef u32x4 raw; };
 template <> struct Row<uint16_t, 8> { typedef u32x4 raw; };
+template <> struct Row<uint16_t, 4> { typedef u32x2 raw; };      // of more taps, whose window and sums take twice the registers
 template <> struct Row<float, 1> { typedef uint32_t raw; };
 template <> struct Row<uint16_t, 1> { typedef uint16_t raw; };
 
@@ -42,7 +46,7 @@ template <typename E, int VEC> __device__ __forceinline__ typename Row<E, VEC>::
     else if constexpr (VEC == 1) r = (uint16_t)pack_bf16x2(v[0], v[0]);
     else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < (int)(VEC * sizeof(E) / 4); ++j) {
             if constexpr (sizeof(E) == 4) r[j] = __float_as_uint(v[j]);
             else r[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
         }
@@ -76,18 +80,47 @@ struct Walk {
         run = (int32_t)(rest - (uint32_t)b * runs);
         live = d < p.D;
         if (!live) d = 0;                     // some other lane's channels, of which nothing is stored
+        if constexpr (VEC > 1 && KT < 8) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) bias[j] = p.b[d + j];
+            for (int j = 0; j < VEC; j += 4) {
+                const f32x4 t = *(const f32x4 *)(p.b + d + j);
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
+                for (int c = 0; c < 4; ++c) bias[j + c] = t[c];
+            }
+            // the channels' taps lie one behind the other, from a multiple of 16 bytes on
+            if (p.w_dtype == DT_F32) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) w[k][j] = taps.has(k) ? load_as_f32(p.w, p.w_dtype, (d + j) * p.K + k - taps.o) : 0.0f;
+                for (int i = 0; i < VEC * KT; i += 4) {
+                    const f32x4 t = *(const f32x4 *)((const float *)p.w + d * KT + i);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) w[(i + c) % KT][(i + c) / KT] = t[c];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC * KT; i += 8) {
+                    const u32x4 t = *(const u32x4 *)((const uint16_t *)p.w + d * KT + i);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        if (i + c < VEC * KT) w[(i + c) % KT][(i + c) / KT] = __uint_as_float(c & 1 ? t[c >> 1] & 0xffff0000u : t[c >> 1] << 16);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) bias[j] = p.b[d + j];
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[k][j] = taps.has(k) ? load_as_f32(p.w, p.w_dtype, (d + j) * p.K + k - taps.o) : 0.0f;
+        }
     }
     __device__ __forceinline__ raw_t row(const void *x, int64_t t) const { return *(const raw_t *)((const E *)x + (b * p.T + t) * p.D + d); }
     __device__ __forceinline__ raw_t state(const void *s, int j) const { return *(const raw_t *)((const E *)s + (b * (p.K - 1) + j - taps.o) * p.D + d); }
     __device__ __forceinline__ void put(void *x, int64_t t, const float (&v)[VEC]) const
     {
-        if (live) *(raw_t *)((E *)x + (b * p.T + t) * p.D + d) = pack<E, VEC>(v);
+        raw_t *const to = (raw_t *)((E *)x + (b * p.T + t) * p.D + d);
+        if (!live) return;
+        if constexpr (VEC > 1) __builtin_nontemporal_store(pack<E, VEC>(v), to);
+        else *to = pack<E, VEC>(v);
     }
     __device__ __forceinline__ void put_state(void *s, int j, const float (&v)[VEC]) const
     {
@@ -140,9 +173,13 @@ struct Walk {
     }
     __device__ __forceinline__ void set(int slot, const raw_t &r)
     {
+        // values chosen, not places: places chosen would put the window into memory
+        float x[VEC];
+        unpack<E, VEC>(r, x);
 #pragma unroll
         for (int j = 0; j < KT - 1; ++j)
-            if (j == slot) unpack<E, VEC>(r, win[j]);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) win[j][v] = j == slot ? x[v] : win[j][v];
     }
     __device__ __forceinline__ void forget()
     {
@@ -196,32 +233,45 @@ __global__ __launch_bounds__(64) void causal_conv_kernel(const CausalConvParams 
     if (KEEP) k.flags(t0, n, tok, first);
     const bool last = k.run + 1 == runs;
     if (!KEEP || tok || last) k.template before<KEEP>(t0);
-    constexpr int AHEAD = 8;
-    for (int i = 0; i < n; i += AHEAD) {
-        raw_t r[AHEAD];
+    auto walk = [&](auto plain) __attribute__((always_inline)) {                 // plain: the rows are all there, and tokens of one document
+        raw_t r[2][AHEAD];
+        auto ask = [&](raw_t (&q)[AHEAD], int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) r[a] = k.row(p.x, t0 + (i + a < n ? i + a : n - 1));
+            for (int a = 0; a < AHEAD; ++a) q[a] = k.row(p.x, t0 + (i + a < n ? i + a : n - 1));
+        };
+        auto rows_of = [&](const raw_t (&q)[AHEAD], int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            if (i + a >= n) break;
-            float x[VEC], u[VEC];
-            if (KEEP && !(tok >> (i + a) & 1)) {
+            for (int a = 0; a < AHEAD; ++a) {
+                float x[VEC], u[VEC];
+                if (!plain && i + a >= n) continue;
+                if (!plain && !(tok >> (i + a) & 1)) {
 #pragma unroll
-                for (int v = 0; v < VEC; ++v) u[v] = 0.0f;
+                    for (int v = 0; v < VEC; ++v) u[v] = 0.0f;
+                    k.put(p.y, t0 + i + a, u);
+                    continue;
+                }
+                if (!plain && (first >> (i + a) & 1)) k.forget();
+                unpack<E, VEC>(q[a], x);
+                k.sum(x, u);
+                if (p.silu) {
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v) u[v] = silu(u[v]);
+                }
                 k.put(p.y, t0 + i + a, u);
-                continue;
+                k.shift(x);
             }
-            if (KEEP && (first >> (i + a) & 1)) k.forget();
-            unpack<E, VEC>(r[a], x);
-            k.sum(x, u);
-            if (p.silu) {
-#pragma unroll
-                for (int v = 0; v < VEC; ++v) u[v] = silu(u[v]);
-            }
-            k.put(p.y, t0 + i + a, u);
-            k.shift(x);
+        };
+        ask(r[0], 0);
+        for (int i = 0; i < n; i += 2 * AHEAD) {
+            if (i + AHEAD < n) ask(r[1], i + AHEAD);
+            rows_of(r[0], i);
+            if (i + 2 * AHEAD < n) ask(r[0], i + 2 * AHEAD);
+            if (i + AHEAD < n) rows_of(r[1], i + AHEAD);
         }
-    }
+    };
+    const uint64_t all = n == 64 ? ~0ull : (1ull << n) - 1;
+    if (n == rows && (tok & all) == all && first == 0) walk(std::true_type{});
+    else walk(std::false_type{});
     if (last) {
 #pragma unroll
         for (int j = 0; j < KT - 1; ++j)
@@ -257,12 +307,12 @@ __global__ __launch_bounds__(64) void causal_conv_grad_kernel(const CausalConvPa
 #pragma unroll
         for (int v = 0; v < VEC; ++v) pend[j][v] = 0.0f;
     }
-    auto flush = [&](int j) {
+    auto flush = [&](int j) __attribute__((always_inline)) {
         if (pos[j] >= 0) k.put(p.dx, pos[j], pend[j]);
         else if (pos[j] <= STATE) k.put_state(p.ds0, (int)(STATE - pos[j]), pend[j]);
         owed -= pos[j] != NOT_MINE;
     };
-    auto forget = [&]() {
+    auto forget = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < KT - 1; ++j) {
             flush(j);
@@ -272,8 +322,8 @@ __global__ __launch_bounds__(64) void causal_conv_grad_kernel(const CausalConvPa
         }
         k.forget();
     };
-    // a token at row t, one of the run's own or behind it
-    auto token = [&](int64_t t, const raw_t &rx, const raw_t &rdy, bool mine) {
+    // a token at row t, one of the run's own or behind it.  plain: all of the run before it are tokens, so that slots' rows are known
+    auto token = [&](int64_t t, const raw_t &rx, const raw_t &rdy, bool mine, auto plain) __attribute__((always_inline)) {
         float x[VEC], g[VEC], u[VEC];
         unpack<E, VEC>(rx, x);
         unpack<E, VEC>(rdy, g);
@@ -298,42 +348,69 @@ __global__ __launch_bounds__(64) void causal_conv_grad_kernel(const CausalConvPa
 #pragma unroll
             for (int v = 0; v < VEC; ++v) pend[j][v] = __builtin_fmaf(k.w[j][v], g[v], pend[j][v]);
         }
+        if (plain) {
+            const int64_t i = t - t0;
+            if (i >= KT - 1) k.put(p.dx, t - (KT - 1), pend[0]);
+            else if (k.run == 0) k.put_state(p.ds0, (int)i, pend[0]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < KT - 1; ++j)
-            if (j == k.taps.o) flush(j);
+            for (int j = 0; j < KT - 1; ++j)
+                if (j == k.taps.o) flush(j);
+        }
 #pragma unroll
         for (int j = 0; j < KT - 1; ++j) {
             const bool end = j + 1 == KT - 1;
-            pos[j] = !k.taps.has(j) ? NOT_MINE : end ? (mine ? t : NOT_MINE) : pos[end ? j : j + 1];
+            if (!plain) pos[j] = !k.taps.has(j) ? NOT_MINE : end ? (mine ? t : NOT_MINE) : pos[end ? j : j + 1];
 #pragma unroll
             for (int v = 0; v < VEC; ++v) pend[j][v] = !k.taps.has(j) ? 0.0f : end ? k.w[KT - 1][v] * g[v] : pend[end ? j : j + 1][v];
         }
-        owed += mine;
+        if (!plain) owed += mine;
         k.shift(x);
     };
     if (!KEEP || tok || owed) k.template before<KEEP>(t0);
-    constexpr int AHEAD = 4;
-    for (int i = 0; i < n; i += AHEAD) {
-        raw_t r[AHEAD], q[AHEAD];
+    constexpr int SOME = AHEAD / 2;               // of two tensors
+    auto walk = [&](auto plain) __attribute__((always_inline)) {
+        raw_t r[2][SOME], q[2][SOME];
+        auto ask = [&](int s, int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            const int64_t t = t0 + (i + a < n ? i + a : n - 1);
-            r[a] = k.row(p.x, t);
-            q[a] = k.row(p.dy, t);
-        }
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            if (i + a >= n) break;
-            if (KEEP && !(tok >> (i + a) & 1)) {
-                float zero[VEC];
-#pragma unroll
-                for (int v = 0; v < VEC; ++v) zero[v] = 0.0f;
-                k.put(p.dx, t0 + i + a, zero);
-                continue;
+            for (int a = 0; a < SOME; ++a) {
+                const int64_t t = t0 + (i + a < n ? i + a : n - 1);
+                r[s][a] = k.row(p.x, t);
+                q[s][a] = k.row(p.dy, t);
             }
-            if (KEEP && (first >> (i + a) & 1)) forget();
-            token(t0 + i + a, r[a], q[a], true);
+        };
+        auto rows_of = [&](auto half, int i) __attribute__((always_inline)) {
+            constexpr int S = decltype(half)::value;
+#pragma unroll
+            for (int a = 0; a < SOME; ++a) {
+                if (!plain && i + a >= n) continue;
+                if (!plain && !(tok >> (i + a) & 1)) {
+                    float zero[VEC];
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v) zero[v] = 0.0f;
+                    k.put(p.dx, t0 + i + a, zero);
+                    continue;
+                }
+                if (!plain && (first >> (i + a) & 1)) forget();
+                token(t0 + i + a, r[S][a], q[S][a], true, plain);
+            }
+        };
+        ask(0, 0);
+        for (int i = 0; i < n; i += 2 * SOME) {
+            if (i + SOME < n) ask(1, i + SOME);
+            rows_of(std::integral_constant<int, 0>{}, i);
+            if (i + 2 * SOME < n) ask(0, i + 2 * SOME);
+            if (i + SOME < n) rows_of(std::integral_constant<int, 1>{}, i + SOME);
         }
+    };
+    const uint64_t all = n == 64 ? ~0ull : (1ull << n) - 1;
+    if (KT < 8 && n == rows && (tok & all) == all && first == 0) {
+        walk(std::true_type{});
+#pragma unroll
+        for (int j = 0; j < KT - 1; ++j) pos[j] = t0 + n - (KT - 1) + j;
+        owed = KT - 1;
+    } else {
+        walk(std::false_type{});
     }
     // what later tokens give to mine
     for (int64_t t = t0 + n; owed && t < p.T; t += 64) {
@@ -344,7 +421,7 @@ __global__ __launch_bounds__(64) void causal_conv_grad_kernel(const CausalConvPa
             const int i = __builtin_ctzll(more);
             more &= more - 1;
             if (KEEP && (starts >> i & 1)) { forget(); break; }
-            token(t + i, k.row(p.x, t + i), k.row(p.dy, t + i), false);
+            token(t + i, k.row(p.x, t + i), k.row(p.dy, t + i), false, std::false_type{});
         }
     }
     if (owed) {                                   // the sequence's end: the new state's derivative is theirs
@@ -372,7 +449,7 @@ __global__ __launch_bounds__(64) void causal_conv_grad_kernel(const CausalConvPa
 }
 
 // ---------------------------------------------------------------------------
-// sums of shares, sixteen of them under way at a time a column: dst[map(j)] = sum_p part[p][j]
+// sums of shares, sixteen of them under way at a time a column
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void sum_shares_kernel(const SumShares q)
 {
@@ -391,13 +468,31 @@ __global__ __launch_bounds__(1024) void sum_shares_kernel(const SumShares q)
         for (int w = 1; w < 16; ++w) v += s[w][lane];
         // rows of `turn` columns become columns of `across` rows
         const int64_t at = q.turn ? (j % q.turn) * q.across + j / q.turn : j;
-        store_from_f32(q.dst, q.dst_dtype, at, v);
+        if (j < q.J1) store_from_f32(q.dst, q.dst_dtype, at, v);
+        else q.dst2[j - q.J1] = v;
     }
+}
+
+// many columns: four of them a thread, one share after the other
+__global__ __launch_bounds__(256) void sum_columns_kernel(const SumShares q)
+{
+    const int64_t j = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (j >= q.J) return;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int64_t i = 0; i < q.P; ++i) v += *(const f32x4 *)(q.part + i * q.stride + j);
+    if (q.dst_dtype == DT_BF16) *(u32x2 *)((uint16_t *)q.dst + j) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    else *(f32x4 *)((float *)q.dst + j) = v;
 }
 
 hipError_t launch_sum_shares(const SumShares &q, hipStream_t s)
 {
     if (q.J < 1 || q.P < 1 || (q.J + 63) / 64 > 0x3fffff) return hipErrorInvalidValue;
+    // (67 MB in 32 shares of 524288 columns 30 -> 14 us)
+    if (q.J >= (1 << 16) && q.P <= 256 && q.J % 4 == 0 && q.stride % 4 == 0 && !q.turn && q.J1 == q.J && (uintptr_t)q.part % 16 == 0) {
+        hipLaunchKernelGGL(sum_columns_kernel, dim3((unsigned)((q.J / 4 + 255) / 256)), dim3(256), 0, s, q);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(sum_shares_kernel, dim3((unsigned)((q.J + 63) / 64)), dim3(1024), 0, s, q);
     return hipGetLastError();
 }
@@ -409,10 +504,12 @@ struct Form { int32_t slabs, runs, rows, vec; };
 Form form_of(const CausalConvParams &p)
 {
     Form f;
-    const int whole = p.dtype == DT_BF16 ? 8 : 4;
+    const int whole = p.dtype == DT_BF16 && p.K <= 4 ? 8 : 4;
     f.vec = p.D % whole == 0 ? whole : 1;
     f.slabs = (int32_t)((p.D + 64 * f.vec - 1) / (64 * f.vec));
-    f.rows = 32;
+    // long runs read fewer tokens before them and leave fewer shares, short ones fill the CUs
+    f.rows = RUN;
+    while (f.rows > 16 && p.B * f.slabs * ((p.T + f.rows - 1) / f.rows) < 2048) f.rows /= 2;
     f.runs = (int32_t)((p.T + f.rows - 1) / f.rows);
     return f;
 }
@@ -433,10 +530,13 @@ void go(bool grad, const CausalConvParams &p, const Form &f, hipStream_t s)
 template <typename E, int VEC>
 void go(bool grad, const CausalConvParams &p, const Form &f, hipStream_t s)
 {
+    if (p.K > 4) {
+        go<E, (VEC < 4 ? VEC : 4), 8>(grad, p, f, s);
+        return;
+    }
     if (p.K == 2) go<E, VEC, 2>(grad, p, f, s);
     else if (p.K == 3) go<E, VEC, 3>(grad, p, f, s);
-    else if (p.K == 4) go<E, VEC, 4>(grad, p, f, s);
-    else go<E, VEC, 8>(grad, p, f, s);
+    else go<E, VEC, 4>(grad, p, f, s);
 }
 
 hipError_t go(bool grad, const CausalConvParams &p, const Form &f, hipStream_t s)
@@ -474,10 +574,7 @@ hipError_t launch_causal_conv_grad(const CausalConvParams &p, hipStream_t s)
     if (er != hipSuccess) return er;
     SumShares q{};
     q.part = p.part; q.P = p.B * f.runs; q.stride = (p.K + 1) * p.D;
-    q.J = p.K * p.D; q.turn = p.D; q.across = p.K; q.dst = p.dw; q.dst_dtype = DT_F32;
-    er = launch_sum_shares(q, s);
-    if (er != hipSuccess) return er;
-    q.part = p.part + p.K * p.D; q.J = p.D; q.turn = 0; q.dst = p.db;
+    q.J = (p.K + 1) * p.D; q.J1 = p.K * p.D; q.turn = p.D; q.across = p.K; q.dst = p.dw; q.dst_dtype = DT_F32; q.dst2 = p.db;
     return launch_sum_shares(q, s);
 }
 

@@ -637,7 +637,7 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
     hipError_t er = hipGetLastError();
     if (er != hipSuccess || k.slices == 1) return er;
     SumShares q{};
-    q.part = acc; q.P = k.slices; q.J = q.stride = p.M * p.K; q.dst = p.dx; q.dst_dtype = p.dtype;
+    q.part = acc; q.P = k.slices; q.J = q.J1 = q.stride = p.M * p.K; q.dst = p.dx; q.dst_dtype = p.dtype;
     return launch_sum_shares(q, s);
 }
 

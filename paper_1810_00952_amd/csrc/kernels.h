@@ -384,8 +384,9 @@ bool causal_conv_fits(const CausalConvParams &p);
 int64_t causal_conv_part_floats(const CausalConvParams &p);
 hipError_t launch_causal_conv(const CausalConvParams &p, hipStream_t s);
 hipError_t launch_causal_conv_grad(const CausalConvParams &p, hipStream_t s);
-// dst[j] = sum over i < P of part[i * stride + j], j < J, in a fixed order; turn > 0: element j goes to (j % turn) * across + j / turn
-struct SumShares { const float *part; void *dst; int64_t P, J, stride, turn, across; int32_t dst_dtype; };
+// dst[j] = sum over i < P of part[i * stride + j], j < J1, in a fixed order; turn > 0: element j goes to (j % turn) * across + j / turn.  Columns J1 .. J - 1
+// go to dst2, as they lie
+struct SumShares { const float *part; void *dst; float *dst2; int64_t P, J, J1, stride, turn, across; int32_t dst_dtype; };
 hipError_t launch_sum_shares(const SumShares &q, hipStream_t s);
 // selective_scan.hip.  z null: no gate; keep null: every row a token.  states: the state before every sel_scan_state_rows-th row,
 // [B][ceil(T / sel_scan_state_rows)][D][N]: the forward pass writes it where it is not null (y and hT may be null then), the gradient reads it.

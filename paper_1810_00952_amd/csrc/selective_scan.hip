@@ -836,13 +836,10 @@ hipError_t go(bool grad, const SelScanParams &p, const Form &f, hipStream_t s)
     if (er != hipSuccess || !grad) return er;
     SumShares q{};
     q.part = shares; q.P = f.chunks * p.B; q.stride = p.D * p.N + p.D; q.dst_dtype = DT_F32;
-    q.J = p.D * p.N; q.dst = p.da;
+    q.J = q.stride; q.J1 = p.D * p.N; q.dst = p.da; q.dst2 = p.dskip;
     er = launch_sum_shares(q, s);
     if (er != hipSuccess) return er;
-    q.part = shares + p.D * p.N; q.J = p.D; q.dst = p.dskip;
-    er = launch_sum_shares(q, s);
-    if (er != hipSuccess) return er;
-    q.part = bc; q.P = f.slabs; q.J = q.stride = p.B * p.T * 2 * p.N; q.dst = p.dbc; q.dst_dtype = p.dtype;
+    q.part = bc; q.P = f.slabs; q.J = q.J1 = q.stride = p.B * p.T * 2 * p.N; q.dst = p.dbc; q.dst_dtype = p.dtype;
     return launch_sum_shares(q, s);
 }
 
