@@ -643,29 +643,29 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
 
 }  // namespace
 
-bool dense_logprobs_fits(const DenseLogprobsParams &p, bool grad)
+bool dense_logprobs_fits(const DenseLogprobsParams &p)
 {
     // a row's bytes, and those of a row of the transposed operands, are reached by 31-bit offsets from a tile's first row
     if (p.M < 1 || p.V < 1 || p.K < 1 || p.M > DENSE_LOGPROBS_MAX_ROWS || p.V > 0x7fffffff || p.K > DENSE_LOGPROBS_MAX_K) return false;
-    if (!launch_has(((p.M + 63) / 64) * ((p.V + 63) / 64), 256)) return false;
-    return !grad || (p.M * p.K + 63) / 64 <= 0x3fffff;
+    return launch_has(((p.M + 63) / 64) * ((p.V + 63) / 64), 256);
 }
 
 int64_t dense_logprobs_part_bytes(const DenseLogprobsParams &p, bool grad)
 {
-    if (!grad) return (2 * ((p.V + 63) / 64) + 1) * p.M * 4;
+    const int32_t side = p.dtype == DT_BF16 ? tile_of<uint16_t>(p.M, p.V) : tile_of<float>(p.M, p.V);
+    if (!grad) return (2 * tiles_along(p.V, side) + 1) * p.M * 4;
     return layout_of(p, pieces_of(p)).bytes;
 }
 
 hipError_t launch_dense_logprobs(const DenseLogprobsParams &p, hipStream_t s)
 {
-    if (!dense_logprobs_fits(p, false) || !p.part || p.ldx % 16 != 0 || p.ldw % 16 != 0) return hipErrorInvalidValue;
+    if (!dense_logprobs_fits(p) || !p.part || p.ldx % 16 != 0 || p.ldw % 16 != 0) return hipErrorInvalidValue;
     return p.dtype == DT_BF16 ? forward<uint16_t>(p, s) : forward<float>(p, s);
 }
 
 hipError_t launch_dense_logprobs_grad(const DenseLogprobsParams &p, hipStream_t s)
 {
-    if (!dense_logprobs_fits(p, true) || !p.part || p.ldx % 16 != 0 || p.ldw % 16 != 0) return hipErrorInvalidValue;
+    if (!dense_logprobs_fits(p) || !p.part || p.ldx % 16 != 0 || p.ldw % 16 != 0) return hipErrorInvalidValue;
     return p.dtype == DT_BF16 ? gradient<uint16_t>(p, s) : gradient<float>(p, s);
 }
 

@@ -412,7 +412,7 @@ struct DenseLogprobsParams {
     int64_t M, V, K, ldx, ldw, piece_bytes; int32_t dtype;
 };
 constexpr int64_t DENSE_LOGPROBS_MAX_ROWS = 1 << 20, DENSE_LOGPROBS_MAX_K = 1 << 20;
-bool dense_logprobs_fits(const DenseLogprobsParams &p, bool grad);
+bool dense_logprobs_fits(const DenseLogprobsParams &p);
 int64_t dense_logprobs_part_bytes(const DenseLogprobsParams &p, bool grad);
 hipError_t launch_dense_logprobs(const DenseLogprobsParams &p, hipStream_t s);
 hipError_t launch_dense_logprobs_grad(const DenseLogprobsParams &p, hipStream_t s);

@@ -1250,7 +1250,7 @@ struct Planner {
         const int64_t row = p.K * (int64_t)dtype_size(x.dtype);
         p.ldx = p.ldw = round_up(row, 16);
         p.piece_bytes = plan.lean ? 1 << 20 : 128 << 20;
-        if (!dense_logprobs_fits(p, grad)) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows or columns than the kernels reach");
+        if (!dense_logprobs_fits(p)) return fail(RL_ERR_UNSUPPORTED, std::string(op_name(o.kind)) + ": more rows or columns than the kernels reach");
         if (grad) plan.spent = true;
         if (row != p.ldx) {                       // rows that start on 16 bytes, made once for the calls of a plan that want them
             auto padded = [&](int src, int64_t rows) {

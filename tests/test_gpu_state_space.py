@@ -293,3 +293,290 @@ def test_logits_that_are_no_numbers(v, dtype):
     assert abs(lse[0] - np.log(v // 2)) < 8 * F * (1 + np.log(v)) + (v / 16 + 60) * F
     g = loss_grad_call(ops + [(tensor(np.array([1.0]), "f32")[0], "f32"), (tensor(np.array([0.0]), "f32")[0], "f32")], lse, 1, v, 1, dtype).run().numbers()
     assert not g[1][0::2].any()
+
+
+# ---- operators together, streams, graphs, large sizes ------------------------------------------------------------------------
+def some_calls():
+    operands, _ = conv_case(5, 70, 72, 4, "bf16", "f32", "some", seed=1)
+    yield conv_call(operands, 5, 70, 72, 4, "bf16", True)
+    yield conv_grad_call(operands, 5, 70, 72, 4, "bf16", True)
+    for b, t, d, n in ((2, 150, 70, 16), (1, 700, 33, 24), (3, 1, 66, 5)):
+        operands, _ = scan_case(b, t, d, n, "bf16", True, "some", seed=2)
+        yield scan_call(operands, b, t, d, n, "bf16")
+        yield scan_grad_call(operands, b, t, d, n, "bf16")
+    for m, v, k, dtype in ((40, 3000, 72, "bf16"), (300, 500, 33, "f32"), (8, 20000, 24, "bf16")):
+        operands, (x, w, tok, dlp, dlse) = loss_case(m, v, k, dtype, seed=3)
+        yield loss_call(operands, m, v, k, dtype)
+        yield loss_grad_call(operands, L.dense_logprobs(x, w, tok)[1], m, v, k, dtype)
+
+
+def test_other_streams_graphs_and_the_same_bits_twice():
+    import torch
+    for call in some_calls():
+        want = call.run().numbers()
+        side = torch.cuda.Stream()
+        for t in call.results:
+            t.view(torch.uint8).fill_(0x5a)
+        torch.cuda.synchronize()
+        for a, b in zip(call.run(side).numbers(), want):
+            np.testing.assert_array_equal(a, b)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call.run()
+        for _ in range(3):                        # replays between eager work on the same memory
+            for t in call.results:
+                t.view(torch.uint8).fill_(0x5a)
+            call.workspace[:call.workspace_bytes].fill_(0xa5)
+            graph.replay()
+            for a, b in zip(call.numbers(), want):
+                np.testing.assert_array_equal(a, b)
+            for a, b in zip(call.run().numbers(), want):
+                np.testing.assert_array_equal(a, b)
+
+
+def test_one_plan_on_two_streams_at_once():
+    """A plan's runs on different streams, each with a workspace and results of its own."""
+    import torch
+    for make in (lambda: loss_grad_call(*loss_args), lambda: scan_grad_call(scan_operands, 2, 300, 130, 16, "bf16")):
+        operands, (x, w, tok, dlp, dlse) = loss_case(500, 3000, 64, "bf16", seed=4)
+        loss_args = (operands, L.dense_logprobs(x, w, tok)[1], 500, 3000, 64, "bf16")
+        scan_operands, _ = scan_case(2, 300, 130, 16, "bf16", True, "some", seed=5)
+        calls = [make(), make()]
+        want = make().run().numbers()
+        streams = [torch.cuda.Stream() for _ in calls]
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for c, s in zip(calls, streams):
+                c.run(s)
+        for c in calls:
+            for a, b in zip(c.numbers(), want):
+                np.testing.assert_array_equal(a, b)
+
+
+def check_graph(spec, data, dtype):
+    """Every call of a graph against its definition on what the library computed for its operands."""
+    import torch
+    import oracle as O
+    from helpers import assert_close
+    from paper_1810_00952_amd import harness
+    for op in spec.ops:                             # everything leaves the plan
+        for v in op.outputs:
+            if v not in spec.outputs:
+                spec.output(v)
+    s = harness.Session(spec)
+    s.load(data)
+    s.run()
+    torch.cuda.synchronize()
+    val = {v: O.widen(harness.to_host(s.raw.get(v, t)), spec.values[v].type.dtype) for v, t in s.tensors.items()}    # raw: before it was packed
+    for i, op in enumerate(spec.ops):
+        a, out, what = [val[v] for v in op.inputs], [val[v] for v in op.outputs], f"call {i}: {op.kind}"
+        if op.kind.startswith("causal_conv"):
+            n = 6 if op.kind.endswith("grad") else 4
+            keep = a[n] if len(a) > n else None
+            zero = np.zeros_like(a[0]), np.zeros_like(a[3])
+            ey, ex, ew, eb, es = conv_bounds(*a[:4], *(a[4:6] if n == 6 else zero), keep, True, dtype)
+            ref = L.causal_conv_grad(*a[:6], keep, True) if n == 6 else L.causal_conv(*a[:4], keep, True)
+            for got, want, tol in zip(out, ref, (ex, ew, eb, es) if n == 6 else (ey, 0)):
+                within(got, want, tol, what)
+        elif op.kind.startswith("selective_scan"):
+            n = 8 if op.kind.endswith("grad") else 6
+            z, keep = a[n], a[n + 1] if len(a) > n + 1 else None
+            zero = np.zeros_like(a[0]), np.zeros_like(a[5])
+            ahead, behind = scan_bounds(*a[:6], *(a[6:8] if n == 8 else zero), z, keep, dtype)
+            ref = getattr(L, op.kind)(*a[:n], z=z, keep=keep)
+            for got, want, tol in zip(out, ref, behind if n == 8 else ahead):
+                within(got, want, tol, what)
+        elif op.kind == "dense_logprobs":
+            zero = np.zeros(len(a[0]))
+            ref = L.dense_logprobs(*a)
+            for got, want, tol in zip(out, ref, loss_bounds(*a, ref[1], zero, zero, dtype)[0]):
+                within(got, want, tol, what)
+        elif op.kind == "dense_logprobs_grad":
+            for got, want, tol in zip(out, L.dense_logprobs_grad(*a), loss_bounds(*a, dtype)[1]):
+                within(got, want, tol, what)
+        else:                                       # what was there: its own gate, where it is a group of its own
+            f = {"dense": O.dense, "dense_grad_x": O.dense_grad_x, "dense_grad_w": O.dense_grad_w, "add": lambda p, q: p + q, "bias_add": lambda p, q: p + q}[op.kind]
+            assert_close(out[0], f(a[0], a[1]), dtype, what)
+    return s
+
+
+@pytest.mark.parametrize("args", [dict(), dict(batch=3, steps=37, dim=72, vocab=1001, states=7, packed=True), dict(batch=9, steps=1, dim=128), dict(batch=2, steps=70, dim=50, dtype="f32", taps=3)])
+def test_state_space_lm(args):
+    import workloads as W
+    spec, data = W.state_space_lm(**args)
+    spec.groups = [[i] for i in range(len(spec.ops))]          # every value leaves, so none is fused away
+    check_graph(spec, data, args.get("dtype", "bf16"))
+
+
+@pytest.mark.parametrize("args", [dict(), dict(batch=2, steps=150, dim=96, vocab=333, states=24, packed=True), dict(batch=3, steps=40, dim=40, dtype="f32", taps=2)])
+def test_state_space_lm_train(args):
+    import workloads as W
+    s = check_graph(*W.state_space_lm_train(**args), args.get("dtype", "bf16"))
+    names = [k["kernel"] for k in s.plan.describe()["steps"]]
+    assert sum("selective_scan" in n for n in names) == 2 and sum("dense_logprobs" in n for n in names) == 2
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_values_of_a_training_step_share_the_workspace(packed):
+    """The step with all its values in memory of their own, and with those between its calls in the workspace: the same bits."""
+    import torch
+    import workloads as W
+    from paper_1810_00952_amd import harness
+    got = []
+    for everything in (True, False):
+        spec, data = W.state_space_lm_train(3, 90, 72, 16, 700, packed=packed)
+        names = list(spec.outputs)
+        if everything:
+            for op in spec.ops:
+                for v in op.outputs:
+                    if v not in spec.outputs:
+                        spec.output(v)
+        s = harness.Session(spec)
+        s.load(data)
+        s.run()
+        torch.cuda.synchronize()
+        got.append(([s.tensors[v].clone() for v in names], s.plan.workspace_bytes()))
+    for a, b in zip(got[0][0], got[1][0]):
+        assert torch.equal(a, b) and bool(torch.isfinite(a.float()).all())
+    assert got[0][1] < got[1][1]
+
+
+def test_generation_continues_a_prompt():
+    """A prompt, then the same tokens one at a time on the states each step left."""
+    import torch
+    import workloads as W
+    from paper_1810_00952_amd import harness
+    b, t, d, layers = 3, 12, 64, 2
+    spec, data = W.state_space_lm(b, t, d, 8, layers, 300, dtype="f32")
+    whole = harness.Session(spec)
+    whole.load(data)
+    whole.run()
+    step_spec, _ = W.state_space_lm(b, 1, d, 8, layers, 300, dtype="f32")
+    step = harness.Session(step_spec)
+    state = {k: data[k] for l in range(layers) for k in (f"c{l}", f"h{l}")}
+    lps = []
+    for i in range(t):
+        step.tensors = {}
+        step.load({**data, "x": data["x"].reshape(b, t, d)[:, i], "tok": data["tok"].reshape(b, t)[:, i], **state})
+        step.alloc()
+        step.run()
+        torch.cuda.synchronize()
+        lps.append(step.output(0).cpu().numpy())
+        for l in range(layers):
+            state[f"c{l}"], state[f"h{l}"] = (step.tensors[step_spec.outputs[2 + 2 * l + j]].cpu().numpy() for j in range(2))
+    # values of some 1 to 10 through 2 layers of five sums of at most 64 terms each, every one off by a few hundred F of itself; a state gathers those of 12 rows
+    tol = 2 * 5 * 64 * 12 * 8 * F * 10
+    want = whole.output(0).cpu().numpy().reshape(b, t)
+    assert np.abs(np.stack(lps, 1) - want).max() < tol
+    for l in range(layers):
+        for j, name in enumerate(("c", "h")):
+            assert np.abs(state[f"{name}{l}"] - whole.tensors[spec.outputs[2 + 2 * l + j]].cpu().numpy()).max() < tol
+
+
+def test_past_32_bits():
+    """Rows behind the first 4 GB of each operator's largest operand."""
+    import torch
+    from language_helpers import plan_of, torch_type
+    dev = "cuda:0"
+
+    def run(kind, operands, results, **attrs):
+        plan, ids, outs = plan_of(kind, [(dt, t.shape) for t, dt in operands], results, **attrs)
+        got = [torch.empty(sh, dtype=torch_type(dt), device=dev) for dt, sh in results]
+        ws = torch.empty(max(256, plan.workspace_bytes()), dtype=torch.uint8, device=dev)
+        plan.run({v: t.data_ptr() for v, t in zip(ids + outs, [t for t, _ in operands] + got)}, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        return got
+
+    num = lambda a: a.double().cpu().numpy()  # noqa: E731
+    torch.manual_seed(3)
+    # a sequence of 600000 x 4096, padding but for its last rows
+    print("sequence", flush=True)
+    t, d, n, k, states = 600000, 4096, 5, 4, 2
+    keep = torch.zeros((t,), dtype=torch.int8, device=dev)
+    keep[-n:] = 1
+
+    def wide(cols=d):
+        a = torch.zeros((t, cols), dtype=torch.bfloat16, device=dev)
+        a[-n:] = torch.randn((n, cols), device=dev).bfloat16()
+        return a
+
+    x, dy = wide(), wide()
+    w, bias = torch.rand((d, k), device=dev) - 0.5, torch.randn((d,), device=dev)
+    s0, dsT = (torch.randn((1, k - 1, d), device=dev).bfloat16() for _ in range(2))
+    tail = [num(a) for a in (x[-n:], w, bias, s0, dy[-n:], dsT)]
+    ey, ex, ew, eb, es = conv_bounds(*tail, None, True, "bf16")
+    y, sT = run("causal_conv", [(x, "bf16"), (w, "f32"), (bias, "f32"), (s0, "bf16"), (keep, "i8")], [("bf16", (t, d)), ("bf16", (1, k - 1, d))], silu=1)
+    ref = L.causal_conv(*tail[:4], None, True)
+    within(num(y[-n:]), ref[0], ey, "last rows")
+    np.testing.assert_array_equal(num(sT), ref[1])
+    assert not bool(y[:-n].any())
+    del y
+    got = run("causal_conv_grad", [(x, "bf16"), (w, "f32"), (bias, "f32"), (s0, "bf16"), (dy, "bf16"), (dsT, "bf16"), (keep, "i8")],
+              [("bf16", (t, d)), ("f32", (d, k)), ("f32", (d,)), ("bf16", (1, k - 1, d))], silu=1)
+    ref = L.causal_conv_grad(*tail, None, True)
+    assert not bool(got[0][:-n].any())
+    for g, want, tol in zip([got[0][-n:]] + got[1:], ref, (ex, ew, eb, es)):
+        within(num(g), want, tol, "last rows' gradient")
+    del got
+    print("scan", flush=True)
+    dt, bc = wide() - 1.0, wide(2 * states)
+    dt[:-n] = 0
+    a, skip = -torch.rand((d, states), device=dev), torch.rand((d,), device=dev)
+    h0, dhT = torch.randn((1, d, states), device=dev), torch.randn((1, d, states), device=dev)
+    tail = [num(v) for v in (x[-n:], dt[-n:], bc[-n:], a, skip, h0, dy[-n:], dhT)]
+    ahead, back = scan_bounds(*tail, None, None, "bf16")
+    got = run("selective_scan", [(x, "bf16"), (dt, "bf16"), (bc, "bf16"), (a, "f32"), (skip, "f32"), (h0, "f32"), (keep, "i8")], [("bf16", (t, d)), ("f32", (1, d, states))])
+    assert not bool(got[0][:-n].any())
+    for g, want, tol in zip((got[0][-n:], got[1]), L.selective_scan(*tail[:6]), ahead):
+        within(num(g), want, tol, "last rows of the scan")
+    del got
+    got = run("selective_scan_grad", [(x, "bf16"), (dt, "bf16"), (bc, "bf16"), (a, "f32"), (skip, "f32"), (h0, "f32"), (dy, "bf16"), (dhT, "f32"), (keep, "i8")],
+              [("bf16", (t, d)), ("bf16", (t, d)), ("bf16", (t, 2 * states)), ("f32", (d, states)), ("f32", (d,)), ("f32", (1, d, states))])
+    for i, (g, want, tol) in enumerate(zip(got, L.selective_scan_grad(*tail), back)):
+        if i < 3:
+            assert not bool(g[:-n].any())
+        within(num(g[-n:] if i < 3 else g), want, tol, "last rows' gradient of the scan")
+    del x, dy, dt, bc, got
+    # a vocabulary of 1200000 x 2048, all logits but the last ones 0; then 1000000 rows
+    print("vocabulary", flush=True)
+    m, v, k, n = 3, 1200000, 2048, 4
+    w = torch.zeros((v, k), dtype=torch.bfloat16, device=dev)
+    w[-n:] = (torch.randn((n, k), device=dev) / 16).bfloat16()
+    x = torch.randn((m, k), device=dev).bfloat16()
+    tok = torch.tensor([v - 1, 5, v - n], dtype=torch.int32, device=dev)
+    lp, lse = run("dense_logprobs", [(x, "bf16"), (w, "bf16"), (tok, "i32")], [("f32", (m,))] * 2)
+    some = num(torch.cat([w[:1], w[-n:]]))
+    logits = num(x) @ some.T
+    total = np.log(v - n + np.exp(logits[:, 1:]).sum(1))
+    size = 2 * k * F * (np.abs(num(x)) @ np.abs(some).T).max() + (v / 16 + 100) * F
+    within(num(lse), total, size, "lse of a long vocabulary")
+    at = np.array([logits[0, n], 0.0, logits[2, 1]])
+    within(num(lp), at - total, size, "lp of a long vocabulary")
+    one, half = torch.ones((m,), device=dev), torch.full((m,), 0.5, device=dev)
+    dx, dw = run("dense_logprobs_grad", [(x, "bf16"), (w, "bf16"), (tok, "i32"), (lse, "f32"), (one, "f32"), (half, "f32")], [("bf16", (m, k)), ("bf16", (v, k))])
+    dl = -0.5 * np.exp(logits - total[:, None])
+    dl[0, n] += 1
+    dl[2, 1] += 1
+    want = dl[:, 1:].T @ num(x)
+    within(num(dw[-n:]), want, 2.0 ** -6 * (np.abs(dl[:, 1:]).T @ np.abs(num(x))) + 1e-7, "last rows of dw")
+    within(num(dx), dl[:, 1:] @ some[1:], 2.0 ** -6 * (np.abs(dl[:, 1:]) @ np.abs(some[1:])) + 1e-7, "dx of a long vocabulary")
+    del w, dw
+    print("rows", flush=True)
+    m, v, k = 1000000, 70, 2400
+    x = torch.zeros((m, k), dtype=torch.bfloat16, device=dev)
+    x[-n:] = torch.randn((n, k), device=dev).bfloat16()
+    w = (torch.randn((v, k), device=dev) / 24).bfloat16()
+    tok = torch.randint(0, v, (m,), dtype=torch.int32, device=dev)
+    dlp, dlse = torch.zeros((m,), device=dev), torch.zeros((m,), device=dev)
+    dlp[-n:], dlse[-n:] = -1.0, 0.25
+    lp, lse = run("dense_logprobs", [(x, "bf16"), (w, "bf16"), (tok, "i32")], [("f32", (m,))] * 2)
+    last = num(x[-n:]), num(w), num(tok[-n:])
+    ref = L.dense_logprobs(*last)
+    ahead, back = loss_bounds(*last, ref[1], num(dlp[-n:]), num(dlse[-n:]), "bf16")
+    for g, want, tol in zip((lp, lse), ref, ahead):
+        within(num(g[-n:]), want, tol, "last rows' loss")
+    dx, dw = run("dense_logprobs_grad", [(x, "bf16"), (w, "bf16"), (tok, "i32"), (lse, "f32"), (dlp, "f32"), (dlse, "f32")], [("bf16", (m, k)), ("bf16", (v, k))])
+    ref = L.dense_logprobs_grad(*last, ref[1], num(dlp[-n:]), num(dlse[-n:]))
+    within(num(dx[-n:]), ref[0], back[0], "last rows of dx")
+    within(num(dw), ref[1], back[1], "dw of many rows")
+    assert not bool(dx[:-n].any())

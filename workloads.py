@@ -751,6 +751,128 @@ def recurrent_lm_train(batch=4, steps=16, dim=64, vocab=500, dtype="bf16", packe
     return g, data
 
 
+def _state_space_params(g, rng, data, dtype, dim, states, taps, name, twice):
+    """A layer's weights as params: {name: value id}; twice: those of products a second time, for the backward pass (a param has one layout
+    in a plan)."""
+    ids = {}
+    for w, dt, a in (("wx", dtype, normal(rng, (dim, dim), dim ** -0.5)), ("wz", dtype, normal(rng, (dim, dim), dim ** -0.5)),
+                     ("wt", dtype, normal(rng, (dim, dim), 0.5 * dim ** -0.5)), ("wbc", dtype, normal(rng, (2 * states, dim), dim ** -0.5)),
+                     ("wo", dtype, normal(rng, (dim, dim), dim ** -0.5)), ("bt", "f32", normal(rng, (dim,), 0.5) - 3.0),
+                     ("wc", "f32", uniform(rng, (dim, taps), -1.0, 1.0) * taps ** -0.5), ("bc", "f32", normal(rng, (dim,), 0.1)),
+                     ("a", "f32", -np.arange(1, states + 1) * uniform(rng, (dim, states), 0.8, 1.2)), ("skip", "f32", uniform(rng, (dim,), 0.5, 1.5))):
+        for back in ("", "_b") if twice and w in ("wx", "wz", "wt", "wbc", "wo") else ("",):
+            data[name + w + back] = as_dtype(a, dt)
+            ids[w + back] = g.param(name + w + back, dt, tuple(np.shape(a)))
+    return ids
+
+
+def state_space_lm(batch=4, steps=16, dim=64, states=16, layers=2, vocab=500, taps=4, dtype="bf16", packed=False, config=33):
+    """A selective state-space language model as it is served, in a float type: every layer projects the stream to what its tokens mix
+    and to a gate, mixes them by a short causal convolution and the selective scan, whose steps, B and C are projected from the convolved
+    tokens, and projects the result back; the head gives the log probability of the tokens in `tok` without the logits in memory.
+    steps = 1 is one generated token; a layer's states come in as c<l> (the convolution's tokens) and h<l>, and leave as the outputs behind
+    the head's, in layer order."""
+    rng, rows = rng_for(config), batch * steps
+    g, data = GraphSpec("state_space_lm"), {}
+
+    def alone(kind, ins, outs, **attrs):
+        o, got = g.op(kind, ins, outs, **attrs)
+        g.group([o])
+        return got
+
+    def project(x, w, n, bias=None):
+        o, y = g.op("dense", [x, w], [(dtype, (rows, n))])
+        ops = [o]
+        if bias is not None:
+            o, y = g.op("bias_add", [y[0], bias], [(dtype, (rows, n))], axis=1)
+            ops.append(o)
+        g.group(ops)
+        return y[0]
+
+    data["x"], data["tok"] = as_dtype(normal(rng, (rows, dim)), dtype), rng.integers(-1, vocab, size=rows).astype(np.int32)
+    x, tok = g.input("x", dtype, (rows, dim)), g.input("tok", "i32", (rows,))
+    keep, kept = [], []
+    if packed:
+        flags = np.where(rng.uniform(size=(batch, steps)) < 0.1, 2, 1)
+        flags[0, steps - steps // 4:] = 0
+        data["keep"] = flags.reshape(-1).astype(np.int8)
+        keep = [g.input("keep", "i8", (rows,))]
+    for l in range(layers):
+        p = _state_space_params(g, rng, data, dtype, dim, states, taps, f"l{l}.", False)
+        data[f"c{l}"], data[f"h{l}"] = as_dtype(normal(rng, (batch, taps - 1, dim)), dtype), as_dtype(normal(rng, (batch, dim, states), 0.3), "f32")
+        c0, h0 = g.input(f"c{l}", dtype, (batch, taps - 1, dim)), g.input(f"h{l}", "f32", (batch, dim, states))
+        u, z = project(x, p["wx"], dim), project(x, p["wz"], dim)
+        c, cT = alone("causal_conv", [u, p["wc"], p["bc"], c0] + keep, [(dtype, (rows, dim)), (dtype, (batch, taps - 1, dim))], silu=1)
+        dt, bc = project(c, p["wt"], dim, p["bt"]), project(c, p["wbc"], 2 * states)
+        y, hT = alone("selective_scan", [c, dt, bc, p["a"], p["skip"], h0, z] + keep, [(dtype, (rows, dim)), ("f32", (batch, dim, states))])
+        kept += [cT, hT]
+        o0, (o,) = g.op("dense", [y, p["wo"]], [(dtype, (rows, dim))])
+        o1, (x,) = g.op("add", [o, x], [(dtype, (rows, dim))])
+        g.group([o0, o1])
+    data["wv"] = as_dtype(normal(rng, (vocab, dim), 2 * dim ** -0.5), dtype)
+    lp, lse = alone("dense_logprobs", [x, g.param("wv", dtype, (vocab, dim)), tok], [("f32", (rows,)), ("f32", (rows,))])
+    for v in [lp, lse] + kept:
+        g.output(v)
+    return g, data
+
+
+def state_space_lm_train(batch=4, steps=16, dim=64, states=16, vocab=500, taps=4, dtype="bf16", packed=False, config=34):
+    """One layer of that model and its training step as one graph: forward pass, loss (mean negative log probability of the tokens and a
+    penalty on the squared normaliser, whose derivatives dlp and dlse are inputs), gradients of all weights, of x and of the states."""
+    rng, rows = rng_for(config), batch * steps
+    g = GraphSpec("state_space_lm_train")
+    wide, many, conv_state, scan_state = (dtype, (rows, dim)), (dtype, (rows, 2 * states)), (dtype, (batch, taps - 1, dim)), ("f32", (batch, dim, states))
+    data = {"x": as_dtype(normal(rng, (rows, dim)), dtype), "tok": rng.integers(-1, vocab, size=rows).astype(np.int32),
+            "c0": as_dtype(normal(rng, (batch, taps - 1, dim)), dtype), "h0": as_dtype(normal(rng, (batch, dim, states), 0.3), "f32"),
+            "dcT": as_dtype(np.zeros((batch, taps - 1, dim)), dtype), "dhT": as_dtype(np.zeros((batch, dim, states)), "f32"),
+            "dlp": as_dtype(np.full(rows, -1.0 / rows), "f32"), "dlse": as_dtype(np.full(rows, 0.01 / rows), "f32")}
+    x, tok = g.input("x", *wide), g.input("tok", "i32", (rows,))
+    c0, h0, dcT, dhT = g.input("c0", *conv_state), g.input("h0", *scan_state), g.input("dcT", *conv_state), g.input("dhT", *scan_state)
+    dlp, dlse = g.input("dlp", "f32", (rows,)), g.input("dlse", "f32", (rows,))
+    p = _state_space_params(g, rng, data, dtype, dim, states, taps, "", True)
+    data["wv"] = as_dtype(normal(rng, (vocab, dim), 2 * dim ** -0.5), dtype)
+    wv = g.param("wv", dtype, (vocab, dim))
+    keep = []
+    if packed:
+        data["keep"] = np.where(rng.uniform(size=rows) < 0.1, 2, np.where(rng.uniform(size=rows) < 0.1, 0, 1)).astype(np.int8)
+        keep = [g.input("keep", "i8", (rows,))]
+
+    def alone(kind, ins, outs, **attrs):
+        o, got = g.op(kind, ins, outs, **attrs)
+        g.group([o])
+        return got
+
+    def project(a, w, t):
+        return alone("dense", [a, p[w]], [t])[0]
+
+    u, z = project(x, "wx", wide), project(x, "wz", wide)
+    c, cT = alone("causal_conv", [u, p["wc"], p["bc"], c0] + keep, [wide, conv_state], silu=1)
+    raw, bc = project(c, "wt", wide), project(c, "wbc", many)
+    dt, = alone("bias_add", [raw, p["bt"]], [wide], axis=1)
+    y, hT = alone("selective_scan", [c, dt, bc, p["a"], p["skip"], h0, z] + keep, [wide, scan_state])
+    o = project(y, "wo", wide)
+    lp, lse = alone("dense_logprobs", [o, wv, tok], [("f32", (rows,)), ("f32", (rows,))])
+    do, dwv = alone("dense_logprobs_grad", [o, wv, tok, lse, dlp, dlse], [wide, (dtype, (vocab, dim))])
+    grads = [dwv]
+
+    def back(dy, w, a, t):
+        """A product's gradients: that of the weight leaves, that of the operand goes on."""
+        grads.append(alone("dense_grad_w", [dy, a], [("f32", g.values[p[w]].type.shape)], out_dtype="f32")[0])
+        return alone("dense_grad_x", [dy, p[w + "_b"]], [t])[0]
+
+    dy = back(do, "wo", y, wide)
+    dc, ddt, dbc, da, dskip, dh0, dz = alone("selective_scan_grad", [c, dt, bc, p["a"], p["skip"], h0, dy, dhT, z] + keep,
+                                             [wide, wide, many, ("f32", (dim, states)), ("f32", (dim,)), scan_state, wide])
+    parts = back(ddt, "wt", c, wide), back(dbc, "wbc", c, wide)
+    for more in parts:
+        dc, = alone("add", [dc, more], [wide])
+    du, dwc, dbias, dc0 = alone("causal_conv_grad", [u, p["wc"], p["bc"], c0, dc, dcT] + keep, [wide, ("f32", (dim, taps)), ("f32", (dim,)), conv_state], silu=1)
+    dx, = alone("add", [back(du, "wx", x, wide), back(dz, "wz", x, wide)], [wide])
+    for v in [lp, lse, cT, hT, dx, da, dskip, dh0, dwc, dbias, dc0] + grads:
+        g.output(v)
+    return g, data
+
+
 # --------------------------------------------------------------------------
 # supplementary set E: purely elementwise groups
 # --------------------------------------------------------------------------
