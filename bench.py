@@ -23,6 +23,8 @@ configurations and the HBM-bound groups:
   grads     the gradient operators of dense / conv2d at the benchmark graph's shapes
   recurrent_lm, recurrent_lm_step, recurrent_lm_train  a gated recurrent language model: a prompt scored in 8 bits, one generated token
             of 64 sequences (states updated in place), and the training step of a layer with its head in bf16
+  state_space_lm, state_space_lm_step, state_space_lm_train  the same of a selective state-space language model in bf16, whose logits are
+            never in memory
   mfma_peak a chain of bf16 MFMAs on register operands on every SIMD: what the
             matrix pipes deliver here, next to the quoted 2.5 PFLOP/s
 The default line also carries that calibration ("peaks") and the HBM-bound groups
@@ -173,7 +175,7 @@ def roofline_of(name, k, peak_tflops):
     tflops = k["flops"] / (k["ms"] * 1e-3) / 1e12
     gbs = k["bytes"] / (k["ms"] * 1e-3) / 1e9
     ridge = peak_tflops * 1e12 / (PEAK_HBM_GBS * 1e9)
-    if name.startswith("igemm") and k["flops"] / max(k["bytes"], 1.0) >= ridge:
+    if name.startswith(("igemm", "dense_logprobs")) and k["flops"] / max(k["bytes"], 1.0) >= ridge:
         roof = {"bound": "mfma", "achieved": tflops, "peak": peak_tflops, "unit": "TFLOP/s", "frac": tflops / peak_tflops}
     else:
         roof = {"bound": "hbm", "achieved": gbs, "peak": PEAK_HBM_GBS, "unit": "GB/s", "frac": gbs / PEAK_HBM_GBS}
@@ -192,7 +194,7 @@ def kernels_json(by_kernel, peak_tflops=None):
     for k, v in sorted(by_kernel.items(), key=lambda kv: -kv[1]["ms"]):
         e = {"ms_per_step": v["ms"], "launches": v["launches"], "tflops": rate(v["flops"], v["ms"], 1e12), "gbs": rate(v["bytes"], v["ms"], 1e9)}
         e["hbm_frac"] = e["gbs"] / PEAK_HBM_GBS
-        if peak_tflops and k.startswith("igemm"):
+        if peak_tflops and k.startswith(("igemm", "dense_logprobs")):
             e["mfma_frac"] = e["tflops"] / peak_tflops
         out[k] = e
     return out
@@ -510,13 +512,40 @@ def bench_recurrent_lm(args):
     return out
 
 
+def bench_state_space_lm(args):
+    import workloads as W
+    from paper_1810_00952_amd import harness
+    dim, states, vocab, layers = 1024, 16, 32000, 4
+    if args.workload == "state_space_lm_train":
+        batch, steps = 8, 1024
+        spec, data = W.state_space_lm_train(batch, steps, dim, states, vocab)
+        what = f"one layer of 1024 with {states} states a channel, head of {vocab}, loss and all gradients, {batch} sequences of {steps}, bf16"
+    else:
+        batch, steps = (64, 1) if args.workload == "state_space_lm_step" else (8, 512)
+        spec, data = W.state_space_lm(batch, steps, dim, states, layers, vocab)
+        what = f"{layers} layers of 1024 with {states} states a channel, head of {vocab}, {batch} sequences of {steps}, bf16"
+    s = harness.Session(spec)
+    s.load(data)
+    if steps == 1:                        # a layer's new states over its old ones
+        for i, v in enumerate(spec.outputs[2:]):
+            s.tensors[v] = s.tensors[s.by_name[("c", "h")[i % 2] + str(i // 2)]]
+    s.alloc()
+    ms = time_steps(s.run, args.steps, args.warmup)
+    desc, by_kernel = kernel_table(s, args.profile_reps, ms)
+    dom_name, dom = max(by_kernel.items(), key=lambda kv: kv[1]["ms"])
+    out = base_json(f"tokens/sec {args.workload}", batch * steps / (ms * 1e-3), "tokens/s", args, ms, "bf16", what)
+    out["roofline"] = roofline_of(dom_name, dom, PEAK_BF16_TFLOPS)
+    out["kernels"] = kernels_json(by_kernel, PEAK_BF16_TFLOPS)
+    return out
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--warmup", type=int, default=20)
     ap.add_argument("--workload", default="resnet18",
-                    choices=["resnet18", "resnet18_f32_b1", "eltwise", "eltwise32", "gates", "lstm", "mlp", "lenet", "conv", "copy", "layout", "layout32", "block_nhwc", "maxpool", "mfma_peak", "grads", "launch_pitch", "gemm", "recurrent_lm", "recurrent_lm_step", "recurrent_lm_train"])
+                    choices=["resnet18", "resnet18_f32_b1", "eltwise", "eltwise32", "gates", "lstm", "mlp", "lenet", "conv", "copy", "layout", "layout32", "block_nhwc", "maxpool", "mfma_peak", "grads", "launch_pitch", "gemm", "recurrent_lm", "recurrent_lm_step", "recurrent_lm_train", "state_space_lm", "state_space_lm_step", "state_space_lm_train"])
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--cpu-images", type=int, default=128)
     ap.add_argument("--elements", type=int, default=0, help="copy: number of f32 elements (default 24 Mi)")
@@ -618,6 +647,8 @@ def main():
         out = bench_grads(args)
     elif wl.startswith("recurrent_lm"):
         out = bench_recurrent_lm(args)
+    elif wl.startswith("state_space_lm"):
+        out = bench_state_space_lm(args)
     elif wl == "mfma_peak":
         pk = measure_peaks()
         out = base_json("TFLOP/s bf16 MFMA chain on register operands", pk["mfma_bf16_tflops_measured"], "TFLOP/s", args, 0.0, "bf16", pk["mfma_measure"])
