@@ -134,6 +134,14 @@ struct Walk {
         tok = __ballot(k != 0);
         first = __ballot(k == 2);
     }
+    // whether there is a token among the 256 rows from t on
+    __device__ __forceinline__ bool any(int64_t t) const
+    {
+        int some = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) some |= p.keep[b * p.T + t + 64 * q + (threadIdx.x & 63)];
+        return __ballot(some != 0) != 0;
+    }
     // the tokens before row t0
     template <bool KEEP> __device__ __forceinline__ void before(int64_t t0)
     {
@@ -152,7 +160,9 @@ struct Walk {
             int have = 0;                     // tokens found, the newest first
             const int want = (int)p.K - 1;
             bool open = true;                 // no document's first token among them
-            for (int64_t end = t0; end > 0 && have < want && open; end -= 64) {
+            int64_t end = t0;
+            while (end >= 256 && !any(end - 256)) end -= 256;        // long padding
+            for (; end > 0 && have < want && open; end -= 64) {
                 const int64_t t = end > 64 ? end - 64 : 0;
                 uint64_t tok, first;
                 flags(t, end - t, tok, first);
@@ -413,7 +423,11 @@ __global__ __launch_bounds__(64) void causal_conv_grad_kernel(const CausalConvPa
         walk(std::false_type{});
     }
     // what later tokens give to mine
-    for (int64_t t = t0 + n; owed && t < p.T; t += 64) {
+    int64_t t = t0 + n;
+    if (KEEP) {
+        while (owed && t + 256 <= p.T && !k.any(t)) t += 256;
+    }
+    for (; owed && t < p.T; t += 64) {
         const int64_t m = p.T - t < 64 ? p.T - t : 64;
         uint64_t more = m == 64 ? ~0ull : (1ull << m) - 1, starts = 0;
         if (KEEP) k.flags(t, m, more, starts);

@@ -65,6 +65,27 @@ def test_conv_padding_is_as_if_it_were_not_there(dtype):
             np.testing.assert_array_equal(wide[3], short[3])
 
 
+@pytest.mark.parametrize("gap", [255, 256, 700, 1999])
+def test_conv_over_long_padding(gap):
+    """Tokens far apart are neighbours; a sequence that is padding in front, or at its end, or at all."""
+    b, t, d, k = 4, 2000, 24, 4
+    operands, v = conv_case(b, t, d, k, "f32", "f32", None, seed=gap)
+    keep = np.zeros((b, t))
+    keep[0, [0, 1, t - 1 - (1999 - gap) // 2 if gap < 1999 else t - 1]] = 1
+    keep[1, gap:gap + 70] = 1
+    keep[2, :max(1, t - gap)] = 1
+    x, w, bias, s0, dy, dsT = [np.array(a) for a in v[:6]]
+    tk, keep = tensor(keep.reshape(-1), "i8")
+    operands = operands + [(tk, "i8")]
+    ey, ex, ew, eb, es = conv_bounds(x, w, bias, s0, dy, dsT, keep, True, "f32")
+    y, sT = conv_call(operands, b, t, d, k, "f32", True).run().numbers()
+    ref = L.causal_conv(x, w, bias, s0, keep, True)
+    within(y, ref[0], ey, "long padding")
+    np.testing.assert_array_equal(sT, ref[1])
+    for got, want, tol in zip(conv_grad_call(operands, b, t, d, k, "f32", True).run().numbers(), L.causal_conv_grad(x, w, bias, s0, dy, dsT, keep, True), (ex, ew, eb, es)):
+        within(got, want, tol, "long padding's gradient")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_conv_steps_continue_a_sequence_in_place(dtype):
     """T single steps, the state over the old one, give the bits of the sequence; a step without a token leaves the state."""
@@ -156,6 +177,44 @@ def test_documents_are_apart(b, t, d, n, dtype):
             device = [(tensor(a, ty)[0], ty) for a, ty in zip(vals, (dtype, "f32", "f32", dtype, dtype, dtype, "i8"))]
             got.append((conv_call if kind == "causal_conv" else conv_grad_call)(device, b, t, d, k, dtype, True).run().numbers())
         np.testing.assert_array_equal(got[0][0][out], got[1][0][out], err_msg=kind)
+
+
+@pytest.mark.parametrize("state", [np.nan, np.inf, 1e30])
+@pytest.mark.parametrize("b,t,d,n", [(2, 70, 66, 16), (1, 900, 40, 8), (3, 40, 5, 33)])
+def test_padding_in_front_of_a_document_holds_a_state_that_reaches_nothing(b, t, d, n, state):
+    """Left-padded sequences whose old state is that of something else: nothing of it is in the gradients, not even in sums over all rows."""
+    operands, v = scan_case(b, t, d, n, "f32", True, None, seed=t)
+    keep = np.ones((b, t))
+    for i in range(b):
+        first = t // 3 + 5 * i
+        keep[i, :first], keep[i, first] = 0, 2
+    values = [np.array(a) for a in v[:9]] + [keep.reshape(-1)]
+    values[5][:] = state
+    values[7][:, 0] = state if np.isfinite(state) else 1.0
+    types = ["f32"] * 9 + ["i8"]
+    device = [(tensor(a, ty)[0], ty) for a, ty in zip(values, types)]
+    x, dt, bc, a, skip, h0, dy, dhT, z, keep = values
+    clean = x, dt, bc, a, skip, np.zeros_like(h0), dy, dhT, z, keep
+    ahead, back = scan_bounds(*clean, "f32")
+    for g, want, tol in zip(scan_call(device, b, t, d, n, "f32").run().numbers(), L.selective_scan(*clean[:6], z, keep), ahead):
+        within(g, want, tol, "left-padded")
+    for name, g, want, tol in zip(NAMES, scan_grad_call(device, b, t, d, n, "f32").run().numbers(), L.selective_scan_grad(*clean[:8], z, keep), back):
+        within(g, want, tol, "left-padded " + name)
+
+
+@pytest.mark.parametrize("b,t,d,n", [(1, 5000, 3, 2), (1, 2500, 64, 16), (2, 1300, 5, 40)])
+def test_scan_of_many_chunks(b, t, d, n):
+    """Few channels: every chunk of rows adds up those before it."""
+    operands, v = scan_case(b, t, d, n, "f32", True, "some", seed=t)
+    x, dt, bc, a, skip, h0, dy, dhT, z, keep = v
+    a[-1, -1] = -0.01                                          # (a state that grows over thousands of rows leaves f32)
+    operands[3] = (tensor(a, "f32")[0], "f32")
+    a = operands[3][0].double().cpu().numpy()
+    ahead, back = scan_bounds(x, dt, bc, a, skip, h0, dy, dhT, z, keep, "f32")
+    for g, want, tol in zip(scan_call(operands, b, t, d, n, "f32").run().numbers(), L.selective_scan(x, dt, bc, a, skip, h0, z, keep), ahead):
+        within(g, want, tol, "many chunks")
+    for name, g, want, tol in zip(NAMES, scan_grad_call(operands, b, t, d, n, "f32").run().numbers(), L.selective_scan_grad(x, dt, bc, a, skip, h0, dy, dhT, z, keep), back):
+        within(g, want, tol, "many chunks " + name)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
