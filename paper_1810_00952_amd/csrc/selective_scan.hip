@@ -754,9 +754,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
             fore.start(mine + l * R, half ^ 1);
             lds_barrier();
             const int32_t t0 = tile * ROWS;
-            for (int i = threadIdx.x; i < ROWS * 2 * (int)p.N; i += 256) {
-                const int n = i % (int)p.N, which = i / (int)p.N % 2, t = i / (2 * (int)p.N);
-                if (t0 + t >= left) break;
+            constexpr int WIDE = LANES * R;
+#pragma unroll
+            for (int e = 0; e < (ROWS * 2 * WIDE + 255) / 256; ++e) {
+                const int i = e * 256 + (int)threadIdx.x, n = i % WIDE, which = i / WIDE % 2, t = i / (2 * WIDE);
+                if (t >= ROWS || n >= p.N || t0 + t >= left) continue;
                 const int r = n % R, slot = slot_of(which, r, n / R);
                 float sum = sc[half][0][t][r / 4][slot];
 #pragma unroll
