@@ -324,7 +324,7 @@ template <int R> __device__ __forceinline__ void from_lds(const float *s, float 
 // B and C of the rows to come, read AHEAD rows before they are used, across the tiles: the compiler, which counts on more waves than there are, would
 // read them where they are used.  Row k of a walk through a tile; from ROWS on the next tile's, which lies in the other half of the wave's LDS.
 template <int R, int ROWS, bool BACK, bool WITH_B, bool WITH_C> struct Coming {
-    static constexpr int AHEAD = R >= 16 ? 1 : R >= 8 ? 2 : 4, RING = 2 * AHEAD;
+    static constexpr int AHEAD = R >= 16 ? 1 : R >= 4 ? 2 : 4, RING = 2 * AHEAD;
     static_assert(ROWS % RING == 0, "a tile's first row is in the ring's first place");
     float b[RING][R], c[RING][R];
     const float *s;                            // the lane's part of the two halves
