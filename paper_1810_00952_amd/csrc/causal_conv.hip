@@ -487,24 +487,35 @@ __global__ __launch_bounds__(1024) void sum_shares_kernel(const SumShares q)
     }
 }
 
-// many columns: four of them a thread, one share after the other
+// many columns: VEC of them a thread, one share after the other
+template <int VEC>
 __global__ __launch_bounds__(256) void sum_columns_kernel(const SumShares q)
 {
-    const int64_t j = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t j = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC;
     if (j >= q.J) return;
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (VEC == 4) {
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
-    for (int64_t i = 0; i < q.P; ++i) v += *(const f32x4 *)(q.part + i * q.stride + j);
-    if (q.dst_dtype == DT_BF16) *(u32x2 *)((uint16_t *)q.dst + j) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    else *(f32x4 *)((float *)q.dst + j) = v;
+        for (int64_t i = 0; i < q.P; ++i) v += *(const f32x4 *)(q.part + i * q.stride + j);
+        if (q.dst_dtype == DT_BF16) *(u32x2 *)((uint16_t *)q.dst + j) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else *(f32x4 *)((float *)q.dst + j) = v;
+    } else {
+        float v = 0.0f;
+#pragma unroll 8
+        for (int64_t i = 0; i < q.P; ++i) v += q.part[i * q.stride + j];
+        store_from_f32(q.dst, q.dst_dtype, j, v);
+    }
 }
 
 hipError_t launch_sum_shares(const SumShares &q, hipStream_t s)
 {
     if (q.J < 1 || q.P < 1 || (q.J + 63) / 64 > 0x3fffff) return hipErrorInvalidValue;
-    // (67 MB in 32 shares of 524288 columns 30 -> 14 us)
-    if (q.J >= (1 << 16) && q.P <= 256 && q.J % 4 == 0 && q.stride % 4 == 0 && !q.turn && q.J1 == q.J && (uintptr_t)q.part % 16 == 0) {
-        hipLaunchKernelGGL(sum_columns_kernel, dim3((unsigned)((q.J / 4 + 255) / 256)), dim3(256), 0, s, q);
+    // (67 MB in 32 shares of 524288 columns 30 -> 12 us)
+    if (q.J >= (1 << 16) && q.P <= 256 && q.J1 == q.J && !q.turn) {
+        if (q.J % 4 == 0 && q.stride % 4 == 0 && ((uintptr_t)q.part | (uintptr_t)q.dst) % 16 == 0)
+            hipLaunchKernelGGL((sum_columns_kernel<4>), dim3((unsigned)((q.J / 4 + 255) / 256)), dim3(256), 0, s, q);
+        else
+            hipLaunchKernelGGL((sum_columns_kernel<1>), dim3((unsigned)((q.J + 255) / 256)), dim3(256), 0, s, q);
         return hipGetLastError();
     }
     hipLaunchKernelGGL(sum_shares_kernel, dim3((unsigned)((q.J + 63) / 64)), dim3(1024), 0, s, q);

@@ -405,15 +405,18 @@ __global__ __launch_bounds__(64 * WM * WN) void nt_tile_kernel(const NtParams p,
     nt_tile<E, WM, WN, TM, TN>(p, epi, blockIdx.x, 0);
 }
 
-// dx's product, its slices of K one behind the other, and dw's
+// dx's product and dw's, the slices of K of each one behind the other
 template <typename E, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN) void nt_pair_kernel(const NtParams a, OutEpi ea, int32_t slices, const NtParams b, const OutEpi eb)
+__global__ __launch_bounds__(64 * WM * WN) void nt_pair_kernel(const NtParams a, const OutEpi ea, int32_t slices_a, const NtParams b, const OutEpi eb)
 {
-    const int32_t tiles = a.nblk_m * a.nblk_n, bid = (int32_t)blockIdx.x;
-    const bool first = bid < tiles * slices;
-    const int32_t slice = first ? bid / tiles : 0;
-    if (ea.sum) ea.sum += (int64_t)slice * ea.M * ea.N;
-    nt_tile<E, WM, WN, TM, TN>(first ? a : b, first ? ea : eb, first ? bid - slice * tiles : bid - tiles * slices, slice);
+    const int32_t of_a = a.nblk_m * a.nblk_n, bid = (int32_t)blockIdx.x;
+    const bool first = bid < of_a * slices_a;
+    const NtParams p = first ? a : b;
+    OutEpi e = first ? ea : eb;
+    const int32_t at = first ? bid : bid - of_a * slices_a, tiles = p.nblk_m * p.nblk_n, slice = at / tiles;
+    if (e.sum) e.sum += (int64_t)slice * e.M * e.N;
+    if (e.before) e.before += (int64_t)slice * e.M * e.N;
+    nt_tile<E, WM, WN, TM, TN>(p, e, at - slice * tiles, slice);
 }
 
 // ---------------------------------------------------------------------------
@@ -489,18 +492,47 @@ struct Tile { int32_t side, threads; float alone, share; };
 constexpr Tile tiles_bf16[] = {{64, 256, 0.70f, 0.25f}, {128, 256, 0.95f, 0.62f}, {256, 512, 1.60f, 2.00f}};
 constexpr Tile tiles_f32[] = {{64, 256, 1.00f, 0.50f}, {128, 256, 3.60f, 1.85f}};
 int64_t tiles_along(int64_t n, int64_t side) { return (n + side - 1) / side; }
-// of the products [M, N] (and [M2, N2], in the same launch, as many lines of K), `slices` times the first one's tiles
-template <typename E> int32_t tile_of(int64_t M, int64_t N, int64_t slices = 1, int64_t M2 = 0, int64_t N2 = 0)
+template <typename E, typename F> void each_tile(const F &look)
+{
+    if constexpr (sizeof(E) == 2) for (const Tile &t : tiles_bf16) look(t);
+    else for (const Tile &t : tiles_f32) look(t);
+}
+// of the product [M, N]
+template <typename E> int32_t tile_of(int64_t M, int64_t N)
 {
     int32_t best = 0;
     float least = INFINITY;
-    auto look = [&](const Tile &t) {
-        const float wgs = (float)(tiles_along(M, t.side) * tiles_along(N, t.side) * slices + tiles_along(M2, t.side) * tiles_along(N2, t.side));
-        const float line = fmaxf(t.alone, t.share * wgs / 256.0f);
+    each_tile<E>([&](const Tile &t) {
+        const float line = fmaxf(t.alone, t.share * (float)(tiles_along(M, t.side) * tiles_along(N, t.side)) / 256.0f);
         if (line < least) { least = line; best = t.side; }
-    };
-    if constexpr (sizeof(E) == 2) for (const Tile &t : tiles_bf16) look(t);
-    else for (const Tile &t : tiles_f32) look(t);
+    });
+    return best;
+}
+
+// Tile and slices of K of two products in one launch, dx [M, K] over `cols` and dw [cols, K] over M: a product of few long tiles is cut into slices near what
+// a CU has of the whole, whose shares are written and read once more (f32 3519 x 7399 x 128 475 -> 131 us, bf16 1809 x 34304 x 869 709 -> 355)
+struct Pair { int32_t side, a, b; };
+template <typename E> Pair pair_of(int64_t M, int64_t K, int64_t cols, int64_t most_bytes)
+{
+    constexpr int64_t per = LINE / sizeof(E);
+    Pair best{0, 1, 1};
+    float least = INFINITY;
+    each_tile<E>([&](const Tile &t) {
+        const int64_t ta = tiles_along(M, t.side) * tiles_along(K, t.side), tb = tiles_along(cols, t.side) * tiles_along(K, t.side);
+        const int64_t la = tiles_along(cols, per), lb = tiles_along(M, per);
+        const float all = (float)(ta * la + tb * lb) / 256.0f;
+        auto slices = [&](int64_t lines, int64_t bytes) {
+            int64_t n = (int64_t)ceilf((float)lines / fmaxf(1.25f * all * t.share / t.alone, 8.0f));
+            n = n > 64 ? 64 : n;
+            if (n * bytes > most_bytes) n = most_bytes / bytes;
+            return (int32_t)(n > 1 ? n : 1);
+        };
+        Pair f{t.side, slices(la, M * K * 4), slices(lb, cols * K * 4)};
+        const float lines = fmaxf((float)la / f.a, (float)lb / f.b);
+        const float shares = (f.a > 1 ? (float)f.a * M * K : 0.0f) + (f.b > 1 ? (float)f.b * cols * K : 0.0f);
+        const float us = fmaxf(lines * t.alone, all * t.share) + shares * 8.0f / 5e6f;
+        if (us < least) { least = us; best = f; }
+    });
     return best;
 }
 
@@ -523,20 +555,20 @@ template <typename E, typename Epi> void go_nt(NtParams q, const Epi &epi, int32
     else hipLaunchKernelGGL((nt_tile_kernel<E, 2, 2, 1, 1, Epi>), grid, dim3(256), 0, s, q, epi);
 }
 
-template <typename E> void go_pair(NtParams a, const OutEpi &ea, int32_t slices, NtParams b, const OutEpi &eb, int32_t side, hipStream_t s)
+template <typename E> void go_pair(NtParams a, const OutEpi &ea, NtParams b, const OutEpi &eb, const Pair &f, hipStream_t s)
 {
-    split<E>(a, side, slices);
-    split<E>(b, side, 1);
-    const dim3 grid((unsigned)((int64_t)a.nblk_m * a.nblk_n * slices + (int64_t)b.nblk_m * b.nblk_n));
+    split<E>(a, f.side, f.a);
+    split<E>(b, f.side, f.b);
+    const dim3 grid((unsigned)((int64_t)a.nblk_m * a.nblk_n * f.a + (int64_t)b.nblk_m * b.nblk_n * f.b));
     if constexpr (sizeof(E) == 2) {
-        if (side == 256) { hipLaunchKernelGGL((nt_pair_kernel<E, 2, 4, 4, 2>), grid, dim3(512), 0, s, a, ea, slices, b, eb); return; }
+        if (f.side == 256) { hipLaunchKernelGGL((nt_pair_kernel<E, 2, 4, 4, 2>), grid, dim3(512), 0, s, a, ea, f.a, b, eb); return; }
     }
-    if (side == 128) hipLaunchKernelGGL((nt_pair_kernel<E, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, ea, slices, b, eb);
-    else hipLaunchKernelGGL((nt_pair_kernel<E, 2, 2, 1, 1>), grid, dim3(256), 0, s, a, ea, slices, b, eb);
+    if (f.side == 128) hipLaunchKernelGGL((nt_pair_kernel<E, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, ea, f.a, b, eb);
+    else hipLaunchKernelGGL((nt_pair_kernel<E, 2, 2, 1, 1>), grid, dim3(256), 0, s, a, ea, f.a, b, eb);
 }
 
-// Pieces of the vocabulary: columns of one, and how many slices of K dx's product takes (one piece only)
-struct Pieces { int64_t cols, count; int32_t slices; };
+// Pieces of the vocabulary: columns of one, and how its gradients' products go
+struct Pieces { int64_t cols, count; Pair pair; };
 Pieces pieces_of(const DenseLogprobsParams &p)
 {
     const int64_t e = (int64_t)esize(p), Mp = up(p.M, LINE / e);
@@ -547,20 +579,12 @@ Pieces pieces_of(const DenseLogprobsParams &p)
     k.count = (p.V + cols - 1) / cols;
     k.cols = up((p.V + k.count - 1) / k.count, 256);
     k.count = (p.V + k.cols - 1) / k.cols;
-    k.slices = 1;
-    const int64_t tiles = ((p.M + 127) / 128) * ((p.K + 127) / 128), lines = up(p.V, LINE / e) * e / LINE;
-    if (k.count == 1 && tiles < 256) {
-        int64_t n = 512 / tiles;
-        if (n > lines / 8) n = lines / 8;
-        if (n > 64) n = 64;
-        k.slices = n < 1 ? 1 : (int32_t)n;
-        const int64_t each = (lines + k.slices - 1) / k.slices;       // no slice is empty
-        k.slices = (int32_t)((lines + each - 1) / each);
-    }
+    const int64_t real = k.cols < p.V ? k.cols : p.V;
+    k.pair = p.dtype == DT_BF16 ? pair_of<uint16_t>(p.M, p.K, real, p.piece_bytes) : pair_of<float>(p.M, p.K, real, p.piece_bytes);
     return k;
 }
 
-struct Layout { int64_t g, gt, wt, xt, acc, bytes; };
+struct Layout { int64_t g, gt, wt, xt, dx, dw, bytes; };
 Layout layout_of(const DenseLogprobsParams &p, const Pieces &k)
 {
     const int64_t e = (int64_t)esize(p), Mp = up(p.M, LINE / e);
@@ -571,7 +595,8 @@ Layout layout_of(const DenseLogprobsParams &p, const Pieces &k)
     l.gt = take(k.cols * Mp * e);
     l.wt = take(p.K * k.cols * e);
     l.xt = take(p.K * Mp * e);
-    l.acc = take(k.count > 1 || k.slices > 1 ? (int64_t)k.slices * p.M * p.K * 4 : 0);
+    l.dx = take(k.count > 1 || k.pair.a > 1 ? (int64_t)k.pair.a * p.M * p.K * 4 : 0);
+    l.dw = take(k.pair.b > 1 ? (int64_t)k.pair.b * k.cols * p.K * 4 : 0);
     l.bytes = at;
     return l;
 }
@@ -605,7 +630,9 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
     const int64_t Mp = up(p.M, LINE / e);
     char *const ws = (char *)p.part;
     E *const g = (E *)(ws + at.g), *const gt = (E *)(ws + at.gt), *const wt = (E *)(ws + at.wt), *const xt = (E *)(ws + at.xt);
-    float *const acc = (float *)(ws + at.acc);
+    float *const of_x = (float *)(ws + at.dx), *const of_w = (float *)(ws + at.dw);
+    SumShares sums{};
+    sums.dst_dtype = p.dtype;
     turn<E>(p.x, xt, p.M, p.K, p.ldx / e, Mp, &p, s);
     for (int64_t i = 0; i < k.count; ++i) {
         const int64_t v0 = i * k.cols, cols = p.V - v0 < k.cols ? p.V - v0 : k.cols, Vp = up(cols, LINE / e);
@@ -622,23 +649,25 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         a.x = g; a.w = wt; a.M = p.M; a.N = p.K; a.ldx = a.ldw = Vp * e; a.kbytes = (int32_t)(Vp * e);
         OutEpi o{};
         o.M = p.M; o.N = p.K; o.y = p.dx; o.y_dtype = p.dtype;
-        if (k.slices > 1) {
-            o.sum = acc;
-        } else {
-            o.before = i > 0 ? acc : nullptr;
-            o.sum = i + 1 < k.count ? acc : nullptr;
-        }
+        // every slice adds up over the pieces
+        o.before = i > 0 ? of_x : nullptr;
+        o.sum = k.pair.a > 1 || i + 1 < k.count ? of_x : nullptr;
         NtParams b{};
         b.x = gt; b.w = xt; b.M = cols; b.N = p.K; b.ldx = b.ldw = Mp * e; b.kbytes = (int32_t)(Mp * e);
         OutEpi d{};
         d.M = cols; d.N = p.K; d.y = (E *)p.dw + v0 * p.K; d.y_dtype = p.dtype;
-        go_pair<E>(a, o, k.slices, b, d, tile_of<E>(p.M, p.K, k.slices, cols, p.K), s);
+        d.sum = k.pair.b > 1 ? of_w : nullptr;
+        go_pair<E>(a, o, b, d, k.pair, s);
+        if (k.pair.b > 1) {
+            sums.part = of_w; sums.P = k.pair.b; sums.J = sums.J1 = sums.stride = cols * p.K; sums.dst = d.y;
+            const hipError_t er = launch_sum_shares(sums, s);
+            if (er != hipSuccess) return er;
+        }
     }
     hipError_t er = hipGetLastError();
-    if (er != hipSuccess || k.slices == 1) return er;
-    SumShares q{};
-    q.part = acc; q.P = k.slices; q.J = q.J1 = q.stride = p.M * p.K; q.dst = p.dx; q.dst_dtype = p.dtype;
-    return launch_sum_shares(q, s);
+    if (er != hipSuccess || k.pair.a == 1) return er;
+    sums.part = of_x; sums.P = k.pair.a; sums.J = sums.J1 = sums.stride = p.M * p.K; sums.dst = p.dx;
+    return launch_sum_shares(sums, s);
 }
 
 }  // namespace

@@ -268,7 +268,7 @@ def loss_grad_call(operands, lse, m, v, k, dtype, **more):
 
 LOSSES = [(1, 1, 1), (1, 700, 64), (3, 2, 5), (5, 129, 17), (17, 1000, 40), (33, 333, 128), (64, 4097, 8), (128, 128, 130), (129, 257, 33), (300, 5003, 96), (1030, 70, 64),
           (8, 20000, 24), (2, 70001, 16), (700, 2000, 200),
-          (1100, 16000, 40), (200, 12000, 1000)]
+          (1100, 16000, 40), (200, 12000, 1000), (6000, 130, 40)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
