@@ -9,6 +9,9 @@
 // the last K - 1 tokens in registers; those before its run it finds by itself.  keep is the same for all lanes: a run's flags are two
 // masks.  Of the gradient the wave also walks on behind its run, until its own tokens have all they get from later ones; its share of
 // dw and db goes to memory, and a second launch adds the shares up, in a fixed order.
+//
+// HBM bounds both: 8 x 4096 x 2048 bf16, K 4, with the gate, forward 54 us (268 MB, 5.0 TB/s), gradient 98 (403 MB, 4.1 TB/s: 136 registers are three waves a
+// SIMD) and 5 of the shares; 1 x 16384 x 4096 in documents of some 400 tokens 63 to 68.  One token of 64 sequences: 3.9 us, a launch's own time.
 #include <type_traits>
 
 #include "igemm_lds.h"
@@ -510,7 +513,7 @@ __global__ __launch_bounds__(256) void sum_columns_kernel(const SumShares q)
 hipError_t launch_sum_shares(const SumShares &q, hipStream_t s)
 {
     if (q.J < 1 || q.P < 1 || (q.J + 63) / 64 > 0x3fffff) return hipErrorInvalidValue;
-    // (67 MB in 32 shares of 524288 columns 30 -> 12 us)
+    // few shares of many columns: a thread of its own for every four (67 MB in 32 shares of 524288 columns 30 -> 12 us); where columns are few, sixteen waves share one's shares
     if (q.J >= (1 << 16) && q.P <= 256 && q.J1 == q.J && !q.turn) {
         if (q.J % 4 == 0 && q.stride % 4 == 0 && ((uintptr_t)q.part | (uintptr_t)q.dst) % 16 == 0)
             hipLaunchKernelGGL((sum_columns_kernel<4>), dim3((unsigned)((q.J / 4 + 255) / 256)), dim3(256), 0, s, q);
@@ -532,7 +535,7 @@ Form form_of(const CausalConvParams &p)
     const int whole = p.dtype == DT_BF16 && p.K <= 4 ? 8 : 4;
     f.vec = p.D % whole == 0 ? whole : 1;
     f.slabs = (int32_t)((p.D + 64 * f.vec - 1) / (64 * f.vec));
-    // long runs read fewer tokens before them and leave fewer shares, short ones fill the CUs
+    // long runs read fewer tokens before them and leave fewer shares, short ones fill the CUs: eight waves of each
     f.rows = RUN;
     while (f.rows > 16 && p.B * f.slabs * ((p.T + f.rows - 1) / f.rows) < 2048) f.rows /= 2;
     f.runs = (int32_t)((p.T + f.rows - 1) / f.rows);

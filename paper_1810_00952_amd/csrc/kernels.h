@@ -390,7 +390,7 @@ struct SumShares { const float *part; void *dst; float *dst2; int64_t P, J, J1, 
 hipError_t launch_sum_shares(const SumShares &q, hipStream_t s);
 // selective_scan.hip.  z null: no gate; keep null: every row a token.  states: the state before every sel_scan_state_rows-th row,
 // [B][ceil(T / sel_scan_state_rows)][D][N]: the forward pass writes it where it is not null (y and hT may be null then), the gradient reads it.
-// gated, keeps: whether there is a z, a keep (the scratch is sized before the pointers are known)
+// gated, keeps: whether there is a z, a keep; a launch whose pointers say otherwise is refused
 struct SelScanParams {
     const void *x, *dt, *bc, *z, *dy; const float *a, *skip, *h0, *dhT; const int8_t *keep;
     void *y, *dx, *ddt, *dbc, *dz; float *hT, *da, *dskip, *dh0;

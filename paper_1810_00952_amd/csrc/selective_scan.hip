@@ -14,6 +14,10 @@
 // padding has s = s x = B = C = du = 0 and leaves state and derivative as they are.  Few channels: the rows are cut into chunks, a workgroup
 // each; a launch ahead finds what each chunk makes of the state before it (P h + H; the derivative alike), P = exp(a sum s), and the workgroups
 // add up the chunks before theirs.
+//
+// The vector units bound it: a state and token is an exponential (four issue slots of a wave) and four more operations forwards, some twenty both ways.
+// 8 x 2048 x 2048 x 16 bf16: forward 215 us, 62 % of what its one wave a SIMD is there for are vector instructions, gradient 590, 67 %; two waves a SIMD of
+// the gradient would spill (656 -> 1690).  1 x 16384 x 2048 x 16 in documents: 148 of the launch ahead and 179.  One token of 64 sequences: 7 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,7 +30,7 @@ namespace {
 constexpr int LANES = 4, CHANNELS = 64;       // lanes of a channel, channels of a workgroup
 constexpr float LOG2E = 1.4426950408889634f;
 
-// Rows of a tile: of the gradient as many as its states and gates fit the registers
+// Rows of a tile: of the gradient as many as its states and gates fit the registers; 32 forwards gave nothing
 constexpr int rows_of(int R) { return R <= 4 ? 16 : 64 / R; }
 
 // Chunks' P of which a document's first row is part: -0, which no product of gates is

@@ -11,7 +11,8 @@ F = U["f32"]
 
 
 def sigmoid(v):
-    return 1 / (1 + np.exp(-v))
+    with np.errstate(over="ignore"):
+        return 1 / (1 + np.exp(-v))
 
 
 def flags(rng, b, t, how):
