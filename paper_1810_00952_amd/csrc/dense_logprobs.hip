@@ -124,7 +124,7 @@ struct StatsEpi {
     }
 };
 
-// dl to g, as it lies, and to gt, transposed
+// dl to g, as it lies, where there is one, and to gt, transposed
 template <typename E> struct GradEpi {
     E *g, *gt; int64_t ldg, ldgt;             // elements
     const int32_t *tok; const float *lse, *dlp, *dlse;
@@ -170,7 +170,7 @@ template <typename E> struct GradEpi {
                         const int64_t n = nj + 8 * k + 4 * half;
                         const f32x4 v = {acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
                         if (n < Vp) {
-                            if (m < M) *(f32x4 *)(g + m * ldg + n) = v;
+                            if (g && m < M) *(f32x4 *)(g + m * ldg + n) = v;
                             if (m < Mp) {
 #pragma unroll
                                 for (int c = 0; c < 4; ++c) gt[(n + c) * ldgt + m] = v[c];
@@ -193,7 +193,7 @@ template <typename E> struct GradEpi {
                             const uint32_t word = odd ? (other >> 16) | (mine & 0xffff0000u) : (mine & 0xffffu) | (other << 16);
                             *(uint32_t *)(block + (8 * k + 4 * half + 2 * d + (odd ? 1 : 0)) * ROW + i * 64 + (frow & 30) * 2) = word;
                         }
-                    put_row((uint16_t *)g + m * ldg + nj, c, half, m < M, nj, Vp);
+                    put_row((uint16_t *)g + m * ldg + nj, c, half, g && m < M, nj, Vp);
                 }
             }
             if constexpr (sizeof(E) == 2) {
@@ -487,8 +487,71 @@ __global__ __launch_bounds__(256) void turn_rows_kernel(const E *src, E *dst, in
         if (c0 + k < C && r0 + c < Rp) dst[(c0 + k) * Rp + r0 + c] = s[c][k];
 }
 
+// ---------------------------------------------------------------------------
+// dx of up to MR rows: w's rows as they lie, 16 bytes a lane, times the wave's numbers of dl; grid's y: slices of w's rows, of which each wave takes every
+// fourth.  The products' way would turn w first, two passes more over it, and multiply tiles of 64 rows.
+// ---------------------------------------------------------------------------
+template <typename E, int MR>
+__global__ __launch_bounds__(256) void few_rows_kernel(const uint32_t *__restrict__ gt, int64_t ldgt, const char *__restrict__ w, int64_t ldw, const float *before, float *sum, int32_t M, int64_t K, int64_t rows, int64_t slice_rows)
+{
+    constexpr int VEC = 16 / sizeof(E), WIDE = 64 * VEC, UNDER_WAY = 8;
+    __shared__ float s[MR][WIDE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t k0 = (int64_t)blockIdx.x * WIDE, k = k0 + lane * VEC;
+    const int64_t begin = (int64_t)blockIdx.y * slice_rows, end = min(begin + slice_rows, rows);
+    const char *const from = w + (k < K ? k : 0) * (int64_t)sizeof(E);         // a lane behind the last column: some other one's, nothing of which is stored
+    float acc[MR][VEC];
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) acc[m][c] = 0.0f;
+    auto add = [&](const u32x4 &q, int64_t v) __attribute__((always_inline)) {
+        const uint32_t *const g = gt + v * ldgt;                     // words: of bf16 two rows' numbers
+        float x[VEC];
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) {
+            if constexpr (sizeof(E) == 4) x[c] = __uint_as_float(q[c]);
+            else x[c] = __uint_as_float(c & 1 ? q[c >> 1] & 0xffff0000u : q[c >> 1] << 16);
+        }
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            float d;
+            if constexpr (sizeof(E) == 4) d = __uint_as_float(g[m]);
+            else d = __uint_as_float(m & 1 ? g[m >> 1] & 0xffff0000u : g[m >> 1] << 16);
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) acc[m][c] = __builtin_fmaf(d, x[c], acc[m][c]);
+        }
+    };
+    int64_t v = begin + wave;
+    for (; v + 4 * (UNDER_WAY - 1) < end; v += 4 * UNDER_WAY) {
+        u32x4 q[UNDER_WAY];
+#pragma unroll
+        for (int u = 0; u < UNDER_WAY; ++u) q[u] = *(const u32x4 *)(from + (v + 4 * u) * ldw);
+#pragma unroll
+        for (int u = 0; u < UNDER_WAY; ++u) add(q[u], v + 4 * u);
+    }
+    for (; v < end; v += 4) add(*(const u32x4 *)(from + v * ldw), v);
+    for (int t = 0; t < 4; ++t) {                                    // the waves' sums, one behind the other
+        if (wave == t) {
+#pragma unroll
+            for (int m = 0; m < MR; ++m)
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) s[m][lane * VEC + c] = t ? s[m][lane * VEC + c] + acc[m][c] : acc[m][c];
+        }
+        __syncthreads();
+    }
+    const int64_t share = (int64_t)blockIdx.y * M * K;
+    for (int i = threadIdx.x; i < M * WIDE; i += 256) {
+        const int m = i / WIDE, c = i % WIDE;
+        if (k0 + c >= K) continue;
+        const int64_t at = share + m * K + k0 + c;
+        sum[at] = before ? before[at] + s[m][c] : s[m][c];
+    }
+}
+
 namespace {
 
+constexpr int64_t FEW = 16;                   // rows: dx by few_rows_kernel
 constexpr int64_t LINE = 128, PIECE_MAX = 1 << 20;      // a piece's columns: a row of dl is reached by 31-bit offsets from its tile's first
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 size_t esize(const DenseLogprobsParams &p) { return p.dtype == DT_BF16 ? 2 : 4; }
@@ -564,7 +627,7 @@ template <typename E, typename Epi> void go_nt(NtParams q, const Epi &epi, int32
 
 template <typename E> void go_pair(NtParams a, const OutEpi &ea, NtParams b, const OutEpi &eb, const Pair &f, hipStream_t s)
 {
-    split(a, f.side, f.a);
+    split(a, f.side, f.a > 0 ? f.a : 1);             // 0: b's alone
     split(b, f.side, f.b);
     const dim3 grid((unsigned)((int64_t)a.nblk_m * a.nblk_n * f.a + (int64_t)b.nblk_m * b.nblk_n * f.b));
     if constexpr (sizeof(E) == 2) {
@@ -587,6 +650,14 @@ Pieces pieces_of(const DenseLogprobsParams &p)
     k.cols = up((p.V + k.count - 1) / k.count, 256);
     k.count = (p.V + k.cols - 1) / k.cols;
     const int64_t real = k.cols < p.V ? k.cols : p.V;
+    if (p.M <= FEW) {
+        // dw's product alone; the slices are those of few_rows_kernel, two workgroups a CU
+        const int64_t wide = tiles_along(p.K, 64 * (16 / e)), most = (real + 63) / 64;
+        int64_t n = 512 / wide > 1 ? 512 / wide : 1;
+        if (n > most) n = most;
+        k.pair = Pair{p.dtype == DT_BF16 ? tile_of<uint16_t>(real, p.K) : tile_of<float>(real, p.K), (int32_t)n, 1};
+        return k;
+    }
     k.pair = p.dtype == DT_BF16 ? pair_of<uint16_t>(p.M, p.K, real, p.piece_bytes) : pair_of<float>(p.M, p.K, real, p.piece_bytes);
     return k;
 }
@@ -598,11 +669,12 @@ Layout layout_of(const DenseLogprobsParams &p, const Pieces &k)
     Layout l;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
-    l.g = take(p.M * k.cols * e);
+    const bool few = p.M <= FEW;
+    l.g = take(few ? 0 : p.M * k.cols * e);
     l.gt = take(k.cols * Mp * e);
-    l.wt = take(p.K * k.cols * e);
+    l.wt = take(few ? 0 : p.K * k.cols * e);
     l.xt = take(p.K * Mp * e);
-    l.dx = take(k.count > 1 || k.pair.a > 1 ? (int64_t)k.pair.a * p.M * p.K * 4 : 0);
+    l.dx = take(few || k.count > 1 || k.pair.a > 1 ? (int64_t)k.pair.a * p.M * p.K * 4 : 0);
     l.dw = take(k.pair.b > 1 ? (int64_t)k.pair.b * k.cols * p.K * 4 : 0);
     l.bytes = at;
     return l;
@@ -629,6 +701,19 @@ template <typename E> void turn(const void *src, void *dst, int64_t R, int64_t C
                        rows ? rows->tok : nullptr, rows ? rows->dlp : nullptr, rows ? rows->dlse : nullptr, rows ? rows->V : 0);
 }
 
+// rows: of w, from w on; dx's shares of them, added to those of the pieces before
+template <typename E> void few_rows(const DenseLogprobsParams &p, const E *gt, int64_t ldgt, const char *w, int64_t rows, int32_t slices, bool first, float *sum, hipStream_t s)
+{
+    constexpr int64_t wide = 64 * (16 / sizeof(E));
+    const dim3 grid((unsigned)tiles_along(p.K, wide), (unsigned)slices), wg(256);
+    auto with = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, wg, 0, s, (const uint32_t *)gt, (int64_t)(ldgt * sizeof(E) / 4), w, p.ldw, first ? nullptr : sum, sum, (int32_t)p.M, p.K, rows, (rows + slices - 1) / slices);
+    };
+    if (p.M <= 4) with(few_rows_kernel<E, 4>);
+    else if (p.M <= 8) with(few_rows_kernel<E, 8>);
+    else with(few_rows_kernel<E, 16>);
+}
+
 template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStream_t s)
 {
     constexpr int64_t e = sizeof(E);
@@ -644,11 +729,12 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
     for (int64_t i = 0; i < k.count; ++i) {
         const int64_t v0 = i * k.cols, cols = p.V - v0 < k.cols ? p.V - v0 : k.cols, Vp = up(cols, LINE / e);
         const char *const w = (const char *)p.w + v0 * p.ldw;
-        turn<E>(w, wt, cols, p.K, p.ldw / e, Vp, nullptr, s);
+        const bool few = p.M <= FEW;
+        if (!few) turn<E>(w, wt, cols, p.K, p.ldw / e, Vp, nullptr, s);
         NtParams q{};
         q.x = p.x; q.w = w; q.M = p.M; q.N = cols; q.ldx = p.ldx; q.ldw = p.ldw; q.kbytes = (int32_t)up(p.K * e, 16);       // the tiles cover the padding of dl
         GradEpi<E> ge{};
-        ge.g = g; ge.gt = gt; ge.ldg = Vp; ge.ldgt = Mp; ge.tok = p.tok; ge.lse = p.lse_in; ge.dlp = p.dlp; ge.dlse = p.dlse;
+        ge.g = few ? nullptr : g; ge.gt = gt; ge.ldg = Vp; ge.ldgt = Mp; ge.tok = p.tok; ge.lse = p.lse_in; ge.dlp = p.dlp; ge.dlse = p.dlse;
         ge.M = p.M; ge.V = p.V; ge.v0 = v0; ge.Vp = Vp; ge.Mp = Mp;
         go_nt<E>(q, ge, tile_of<E>(p.M, cols), s);
         NtParams a{};
@@ -663,6 +749,11 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         OutEpi d{};
         d.M = cols; d.N = p.K; d.y = (E *)p.dw + v0 * p.K; d.y_dtype = p.dtype;
         d.sum = k.pair.b > 1 ? of_w : nullptr;
+        if (few) {
+            few_rows<E>(p, gt, Mp, w, cols, k.pair.a, i == 0, of_x, s);
+            go_pair<E>(NtParams{}, OutEpi{}, b, d, Pair{k.pair.side, 0, 1}, s);
+            continue;
+        }
         go_pair<E>(a, o, b, d, k.pair, s);
         if (k.pair.b > 1) {
             sums.part = of_w; sums.P = k.pair.b; sums.J = sums.J1 = sums.stride = cols * p.K; sums.dst = d.y;
@@ -671,7 +762,7 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         }
     }
     hipError_t er = hipGetLastError();
-    if (er != hipSuccess || k.pair.a == 1) return er;
+    if (er != hipSuccess || (k.pair.a == 1 && p.M > FEW)) return er;
     sums.part = of_x; sums.P = k.pair.a; sums.J = sums.J1 = sums.stride = p.M * p.K; sums.dst = p.dx;
     return launch_sum_shares(sums, s);
 }

@@ -304,6 +304,37 @@ def test_dense_logprobs_by_pieces_of_the_vocabulary(m, v, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,v,k", [(1, 3, 2), (2, 1030, 260), (4, 63, 700), (5, 65, 513), (8, 2500, 1100), (9, 5000, 515), (12, 129, 1024), (15, 257, 2049), (16, 2600, 72)])
+def test_gradient_of_few_rows(m, v, k, dtype):
+    """Up to sixteen rows: their derivatives from the vocabulary's rows as they lie, run twice to the same bits."""
+    operands, (x, w, tok, dlp, dlse) = loss_case(m, v, k, dtype, seed=7 * m + v + k)
+    lse = L.dense_logprobs(x, w, tok)[1]
+    _, back = loss_bounds(x, w, tok, lse, dlp, dlse, dtype)
+    call = loss_grad_call(operands, lse, m, v, k, dtype)
+    once = call.run().numbers()
+    for name, g, want, tol in zip(("dx", "dw"), once, L.dense_logprobs_grad(x, w, tok, lse, dlp, dlse), back):
+        within(g, want, tol, f"few rows {m}x{v}x{k} {dtype} {name}")
+    for g, want in zip(call.run().numbers(), once):
+        np.testing.assert_array_equal(g, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,v,k", [(3, 270001, 5), (16, 300000, 8)])
+def test_gradient_of_few_rows_by_pieces(m, v, k, dtype):
+    """Pieces of the vocabulary of which the last is short, in the library's own workspace."""
+    import torch
+    from paper_1810_00952_amd import binding as B
+    operands, (x, w, tok, dlp, dlse) = loss_case(m, v, k, dtype, seed=m)
+    lse = L.dense_logprobs(x, w, tok)[1]
+    _, back = loss_bounds(x, w, tok, lse, dlp, dlse, dtype)
+    call = loss_grad_call(operands, lse, m, v, k, dtype)
+    assert call.plan.workspace_bytes() > B.STATIC_WORKSPACE_BYTES
+    call.plan.run_static(call.bound, torch.cuda.current_stream().cuda_stream)
+    for name, g, want, tol in zip(("dx", "dw"), call.numbers(), L.dense_logprobs_grad(x, w, tok, lse, dlp, dlse), back):
+        within(g, want, tol, f"few rows by pieces {m}x{v}x{k} {dtype} {name}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,v,k", [(9, 700, 24), (300, 3000, 64)])
 def test_rows_that_take_no_part(m, v, k, dtype):
     """NaN and infinities in rows whose derivatives are 0 (padding behind a batch's last token) reach neither dw nor the other rows."""
