@@ -6,7 +6,7 @@
 // Forward: a product's tile leaves a maximum and a sum of exponentials a row, and the token's logit where it is its column; a second launch joins
 // them.  Gradient, for pieces of the vocabulary: the piece's logits once more, dl from them, rounded to x's type as a product's operand and stored
 // as it lies and transposed; then dx += dl w and dw = dl^T x in one launch, all three products of rows that lie along the contraction.  x and w are
-// transposed for the last two.
+// transposed for the last two.  Of up to sixteen rows both gradients are one pass over w.
 //
 // The matrix pipes bound it, few rows HBM.  bf16: 8192 x 50001 x 1024 the logits 728 to 752 us (1.13 PF/s), seven pieces of dl 160 each, of both gradients 205
 // (1.17 PF/s); 4096 x 32000 x 1024 forward 246 (1.09); 8 x 131072 x 1024 50 (5.4 TB/s of w).  The pipes are busy 58 % of the cycles, at 1.6 to 1.9 GHz.
@@ -461,6 +461,13 @@ __global__ __launch_bounds__(1024) void dense_logprobs_join_kernel(const float2 
     }
 }
 
+// whether a row has a derivative; what stands in one without reaches nothing
+__device__ __forceinline__ bool takes_part(const int32_t *tok, const float *dlp, const float *dlse, int64_t m, int64_t V)
+{
+    const int32_t k = tok[m];
+    return dlse[m] != 0.0f || (k >= 0 && k < V && dlp[m] != 0.0f);
+}
+
 // ---------------------------------------------------------------------------
 // src[R][C] (rows ld elements apart) -> dst[C][Rp], zeros behind R; rows without a derivative are zeros
 // ---------------------------------------------------------------------------
@@ -474,10 +481,7 @@ __global__ __launch_bounds__(256) void turn_rows_kernel(const E *src, E *dst, in
         E v = 0;
         if (r0 + r < Rr && c0 + c < C) {
             bool part = true;
-            if (tok) {
-                const int32_t k = tok[r0 + r];
-                part = dlse[r0 + r] != 0.0f || (k >= 0 && k < V && dlp[r0 + r] != 0.0f);
-            }
+            if (tok) part = takes_part(tok, dlp, dlse, r0 + r, V);
             if (part) v = src[(r0 + r) * ld + c0 + c];
         }
         s[r][c] = v;
@@ -488,49 +492,106 @@ __global__ __launch_bounds__(256) void turn_rows_kernel(const E *src, E *dst, in
 }
 
 // ---------------------------------------------------------------------------
-// dx of up to MR rows: w's rows as they lie, 16 bytes a lane, times the wave's numbers of dl; grid's y: slices of w's rows, of which each wave takes every
-// fourth.  The products' way would turn w first, two passes more over it, and multiply tiles of 64 rows.
+// Both gradients of up to MR rows: a lane has VEC columns of all of them, reads w's rows as they lie and writes dw's, with the wave's numbers of dl; grid's
+// y: slices of w's rows, of which each wave takes every fourth and whose dx are added up behind.  The products' way would turn w first, two passes more
+// over it, and multiply tiles of 64 rows.  HBM bounds it: f32 5 x 44311 x 3144 240 us (w read, dw written: 4.6 TB/s; logits and gradients together
+// 954 -> 569), bf16 3 x 24355 x 2240 46 (175 -> 94).  Of more rows the vector units would: sixteen are 32 operations a number of w.
 // ---------------------------------------------------------------------------
+template <typename E, int MR> struct Few {
+    static constexpr int VEC = sizeof(E) == 2 && MR < 16 ? 8 : 4, WORDS = VEC * (int)sizeof(E) / 4, WIDE = 64 * VEC;
+    struct raw { uint32_t r[WORDS]; };
+    static __device__ __forceinline__ raw load(const char *p)
+    {
+        raw q;
+        if constexpr (WORDS == 4) {
+            const u32x4 v = *(const u32x4 *)p;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) q.r[c] = v[c];
+        } else {
+            const u32x2 v = *(const u32x2 *)p;
+            q.r[0] = v[0]; q.r[1] = v[1];
+        }
+        return q;
+    }
+    static __device__ __forceinline__ void unpack(const raw &q, float (&x)[VEC])
+    {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) {
+            if constexpr (sizeof(E) == 4) x[c] = __uint_as_float(q.r[c]);
+            else x[c] = __uint_as_float(c & 1 ? q.r[c >> 1] & 0xffff0000u : q.r[c >> 1] << 16);
+        }
+    }
+    // whole vectors, which need not lie at their size's multiple, and the row's last elements
+    static __device__ __forceinline__ void store(E *p, const float (&x)[VEC], int64_t left)
+    {
+        typedef u32x4 u32x4_any __attribute__((aligned(2)));
+        typedef u32x2 u32x2_any __attribute__((aligned(2)));
+        uint32_t q[WORDS];
+#pragma unroll
+        for (int c = 0; c < WORDS; ++c) {
+            if constexpr (sizeof(E) == 4) q[c] = __float_as_uint(x[c]);
+            else q[c] = pack_bf16x2(x[2 * c], x[2 * c + 1]);
+        }
+        if (left >= VEC) {
+            if constexpr (WORDS == 4) *(u32x4_any *)p = u32x4{q[0], q[1], q[2], q[3]};
+            else *(u32x2_any *)p = u32x2{q[0], q[1]};
+        } else {
+#pragma unroll
+            for (int c = 0; c < VEC; ++c)
+                if (c < left) store_from_f32(p, sizeof(E) == 4 ? DT_F32 : DT_BF16, c, x[c]);
+        }
+    }
+};
+
 template <typename E, int MR>
-__global__ __launch_bounds__(256) void few_rows_kernel(const uint32_t *__restrict__ gt, int64_t ldgt, const char *__restrict__ w, int64_t ldw, const float *before, float *sum, int32_t M, int64_t K, int64_t rows, int64_t slice_rows)
+__global__ __launch_bounds__(256) void few_rows_kernel(const uint32_t *__restrict__ gt, int64_t ldgt, const char *__restrict__ w, int64_t ldw, const char *__restrict__ x, int64_t ldx, const int32_t *tok, const float *dlp,
+                                                       const float *dlse, const float *before, float *sum, E *dw, int32_t M, int64_t V, int64_t K, int64_t rows, int64_t slice_rows)
 {
-    constexpr int VEC = 16 / sizeof(E), WIDE = 64 * VEC, UNDER_WAY = 8;
+    typedef Few<E, MR> F;
+    constexpr int VEC = F::VEC, WIDE = F::WIDE, UNDER_WAY = 8;
     __shared__ float s[MR][WIDE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t k0 = (int64_t)blockIdx.x * WIDE, k = k0 + lane * VEC;
     const int64_t begin = (int64_t)blockIdx.y * slice_rows, end = min(begin + slice_rows, rows);
-    const char *const from = w + (k < K ? k : 0) * (int64_t)sizeof(E);         // a lane behind the last column: some other one's, nothing of which is stored
-    float acc[MR][VEC];
+    const int64_t left = K - k, at_k = (left > 0 ? k : 0) * (int64_t)sizeof(E);         // a lane behind the last column: the first one's, of which nothing is stored
+    float acc[MR][VEC], xs[MR][VEC];
 #pragma unroll
-    for (int m = 0; m < MR; ++m)
+    for (int m = 0; m < MR; ++m) {
+        typename F::raw q{};
+        if (m < M && takes_part(tok, dlp, dlse, m, V)) q = F::load(x + m * ldx + at_k);
+        F::unpack(q, xs[m]);
 #pragma unroll
         for (int c = 0; c < VEC; ++c) acc[m][c] = 0.0f;
-    auto add = [&](const u32x4 &q, int64_t v) __attribute__((always_inline)) {
+    }
+    auto row = [&](const typename F::raw &q, int64_t v) __attribute__((always_inline)) {
         const uint32_t *const g = gt + v * ldgt;                     // words: of bf16 two rows' numbers
-        float x[VEC];
+        float wv[VEC], d[VEC];
+        F::unpack(q, wv);
 #pragma unroll
-        for (int c = 0; c < VEC; ++c) {
-            if constexpr (sizeof(E) == 4) x[c] = __uint_as_float(q[c]);
-            else x[c] = __uint_as_float(c & 1 ? q[c >> 1] & 0xffff0000u : q[c >> 1] << 16);
-        }
+        for (int c = 0; c < VEC; ++c) d[c] = 0.0f;
 #pragma unroll
         for (int m = 0; m < MR; ++m) {
-            float d;
-            if constexpr (sizeof(E) == 4) d = __uint_as_float(g[m]);
-            else d = __uint_as_float(m & 1 ? g[m >> 1] & 0xffff0000u : g[m >> 1] << 16);
+            float dl;
+            if constexpr (sizeof(E) == 4) dl = __uint_as_float(g[m]);
+            else dl = __uint_as_float(m & 1 ? g[m >> 1] & 0xffff0000u : g[m >> 1] << 16);
 #pragma unroll
-            for (int c = 0; c < VEC; ++c) acc[m][c] = __builtin_fmaf(d, x[c], acc[m][c]);
+            for (int c = 0; c < VEC; ++c) {
+                acc[m][c] = __builtin_fmaf(dl, wv[c], acc[m][c]);
+                d[c] = __builtin_fmaf(dl, xs[m][c], d[c]);
+            }
         }
+        if (left > 0) F::store(dw + v * K + k, d, left);
     };
+    const char *const from = w + at_k;
     int64_t v = begin + wave;
     for (; v + 4 * (UNDER_WAY - 1) < end; v += 4 * UNDER_WAY) {
-        u32x4 q[UNDER_WAY];
+        typename F::raw q[UNDER_WAY];
 #pragma unroll
-        for (int u = 0; u < UNDER_WAY; ++u) q[u] = *(const u32x4 *)(from + (v + 4 * u) * ldw);
+        for (int u = 0; u < UNDER_WAY; ++u) q[u] = F::load(from + (v + 4 * u) * ldw);
 #pragma unroll
-        for (int u = 0; u < UNDER_WAY; ++u) add(q[u], v + 4 * u);
+        for (int u = 0; u < UNDER_WAY; ++u) row(q[u], v + 4 * u);
     }
-    for (; v < end; v += 4) add(*(const u32x4 *)(from + v * ldw), v);
+    for (; v < end; v += 4) row(F::load(from + v * ldw), v);
     for (int t = 0; t < 4; ++t) {                                    // the waves' sums, one behind the other
         if (wave == t) {
 #pragma unroll
@@ -551,7 +612,9 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const uint32_t *__restric
 
 namespace {
 
-constexpr int64_t FEW = 16;                   // rows: dx by few_rows_kernel
+constexpr int64_t FEW = 16;                   // rows whose gradients are few_rows_kernel's
+// columns of one of its workgroups
+int64_t few_wide(const DenseLogprobsParams &p) { return p.dtype == DT_BF16 && p.M <= 8 ? 512 : 256; }
 constexpr int64_t LINE = 128, PIECE_MAX = 1 << 20;      // a piece's columns: a row of dl is reached by 31-bit offsets from its tile's first
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 size_t esize(const DenseLogprobsParams &p) { return p.dtype == DT_BF16 ? 2 : 4; }
@@ -627,7 +690,7 @@ template <typename E, typename Epi> void go_nt(NtParams q, const Epi &epi, int32
 
 template <typename E> void go_pair(NtParams a, const OutEpi &ea, NtParams b, const OutEpi &eb, const Pair &f, hipStream_t s)
 {
-    split(a, f.side, f.a > 0 ? f.a : 1);             // 0: b's alone
+    split(a, f.side, f.a);
     split(b, f.side, f.b);
     const dim3 grid((unsigned)((int64_t)a.nblk_m * a.nblk_n * f.a + (int64_t)b.nblk_m * b.nblk_n * f.b));
     if constexpr (sizeof(E) == 2) {
@@ -651,11 +714,11 @@ Pieces pieces_of(const DenseLogprobsParams &p)
     k.count = (p.V + k.cols - 1) / k.cols;
     const int64_t real = k.cols < p.V ? k.cols : p.V;
     if (p.M <= FEW) {
-        // dw's product alone; the slices are those of few_rows_kernel, two workgroups a CU
-        const int64_t wide = tiles_along(p.K, 64 * (16 / e)), most = (real + 63) / 64;
+        // slices: two workgroups a CU
+        const int64_t wide = tiles_along(p.K, few_wide(p)), most = (real + 63) / 64;
         int64_t n = 512 / wide > 1 ? 512 / wide : 1;
         if (n > most) n = most;
-        k.pair = Pair{p.dtype == DT_BF16 ? tile_of<uint16_t>(real, p.K) : tile_of<float>(real, p.K), (int32_t)n, 1};
+        k.pair = Pair{0, (int32_t)n, 1};
         return k;
     }
     k.pair = p.dtype == DT_BF16 ? pair_of<uint16_t>(p.M, p.K, real, p.piece_bytes) : pair_of<float>(p.M, p.K, real, p.piece_bytes);
@@ -673,7 +736,7 @@ Layout layout_of(const DenseLogprobsParams &p, const Pieces &k)
     l.g = take(few ? 0 : p.M * k.cols * e);
     l.gt = take(k.cols * Mp * e);
     l.wt = take(few ? 0 : p.K * k.cols * e);
-    l.xt = take(p.K * Mp * e);
+    l.xt = take(few ? 0 : p.K * Mp * e);
     l.dx = take(few || k.count > 1 || k.pair.a > 1 ? (int64_t)k.pair.a * p.M * p.K * 4 : 0);
     l.dw = take(k.pair.b > 1 ? (int64_t)k.pair.b * k.cols * p.K * 4 : 0);
     l.bytes = at;
@@ -701,13 +764,13 @@ template <typename E> void turn(const void *src, void *dst, int64_t R, int64_t C
                        rows ? rows->tok : nullptr, rows ? rows->dlp : nullptr, rows ? rows->dlse : nullptr, rows ? rows->V : 0);
 }
 
-// rows: of w, from w on; dx's shares of them, added to those of the pieces before
-template <typename E> void few_rows(const DenseLogprobsParams &p, const E *gt, int64_t ldgt, const char *w, int64_t rows, int32_t slices, bool first, float *sum, hipStream_t s)
+// of a piece: `rows` of the vocabulary from the v0-th on
+template <typename E> void few_rows(const DenseLogprobsParams &p, const E *gt, int64_t ldgt, int64_t v0, int64_t rows, int32_t slices, float *sum, hipStream_t s)
 {
-    constexpr int64_t wide = 64 * (16 / sizeof(E));
-    const dim3 grid((unsigned)tiles_along(p.K, wide), (unsigned)slices), wg(256);
+    const dim3 grid((unsigned)tiles_along(p.K, few_wide(p)), (unsigned)slices), wg(256);
     auto with = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, wg, 0, s, (const uint32_t *)gt, (int64_t)(ldgt * sizeof(E) / 4), w, p.ldw, first ? nullptr : sum, sum, (int32_t)p.M, p.K, rows, (rows + slices - 1) / slices);
+        hipLaunchKernelGGL(kernel, grid, wg, 0, s, (const uint32_t *)gt, (int64_t)(ldgt * sizeof(E) / 4), (const char *)p.w + v0 * p.ldw, p.ldw, (const char *)p.x, p.ldx, p.tok, p.dlp, p.dlse,
+                           v0 > 0 ? sum : nullptr, sum, (E *)p.dw + v0 * p.K, (int32_t)p.M, p.V, p.K, rows, (rows + slices - 1) / slices);
     };
     if (p.M <= 4) with(few_rows_kernel<E, 4>);
     else if (p.M <= 8) with(few_rows_kernel<E, 8>);
@@ -725,11 +788,11 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
     float *const of_x = (float *)(ws + at.dx), *const of_w = (float *)(ws + at.dw);
     SumShares sums{};
     sums.dst_dtype = p.dtype;
-    turn<E>(p.x, xt, p.M, p.K, p.ldx / e, Mp, &p, s);
+    const bool few = p.M <= FEW;
+    if (!few) turn<E>(p.x, xt, p.M, p.K, p.ldx / e, Mp, &p, s);
     for (int64_t i = 0; i < k.count; ++i) {
         const int64_t v0 = i * k.cols, cols = p.V - v0 < k.cols ? p.V - v0 : k.cols, Vp = up(cols, LINE / e);
         const char *const w = (const char *)p.w + v0 * p.ldw;
-        const bool few = p.M <= FEW;
         if (!few) turn<E>(w, wt, cols, p.K, p.ldw / e, Vp, nullptr, s);
         NtParams q{};
         q.x = p.x; q.w = w; q.M = p.M; q.N = cols; q.ldx = p.ldx; q.ldw = p.ldw; q.kbytes = (int32_t)up(p.K * e, 16);       // the tiles cover the padding of dl
@@ -737,6 +800,10 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         ge.g = few ? nullptr : g; ge.gt = gt; ge.ldg = Vp; ge.ldgt = Mp; ge.tok = p.tok; ge.lse = p.lse_in; ge.dlp = p.dlp; ge.dlse = p.dlse;
         ge.M = p.M; ge.V = p.V; ge.v0 = v0; ge.Vp = Vp; ge.Mp = Mp;
         go_nt<E>(q, ge, tile_of<E>(p.M, cols), s);
+        if (few) {
+            few_rows<E>(p, gt, Mp, v0, cols, k.pair.a, of_x, s);
+            continue;
+        }
         NtParams a{};
         a.x = g; a.w = wt; a.M = p.M; a.N = p.K; a.ldx = a.ldw = Vp * e; a.kbytes = (int32_t)(Vp * e);
         OutEpi o{};
@@ -749,11 +816,6 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         OutEpi d{};
         d.M = cols; d.N = p.K; d.y = (E *)p.dw + v0 * p.K; d.y_dtype = p.dtype;
         d.sum = k.pair.b > 1 ? of_w : nullptr;
-        if (few) {
-            few_rows<E>(p, gt, Mp, w, cols, k.pair.a, i == 0, of_x, s);
-            go_pair<E>(NtParams{}, OutEpi{}, b, d, Pair{k.pair.side, 0, 1}, s);
-            continue;
-        }
         go_pair<E>(a, o, b, d, k.pair, s);
         if (k.pair.b > 1) {
             sums.part = of_w; sums.P = k.pair.b; sums.J = sums.J1 = sums.stride = cols * p.K; sums.dst = d.y;
@@ -762,7 +824,7 @@ template <typename E> hipError_t gradient(const DenseLogprobsParams &p, hipStrea
         }
     }
     hipError_t er = hipGetLastError();
-    if (er != hipSuccess || (k.pair.a == 1 && p.M > FEW)) return er;
+    if (er != hipSuccess || (k.pair.a == 1 && !few)) return er;
     sums.part = of_x; sums.P = k.pair.a; sums.J = sums.J1 = sums.stride = p.M * p.K; sums.dst = p.dx;
     return launch_sum_shares(sums, s);
 }
