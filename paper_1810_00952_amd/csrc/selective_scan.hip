@@ -33,13 +33,15 @@ constexpr float LOG2E = 1.4426950408889634f;
 // Rows of a tile: of the gradient as many as its states and gates fit the registers; 32 forwards gave nothing
 constexpr int rows_of(int R) { return R <= 4 ? 16 : 64 / R; }
 
-// Chunks' P of which a document's first row is part: -0, which no product of gates is
+// A chunk makes P h + H of the state h before it.  P h is a number of f32 where P = exp(a sum s) is none: of a state that grows what was small before, or
+// zero.  So P is there as its fourth root, between 2^-126 and 2^127, which takes an h of any size to zero or infinity, but zero and infinity to themselves.
+// -0, which is no such root, where a document's first row is part of the chunk.
 constexpr float FIRST = -0.0f;
-__device__ __forceinline__ bool is_first(float P) { return __float_as_uint(P) == 0x80000000u; }
-__device__ __forceinline__ float through(float P, float h, float H)
+__device__ __forceinline__ bool is_first(float root) { return __float_as_uint(root) == 0x80000000u; }
+__device__ __forceinline__ float through(float root, float h, float H)
 {
-    const float y = __builtin_fmaf(P, h, H);
-    return is_first(P) ? H : y;
+    const float y = __builtin_fmaf(h * root * root * root, root, H);
+    return is_first(root) ? H : y;
 }
 __device__ __forceinline__ float exp2_(float v)
 {
@@ -49,6 +51,9 @@ __device__ __forceinline__ float exp2_(float v)
     return v;
 #endif
 }
+
+// the fourth root of 2^v
+__device__ __forceinline__ float root_of(float v) { return exp2_(fminf(fmaxf(0.25f * v, -126.0f), 127.0f)); }
 
 __device__ __forceinline__ float log2_(float v)
 {
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanP
 }
 
 // ---------------------------------------------------------------------------
-// forward.  AHEAD: what a chunk makes of the state before it, into part ([chunk][b] P, H of [D][N])
+// forward.  AHEAD: what a chunk makes of the state before it, into part ([chunk][b] P's root, H of [D][N])
 // ---------------------------------------------------------------------------
 template <typename E, int R, bool KEEP, bool GATED, bool AHEAD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) void selective_scan_kernel(const SelScanParams p, int32_t slabs, int32_t chunks, int32_t chunk_rows)
@@ -541,7 +546,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
         total += moved<0x4e>(total);
         float f[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) f[r] = began ? FIRST : exp2_(fmaxf(total * a2[r], -126.0f));
+        for (int r = 0; r < R; ++r) f[r] = began ? FIRST : root_of(total * a2[r]);
         at_.store(p, p.part + (2 * ((int64_t)at_.chunk * p.B + at_.b)) * DN, f);
         at_.store(p, p.part + (2 * ((int64_t)at_.chunk * p.B + at_.b) + 1) * DN, h);
     } else if (p.hT && at_.chunk + 1 == chunks) {
@@ -778,7 +783,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         total += moved<0x4e>(total);
         float f[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) f[r] = began ? FIRST : exp2_(fmaxf(total * a2[r], -126.0f));
+        for (int r = 0; r < R; ++r) f[r] = began ? FIRST : root_of(total * a2[r]);
         at_.store(p, p.part + (2 * ((int64_t)at_.chunk * p.B + at_.b)) * DN, f);
         at_.store(p, p.part + (2 * ((int64_t)at_.chunk * p.B + at_.b) + 1) * DN, G);
         return;

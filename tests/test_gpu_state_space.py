@@ -217,6 +217,51 @@ def test_scan_of_many_chunks(b, t, d, n):
         within(g, want, tol, "many chunks " + name)
 
 
+@pytest.mark.parametrize("padded", [False, True])
+@pytest.mark.parametrize("dtype,n", [("f32", 3), ("f32", 16), ("bf16", 8), ("f32", 40)])
+def test_a_chunk_of_rows_in_which_states_grow_past_f32(dtype, n, padded):
+    """A chunk of 64 rows between two that hold makes a state some e^100 times what it was, more than f32 reaches: what was small enough before is a number behind it, zero is zero."""
+    b, t, d = 1, 192, 40
+    operands, v = scan_case(b, t, d, n, dtype, True, None, seed=n)
+    values = [np.array(a) for a in v[:9]] + [np.ones(b * t)]
+    small = 1e-28
+    for i in (0, 5, 6, 7):
+        values[i] *= small
+    values[1][:] = -10.0                                       # steps of some 5e-5, in the middle of 1
+    values[1][64:128] = np.log(np.e - 1)
+    values[3] = np.random.default_rng(n).uniform(1.5, 1.6, size=(d, n))
+    values[5][0, 0], values[7][0, 0], values[0][:, 0], values[6][:, 0] = 0.0, 0.0, 0.0, 0.0      # a channel that stays zero
+    if padded:
+        for i in (0, 1, 2, 6, 8):
+            values[i][5:20] = values[i][150:190] = np.nan
+        values[9][5:20] = values[9][150:190] = 0
+    types = [dtype, dtype, dtype, "f32", "f32", "f32", dtype, "f32", dtype, "i8"]
+    both = [tensor(a, ty) for a, ty in zip(values, types)]
+    device, v = [(tt, ty) for (tt, _), ty in zip(both, types)], [a for _, a in both]
+    if not padded:
+        device[9], v[9] = None, None
+    x, dt, bc, a, skip, h0, dy, dhT, z, keep = v
+    ahead, back = scan_bounds(*v, dtype)
+    got = scan_call(device, b, t, d, n, dtype).run().numbers()
+    for name, g, want, tol in zip(("y", "hT"), got, L.selective_scan(*v[:6], z, keep), ahead):
+        within(g, want, tol, f"growth {name}")
+    assert np.abs(got[1]).max() > 1e10 and not got[1][0, 0].any()
+    got = scan_grad_call(device, b, t, d, n, dtype).run().numbers()
+    for name, g, want, tol in zip(NAMES, got, L.selective_scan_grad(*v[:8], z, keep), back):
+        within(g, want, tol, f"growth {name}")
+    assert np.abs(got[5]).max() > 1e10 and not got[5][0, 0].any()
+
+
+def test_chunks_of_a_growing_state_that_is_zero():
+    """Hundreds of rows with gates of e^2: a state and a derivative of zero stay so, as in a scan of one chunk."""
+    b, t, d, n = 1, 600, 64, 4
+    operands, v = scan_case(b, t, d, n, "f32", False, None, seed=3)
+    for i, value in ((0, 0.0), (1, np.log(np.e - 1)), (3, 2.0), (5, 0.0), (6, 0.0), (7, 0.0)):
+        operands[i][0].fill_(value)
+    for g in scan_call(operands, b, t, d, n, "f32").run().numbers() + scan_grad_call(operands, b, t, d, n, "f32").run().numbers():
+        np.testing.assert_array_equal(g, 0.0)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [3, 16, 64])
 def test_scan_steps_continue_a_sequence_in_place(n, dtype):
