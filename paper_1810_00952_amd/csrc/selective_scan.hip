@@ -679,7 +679,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
             }
             began |= KEEP && first != 0;
         } else {
-            // with padding or a document's first row among them, and without
+            // with padding, rows behind the sequence's last or a document's first row among them, and without
             auto walk = [&](auto masked) {
                 float decayed[ROWS][R], gate[ROWS][R], u[ROWS / 4], dat[R];       // the state before a row times its gate
                 Coming<R, ROWS, true, true, true> back;
@@ -758,7 +758,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
 #pragma unroll
                 for (int r = 0; r < R; ++r) da[r] += dat[r];             // tile by tile: fewer roundings on the way
             };
-            if (KEEP && (first || (tok & FULL) != FULL)) walk(std::true_type{});
+            if ((KEEP && first) || (tok & FULL) != FULL) walk(std::true_type{});
             else walk(std::false_type{});
             fore.start(mine + l * R, half ^ 1);
             lds_barrier();

@@ -202,6 +202,30 @@ def test_padding_in_front_of_a_document_holds_a_state_that_reaches_nothing(b, t,
         within(g, want, tol, "left-padded " + name)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,t,d,n", [(1, 5, 3, 3), (2, 17, 66, 16), (1, 700, 33, 16), (3, 30, 20, 40)])
+def test_a_last_state_past_f32_is_in_no_sum_over_rows(b, t, d, n, dtype):
+    """The last token makes every state infinite, in sequences of no whole number of tiles and without padding: the gradient of a is of the states before it."""
+    operands, v = scan_case(b, t, d, n, dtype, True, None, seed=t)
+    values = [np.array(a) for a in v[:9]]
+    last = np.arange(b) * t + t - 1
+    values[1][last] = 1.0
+    values[0][last], values[2][last, :n] = 1e20, 1e20          # their product leaves f32
+    types = [dtype, dtype, dtype, "f32", "f32", "f32", dtype, "f32", dtype]
+    both = [tensor(a, ty) for a, ty in zip(values, types)]
+    device, v = [(tt, ty) for (tt, _), ty in zip(both, types)] + [None], [a for _, a in both] + [None]
+    y, hT = scan_call(device, b, t, d, n, dtype).run().numbers()
+    assert np.isposinf(hT).all()
+    _, back = scan_bounds(*v, dtype)
+    got = scan_grad_call(device, b, t, d, n, dtype).run().numbers()
+    rows = np.setdiff1d(np.arange(b * t), last)
+    for name, g, want, tol in zip(NAMES, got, L.selective_scan_grad(*v[:8], v[8]), back):
+        if name in ("da", "dskip", "dh0"):
+            within(g, want, tol, f"infinite last state {name}")
+        else:
+            within(g[rows], want[rows], tol[rows], f"infinite last state {name}")
+
+
 @pytest.mark.parametrize("b,t,d,n", [(1, 5000, 3, 2), (1, 2500, 64, 16), (2, 1300, 5, 40)])
 def test_scan_of_many_chunks(b, t, d, n):
     """Few channels: every chunk of rows adds up those before it."""
