@@ -702,8 +702,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
                             gate[t][r] = exp2_(of_lane<K>(s[i]) * a2[r]);
                             decayed[t][r] = gate[t][r] * h[r];
                             h[r] = __builtin_fmaf(of_lane<K>(v), fore.B(t, r), decayed[t][r]);
-                            // in the sums over rows a state that padding holds, were it infinite or NaN, is none
-                            if (masked && !(tok >> t & 1)) decayed[t][r] = 0.0f;
                             if (GATED) sum[K] = __builtin_fmaf(fore.C(t, r), h[r], sum[K]);
                         }
                     };
@@ -731,7 +729,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
                         for (int r = 0; r < R; ++r) {
                             const float he = decayed[t][r], B = back.B(ROWS - 1 - t, r);
                             G[r] = __builtin_fmaf(back.C(ROWS - 1 - t, r), of_lane<K>(du[i]), G[r]);
-                            const float arg = G[r] * he;
+                            // in the sum over rows a state and a derivative that padding holds, were they infinite or NaN, are none; its other results are masked as they leave
+                            const float arg = masked && !(tok >> t & 1) ? 0.0f : G[r] * he;
                             dat[r] = __builtin_fmaf(of_lane<K>(s[i]), arg, dat[r]);
                             ga[K] = __builtin_fmaf(arg, a[r], ga[K]);
                             gb[K] = __builtin_fmaf(G[r], B, gb[K]);

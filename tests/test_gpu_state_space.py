@@ -226,6 +226,45 @@ def test_a_last_state_past_f32_is_in_no_sum_over_rows(b, t, d, n, dtype):
             within(g[rows], want[rows], tol[rows], f"infinite last state {name}")
 
 
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf, 1e30])
+@pytest.mark.parametrize("b,t,d,n", [(3, 5, 5, 33), (3, 40, 66, 16), (2, 900, 40, 8), (40, 19, 70, 5)])
+def test_a_sequence_of_padding_reaches_nothing(b, t, d, n, value):
+    """Its states and derivatives go through as they are, whatever they are, and are in no sum over the batch: the other results have the bits they have beside zeros there."""
+    operands, v = scan_case(b, t, d, n, "f32", True, "ends", seed=t)       # the last sequence is without a token
+    runs = []
+    for held in (0.0, value):
+        h0, dhT = np.array(v[5]), np.array(v[7])
+        h0[-1], dhT[-1] = held, held
+        ops = list(operands)
+        ops[5], ops[7] = (tensor(h0, "f32")[0], "f32"), (tensor(dhT, "f32")[0], "f32")
+        runs.append(scan_call(ops, b, t, d, n, "f32").run().numbers() + scan_grad_call(ops, b, t, d, n, "f32").run().numbers())
+    for i, (name, clean, got) in enumerate(zip(("y", "hT") + NAMES, *runs)):
+        if name in ("hT", "dh0"):
+            np.testing.assert_array_equal(got[-1], np.full_like(got[-1], np.float32(value)), err_msg=name)
+            clean, got = clean[:-1], got[:-1]
+        np.testing.assert_array_equal(got, clean, err_msg=name)
+        assert np.isfinite(got).all(), name
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+def test_conv_of_a_sequence_of_padding_reaches_nothing(value):
+    b, t, d, k = 3, 130, 72, 4
+    operands, v = conv_case(b, t, d, k, "f32", "f32", "ends", seed=2)
+    runs = []
+    for held in (0.0, value):
+        ops = list(operands)
+        for i in (3, 5):
+            a = np.array(v[i])
+            a[-1] = held
+            ops[i] = (tensor(a, "f32")[0], "f32")
+        runs.append(conv_call(ops, b, t, d, k, "f32", True).run().numbers() + conv_grad_call(ops, b, t, d, k, "f32", True).run().numbers())
+    for name, clean, got in zip(("y", "sT", "dx", "dw", "db", "ds0"), *runs):
+        if name in ("sT", "ds0"):
+            np.testing.assert_array_equal(got[-1], np.full_like(got[-1], value), err_msg=name)
+            clean, got = clean[:-1], got[:-1]
+        np.testing.assert_array_equal(got, clean, err_msg=name)
+
+
 @pytest.mark.parametrize("b,t,d,n", [(1, 5000, 3, 2), (1, 2500, 64, 16), (2, 1300, 5, 40)])
 def test_scan_of_many_chunks(b, t, d, n):
     """Few channels: every chunk of rows adds up those before it."""
