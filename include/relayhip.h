@@ -153,7 +153,8 @@ enum {
                                  -> (y e[B*T,D], hT f32[B,D,N]); N at most 64 (else RL_ERR_UNSUPPORTED).  s = softplus(dt[t,d]);
                                  h_t[d,n] = exp(s a[d,n]) h_(t-1)[d,n] + s x[t,d] B[t,n]; y[t,d] = (sum_n C[t,n] h_t[d,n] + skip[d] x[t,d]) z sigmoid(z), the
                                  last factor only where there is a z.  The state is f32, and so is a token's exp(s a): below 2^-126 it may be 0,
-                                 past 2^128 it is infinite; of the product of several tokens' only what it makes of the state has to be within f32.  hT may lie over h0 as linear_scan's */
+                                 past 2^128 it is infinite; of the product of several tokens' only what it makes of the state has to be within f32.
+                                 An infinite a counts as the f32 next to it, so that 0 times it is 0.  hT may lie over h0 as linear_scan's */
     RL_OP_SELECTIVE_SCAN_GRAD = 32, /* (x, dt, bc, a, skip, h0, dy e[B*T,D], dhT f32[B,D,N][, z][, keep]) -> (dx e[B*T,D], ddt e[B*T,D], dbc e[B*T,2N],
                                  da f32[D,N], dskip f32[D], dh0 f32[B,D,N][, dz e[B*T,D]]): seven results with z, six without; the states between are computed anew */
     RL_OP_DENSE_LOGPROBS = 33, /* (x e[M,K], w e[V,K], tok i32[M]) -> (lp f32[M], lse f32[M]): with the logits l = x w^T, which are never in memory as a whole,

@@ -52,6 +52,10 @@ __device__ __forceinline__ float exp2_(float v)
 #endif
 }
 
+// An infinite number as the largest finite one, NaN as it is.  Rows that are no tokens hold a state as such of step 0, and 0 times a has to be 0 in them; a token's
+// exp(s a) is the same number.
+__device__ __forceinline__ float finite_(float v) { return fabsf(v) == INFINITY ? copysignf(3.402823466e38f, v) : v; }
+
 // the fourth root of 2^v
 __device__ __forceinline__ float root_of(float v) { return exp2_(fminf(fmaxf(0.25f * v, -126.0f), 127.0f)); }
 
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(256) void selective_scan_step_kernel(const SelScanP
     if (flag) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float e = exp2_(s * (a[r] * LOG2E));
+            const float e = exp2_(s * finite_(a[r] * LOG2E));
             h[r] = __builtin_fmaf(e, flag == 2 ? 0.0f : h[r], v * B[r]);
             sum[0] = __builtin_fmaf(C[r], h[r], sum[0]);
         }
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) voi
     float a2[R], h[R], total = 0.0f;
     at_.load(p, p.a, a2);
 #pragma unroll
-    for (int r = 0; r < R; ++r) { a2[r] *= LOG2E; h[r] = 0.0f; }
+    for (int r = 0; r < R; ++r) { a2[r] = finite_(a2[r] * LOG2E); h[r] = 0.0f; }
     bool began = false;                                              // a document's first row was there
     if (!AHEAD) {
         at_.load(p, p.h0 + at_.b * DN, h);
@@ -570,7 +574,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
     float a[R], a2[R], G[R], da[R], total = 0.0f, dskip = 0.0f;
     at_.load(p, p.a, a);
 #pragma unroll
-    for (int r = 0; r < R; ++r) { a2[r] = a[r] * LOG2E; G[r] = 0.0f; da[r] = 0.0f; }
+    for (int r = 0; r < R; ++r) { a[r] = finite_(a[r]); a2[r] = finite_(a[r] * LOG2E); G[r] = 0.0f; da[r] = 0.0f; }
     bool began = false;
     if (!AHEAD) {
         at_.load(p, p.dhT + at_.b * DN, G);

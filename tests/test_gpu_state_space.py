@@ -265,6 +265,28 @@ def test_conv_of_a_sequence_of_padding_reaches_nothing(value):
         np.testing.assert_array_equal(got, clean, err_msg=name)
 
 
+@pytest.mark.parametrize("how", [None, "some", "ends"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,t,d,n", [(3, 1, 5, 3), (2, 37, 66, 16), (1, 200, 9, 40), (1, 700, 33, 4)])
+def test_a_state_that_forgets_everything(b, t, d, n, dtype, how):
+    """exp(s a) of an a of -infinity, or of one whose multiples leave f32, is 0 for a token, and rows that are none hold the state all the same.  The
+    definition's 0 times infinity is its limit, which any a far below 0 gives."""
+    operands, v = scan_case(b, t, d, n, dtype, True, how, seed=t + n)
+    a = np.array(v[3])
+    rng = np.random.default_rng(t)
+    forgets = rng.uniform(size=a.shape) < 0.5
+    forgets[0, 0] = True
+    a[forgets] = rng.choice([-np.inf, -3e38], size=forgets.sum())
+    operands[3] = (tensor(a, "f32")[0], "f32")
+    v[3] = np.where(forgets, -1e30, v[3])
+    ahead, back = scan_bounds(*v, dtype)
+    z, keep = v[8], v[9]
+    for name, g, want, tol in zip(("y", "hT"), scan_call(operands, b, t, d, n, dtype).run().numbers(), L.selective_scan(*v[:6], z, keep), ahead):
+        within(g, want, tol, f"forgets {name}")
+    for name, g, want, tol in zip(NAMES, scan_grad_call(operands, b, t, d, n, dtype).run().numbers(), L.selective_scan_grad(*v[:8], z, keep), back):
+        within(g, want, tol, f"forgets {name}")
+
+
 @pytest.mark.parametrize("b,t,d,n", [(1, 5000, 3, 2), (1, 2500, 64, 16), (2, 1300, 5, 40)])
 def test_scan_of_many_chunks(b, t, d, n):
     """Few channels: every chunk of rows adds up those before it."""
