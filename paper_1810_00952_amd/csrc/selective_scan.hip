@@ -205,6 +205,9 @@ struct Place {
     }
 };
 
+// floats from one share of da and dskip to the next: whole vectors, by which da goes
+__host__ __device__ __forceinline__ int64_t share_floats(const SelScanParams &p) { return (p.D * p.N + p.D + 3) / 4 * 4; }
+
 // rows of a tile that are tokens, that are a document's first; their flags are asked for a tile before
 template <bool KEEP, int ROWS> struct Flags {
     uint32_t tok, first;
@@ -792,7 +795,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, AHEAD ? 
         return;
     }
     if (at_.chunk == 0) at_.store(p, p.dh0 + at_.b * DN, G);
-    float *share = shares + ((int64_t)at_.chunk * p.B + at_.b) * (DN + p.D);
+    float *share = shares + ((int64_t)at_.chunk * p.B + at_.b) * share_floats(p);
     at_.store(p, share, da);
     dskip += moved<0xb1>(dskip);
     dskip += moved<0x4e>(dskip);
@@ -827,13 +830,13 @@ Form form_of(const SelScanParams &p, bool grad)
     return f;
 }
 
-struct Scratch { int64_t chunks, shares, bc; };          // floats of each
+struct Scratch { int64_t chunks, shares, bc; };          // floats of each, whole vectors but for the last
 Scratch scratch_of(const SelScanParams &p, const Form &f, bool grad)
 {
     Scratch s{};
-    s.chunks = f.chunks > 1 ? 2 * f.chunks * p.B * p.D * p.N : 0;
+    s.chunks = f.chunks > 1 ? (2 * f.chunks * p.B * p.D * p.N + 3) / 4 * 4 : 0;
     if (grad) {
-        s.shares = f.chunks * p.B * (p.D * p.N + p.D);
+        s.shares = f.chunks * p.B * share_floats(p);
         s.bc = f.slabs * p.B * p.T * 2 * p.N;
     }
     return s;
@@ -861,8 +864,8 @@ hipError_t go(bool grad, const SelScanParams &p, const Form &f, hipStream_t s)
     hipError_t er = hipGetLastError();
     if (er != hipSuccess || !grad) return er;
     SumShares q{};
-    q.part = shares; q.P = f.chunks * p.B; q.stride = p.D * p.N + p.D; q.dst_dtype = DT_F32;
-    q.J = q.stride; q.J1 = p.D * p.N; q.dst = p.da; q.dst2 = p.dskip;
+    q.part = shares; q.P = f.chunks * p.B; q.stride = share_floats(p); q.dst_dtype = DT_F32;
+    q.J = p.D * p.N + p.D; q.J1 = p.D * p.N; q.dst = p.da; q.dst2 = p.dskip;
     er = launch_sum_shares(q, s);
     if (er != hipSuccess) return er;
     q.part = bc; q.P = f.slabs; q.J = q.J1 = q.stride = p.B * p.T * 2 * p.N; q.dst = p.dbc; q.dst_dtype = p.dtype;
