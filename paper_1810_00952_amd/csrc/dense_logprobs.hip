@@ -621,9 +621,9 @@ size_t esize(const DenseLogprobsParams &p) { return p.dtype == DT_BF16 ? 2 : 4; 
 
 // Which tile, by an estimate of the time: us per 128-byte line of K of a workgroup that is alone on its CU, and per line and 256 workgroups where there are more
 // (measured on products of one and of many workgroups a CU; 256 x 256 against 128 x 128 for dl of the first case above 170 against 180 us)
-struct Tile { int32_t side, threads; float alone, share; };
-constexpr Tile tiles_bf16[] = {{64, 256, 0.70f, 0.25f}, {128, 256, 0.95f, 0.62f}, {256, 512, 1.60f, 2.00f}};
-constexpr Tile tiles_f32[] = {{64, 256, 1.00f, 0.50f}, {128, 256, 3.60f, 1.85f}};
+struct Tile { int32_t side; float alone, share; };
+constexpr Tile tiles_bf16[] = {{64, 0.70f, 0.25f}, {128, 0.95f, 0.62f}, {256, 1.60f, 2.00f}};
+constexpr Tile tiles_f32[] = {{64, 1.00f, 0.50f}, {128, 3.60f, 1.85f}};
 int64_t tiles_along(int64_t n, int64_t side) { return (n + side - 1) / side; }
 template <typename E, typename F> void each_tile(const F &look)
 {

@@ -14,7 +14,7 @@ namespace rl {
 enum StepKind { S_IGEMM = 0, S_ELTWISE, S_GATES, S_MAXPOOL, S_GAVG, S_TO_NHWC, S_TO_NCHW, S_STEM_PAD, S_STEM_POOL, S_PERMUTE, S_PACK, S_WGRAD, S_WGRAD_REDUCE, S_DILATE, S_TN, S_PAD_NHWC, S_PAD_BYTES,
                 S_NORM_Q8, S_DENSE_Q8, S_SCAN, S_SCAN_GRAD, S_LOGPROBS, S_LOGPROBS_GRAD,
                 S_CAUSAL_CONV, S_CAUSAL_CONV_GRAD, S_SEL_SCAN, S_SEL_SCAN_GRAD, S_DENSE_LOGPROBS, S_DENSE_LOGPROBS_GRAD };
-enum Slot { SL_X = 0, SL_X2, SL_W, SL_Y, SL_E0, SL_E1, SL_E2, SL_E3, SL_E4, SL_E5, SL_CIN, SL_COUT, SL_HOUT, SL_PART, SL_OUT4, SL_I0, SL_I1, SL_I2, SL_I3, SL_I4, SL_I5, SL_O0, SL_O1, SL_O2, SL_O3, SL_COUNT };
+enum Slot { SL_X = 0, SL_X2, SL_W, SL_Y, SL_E0, SL_E1, SL_E2, SL_E3, SL_E4, SL_E5, SL_CIN, SL_COUT, SL_HOUT, SL_PART, SL_OUT4, SL_I0, SL_I1, SL_I2, SL_I3, SL_O0, SL_O1, SL_O2, SL_O3, SL_COUNT };
 
 struct BufDesc {
     int bound_value = -1;     // >= 0: caller-bound pointer of that value id; -1: workspace
