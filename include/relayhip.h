@@ -296,7 +296,8 @@ void rl_plan_destroy(rl_plan *plan);
  * Writes at most cap bytes including the terminator; *needed gets the full size. */
 rl_status rl_plan_describe(const rl_plan *plan, char *buf, size_t cap, size_t *needed);
 rl_status rl_plan_workspace_bytes(const rl_plan *plan, size_t *bytes);
-/* Bytes of the kernel-native copy of a param, or 0 when the param is bound as is. */
+/* Bytes of the kernel-native copy of a param, or 0 when the param is bound as is.  A param whose copy contractions read is read by nothing
+ * else: rl_plan_create refuses such a graph (RL_ERR_UNSUPPORTED); declare it twice, one of which the contractions alone read. */
 rl_status rl_plan_packed_bytes(const rl_plan *plan, int32_t param_value_id, size_t *bytes);
 /* Enqueue the re-layout of one param: src_dev holds it in boundary layout (dense row-major in the order of its
  * Shape), dst_dev (rl_plan_packed_bytes bytes, caller-owned) receives the kernel-native copy, which is what

@@ -1784,6 +1784,15 @@ struct Planner {
             rl_status st = plan_group(gi, groups[gi]);
             if (st != RL_OK) return st;
         }
+        // what is bound for a packed param is its packed copy: no other kind of call can read that
+        for (const auto &k : plan.packs) {
+            if (consumers[k.first].size() == 1) continue;
+            for (int c : consumers[k.first]) {
+                const OpNode &o = g.ops[c];
+                if (!is_anchor(o.kind) || o.in[1] != k.first || o.in[0] == k.first)
+                    return fail(RL_ERR_UNSUPPORTED, std::string("one param needs two different kernel-native layouts: a contraction reads it packed, ") + op_name(o.kind) + " as it lies (declare it twice)");
+            }
+        }
         // every output must end up in its bound buffer in boundary order
         for (int v : g.outputs) {
             int b = bound(v);

@@ -170,6 +170,37 @@ def test_gradient_takes_states_from_the_forward_pass():
     assert steps(False) == ["selective_scan_states", "selective_scan_grad"]
 
 
+@pytest.mark.parametrize("k", [33, 64])
+@pytest.mark.parametrize("other", ["dense_logprobs", "dense_logprobs_grad", "dense_grad_x", "add"])
+def test_a_packed_param_has_no_reader_that_wants_it_as_it_lies(other, k):
+    """A head's matrix that a contraction reads too: packed where its rows are no whole vectors (33), and then for the contraction alone; declared twice it serves both."""
+    m, v = 20, 300
+    x_t, w_t, tok_t, row = ("bf16", (m, k)), ("bf16", (v, k)), ("i32", (m,)), ("f32", (m,))
+
+    def plan(first, twice):
+        g = B.Graph(B.Context())
+        x, w, tok, dy = g.input(*x_t), g.param(*w_t), g.input(*tok_t), g.input("bf16", (m, v))
+        rows = [g.input(*row) for _ in range(3)]
+        w2 = g.param(*w_t) if twice else w
+        calls = [lambda: g.op("dense", [x, w], [("bf16", (m, v))]),
+                 lambda: {"dense_logprobs": lambda: g.op(other, [x, w2, tok], [row, row]), "dense_logprobs_grad": lambda: g.op(other, [x, w2, tok] + rows, [x_t, w_t]),
+                          "dense_grad_x": lambda: g.op(other, [dy, w2], [x_t]), "add": lambda: g.op(other, [w2, w2], [w_t])}[other]()]
+        for call in calls if first == "dense" else calls[::-1]:
+            for o in call()[1]:
+                g.output(o)
+        return g.plan(), w
+
+    for first in ("dense", "other"):
+        p, w = plan(first, True)
+        assert bool(p.packed_bytes(w)) == (k == 33)
+        if k == 64:
+            plan(first, False)
+            continue
+        with pytest.raises(B.RelayError) as e:
+            plan(first, False)
+        assert e.value.category == "unsupported" and "two different" in str(e.value)
+
+
 # ---- the oracle ------------------------------------------------------------------------------------------------------------
 def _differences(f, at, step=1e-6):
     got = np.zeros(at.size)
