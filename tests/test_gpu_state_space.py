@@ -573,6 +573,29 @@ def test_one_plan_on_two_streams_at_once():
                 np.testing.assert_array_equal(a, b)
 
 
+def test_one_plan_run_on_two_streams_at_once():
+    """One plan, its operands shared, the runs that are under way at a time each with results and a workspace of its own."""
+    import torch
+    loss, (x, w, tok, dlp, dlse) = loss_case(500, 3000, 64, "bf16", seed=4)
+    scan, _ = scan_case(2, 300, 130, 16, "bf16", True, "some", seed=5)
+    for call in (loss_grad_call(loss, L.dense_logprobs(x, w, tok)[1], 500, 3000, 64, "bf16"), scan_grad_call(scan, 2, 300, 130, 16, "bf16")):
+        want = call.run().numbers()
+        ids = [next(v for v, p in call.bound.items() if p == t.data_ptr()) for t in call.results]
+        streams, runs = [torch.cuda.Stream() for _ in range(2)], []
+        for _ in streams:
+            results = [torch.zeros_like(t) for t in call.results]
+            workspace = torch.full((max(256, call.workspace_bytes),), 0xa5, dtype=torch.uint8, device="cuda:0")
+            runs.append((results, workspace, {**call.bound, **{v: t.data_ptr() for v, t in zip(ids, results)}}))
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for (results, workspace, bound), s in zip(runs, streams):
+                call.plan.run(bound, workspace.data_ptr(), workspace.numel(), s.cuda_stream)
+        torch.cuda.synchronize()
+        for results, workspace, bound in runs:
+            for got, ref in zip(results, want):
+                np.testing.assert_array_equal(got.double().cpu().numpy(), ref)
+
+
 def check_graph(spec, data, dtype):
     """Every call of a graph against its definition on what the library computed for its operands."""
     import torch
