@@ -434,6 +434,22 @@ def test_dense_logprobs_by_pieces_of_the_vocabulary(m, v, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,v,k", [(40, 100001, 16), (129, 40001, 72), (17, 300007, 8)])
+def test_gradients_by_several_pieces_of_the_vocabulary(m, v, k, dtype):
+    """More than sixteen rows by pieces, the last of them short: in the library's own workspace dl has less than its whole size."""
+    import torch
+    from paper_1810_00952_amd import binding as B
+    operands, (x, w, tok, dlp, dlse) = loss_case(m, v, k, dtype, seed=m + v)
+    lse = L.dense_logprobs(x, w, tok)[1]
+    _, back = loss_bounds(x, w, tok, lse, dlp, dlse, dtype)
+    call = loss_grad_call(operands, lse, m, v, k, dtype)
+    assert call.plan.workspace_bytes() > B.STATIC_WORKSPACE_BYTES
+    call.plan.run_static(call.bound, torch.cuda.current_stream().cuda_stream)
+    for name, g, want, tol in zip(("dx", "dw"), call.numbers(), L.dense_logprobs_grad(x, w, tok, lse, dlp, dlse), back):
+        within(g, want, tol, f"pieces {m}x{v}x{k} {dtype} {name}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,v,k", [(1, 3, 2), (2, 1030, 260), (4, 63, 700), (5, 65, 513), (8, 2500, 1100), (9, 5000, 515), (12, 129, 1024), (15, 257, 2049), (16, 2600, 72)])
 def test_gradient_of_few_rows(m, v, k, dtype):
     """Up to sixteen rows: their derivatives from the vocabulary's rows as they lie, run twice to the same bits."""
