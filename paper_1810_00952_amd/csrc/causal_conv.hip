@@ -10,8 +10,9 @@
 // masks.  Of the gradient the wave also walks on behind its run, until its own tokens have all they get from later ones; its share of
 // dw and db goes to memory, and a second launch adds the shares up, in a fixed order.
 //
-// HBM bounds both: 8 x 4096 x 2048 bf16, K 4, with the gate, forward 54 us (268 MB, 5.0 TB/s), gradient 98 (403 MB, 4.1 TB/s: 136 registers are three waves a
-// SIMD) and 5 of the shares; 1 x 16384 x 4096 in documents of some 400 tokens 63 to 68.  One token of 64 sequences: 3.9 us, a launch's own time.
+// Bound by the bytes that few waves have under way: two a SIMD are launched, and none follow those that have ended.  8 x 4096 x 2048 bf16, K 4, with the gate: forward 54 us
+// (268 MB, 5.0 TB/s; 1.37 waves a SIMD are there on average, vector instructions take 35 % of its time), gradient 98 (403 MB, 4.1 TB/s; 0.88 waves, 56 %) and 5 of the
+// shares; 1 x 16384 x 4096 in documents of some 400 tokens 63 to 68 (268 MB; 1.17 waves, 33 %).  One token of 64 sequences: 3.9 us, a launch's own time.
 #include <type_traits>
 
 #include "igemm_lds.h"

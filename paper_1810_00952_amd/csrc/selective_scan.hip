@@ -12,12 +12,12 @@
 // lane ends with one row's.  B and C meet the lanes in LDS.  The sums over channels (dB, dC) halve the values a lane has with every step, by exchanges of the
 // wave's halves and rows; the waves' meet in LDS, the workgroups' in memory, where another launch adds them up in a fixed order.  A row that is
 // padding has s = s x = B = C = du = 0 and leaves state and derivative as they are.  Few channels: the rows are cut into chunks, a workgroup
-// each; a launch ahead finds what each chunk makes of the state before it (P h + H; the derivative alike), P = exp(a sum s), and the workgroups
+// each; a launch ahead finds what each chunk makes of the state before it (P h + H; the derivative alike), P = exp(a sum s) as its fourth root, and the workgroups
 // add up the chunks before theirs.
 //
 // The vector units bound it: a state and token is an exponential (four issue slots of a wave) and four more operations forwards, some twenty both ways.
-// 8 x 2048 x 2048 x 16 bf16: forward 215 us, 62 % of what its one wave a SIMD is there for are vector instructions, gradient 590, 67 %; two waves a SIMD of
-// the gradient would spill (656 -> 1690).  1 x 16384 x 2048 x 16 in documents: 148 of the launch ahead and 179.  One token of 64 sequences: 7 us.
+// 8 x 2048 x 2048 x 16 bf16: forward 215 us, 57 % of them vector instructions of its one wave a SIMD, gradient 590, 67 %; two waves a SIMD of
+// the gradient would spill (656 -> 1690).  1 x 16384 x 2048 x 16 in documents: 148 of the launch ahead and 179, 77 % by two waves.  One token of 64 sequences: 7 us.
 #include <algorithm>
 #include <type_traits>
 
