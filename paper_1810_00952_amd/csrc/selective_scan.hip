@@ -818,12 +818,12 @@ Form form_of(const SelScanParams &p, bool grad)
     f.slabs = (int32_t)((p.D + CHANNELS - 1) / CHANNELS);
     const int64_t wgs = p.B * f.slabs, most = tiles * rows / 64;
     int64_t chunks = wgs < 256 ? (grad ? 256 : 512) / wgs : 1;
-    // not two forwards, whose launch ahead walks half of the rows once more and leaves the CUs as they were: 2048 rows of 16 states in 192 workgroups 230 us in two chunks, 196
-    // in one, in 255 235 and 198, in 256 238 and 199 (64 states in 192: 949 and 668); in 160 three chunks take 184, one 195 (64 states 715 and 667).  The gradient's gain: in 128 two 534, one 725
-    if (!grad && chunks < 3) chunks = 1;
     if (chunks > most) chunks = most > 0 ? most : 1;
     // a chunk's rows against the chunks before it, which each workgroup adds up: some 0.3 us a row, 0.15 a chunk
     while (chunks * chunks > 2 * p.T) chunks -= chunks / 8 + 1;
+    // not two forwards, whose launch ahead walks half of the rows once more and leaves the CUs as they were: 2048 rows of 16 states in 192 workgroups 230 us in two chunks, 196
+    // in one, in 255 235 and 198, in 256 238 and 199 (64 states in 192: 949 and 668); in 160 three chunks take 184, one 195 (64 states 715 and 667); 128 rows in 32 workgroups 16.9 and 15.5.  The gradient's gain: in 128 two 534, one 725
+    if (!grad && chunks < 3) chunks = 1;
     // a chunk's rows are reached by 31-bit offsets
     const int64_t line = std::max(p.D, 2 * p.N) * (p.dtype == DT_BF16 ? 2 : 4), reach = ((int64_t)1 << 30) / (line * rows);
     if (chunks < (tiles + reach - 1) / reach) chunks = (tiles + reach - 1) / reach;
