@@ -201,9 +201,10 @@ def test_a_packed_param_has_no_reader_that_wants_it_as_it_lies(other, k):
         assert e.value.category == "unsupported" and "two different" in str(e.value)
 
 
-@pytest.mark.parametrize("b,t,cut", [(8, 512, True), (10, 512, True), (11, 512, False), (12, 512, False), (15, 512, False), (16, 512, False), (2, 192, True), (2, 191, False), (2, 128, False)])
+@pytest.mark.parametrize("b,t,cut", [(8, 512, True), (10, 512, True), (11, 512, False), (12, 512, False), (15, 512, False), (16, 512, False), (2, 191, True), (2, 176, False), (2, 128, False)])
 def test_a_scan_is_cut_into_three_chunks_or_not_at_all(b, t, cut):
-    """Sixteen workgroups a sequence: two chunks would do half of the rows twice and fill no more CUs.  The chunks' states are workspace."""
+    """Sixteen workgroups a sequence: two chunks would do half of the rows twice and fill no more CUs.  A chunk has four tiles of 16 rows and more.  The
+    chunks' states are workspace."""
     d, n = 1024, 16
     x, h = ("bf16", (b * t, d)), ("f32", (b, d, n))
     p, _, _ = plan_of("selective_scan", [x, x, ("bf16", (b * t, 2 * n)), ("f32", (d, n)), ("f32", (d,)), h], [x, h])
